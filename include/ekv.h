@@ -35,6 +35,17 @@
  * 0..base_blocks-1 are backed by the base handle, blocks base_blocks..base_blocks+elastic_blocks-1
  * by the elastic handle.  A slot is block*block_size + t.
  *
+ * 8-bit pools (dtype EKV_E4M3).  The same geometry with ONE byte an element -- channel x of token-in-block t of
+ * kv-head h is the byte at n*block_stride_bytes + ((kv*num_kv_heads + h)*block_size + t)*head_dim + x, and
+ * block_bytes is half of the bf16 pool's -- holding an e4m3 code c, and beside the range an fp32 array
+ * scales[n][kv][h] per layer (ekv_layer_scales; plain device memory for base and elastic ids, 8*num_kv_heads bytes a
+ * block).  The element's value is c * scales[n][kv][h].  A scale is a power of two 2^e with -112 <= e <= 120, or 0
+ * while nothing was written: e4m3 is a floating-point format, so a finer scale would buy no precision, and with powers
+ * of two applying a scale is exact and raising one loses only bits below the code's smallest step.
+ * ekv_write_kv quantises (see there); decode and prefill read codes and scales, accumulate in fp32 and give what they
+ * would give on a bf16 pool that held the same values.  Grow, shrink, EKV_FUSED_RANGE, ekv_move_blocks and
+ * ekv_hoststep_* work as on a bf16 pool.  The EKV_PREFILL_* flags and ekv_attn_decode_two_tensor are refused.
+ *
  * EKV_FUSED_RANGE (this build's variation on the paper's arrangement, for a cheaper toggle): the
  * driver's map / unmap / set-access cost is per call, not per byte, and one call per layer is what
  * makes a toggle take milliseconds.  With this flag the pool reserves ONE range for the whole model
@@ -66,14 +77,19 @@ typedef enum ekv_status {
     EKV_OK = 0,
     EKV_ERR_INVALID = 1,   /* bad argument; nothing changed */
     EKV_ERR_CUDA = 2,      /* a CUDA runtime / driver call failed, or no device / driver */
-    EKV_ERR_OOM = 3,       /* physical memory could not be created; pool left in its prior state */
+    EKV_ERR_OOM = 3,       /* physical memory could not be created; pool left in its prior state; latched by
+                              ekv_extend_tables: the list of free block ids is too short */
     EKV_ERR_STATE = 4,     /* e.g. grow when grown, shrink when shrunk, compute on a host-only pool */
     EKV_ERR_BLOCK_OOB = 5, /* latched by a kernel: a block id or slot was outside [0, live_blocks) */
     EKV_ERR_TIMEOUT = 6,   /* latched by a kernel: a bounded wait on a copy barrier ran out */
     EKV_ERR_WORKSPACE = 7  /* workspace missing, misaligned (256 B) or too small */
 } ekv_status_t;
 
-enum { EKV_BF16 = 0 };
+/* element type of a pool's K and V (the queries, the outputs and the rows handed to ekv_write_kv are bf16 always) */
+enum {
+    EKV_BF16 = 0,
+    EKV_E4M3 = 1 /* 8 bits an element with one scale per (block, K|V, kv-head): see "8-bit pools" below */
+};
 
 /* flag bits */
 enum {
@@ -103,7 +119,7 @@ typedef struct ekv_pool_desc {
     int32_t num_kv_heads;
     int32_t head_dim;       /* 64 or 128 */
     int32_t block_size;     /* 16 */
-    int32_t dtype;          /* EKV_BF16 */
+    int32_t dtype;          /* EKV_BF16 or EKV_E4M3 */
     uint32_t flags;         /* EKV_START_GROWN | EKV_FUSED_RANGE | EKV_PREFILL_* */
     int64_t base_blocks;    /* per layer, >= 1; rounded UP to whole granules */
     int64_t elastic_blocks; /* per layer, >= 0; rounded UP to whole granules */
@@ -111,7 +127,7 @@ typedef struct ekv_pool_desc {
 
 typedef struct ekv_pool_info {
     uint64_t granularity;    /* VMM minimum allocation granularity in bytes (2 MiB in the paper) */
-    uint64_t block_bytes;    /* 2*num_kv_heads*block_size*head_dim*2 */
+    uint64_t block_bytes;    /* 2*num_kv_heads*block_size*head_dim*2; half of that for EKV_E4M3 */
     uint64_t base_bytes;     /* per layer, after rounding */
     uint64_t elastic_bytes;  /* per layer, after rounding */
     int64_t base_blocks;     /* after rounding */
@@ -147,6 +163,11 @@ EKV_API ekv_status_t ekv_pool_info(const ekv_pool_t *pool, ekv_pool_info_t *info
  * address.  Touching bytes of the elastic sub-range while it is unmapped faults the context. */
 EKV_API ekv_status_t ekv_layer_ptr(const ekv_pool_t *pool, int32_t layer, void **dptr);
 
+/* Device address of the layer's scales (EKV_E4M3 pools; EKV_ERR_INVALID on others): fp32
+ * [base_blocks + elastic_blocks, 2 (K|V), num_kv_heads], dense, constant for the pool's life and always
+ * readable, the elastic ids' part too.  dptr: HOST, receives a DEVICE address. */
+EKV_API ekv_status_t ekv_layer_scales(const ekv_pool_t *pool, int32_t layer, void **dptr);
+
 /*
  * ekv_grow -- commit ("Toggle cost", "Controller"): for every layer create the elastic handle if
  * it is not held, map it at the top of the range, grant access; then raise the device-side live
@@ -180,9 +201,59 @@ EKV_API ekv_status_t ekv_shrink(ekv_pool_t *pool, void *stream, uint32_t flags, 
  * slot_mapping: DEVICE int64 [T]; negative = skip the token; a slot whose block is >= the live
  * limit is skipped and latches EKV_ERR_BLOCK_OOB.  Duplicate slots in one call: unspecified
  * winner.  T == 0 is a no-op.
+ *
+ * On an EKV_E4M3 pool the call quantises, for each block it names and each (K|V, kv-head) of it:
+ *   a = the largest finite |x| among the call's rows for that block; e = the smallest exponent in [-112, 120] with
+ *   a <= 448 * 2^e (-112 if a = 0); old = the stored scale, or 0 if the call writes the block's FIRST slot;
+ *   scale = max(old, 2^e), stored;
+ *   every slot written: code = x / scale rounded to the nearest e4m3, ties to even; a NaN or infinite x is stored as
+ *   NaN (and takes no part in a); at the largest scale codes are held to 240, so that every value is finite in bf16;
+ *   every other slot of the block, if old > 0: code = code * old / scale, rounded the same way.
+ * Writing a block's first slot thus starts the block anew: what its other slots held is not kept.  That is how a
+ * block passes from one request to the next without a reset, and it asks that a block be filled from its first slot on
+ * (rewriting later slots is allowed at any time).  Slots may come in any order and a block's tokens from anywhere in the
+ * call; of duplicate slots the last one wins.  Two calls that write the same block must be stream-ordered.
  */
 EKV_API ekv_status_t ekv_write_kv(ekv_pool_t *pool, int32_t layer, const void *k, const void *v,
                           const int64_t *slot_mapping, int32_t T, void *stream);
+
+/*
+ * ekv_read_kv -- the inverse of ekv_write_kv: row i of k_out and v_out receives the values stored in slot
+ * slot_mapping[i] of `layer` as bf16 (a bf16 pool's bit patterns; an EKV_E4M3 pool's code * scale, which bf16 holds
+ * exactly), for a host that exports, moves or inspects a request's keys and values.
+ * k_out, v_out: DEVICE, bf16 [T, num_kv_heads, head_dim], contiguous, 16-byte aligned.
+ * slot_mapping: DEVICE int64 [T]; a negative slot leaves its rows of the outputs as they were; so does a slot whose
+ * block is >= the live limit, which latches EKV_ERR_BLOCK_OOB.  The same slot may appear more than once.
+ */
+EKV_API ekv_status_t ekv_read_kv(ekv_pool_t *pool, int32_t layer, void *k_out, void *v_out, const int64_t *slot_mapping,
+                         int32_t T, void *stream);
+
+/*
+ * ekv_extend_tables -- the bookkeeping of one step on the GPU: request r, with seq_lens[r] tokens in the cache, gets
+ * new_tokens[r] more.  New blocks are taken from a list of free ids, the block tables extended, and the slot
+ * mapping, offsets and lengths made that ekv_write_kv and the attention calls of the step take, in one launch and without a
+ * word from the host (so a captured step can be replayed while requests grow).  With have = ceil(seq_lens[r]/block_size),
+ * total = ceil((seq_lens[r]+new_tokens[r])/block_size) and requests in order:
+ *   block_tables[r][have .. total-1] = the next total-have ids of free_ids, from free_ids[*free_cursor] on;
+ *   cu_q_lens[r] = new_tokens[0] + .. + new_tokens[r-1] (cu_q_lens[R] = all of them);
+ *   slot_mapping[cu_q_lens[r] + i] = block_tables[r][p/block_size]*block_size + p%block_size, p = seq_lens[r] + i;
+ *   slot_mapping[cu_q_lens[R] .. T_cap-1] = -1 (ekv_write_kv skips them: a padded batch);
+ *   seq_lens_out[r] = seq_lens[r] + new_tokens[r]; *free_cursor_out = *free_cursor + ids taken.
+ * All or nothing: if a length is negative or does not fit its table row, or the tokens do not fit T_cap (latches
+ * EKV_ERR_INVALID), if the list is too short (latches EKV_ERR_OOM), or if an id to be taken, or the id of a partly filled
+ * block, is outside the live range (latches EKV_ERR_BLOCK_OOB), then no table entry changes, seq_lens_out and
+ * *free_cursor_out are copies of the inputs, cu_q_lens is all 0 and slot_mapping all -1.
+ * new_tokens, seq_lens: DEVICE int32 [R].  block_tables: DEVICE int32 [R, max_blocks_per_seq]; entries other than those
+ * above are neither read (but the one of a partly filled block) nor written.  free_ids: DEVICE int32 [n_free].
+ * free_cursor: DEVICE int32 [1].  slot_mapping: DEVICE int64 [T_cap].  cu_q_lens: DEVICE int32 [R+1].
+ * seq_lens_out, free_cursor_out: DEVICE int32, may be the same addresses as seq_lens and free_cursor.
+ * R <= 16384.  The ids come from ekv_blockpool_alloc (the host leases a batch of ids to the device and hears of
+ * their use from *free_cursor).
+ */
+EKV_API ekv_status_t ekv_extend_tables(ekv_pool_t *pool, const int32_t *new_tokens, const int32_t *seq_lens, int32_t R,
+                               int32_t *block_tables, int32_t max_blocks_per_seq, const int32_t *free_ids, int32_t n_free,
+                               const int32_t *free_cursor, int64_t *slot_mapping, int32_t T_cap, int32_t *cu_q_lens,
+                               int32_t *seq_lens_out, int32_t *free_cursor_out, void *stream);
 
 /* Bytes of scratch that cover EVERY ekv_attn_decode call with 1 <= B <= max_batch and
  * max_blocks_per_seq*block_size <= max_seq_len (rounded up to a block) -- an upper bound over all
@@ -253,7 +324,8 @@ EKV_API ekv_status_t ekv_attn_decode_static_scratch(ekv_pool_t *pool, int32_t la
  * range of `layer` and ids base_blocks..base_blocks+second_blocks-1 address `second_tensor`, a
  * separately allocated DEVICE buffer of second_blocks*block_bytes with the same block layout (16-byte
  * aligned; the pool's elastic range plays no part and may be unmapped).  Ids at or beyond
- * base_blocks+second_blocks are skipped and latch EKV_ERR_BLOCK_OOB.  It exists to measure what the
+ * base_blocks+second_blocks are skipped and latch EKV_ERR_BLOCK_OOB.  EKV_BF16 pools only (a second tensor would need
+ * scales of its own).  It exists to measure what the
  * single-range design saves (a second tensor map and a choice per block inside the kernel); results
  * are bitwise identical to ekv_attn_decode on the same logical data.
  */
@@ -375,7 +447,8 @@ EKV_API ekv_status_t ekv_blockpool_stats(const ekv_blockpool_t *bp, ekv_blockpoo
 
 /* Copies whole blocks src_ids[i] -> dst_ids[i] in EVERY layer of the pool (the data movement of a
  * drain), asynchronously on `stream`.  src_ids, dst_ids: DEVICE int32 [n]; the two sets must be
- * disjoint.  Ids outside the live range are skipped and latch EKV_ERR_BLOCK_OOB.  Bit-exact copy. */
+ * disjoint.  Ids outside the live range are skipped and latch EKV_ERR_BLOCK_OOB.  Bit-exact copy; on an EKV_E4M3
+ * pool a block's scales go with it. */
 EKV_API ekv_status_t ekv_move_blocks(ekv_pool_t *pool, const int32_t *src_ids, const int32_t *dst_ids, int32_t n, void *stream);
 
 typedef struct ekv_controller_desc {
@@ -412,7 +485,8 @@ EKV_API ekv_status_t ekv_controller_stats(const ekv_controller_t *ctrl, ekv_cont
 EKV_API ekv_status_t ekv_selftest_bounded_wait(ekv_pool_t *pool, int32_t limit_us, uint64_t *waited_ns_device, void *stream);
 
 /* Non-blocking read-and-clear of the status latched by kernels (EKV_OK, EKV_ERR_BLOCK_OOB or
- * EKV_ERR_TIMEOUT; the latter wins).  Meaningful after the launching stream was synchronised. */
+ * EKV_ERR_TIMEOUT; the latter wins; between them come EKV_ERR_INVALID, then EKV_ERR_OOM, which only ekv_extend_tables
+ * latches).  Meaningful after the launching stream was synchronised. */
 EKV_API ekv_status_t ekv_poll_status(ekv_pool_t *pool);
 
 EKV_API const char *ekv_status_string(ekv_status_t status);

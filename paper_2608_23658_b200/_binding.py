@@ -10,6 +10,7 @@ _LIB_PATH = os.path.join(_HERE, "libekv.so")
 _lib = None
 
 EKV_BF16 = 0
+EKV_E4M3 = 1
 EKV_START_GROWN = 1
 EKV_KEEP_PHYSICAL = 2
 EKV_FUSED_RANGE = 4
@@ -110,9 +111,12 @@ def load_library():
         "ekv_pool_destroy": (i32, [vp]),
         "ekv_pool_info": (i32, [vp, ctypes.POINTER(PoolInfo)]),
         "ekv_layer_ptr": (i32, [vp, i32, ctypes.POINTER(vp)]),
+        "ekv_layer_scales": (i32, [vp, i32, ctypes.POINTER(vp)]),
         "ekv_grow": (i32, [vp, vp, u32, dblp]),
         "ekv_shrink": (i32, [vp, vp, u32, dblp]),
         "ekv_write_kv": (i32, [vp, i32, vp, vp, vp, i32, vp]),
+        "ekv_read_kv": (i32, [vp, i32, vp, vp, vp, i32, vp]),
+        "ekv_extend_tables": (i32, [vp, vp, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, vp]),
         "ekv_attn_workspace_bytes": (sz, [vp, i32, i32]),
         "ekv_attn_decode_plan": (i32, [vp, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(sz)]),
         "ekv_attn_decode": (i32, [vp, i32, vp, vp, vp, i32, vp, i32, f32, vp, sz, vp]),
@@ -209,6 +213,13 @@ def ekv_layer_ptr(pool: int, layer: int) -> int:
     return out.value
 
 
+def ekv_layer_scales(pool: int, layer: int) -> int:
+    """Device address of an EKV_E4M3 pool's scales of a layer: float32 [base + elastic blocks, 2, num_kv_heads]."""
+    out = ctypes.c_void_p()
+    _check(load_library().ekv_layer_scales(pool, layer, ctypes.byref(out)))
+    return out.value
+
+
 def _toggle(fn, pool, stream, flags, host_only):
     ms = (ctypes.c_double * 2)()
     _check(fn(pool, None if host_only else _stream(stream), flags, ms))
@@ -228,6 +239,30 @@ def ekv_shrink(pool: int, stream=None, flags: int = 0, host_only: bool = False):
 def ekv_write_kv(pool: int, layer: int, k, v, slot_mapping, stream=None):
     T = int(slot_mapping.shape[0])
     _check(load_library().ekv_write_kv(pool, layer, _dptr(k), _dptr(v), _dptr(slot_mapping), T, _stream(stream)))
+
+
+def ekv_read_kv(pool: int, layer: int, k_out, v_out, slot_mapping, stream=None):
+    """Values stored in the slots -> bf16 rows (the inverse of ekv_write_kv); rows of negative slots stay as they were."""
+    T = int(slot_mapping.shape[0])
+    _check(load_library().ekv_read_kv(pool, layer, _dptr(k_out), _dptr(v_out), _dptr(slot_mapping), T, _stream(stream)))
+
+
+def ekv_extend_tables(pool: int, new_tokens, seq_lens, block_tables, free_ids, free_cursor, slot_mapping, cu_q_lens,
+                      seq_lens_out=None, free_cursor_out=None, stream=None):
+    """Block tables, slot mapping, offsets and lengths of a step, on the GPU.  seq_lens and free_cursor are updated in
+    place unless seq_lens_out / free_cursor_out are given."""
+    R, max_blocks = int(seq_lens.shape[0]), int(block_tables.shape[1])
+    assert new_tokens.shape[0] == R and block_tables.shape[0] == R and cu_q_lens.numel() == R + 1
+    out = seq_lens if seq_lens_out is None else seq_lens_out
+    cursor_out = free_cursor if free_cursor_out is None else free_cursor_out
+    assert out.shape[0] == R and free_cursor.numel() == 1 and cursor_out.numel() == 1
+    for t in (new_tokens, seq_lens, block_tables, free_ids, free_cursor, cu_q_lens, out, cursor_out):
+        assert t.element_size() == 4, "lengths, tables, ids and offsets are int32"
+    assert slot_mapping.element_size() == 8, "the slot mapping is int64"
+    _check(load_library().ekv_extend_tables(pool, _dptr(new_tokens), _dptr(seq_lens), R, _dptr(block_tables), max_blocks,
+                                            _dptr(free_ids), int(free_ids.shape[0]), _dptr(free_cursor), _dptr(slot_mapping),
+                                            int(slot_mapping.shape[0]), _dptr(cu_q_lens), _dptr(out), _dptr(cursor_out),
+                                            _stream(stream)))
 
 
 def ekv_attn_workspace_bytes(pool: int, max_batch: int, max_seq_len: int) -> int:

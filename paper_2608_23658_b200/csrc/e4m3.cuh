@@ -1,0 +1,43 @@
+// Conversions of e4m3 codes (sm_100a has them as instructions on pairs) and the power-of-two scales of an 8-bit pool.
+#pragma once
+#include <cuda_bf16.h>
+#include <stdint.h>
+
+namespace ekv {
+
+static constexpr int kScaleMinExp = -112, kScaleMaxExp = 120;
+static constexpr float kMaxScale = 1.329227995784916e36f;  // 2^120
+
+// two codes (low byte first) -> two f16, exactly (e4m3 is a subset of f16; NaN stays NaN)
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t v) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
+    return r;
+}
+// the same for the low / high half of a word of four codes
+__device__ __forceinline__ uint32_t e4m3_lo(uint32_t w) { return e4m3x2_to_f16x2((uint16_t)(w & 0xffffu)); }
+__device__ __forceinline__ uint32_t e4m3_hi(uint32_t w) { return e4m3x2_to_f16x2((uint16_t)(w >> 16)); }
+
+__device__ __forceinline__ float2 f16x2_to_float2(uint32_t h) {
+    float2 r;
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.f32.f16 %0, lo;\n\tcvt.f32.f16 %1, hi;\n\t}" : "=f"(r.x), "=f"(r.y) : "r"(h));
+    return r;
+}
+// two floats -> two codes (lo in the low byte), round to nearest even, beyond 448 held to 448, NaN to NaN
+__device__ __forceinline__ uint32_t floats_to_e4m3x2(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// 2^-e for a scale 2^e (a normal power of two): by its bits, no reciprocal
+__device__ __forceinline__ float pow2_inverse(float s) { return __uint_as_float((254u << 23) - (__float_as_uint(s) & 0x7f800000u)); }
+
+// the smallest 2^e, -112 <= e <= 120, with a <= 448 * 2^e; a: magnitude bits of a finite bf16
+__device__ __forceinline__ float scale_of_bf16_bits(uint32_t a) {
+    const int e = (int)(a >> 7) - 127 - ((a & 0x7fu) <= 0x60u ? 8 : 7);  // 448 = 1.75 * 2^8; 0x60 is a mantissa of .75
+    const int c = e < kScaleMinExp ? kScaleMinExp : (e > kScaleMaxExp ? kScaleMaxExp : e);
+    return __uint_as_float((uint32_t)(c + 127) << 23);
+}
+
+}  // namespace ekv

@@ -283,6 +283,7 @@ namespace ekv {
 __global__ void __launch_bounds__(256) move_blocks_kernel(const unsigned long long *__restrict__ layer_base, int num_layers,
                                                           const int *__restrict__ src_ids, const int *__restrict__ dst_ids,
                                                           int pieces_per_block, long long block_stride_pieces,
+                                                          float *__restrict__ scales, long long scales_per_layer, int scales_per_block,
                                                           const long long *__restrict__ live_ptr, unsigned *status) {
     const int pair = blockIdx.x, layer = blockIdx.y;
     const long long live = *live_ptr;
@@ -294,6 +295,10 @@ __global__ void __launch_bounds__(256) move_blocks_kernel(const unsigned long lo
     const uint4 *src = reinterpret_cast<const uint4 *>(layer_base[layer]) + s * block_stride_pieces;
     uint4 *dst = reinterpret_cast<uint4 *>(layer_base[layer]) + d * block_stride_pieces;
     for (int i = threadIdx.x; i < pieces_per_block; i += blockDim.x) dst[i] = src[i];
+    if (scales) {  // EKV_E4M3: a block's scales go with its bytes
+        float *of_layer = scales + layer * scales_per_layer;
+        for (int i = threadIdx.x; i < scales_per_block; i += blockDim.x) of_layer[d * scales_per_block + i] = of_layer[s * scales_per_block + i];
+    }
 }
 
 }  // namespace ekv
@@ -309,6 +314,7 @@ extern "C" ekv_status_t ekv_move_blocks(ekv_pool_t *pool, const int32_t *src_ids
     dim3 grid((unsigned)n, (unsigned)pool->desc.num_layers);
     move_blocks_kernel<<<grid, 256, 0, (cudaStream_t)stream>>>(pool->d_layer_base, pool->desc.num_layers, src_ids, dst_ids,
                                                                (int)(pool->block_bytes / 16), (long long)(pool->block_stride / 16),
+                                                               pool->d_scales, (long long)pool->scales_per_layer(), 2 * pool->desc.num_kv_heads,
                                                                pool->d_live, pool->d_status);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, "ekv_move_blocks launch");

@@ -19,6 +19,7 @@
 // on logical key positions, so results are bitwise reproducible and independent of which physical
 // blocks (base or elastic) hold the data.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include "ekv_internal.h"
@@ -286,6 +287,12 @@ decode_split_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_cons
     }
 }
 
+}  // namespace ekv
+
+#include "ekv_decode_e4m3.cuh"  // the split pass over an 8-bit pool: same parameters, same partials
+
+namespace ekv {
+
 // Block-wide max / sum over D threads (D = 64 or 128), fixed order: bitwise reproducible.
 template <int D, bool kMax>
 __device__ __forceinline__ float block_reduce(float v, float *scratch) {
@@ -449,7 +456,29 @@ static DecodeParams make_decode_params(const ekv_pool *pool, const DecodePlan &p
     return p;
 }
 
+template <int D>
+static ekv_status_t launch_decode8(ekv_pool *pool, int layer, const DecodeParams &p, int B, cudaStream_t stream) {
+    constexpr int kBytes = kDecodeWarps * kDecode8Stages * (2 * 16 * D + 8) + 1024;
+    static bool attr_set[64] = {false};
+    const int dev = pool->desc.device;
+    if (dev >= 64 || !attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(decode8_split_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+        if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_decode: shared-memory attribute");
+        if (dev < 64) attr_set[dev] = true;
+    }
+    dim3 grid(p.nsplit, pool->desc.num_kv_heads, B);
+    decode8_split_kernel<D><<<grid, kDecodeWarps * 32, kBytes, stream>>>(pool->kv_map[layer], p, pool->layer_scales(layer));
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_decode: split launch");
+    if (p.nsplit == 1) return EKV_OK;  // the split kernel wrote the final rows itself
+    decode_combine_kernel<D><<<B * pool->desc.num_q_heads, D, 0, stream>>>(p);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_decode: combine launch");
+    return EKV_OK;
+}
+
 static ekv_status_t dispatch_decode(ekv_pool *pool, int layer, const DecodeParams &p, int B, cudaStream_t stream) {
+    if (pool->e4m3()) return pool->desc.head_dim == 128 ? launch_decode8<128>(pool, layer, p, B, stream) : launch_decode8<64>(pool, layer, p, B, stream);
     if (pool->desc.head_dim == 128) return launch_decode<128>(pool, layer, p, B, stream);
     return launch_decode<64>(pool, layer, p, B, stream);
 }
@@ -589,6 +618,10 @@ extern "C" ekv_status_t ekv_attn_decode_two_tensor(ekv_pool_t *pool, int32_t lay
     ekv_status_t st = check_compute(pool, layer, "ekv_attn_decode_two_tensor");
     if (st == EKV_OK) st = check_decode_args("ekv_attn_decode_two_tensor", q, out, block_tables, max_blocks_per_seq, seq_lens, B);
     if (st != EKV_OK) return st;
+    if (pool->e4m3()) {
+        set_error("ekv_attn_decode_two_tensor: EKV_BF16 pools only (the second tensor has no scales)");
+        return EKV_ERR_INVALID;
+    }
     if (second_blocks < 1 || second_blocks >= (1ll << 31) || !second_tensor || ((uintptr_t)second_tensor & 15)) {
         set_error("ekv_attn_decode_two_tensor: bad second tensor (%p, %lld blocks)", second_tensor, (long long)second_blocks);
         return EKV_ERR_INVALID;

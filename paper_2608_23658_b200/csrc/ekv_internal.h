@@ -11,6 +11,8 @@
 // Bits latched by kernels into the pool's status word (host-mapped, read by ekv_poll_status).
 #define EKV_DEV_FLAG_OOB 1u
 #define EKV_DEV_FLAG_TIMEOUT 2u
+#define EKV_DEV_FLAG_NO_BLOCKS 4u  // ekv_extend_tables: fewer free ids than the step needs
+#define EKV_DEV_FLAG_BAD_LEN 8u    // ekv_extend_tables: a length that the tables or the slot map cannot hold
 
 // Prefill launches of one pool that may be in flight at the same time (each owns one device word while it runs).
 #define EKV_LAUNCH_SLOTS 64
@@ -46,8 +48,18 @@ struct ekv_pool {
     unsigned *h_status;     // pinned, host-mapped status word
     unsigned *d_status;     // its device alias
     unsigned long long *d_layer_base;  // device array: start address of every layer's range
-    std::vector<CUtensorMap> kv_map;  // per layer: 3-D view (channel, row in block, block id), box 64 x block_size x 1, 128B swizzle
+    // EKV_E4M3 pools: scales[layer][block id][K|V][kv-head], base and elastic ids alike (2^e as fp32; 0 = never written),
+    // and two words per (layer, block id) in which a large write_kv call finds the tokens of a block (zero between calls)
+    float *d_scales;
+    int2 *d_claims;
+    std::vector<CUtensorMap> kv_map;  // per layer: 3-D view (channel, row in block, block id); bf16: box 64 x block_size x 1, 128B
+                                      // swizzle; e4m3: box head_dim x block_size x 1, swizzle of one row (128 or 64 bytes)
     int sm_count;
+
+    bool e4m3() const { return desc.dtype == EKV_E4M3; }
+    int64_t total_blocks() const { return base_blocks + elastic_blocks; }
+    size_t scales_per_layer() const { return (size_t)total_blocks() * 2 * desc.num_kv_heads; }
+    float *layer_scales(int layer) const { return d_scales + (size_t)layer * scales_per_layer(); }
 };
 
 namespace ekv {
@@ -71,6 +83,10 @@ ekv_status_t launch_set_live(ekv_pool *pool, long long value, cudaStream_t strea
 // (K|V, kv-head, token, channel): dims (channel, row in block, block), box 64 x block_size x 1, 128-byte swizzle.
 ekv_status_t encode_kv_map(void *base, uint64_t blocks, uint64_t block_stride, int num_kv_heads, int head_dim, int block_size,
                            CUtensorMap *out);
+
+// The same over a layer of an EKV_E4M3 pool: one byte a channel, box head_dim x block_size x 1, swizzle = one row.
+ekv_status_t encode_kv8_map(void *base, uint64_t blocks, uint64_t block_stride, int num_kv_heads, int head_dim, int block_size,
+                            CUtensorMap *out);
 
 // Tensor map over a query tensor [tokens, num_q_heads, head_dim] bf16: dims (channel, head, token), box 64 channels x
 // 1 head x box_rows tokens, 128-byte swizzle: one box lands as the K-major [row][128 B] half tile the MMAs read.

@@ -194,6 +194,24 @@ ekv_status_t encode_kv_map(void *base, uint64_t blocks, uint64_t block_stride, i
     return EKV_OK;
 }
 
+ekv_status_t encode_kv8_map(void *base, uint64_t blocks, uint64_t block_stride, int num_kv_heads, int head_dim, int block_size,
+                            CUtensorMap *out) {
+    if (!load_driver()) return EKV_ERR_CUDA;
+    cuuint64_t gdim[3] = {(cuuint64_t)head_dim, (cuuint64_t)2 * num_kv_heads * block_size, (cuuint64_t)blocks};
+    cuuint64_t gstride[2] = {(cuuint64_t)head_dim, (cuuint64_t)block_stride};
+    cuuint32_t box[3] = {(cuuint32_t)head_dim, (cuuint32_t)block_size, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = g_drv.encode_tiled(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, base, gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                    head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_error("cuTensorMapEncodeTiled failed (CUresult %d) for an e4m3 KV tensor at %p with %llu blocks, block stride %llu", (int)r, base,
+                  (unsigned long long)blocks, (unsigned long long)block_stride);
+        return EKV_ERR_CUDA;
+    }
+    return EKV_OK;
+}
+
 ekv_status_t encode_q_map(const void *q, uint64_t tokens, int num_q_heads, int head_dim, int box_rows, CUtensorMap *out) {
     if (!load_driver()) return EKV_ERR_CUDA;
     cuuint64_t gdim[3] = {(cuuint64_t)head_dim, (cuuint64_t)num_q_heads, (cuuint64_t)tokens};
@@ -232,6 +250,8 @@ static void teardown(ekv_pool *p) {
     }
     if (p->d_live) cudaFree(p->d_live);
     if (p->d_layer_base) cudaFree(p->d_layer_base);
+    if (p->d_scales) cudaFree(p->d_scales);
+    if (p->d_claims) cudaFree(p->d_claims);
     if (p->h_status) cudaFreeHost(p->h_status);
 }
 
@@ -332,12 +352,16 @@ ekv_status_t ekv_pool_create(const ekv_pool_desc_t *desc, ekv_pool_t **out) {
     const ekv_pool_desc_t d = *desc;
     if (d.num_layers < 1 || d.num_kv_heads < 1 || d.num_q_heads < d.num_kv_heads || d.num_q_heads % d.num_kv_heads != 0 ||
         d.num_q_heads / d.num_kv_heads > 8 || (d.head_dim != 64 && d.head_dim != 128) || d.block_size != 16 ||
-        d.dtype != EKV_BF16 || d.base_blocks < 1 || d.elastic_blocks < 0 || d.device < 0 ||
+        (d.dtype != EKV_BF16 && d.dtype != EKV_E4M3) || d.base_blocks < 1 || d.elastic_blocks < 0 || d.device < 0 ||
         (d.flags & ~(uint32_t)(EKV_START_GROWN | EKV_FUSED_RANGE | EKV_PREFILL_WARP_MMA | EKV_PREFILL_ONE_HEAD | EKV_PREFILL_TWO_HEAD)) != 0) {
         set_error("ekv_pool_create: unsupported geometry (layers %d, heads %d/%d, head_dim %d, block_size %d, dtype %d, "
                   "blocks %lld+%lld, flags 0x%x)",
                   d.num_layers, d.num_q_heads, d.num_kv_heads, d.head_dim, d.block_size, d.dtype, (long long)d.base_blocks,
                   (long long)d.elastic_blocks, d.flags);
+        return EKV_ERR_INVALID;
+    }
+    if (d.dtype == EKV_E4M3 && (d.flags & (uint32_t)(EKV_PREFILL_WARP_MMA | EKV_PREFILL_ONE_HEAD | EKV_PREFILL_TWO_HEAD)) != 0) {
+        set_error("ekv_pool_create: the EKV_PREFILL_* flags name kernels of bf16 pools (dtype EKV_E4M3, flags 0x%x)", d.flags);
         return EKV_ERR_INVALID;
     }
 
@@ -374,8 +398,10 @@ ekv_status_t ekv_pool_create(const ekv_pool_desc_t *desc, ekv_pool_t **out) {
     p->h_status = nullptr;
     p->d_status = nullptr;
     p->d_layer_base = nullptr;
+    p->d_scales = nullptr;
+    p->d_claims = nullptr;
     p->sm_count = replaced ? 148 : prop.multiProcessorCount;
-    p->block_bytes = 2ull * d.num_kv_heads * d.block_size * d.head_dim * 2ull;
+    p->block_bytes = 2ull * d.num_kv_heads * d.block_size * d.head_dim * (d.dtype == EKV_E4M3 ? 1ull : 2ull);
 
     uint64_t gran = 0;
     int rc = be.granularity(be.user, d.device, &gran);
@@ -454,13 +480,22 @@ ekv_status_t ekv_pool_create(const ekv_pool_desc_t *desc, ekv_pool_t **out) {
             for (int l = 0; l < d.num_layers; ++l) bases[l] = p->layer_base(l);
             e = cudaMemcpy(p->d_layer_base, bases.data(), sizeof(unsigned long long) * d.num_layers, cudaMemcpyHostToDevice);
         }
+        if (p->e4m3()) {
+            const size_t scale_bytes = (size_t)d.num_layers * p->scales_per_layer() * sizeof(float);
+            const size_t claim_bytes = (size_t)d.num_layers * (size_t)p->total_blocks() * sizeof(int2);
+            if (e == cudaSuccess) e = cudaMalloc((void **)&p->d_scales, scale_bytes);
+            if (e == cudaSuccess) e = cudaMemset(p->d_scales, 0, scale_bytes);
+            if (e == cudaSuccess) e = cudaMalloc((void **)&p->d_claims, claim_bytes);
+            if (e == cudaSuccess) e = cudaMemset(p->d_claims, 0, claim_bytes);
+            if (e == cudaSuccess) e = cudaDeviceSynchronize();  // the fills are done before the first call on any stream
+        }
         if (e != cudaSuccess) st = cuda_fail(e, "ekv_pool_create: device state");
         // One tensor map per layer over ALL its block ids (base + elastic).  Encoding reads no memory,
         // and the map never changes when the elastic slice is mapped or unmapped.
         for (int l = 0; l < d.num_layers && st == EKV_OK; ++l) {
             CUtensorMap m;
-            st = encode_kv_map((void *)p->layer_base(l), (uint64_t)(p->base_blocks + p->elastic_blocks), p->block_stride,
-                               d.num_kv_heads, d.head_dim, d.block_size, &m);
+            st = (p->e4m3() ? encode_kv8_map : encode_kv_map)((void *)p->layer_base(l), (uint64_t)p->total_blocks(), p->block_stride,
+                                                              d.num_kv_heads, d.head_dim, d.block_size, &m);
             if (st != EKV_OK) break;
             p->kv_map.push_back(m);
         }
@@ -524,6 +559,19 @@ ekv_status_t ekv_layer_ptr(const ekv_pool_t *pool, int32_t layer, void **dptr) {
         return EKV_ERR_INVALID;
     }
     *dptr = (void *)pool->layer_base(layer);
+    return EKV_OK;
+}
+
+ekv_status_t ekv_layer_scales(const ekv_pool_t *pool, int32_t layer, void **dptr) {
+    if (!pool || !dptr || layer < 0 || layer >= pool->desc.num_layers || !pool->e4m3()) {
+        set_error("ekv_layer_scales: bad argument, or a pool whose dtype is not EKV_E4M3");
+        return EKV_ERR_INVALID;
+    }
+    if (pool->host_only) {
+        set_error("ekv_layer_scales: pool was created through a replacement VMM backend and holds no device state");
+        return EKV_ERR_STATE;
+    }
+    *dptr = (void *)pool->layer_scales(layer);
     return EKV_OK;
 }
 
@@ -628,6 +676,14 @@ ekv_status_t ekv_poll_status(ekv_pool_t *pool) {
         set_error("ekv_poll_status: a kernel gave up a bounded wait since the last poll%s",
                   (v & EKV_DEV_FLAG_OOB) ? " (and skipped a block id outside the live range)" : "");
         return EKV_ERR_TIMEOUT;
+    }
+    if (v & EKV_DEV_FLAG_BAD_LEN) {
+        set_error("ekv_poll_status: an ekv_extend_tables call since the last poll found a length that its tables or slot map cannot hold");
+        return EKV_ERR_INVALID;
+    }
+    if (v & EKV_DEV_FLAG_NO_BLOCKS) {
+        set_error("ekv_poll_status: an ekv_extend_tables call since the last poll needed more free ids than its list had");
+        return EKV_ERR_OOM;
     }
     if (v & EKV_DEV_FLAG_OOB) {
         set_error("ekv_poll_status: a kernel skipped a block id (or slot) outside the live range since the last poll");

@@ -25,6 +25,10 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
         set_error("ekv_attn_prefill_chunk: cu_q_lens[0] must be 0");
         return EKV_ERR_INVALID;
     }
+    if (pool->e4m3()) {
+        set_error("ekv_attn_prefill_chunk: EKV_BF16 pools only");
+        return EKV_ERR_INVALID;
+    }
     // Kernels (scale > 0 unless stated):
     //   two-head tcgen05 kernel   head_dim 128, query groups of 2 or more: a persistent CTA per SM, every K/V tile feeds two
     //                             heads (an odd group is cut into pairs and one single-head item per kv-head).

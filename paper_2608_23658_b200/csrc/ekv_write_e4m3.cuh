@@ -1,0 +1,234 @@
+// ekv_write_kv on an 8-bit pool: rows of bf16 -> e4m3 codes with one power-of-two scale per (block, K|V, kv-head).
+//
+//   e = min{ e : max|x| <= 448 * 2^e },  s = max(old, 2^e),  code(x) = rne(x / s),  kept codes *= old / s  (rne again)
+//
+// The scale ties all tokens of a block together, so the unit of work is a BLOCK the call names, not a token: one
+// CTA finds the block's tokens in the slot mapping, and each of its warps takes (K|V, head) pairs whole -- 16 rows of
+// head_dim channels, at most 4 KiB, held in registers between the maximum and the conversion, so a row is read once
+// and nothing is shared between warps.  A slot mapping may be in any order; the CTA that does a block's work
+// is the one of its first token in the mapping:
+//   T <= kScanTokens   one launch, a CTA per token; each looks through the whole mapping (8 KiB at most, from L2) for its block
+//   more               a first launch leaves the range [first, last] of every block's tokens in two words per block
+//                      (atomic maxima: no order matters), the second takes 16 tokens a CTA, does the blocks that begin
+//                      there and puts their words back to zero
+// Bound by memory: 4 bytes in and 2 out a channel pair of K and V, scales and mapping beside it.
+#pragma once
+#include "e4m3.cuh"
+#include "ekv_internal.h"
+
+namespace ekv {
+
+static constexpr int kW8Threads = 256;
+static constexpr int kW8Warps = kW8Threads / 32;
+static constexpr int kW8TokensPerCta = 16;
+static constexpr int kScanTokens = 1024;
+
+struct Write8Params {
+    uint8_t *cache;         // layer base
+    float *scales;          // of the layer: [block][2][Hk]
+    int2 *claims;           // of the layer: [block]
+    const uint4 *k, *v;
+    const long long *slots;
+    const long long *live;
+    unsigned *status;
+    long long block_stride;
+    int T, num_kv_heads;
+};
+
+// One (block, K|V, head): tok[t] = 1 + index of the row for slot t of the block, or 0.
+template <int D>
+__device__ __forceinline__ void write8_task(const Write8Params &p, long long n, int kv, int h, const int *tok, int lane) {
+    constexpr int kLanesPerRow = D / 8;  // 8 channels a lane: 16 bytes of bf16, 8 of codes
+    constexpr int kRows = 32 / kLanesPerRow;
+    constexpr int kIts = 16 / kRows;
+    const int sub = lane / kLanesPerRow, piece = lane % kLanesPerRow;
+    const uint4 *src = (kv ? p.v : p.k) + (long long)h * kLanesPerRow + piece;
+    const long long row_pieces = (long long)p.num_kv_heads * kLanesPerRow;
+    float *scale_at = p.scales + (n * 2 + kv) * p.num_kv_heads + h;
+    const float old = tok[0] ? 0.f : *scale_at;
+    uint4 x[kIts];
+    uint32_t m2 = 0;  // maxima of the magnitudes, two channels side by side (magnitudes of bf16 are ordered as integers)
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+        const int t = tok[it * kRows + sub];
+        x[it] = t ? __ldg(src + (t - 1) * row_pieces) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+        m2 = __vmaxu2(m2, __vmaxu2(__vmaxu2(x[it].x & 0x7fff7fffu, x[it].y & 0x7fff7fffu), __vmaxu2(x[it].z & 0x7fff7fffu, x[it].w & 0x7fff7fffu)));
+    }
+    uint32_t m = max(m2 & 0xffffu, m2 >> 16);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const bool nonfinite = m >= 0x7f80u;  // same in every lane
+    if (nonfinite) {  // the maximum again, over the finite ones
+        m = 0;
+#pragma unroll
+        for (int it = 0; it < kIts; ++it) {
+            const uint32_t w[4] = {x[it].x, x[it].y, x[it].z, x[it].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t a = (w[i >> 1] >> (16 * (i & 1))) & 0x7fffu;
+                if (a < 0x7f80u) m = max(m, a);
+            }
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    }
+    const float s = fmaxf(old, scale_of_bf16_bits(m));
+    const float inv = pow2_inverse(s);
+    const bool special = nonfinite || s >= kMaxScale;
+    uint8_t *tile = p.cache + n * p.block_stride + (long long)(kv * p.num_kv_heads + h) * (16 * D);
+#pragma unroll
+    for (int it = 0; it < kIts; ++it) {
+        const int row = it * kRows + sub;
+        if (!tok[row]) continue;
+        const uint32_t w[4] = {x[it].x, x[it].y, x[it].z, x[it].w};
+        uint32_t c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float a = __uint_as_float(w[i] << 16) * inv, b = __uint_as_float(w[i] & 0xffff0000u) * inv;
+            if (special) {  // 256 * 2^120 is not a finite bf16, and a conversion would make 448 of an infinity
+                const uint32_t la = w[i] & 0x7fffu, lb = (w[i] >> 16) & 0x7fffu;
+                if (s >= kMaxScale) a = fminf(fmaxf(a, -240.f), 240.f), b = fminf(fmaxf(b, -240.f), 240.f);
+                if (la >= 0x7f80u) a = __uint_as_float(0x7fffffffu);
+                if (lb >= 0x7f80u) b = __uint_as_float(0x7fffffffu);
+            }
+            c[i] = floats_to_e4m3x2(a, b);
+        }
+        *reinterpret_cast<uint2 *>(tile + row * D + piece * 8) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+    }
+    if (s > old) {
+        if (old > 0.f) {  // the scale rises: the codes that stay are brought to it
+            const float f = __uint_as_float(__float_as_uint(old) & 0x7f800000u) * inv;  // 2^(old - new); an underflow to 0 is what rounding gives too
+#pragma unroll
+            for (int it = 0; it < kIts; ++it) {
+                const int row = it * kRows + sub;
+                if (tok[row]) continue;
+                uint2 *at = reinterpret_cast<uint2 *>(tile + row * D + piece * 8);
+                const uint2 v = *at;
+                const uint32_t w[2] = {v.x, v.y};
+                uint32_t c[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float2 a = f16x2_to_float2(e4m3_lo(w[i])), b = f16x2_to_float2(e4m3_hi(w[i]));
+                    c[i] = floats_to_e4m3x2(a.x * f, a.y * f) | floats_to_e4m3x2(b.x * f, b.y * f) << 16;
+                }
+                *at = make_uint2(c[0], c[1]);
+            }
+        }
+        if (lane == 0) *scale_at = s;
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void write8_block(const Write8Params &p, long long n, const int *tok) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = warp; i < 2 * p.num_kv_heads; i += kW8Warps) {
+        const int kv = i >= p.num_kv_heads;
+        write8_task<D>(p, n, kv, i - kv * p.num_kv_heads, tok, lane);
+    }
+}
+
+// A CTA per token: goes on only for the first token of its block.
+template <int D>
+__global__ void __launch_bounds__(kW8Threads) write8_scan_kernel(const Write8Params p) {
+    __shared__ int tok[16];
+    __shared__ int earlier;
+    const int t = blockIdx.x;
+    const long long s = p.slots[t];
+    if (s < 0) return;
+    const long long n = s >> 4;
+    if (n >= *p.live) {
+        if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+        return;
+    }
+    if (threadIdx.x < 16) tok[threadIdx.x] = 0;
+    if (threadIdx.x == 16) earlier = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.T; i += kW8Threads) {
+        const long long o = p.slots[i];
+        if (o >= 0 && (o >> 4) == n) {
+            if (i < t) earlier = 1;
+            atomicMax(&tok[(int)(o & 15)], i + 1);  // of duplicate slots the last one
+        }
+    }
+    __syncthreads();
+    if (earlier) return;
+    write8_block<D>(p, n, tok);
+}
+
+// claims[n] = {T - first token, last token + 1} of block n, both by atomic maximum over zeros
+__global__ void __launch_bounds__(256) write8_claim_kernel(const Write8Params p) {
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    if (t >= p.T) return;
+    const long long s = p.slots[t];
+    if (s < 0) return;
+    const long long n = s >> 4;
+    if (n >= *p.live) {
+        atomicOr(p.status, EKV_DEV_FLAG_OOB);
+        return;
+    }
+    atomicMax(&p.claims[n].x, p.T - t);
+    atomicMax(&p.claims[n].y, t + 1);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kW8Threads) write8_claimed_kernel(const Write8Params p) {
+    __shared__ int tok[16];
+    __shared__ int todo[kW8TokensPerCta], last_of[kW8TokensPerCta];
+    __shared__ int count;
+    const int t0 = blockIdx.x * kW8TokensPerCta;
+    if (threadIdx.x < 32) {
+        const int t = t0 + (int)threadIdx.x;
+        bool mine = false;
+        int last = 0;
+        if (threadIdx.x < kW8TokensPerCta && t < p.T) {
+            const long long s = p.slots[t];
+            if (s >= 0 && (s >> 4) < *p.live) {
+                const volatile int2 *c = p.claims + (s >> 4);
+                mine = c->x == p.T - t;  // first token of its block; a block done already reads 0, which no token is
+                last = c->y - 1;
+            }
+        }
+        const unsigned mask = __ballot_sync(0xffffffffu, mine);
+        if (mine) {
+            const int at = __popc(mask & ((1u << threadIdx.x) - 1u));
+            todo[at] = t;
+            last_of[at] = last;
+        }
+        if (threadIdx.x == 0) count = __popc(mask);
+    }
+    __syncthreads();
+    for (int b = 0; b < count; ++b) {
+        const int first = todo[b], last = last_of[b];
+        const long long n = p.slots[first] >> 4;
+        if (threadIdx.x < 16) tok[threadIdx.x] = 0;
+        if (threadIdx.x == 0) p.claims[n] = make_int2(0, 0);
+        __syncthreads();
+        for (int i = first + threadIdx.x; i <= last; i += kW8Threads) {
+            const long long o = p.slots[i];
+            if (o >= 0 && (o >> 4) == n) atomicMax(&tok[(int)(o & 15)], i + 1);
+        }
+        __syncthreads();
+        write8_block<D>(p, n, tok);
+        __syncthreads();  // tok is used again
+    }
+}
+
+template <int D>
+static ekv_status_t launch_write8(ekv_pool *pool, const Write8Params &p, cudaStream_t stream) {
+    if (p.T <= kScanTokens) {
+        write8_scan_kernel<D><<<p.T, kW8Threads, 0, stream>>>(p);
+    } else {
+        write8_claim_kernel<<<(unsigned)(((long long)p.T + 255) / 256), 256, 0, stream>>>(p);
+        cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return cuda_fail(e, "ekv_write_kv: claim launch");
+        write8_claimed_kernel<D><<<(unsigned)(((long long)p.T + kW8TokensPerCta - 1) / kW8TokensPerCta), kW8Threads, 0, stream>>>(p);
+    }
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "ekv_write_kv launch");
+    return EKV_OK;
+}
+
+}  // namespace ekv

@@ -1,7 +1,11 @@
 // ekv_write_kv: slot-mapped KV write = exact scatter of bf16 bit patterns into the paged pool.
 // HBM-bound copy: every thread moves one 16-byte piece; a token's K (and V) row of one kv-head is
 // head_dim*2 contiguous bytes on both sides, so loads and stores are fully coalesced.
+// 8-bit pools: ekv_write_e4m3.cuh.  ekv_read_kv, the inverse, is here for both.
+#include "e4m3.cuh"
 #include "ekv_internal.h"
+#include "ekv_write_e4m3.cuh"
+#include "ptx.cuh"
 
 namespace ekv {
 
@@ -63,9 +67,70 @@ __global__ void __launch_bounds__(kWriteThreads) write_kv_kernel(uint4 *__restri
     }
 }
 
+// ekv_read_kv: a thread takes 8 channels of one row -- 16 bytes of bf16, or 8 codes and their scale -- and stores 16 bytes.
+// Bound by memory; a code times a power of two needs 4 significant bits, so the bf16 is exact.
+template <bool kE4m3>
+__global__ void __launch_bounds__(256) read_kv_kernel(const uint8_t *__restrict__ cache, const float *__restrict__ scales,
+                                                      uint4 *__restrict__ k, uint4 *__restrict__ v, const long long *__restrict__ slot_mapping,
+                                                      int T, int tokens_per_cta, int num_kv_heads, int pieces_per_row,
+                                                      long long block_stride, const long long *__restrict__ live_ptr, unsigned *status) {
+    const long long live = *live_ptr;
+    const int row_pieces = num_kv_heads * pieces_per_row, token_pieces = 2 * row_pieces;
+    const long long first = (long long)blockIdx.x * tokens_per_cta;
+    const int tokens = (int)min((long long)tokens_per_cta, (long long)T - first);
+    for (int i = threadIdx.x; i < tokens * token_pieces; i += 256) {
+        const int dt = i / token_pieces, rem = i - dt * token_pieces;
+        const int kv = rem >= row_pieces, hp = rem - kv * row_pieces;
+        const int h = hp / pieces_per_row, c = hp - h * pieces_per_row;
+        const long long t = first + dt, s = slot_mapping[t];
+        if (s < 0) continue;
+        const long long n = s >> 4;
+        if (n >= live) {
+            if (rem == 0) atomicOr(status, EKV_DEV_FLAG_OOB);
+            continue;
+        }
+        const int row = (kv * num_kv_heads + h) * 16 + (int)(s & 15);
+        const uint8_t *src = cache + n * block_stride + ((long long)row * pieces_per_row + c) * (kE4m3 ? 8 : 16);
+        uint4 out;
+        if (kE4m3) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(src);
+            const float sc = scales[(n * 2 + kv) * num_kv_heads + h];
+            const float2 a = f16x2_to_float2(e4m3_lo(w.x)), b = f16x2_to_float2(e4m3_hi(w.x));
+            const float2 e = f16x2_to_float2(e4m3_lo(w.y)), f = f16x2_to_float2(e4m3_hi(w.y));
+            out = make_uint4(pack_bf16x2(a.x * sc, a.y * sc), pack_bf16x2(b.x * sc, b.y * sc), pack_bf16x2(e.x * sc, e.y * sc),
+                             pack_bf16x2(f.x * sc, f.y * sc));
+        } else {
+            out = *reinterpret_cast<const uint4 *>(src);
+        }
+        (kv ? v : k)[t * row_pieces + hp] = out;
+    }
+}
+
 }  // namespace ekv
 
 using namespace ekv;
+
+extern "C" ekv_status_t ekv_read_kv(ekv_pool_t *pool, int32_t layer, void *k_out, void *v_out, const int64_t *slot_mapping, int32_t T,
+                                    void *stream) {
+    ekv_status_t st = check_compute(pool, layer, "ekv_read_kv");
+    if (st != EKV_OK) return st;
+    if (T < 0 || (T > 0 && (!k_out || !v_out || !slot_mapping)) || ((uintptr_t)k_out & 15) || ((uintptr_t)v_out & 15)) {
+        set_error("ekv_read_kv: bad argument (T=%d, k_out=%p, v_out=%p, slot_mapping=%p)", T, k_out, v_out, (const void *)slot_mapping);
+        return EKV_ERR_INVALID;
+    }
+    if (T == 0) return EKV_OK;
+    const int pieces_per_row = pool->desc.head_dim / 8, token_pieces = 2 * pool->desc.num_kv_heads * pieces_per_row;
+    const int tokens_per_cta = token_pieces >= 1024 ? 1 : 1024 / token_pieces;  // about four pieces a thread
+    const unsigned grid = (unsigned)(((long long)T + tokens_per_cta - 1) / tokens_per_cta);
+    const auto kernel = pool->e4m3() ? read_kv_kernel<true> : read_kv_kernel<false>;
+    kernel<<<grid, 256, 0, (cudaStream_t)stream>>>((const uint8_t *)pool->layer_base(layer), pool->e4m3() ? pool->layer_scales(layer) : nullptr,
+                                                   (uint4 *)k_out, (uint4 *)v_out, (const long long *)slot_mapping, T, tokens_per_cta,
+                                                   pool->desc.num_kv_heads, pieces_per_row, (long long)pool->block_stride, pool->d_live,
+                                                   pool->d_status);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "ekv_read_kv launch");
+    return EKV_OK;
+}
 
 extern "C" ekv_status_t ekv_write_kv(ekv_pool_t *pool, int32_t layer, const void *k, const void *v,
                                      const int64_t *slot_mapping, int32_t T, void *stream) {
@@ -76,6 +141,21 @@ extern "C" ekv_status_t ekv_write_kv(ekv_pool_t *pool, int32_t layer, const void
         return EKV_ERR_INVALID;
     }
     if (T == 0) return EKV_OK;
+    if (pool->e4m3()) {
+        Write8Params p;
+        p.cache = (uint8_t *)pool->layer_base(layer);
+        p.scales = pool->layer_scales(layer);
+        p.claims = pool->d_claims + (size_t)layer * pool->total_blocks();
+        p.k = (const uint4 *)k;
+        p.v = (const uint4 *)v;
+        p.slots = (const long long *)slot_mapping;
+        p.live = pool->d_live;
+        p.status = pool->d_status;
+        p.block_stride = (long long)pool->block_stride;
+        p.T = T;
+        p.num_kv_heads = pool->desc.num_kv_heads;
+        return pool->desc.head_dim == 128 ? launch_write8<128>(pool, p, (cudaStream_t)stream) : launch_write8<64>(pool, p, (cudaStream_t)stream);
+    }
     const int pieces_per_row = pool->desc.head_dim * 2 / 16;
     int block_shift = 0, row_shift = 0, token_shift = -1;
     while ((1 << block_shift) < pool->desc.block_size) ++block_shift;

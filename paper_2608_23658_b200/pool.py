@@ -8,28 +8,29 @@ from . import _binding as B
 
 
 class _RawCuda:
-    """Minimal __cuda_array_interface__ carrier for a raw device range (int16 elements)."""
+    """Minimal __cuda_array_interface__ carrier for a raw device range (int16 elements unless told otherwise)."""
 
-    def __init__(self, ptr: int, nelem: int):
-        self.__cuda_array_interface__ = {"shape": (nelem,), "typestr": "<i2", "data": (ptr, False), "version": 3,
+    def __init__(self, ptr: int, nelem: int, typestr: str = "<i2"):
+        self.__cuda_array_interface__ = {"shape": (nelem,), "typestr": typestr, "data": (ptr, False), "version": 3,
                                          "strides": None}
 
 
 class Pool:
     def __init__(self, *, num_q_heads, num_kv_heads, head_dim, base_blocks, elastic_blocks=0, num_layers=1,
                  block_size=16, device=0, start_grown=False, fused_range=False, prefill_warp_mma=False,
-                 prefill_one_head=False, prefill_two_head=False):
+                 prefill_one_head=False, prefill_two_head=False, dtype=B.EKV_BF16):
         self.device = torch.device("cuda", device)
         torch.cuda.set_device(self.device)
         self.handle = B.ekv_pool_create(device=device, num_layers=num_layers, num_q_heads=num_q_heads,
                                         num_kv_heads=num_kv_heads, head_dim=head_dim, block_size=block_size,
-                                        base_blocks=base_blocks, elastic_blocks=elastic_blocks,
+                                        base_blocks=base_blocks, elastic_blocks=elastic_blocks, dtype=dtype,
                                         flags=(B.EKV_START_GROWN if start_grown else 0) | (B.EKV_FUSED_RANGE if fused_range else 0) |
                                         (B.EKV_PREFILL_WARP_MMA if prefill_warp_mma else 0) |
                                         (B.EKV_PREFILL_ONE_HEAD if prefill_one_head else 0) |
                                         (B.EKV_PREFILL_TWO_HEAD if prefill_two_head else 0))
         self.num_q_heads, self.num_kv_heads, self.head_dim, self.block_size = num_q_heads, num_kv_heads, head_dim, block_size
         self.num_layers = num_layers
+        self.dtype = dtype
         self._ws = None
 
     # -- lifetime
@@ -61,21 +62,35 @@ class Pool:
         return B.ekv_layer_ptr(self.handle, layer)
 
     def layer_tensor(self, layer: int, first_block: int = 0, num_blocks: int | None = None) -> torch.Tensor:
-        """bf16 view [blocks, 2, Hkv, block_size, head_dim] of blocks first_block.. of a layer.
+        """View [blocks, 2, Hkv, block_size, head_dim] of blocks first_block.. of a layer: bf16, or the e4m3 codes of an
+        EKV_E4M3 pool (layer_scales has their scales).
         Only LIVE blocks may be viewed: unmapped elastic addresses fault when touched."""
         info = self.info
         if num_blocks is None:
             num_blocks = info.live_blocks - first_block
         if first_block < 0 or first_block + num_blocks > info.live_blocks:
             raise ValueError("view would reach past the live (mapped) blocks")
-        elems = info.block_bytes // 2
-        stride = info.block_stride_bytes // 2      # elements between consecutive block ids of this layer
+        size = 1 if self.dtype == B.EKV_E4M3 else 2
+        elems = info.block_bytes // size
+        stride = info.block_stride_bytes // size   # elements between consecutive block ids of this layer
         span = (num_blocks - 1) * stride + elems if num_blocks > 0 else 0
-        raw = _RawCuda(self.layer_ptr(layer) + first_block * info.block_stride_bytes, max(span, 1))
-        flat = torch.as_tensor(raw, device=self.device).view(torch.bfloat16)
+        raw = _RawCuda(self.layer_ptr(layer) + first_block * info.block_stride_bytes, max(span, 1),
+                       "|u1" if size == 1 else "<i2")
+        flat = torch.as_tensor(raw, device=self.device).view(torch.float8_e4m3fn if size == 1 else torch.bfloat16)
         d, bs, hk = self.head_dim, self.block_size, self.num_kv_heads
         # dense when stride == elems (one range per layer); a strided view over the fused range otherwise
         return torch.as_strided(flat, (num_blocks, 2, hk, bs, d), (stride, hk * bs * d, bs * d, d, 1))
+
+    def layer_scales(self, layer: int, first_block: int = 0, num_blocks: int | None = None) -> torch.Tensor:
+        """float32 view [blocks, 2, Hkv] of an EKV_E4M3 pool's scales (elastic ids included, mapped or not)."""
+        info = self.info
+        total = info.base_blocks + info.elastic_blocks
+        if num_blocks is None:
+            num_blocks = total - first_block
+        if first_block < 0 or num_blocks < 0 or first_block + num_blocks > total:
+            raise ValueError("view would reach past the pool's blocks")
+        raw = _RawCuda(B.ekv_layer_scales(self.handle, layer), total * 2 * self.num_kv_heads, "<f4")
+        return torch.as_tensor(raw, device=self.device).view(total, 2, self.num_kv_heads)[first_block:first_block + num_blocks]
 
     def grow(self, stream=None):
         return B.ekv_grow(self.handle, stream)
@@ -89,6 +104,22 @@ class Pool:
     # -- compute (argument marshalling only)
     def write_kv(self, layer, k, v, slot_mapping, stream=None):
         B.ekv_write_kv(self.handle, layer, k, v, slot_mapping, stream)
+
+    def read_kv(self, layer, slot_mapping, k_out=None, v_out=None, stream=None):
+        """Values stored in the slots as bf16 rows (k, v), each [T, Hkv, head_dim].  Rows of negative slots are left as they
+        were: hand in tensors of your own if the mapping has any."""
+        shape = (int(slot_mapping.shape[0]), self.num_kv_heads, self.head_dim)
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        B.ekv_read_kv(self.handle, layer, k_out, v_out, slot_mapping, stream)
+        return k_out, v_out
+
+    def extend_tables(self, new_tokens, seq_lens, block_tables, free_ids, free_cursor, slot_mapping, cu_q_lens,
+                      seq_lens_out=None, free_cursor_out=None, stream=None):
+        B.ekv_extend_tables(self.handle, new_tokens, seq_lens, block_tables, free_ids, free_cursor, slot_mapping, cu_q_lens,
+                            seq_lens_out, free_cursor_out, stream)
 
     def workspace(self, batch: int, max_seq_len: int) -> torch.Tensor:
         need = B.ekv_attn_workspace_bytes(self.handle, batch, max_seq_len)
