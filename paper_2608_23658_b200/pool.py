@@ -8,9 +8,12 @@ from . import _binding as B
 
 
 class _RawCuda:
-    """Minimal __cuda_array_interface__ carrier for a raw device range (int16 elements unless told otherwise)."""
+    """Minimal __cuda_array_interface__ carrier for a raw device range (int16 elements unless told otherwise).  A tensor
+    made of it keeps it, and so the pool whose memory it views: a view that outlives the caller's last name for the pool
+    stays readable until the view goes too (an explicit close() still ends it)."""
 
-    def __init__(self, ptr: int, nelem: int, typestr: str = "<i2"):
+    def __init__(self, ptr: int, nelem: int, typestr: str = "<i2", owner=None):
+        self.owner = owner
         self.__cuda_array_interface__ = {"shape": (nelem,), "typestr": typestr, "data": (ptr, False), "version": 3,
                                          "strides": None}
 
@@ -75,7 +78,7 @@ class Pool:
         stride = info.block_stride_bytes // size   # elements between consecutive block ids of this layer
         span = (num_blocks - 1) * stride + elems if num_blocks > 0 else 0
         raw = _RawCuda(self.layer_ptr(layer) + first_block * info.block_stride_bytes, max(span, 1),
-                       "|u1" if size == 1 else "<i2")
+                       "|u1" if size == 1 else "<i2", self)
         flat = torch.as_tensor(raw, device=self.device).view(torch.float8_e4m3fn if size == 1 else torch.bfloat16)
         d, bs, hk = self.head_dim, self.block_size, self.num_kv_heads
         # dense when stride == elems (one range per layer); a strided view over the fused range otherwise
@@ -89,7 +92,7 @@ class Pool:
             num_blocks = total - first_block
         if first_block < 0 or num_blocks < 0 or first_block + num_blocks > total:
             raise ValueError("view would reach past the pool's blocks")
-        raw = _RawCuda(B.ekv_layer_scales(self.handle, layer), total * 2 * self.num_kv_heads, "<f4")
+        raw = _RawCuda(B.ekv_layer_scales(self.handle, layer), total * 2 * self.num_kv_heads, "<f4", self)
         return torch.as_tensor(raw, device=self.device).view(total, 2, self.num_kv_heads)[first_block:first_block + num_blocks]
 
     def grow(self, stream=None):

@@ -365,6 +365,22 @@ def test_hoststep_runs_on_an_8_bit_pool():
         step.close()
 
 
+def test_a_view_keeps_its_pool():
+    """The pool goes with its last name or view, whichever is later."""
+    import weakref
+    pool = make_pool(I.TINY, 64)
+    ref = weakref.ref(pool)
+    codes, scales = pool.layer_tensor(0, 0, 3)[1:], pool.layer_scales(0, 0, 3).view(-1)
+    del pool
+    assert ref() is not None
+    del codes
+    assert ref() is not None and ref().handle
+    scales.fill_(2.0)
+    assert float(scales.sum()) == 2.0 * 3 * 2 * 2
+    del scales
+    assert ref() is None
+
+
 def test_refusals():
     shape = I.TINY
     with make_pool(shape, 64) as pool:
