@@ -36,14 +36,6 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) {
     return pack_bf16x2(f.x, f.y);
 }
 
-// 2^k that brings a positive finite magnitude a into [2^13, 2^14); 1 for 0 and for what is not finite
-__device__ __forceinline__ float to_f16_range(float a) {
-    const int e = (int)(__float_as_uint(a) >> 23) & 0xff;
-    if (e == 0xff || a == 0.f) return 1.f;
-    const int k = 13 - (e - 127);
-    return __uint_as_float((uint32_t)(min(k, 126) + 127) << 23);
-}
-
 template <int D>
 __global__ void __launch_bounds__(kDecodeWarps * 32, 2)
 decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodeParams p, const float *__restrict__ scales) {

@@ -4,6 +4,7 @@
 #include "ekv_prefill_mma.cuh"
 #include "ekv_prefill_tc.cuh"
 #include "ekv_prefill_tc1.cuh"
+#include "ekv_prefill_e4m3.cuh"
 #include "ekv_prefill_tcs.cuh"
 
 using namespace ekv;
@@ -23,10 +24,6 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
     if (R == 0) return EKV_OK;
     if (cu_q_lens_host[0] != 0) {
         set_error("ekv_attn_prefill_chunk: cu_q_lens[0] must be 0");
-        return EKV_ERR_INVALID;
-    }
-    if (pool->e4m3()) {
-        set_error("ekv_attn_prefill_chunk: EKV_BF16 pools only");
         return EKV_ERR_INVALID;
     }
     // Kernels (scale > 0 unless stated):
@@ -53,12 +50,14 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
     } else {
         kernel = K_TWO_HEAD;
     }
-    const int bm = kernel == K_WARP_MMA ? kPmBM : tc::kBM;
+    // An 8-bit pool has one kernel, whose items are rows of all heads of a group (ekv_prefill_e4m3.cuh).
+    const bool e4m3 = pool->e4m3();
+    const int bm = e4m3 ? tc8::kItemRows : kernel == K_WARP_MMA ? kPmBM : tc::kBM;
     PrefillParams p;
     p.n_prefix = R <= kPrefixMax ? 1 : 0;
     long long q_tiles = 0;
     for (int r = 0; r < R; ++r) {
-        const int c = cu_q_lens_host[r + 1] - cu_q_lens_host[r];
+        const long long c = ((long long)cu_q_lens_host[r + 1] - cu_q_lens_host[r]) * (e4m3 ? group : 1);
         if (c < 0) {
             set_error("ekv_attn_prefill_chunk: cu_q_lens decreases at request %d", r);
             return EKV_ERR_INVALID;
@@ -69,7 +68,7 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
     }
     if (p.n_prefix && q_tiles <= 0x7fffffffLL) p.tile_prefix[R] = (int)q_tiles;
     if (q_tiles == 0) return EKV_OK;
-    if (q_tiles > 0x7fffffffLL) {
+    if (q_tiles > 0x7fffffffLL || (e4m3 && (q_tiles * pool->desc.num_kv_heads > 0x7fffffffLL || (long long)cu_q_lens_host[R] * group > 0x7fffffffLL))) {
         set_error("ekv_attn_prefill_chunk: too many query tiles");
         return EKV_ERR_INVALID;
     }
@@ -91,6 +90,16 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
     p.q_tiles = (int)q_tiles;
     p.scale_log2 = scale * 1.4426950408889634f;
     const bool d128 = pool->desc.head_dim == 128;
+    if (e4m3) {
+        tc8::Params pp;
+        pp.p = p;
+        pp.p.scale_log2 = fabsf(p.scale_log2);
+        pp.q_sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
+        pp.cache = (const uint8_t *)pool->layer_base(layer);
+        pp.scales = pool->layer_scales(layer);
+        pp.block_stride = (long long)pool->block_stride;
+        return d128 ? tc8::launch_prefill8<128>(pool, pp, (cudaStream_t)stream) : tc8::launch_prefill8<64>(pool, pp, (cudaStream_t)stream);
+    }
     if (kernel == K_TWO_HEAD) return tc::launch_prefill_tc(pool, layer, p, q, out, cu_q_lens_host[R], (cudaStream_t)stream);
     if (kernel == K_ONE_HEAD)
         return d128 ? tcs::launch_prefill_tcs(pool, layer, p, q, out, cu_q_lens_host[R], (cudaStream_t)stream)

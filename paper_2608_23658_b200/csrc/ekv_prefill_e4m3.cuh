@@ -1,0 +1,565 @@
+// ekv_attn_prefill_chunk over an 8-bit pool, on the 5th-generation tensor cores.
+//
+//   S = (Q K_code^T) * s_K(block),   P = exp2(S - m),   O = sum P (V_code * s_V(block)) / sum P,   keys 0 .. position of the row
+//
+// tcgen05 takes no operand pair of bf16 and e4m3, and Q or P rounded to e4m3 would lose half their bits, so the codes become
+// 16-bit operands on their way into shared memory.  That costs instructions for every key the CTA reads, and the whole shape
+// of the kernel follows from spreading them over as many query rows as one SM can hold:
+//   - A work item is 256 rows of ONE kv-head: rows are (position, head of the group) pairs in that order, so all query heads
+//     that share the kv-head read the converted tile, whatever their number (groups of seven as well as of eight), and a
+//     few drafted tokens of a request fill a tile that would be 128 times one head's few rows otherwise.
+//   - The rows are two tiles of 128 (TMEM lanes) that take turns: the softmax of one runs beside the MMAs of the other.
+//   - K goes to f16: one conversion instruction for two codes and nothing else, as its scale is applied to the scores, where
+//     a multiplication by the softmax scale stands anyway.  Q becomes f16 with each row brought to a maximum in
+//     [2^13, 2^14) by a power of two, as in decode (what f16 then drops lies 2^-37 below the row's largest element).
+//   - V goes to bf16 with its scale multiplied in (exact, a power of two), since only bf16 has the scales' range; P is bf16.
+//
+//   warp 0        MMA issuer: S = Q K^T (both from shared memory) and O += P V (P from TMEM, V MN-major)
+//   warp 1        TMEM allocation; warps 2, 3 complete the warpgroup
+//   warps 4-7     rows 0-127: Q into shared memory, softmax (a thread a row), write-out
+//   warps 8-11    rows 128-255
+//   warps 12-15   converters: 16-byte loads of codes through the block table, one tile ahead in registers, conversion, swizzled
+//                 stores.  Keys past the item's last visible one become zero rows of V, so nothing a slot that was never
+//                 written holds can reach a sum (0 * NaN), and no code is needed for that elsewhere.
+// Softmax: online with lazy rescaling, as in the other tcgen05 kernels.  The sign of the scale is folded into Q.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "e4m3.cuh"
+#include "ekv_prefill_tc.cuh"
+
+namespace ekv {
+namespace tc8 {
+
+namespace cp = cuda::ptx;
+using tc::fence_after;
+using tc::fence_before;
+
+static constexpr int kBM = 128, kBN = 128;
+static constexpr int kItemRows = 2 * kBM;
+static constexpr int kThreads = 512;
+static constexpr int kHalfBytes = 128 * 128;  // [128 rows][64 16-bit channels], 128-byte swizzle
+static constexpr int kStages = 2;
+// setmaxnreg: warps 0-3 kRegsUtil, 4-11 kRegsSoftmax, 12-15 kRegsConv; the shares add up to what the CTA is launched with
+static constexpr int kLaunchRegs = 128, kRegsUtil = 40, kRegsSoftmax = 184, kRegsConv = 104;
+static_assert(128 * (kRegsUtil + kRegsConv) + 256 * kRegsSoftmax <= kLaunchRegs * kThreads, "setmaxnreg split exceeds the CTA's registers");
+static_assert(kRegsUtil == 40 && kRegsSoftmax == 184 && kRegsConv == 104, "the setmaxnreg instructions in the kernel carry these numbers as literals");
+
+struct Params {
+    PrefillParams p;  // q_tiles, tile_prefix: in items of kItemRows rows per kv-head; scale_log2 >= 0
+    const uint8_t *cache;
+    const float *scales;
+    long long block_stride;
+    float q_sign;  // -1 for a negative scale; 0 for a scale of 0
+};
+
+template <int D>
+struct Geo {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kTileBytes = kHalves * kHalfBytes;
+    static constexpr int kOffQ = 0;
+    static constexpr int kOffK = 2 * kTileBytes;
+    static constexpr int kOffV = kOffK + kStages * kTileBytes;
+    static constexpr int kOffBar = kOffV + kStages * kTileBytes;
+    enum Bar { Q_READY = 0, K_FULL = 2, K_EMPTY = 4, V_FULL = 6, V_EMPTY = 8, S_READY = 10, P_PART = 12, P_READY = 14, DRAIN = 16, NBAR = 17 };
+    static constexpr int kOffFlags = kOffBar + 8 * NBAR;       // abort flag, TMEM address, 4 masks of invalid blocks
+    static constexpr int kOffKScale = kOffBar + 192;           // [4 tiles][8 blocks] floats
+    static constexpr int kOffQInv = kOffKScale + 128;          // [256 rows] floats
+    static constexpr int kSmemBytes = kOffQInv + 1024 + 1024;  // + alignment slack
+    static_assert(kOffFlags + 24 <= kOffKScale && kSmemBytes <= 232448, "shared memory");
+    // kind::f16 instruction descriptors, D = f32, M = 128: QK with f16 operands, PV with bf16 ones and V MN-major
+    static constexpr uint32_t kIdescQK = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+    static constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
+};
+
+template <int D>
+struct Smem {
+    uint32_t base;
+    uint8_t *ptr;
+    __device__ __forceinline__ uint32_t bar(int i) const { return base + Geo<D>::kOffBar + 8 * i; }
+    __device__ __forceinline__ volatile int *abort_flag() const { return (volatile int *)(ptr + Geo<D>::kOffFlags); }
+    __device__ __forceinline__ uint32_t *tmem_slot() const { return (uint32_t *)(ptr + Geo<D>::kOffFlags + 4); }
+    // rings of 4 by key tile: the converters start on tile j + 3 only after the MMAs of tile j + 1's scores, i.e. after the
+    // softmax of tile j has read its entry
+    __device__ __forceinline__ volatile int *bad_mask(int tile) const { return (volatile int *)(ptr + Geo<D>::kOffFlags + 8 + 4 * (tile & 3)); }
+    __device__ __forceinline__ float *k_scale(int tile) const { return (float *)(ptr + Geo<D>::kOffKScale) + 8 * (tile & 3); }
+    __device__ __forceinline__ float *q_inv() const { return (float *)(ptr + Geo<D>::kOffQInv); }
+};
+
+// Bounded wait of a whole warp that also gives up as soon as another role has flagged an abort.
+template <int D>
+__device__ __forceinline__ bool wait_warp(const Smem<D> &sh, int bar, uint32_t parity, const PrefillParams &p) {
+    const uint32_t b = sh.bar(bar);
+    bool ok = mbar_try_wait(b, parity);
+    if (!ok) {
+        const uint64_t t0 = global_timer_ns();
+        for (uint32_t i = 1;; ++i) {
+            if (mbar_try_wait(b, parity)) {
+                ok = true;
+                break;
+            }
+            if ((i & 31u) == 0u) {
+                if (*sh.abort_flag()) break;
+                if (global_timer_ns() - t0 > 2000000000ull) {
+                    *sh.abort_flag() = 1;
+                    *(volatile int *)p.abort_word = 1;
+                    atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);
+                    break;
+                }
+            }
+        }
+    }
+    return __all_sync(0xffffffffu, ok);
+}
+
+// Which request owns item `idx` (items of kItemRows (position, head) rows, requests in order)?
+__device__ __forceinline__ bool find_item(const PrefillParams &p, int idx, int &req, int &first, int &q0, int &c_r) {
+    if (p.n_prefix) return find_request(p, idx, kItemRows, req, first, q0, c_r);
+    int acc = 0;
+    for (req = 0; req < p.R; ++req) {
+        q0 = p.cu_q_lens[req];
+        c_r = p.cu_q_lens[req + 1] - q0;
+        const int n = (int)(((long long)c_r * p.group + kItemRows - 1) / kItemRows);
+        if (idx < acc + n) {
+            first = acc;
+            return true;
+        }
+        acc += n;
+    }
+    return false;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_constant__ Params pp) {
+    using G = Geo<D>;
+    const PrefillParams &p = pp.p;
+    constexpr int kPieces = D / 8;              // 16-byte pieces of a row of Q / O
+    constexpr int kRowsPerInst = 32 / kPieces;  // rows one warp-wide 16-byte access covers
+    if (*(volatile int *)p.abort_word) return;  // an earlier CTA of this launch timed out
+
+    // ---- which (request, rows, kv-head)?  Heaviest (latest) items first, all kv-heads of one next to each other.
+    const int rank = blockIdx.x / p.num_kv_heads, g = blockIdx.x - rank * p.num_kv_heads;
+    const int idx = p.q_tiles - 1 - rank;
+    int req = 0, first = 0, c_r = 0, q0 = 0;
+    if (!find_item(p, idx, req, first, q0, c_r)) return;
+    const int group = p.group;
+    const int row0 = (idx - first) * kItemRows;               // first of the request's c_r * group rows
+    const int rows_here = min(kItemRows, c_r * group - row0);
+    if (rows_here <= 0) return;  // the device's offsets say less than the host's
+    const int L = min(p.seq_lens[req], p.max_blocks * 16);
+    const int prefix = L - c_r;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // element offset of a row of the item in q and out
+    auto row_offset = [&](int r) {
+        const int pos = (row0 + r) / group, hg = row0 + r - pos * group;
+        return ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D;
+    };
+
+    if (prefix < 0) {  // malformed request: zero rows, latch
+        if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+        for (int e = threadIdx.x; e < rows_here * kPieces; e += kThreads)
+            *reinterpret_cast<uint4 *>(p.out + row_offset(e / kPieces) + (e % kPieces) * 8) = make_uint4(0u, 0u, 0u, 0u);
+        return;
+    }
+    const int kv_end = min(L, prefix + (row0 + rows_here - 1) / group + 1);  // keys any row of the item may see
+    const int n_tiles = (kv_end + kBN - 1) / kBN;
+    const int n_blocks = (kv_end + 15) >> 4;
+    const int nx = rows_here > kBM ? 2 : 1;  // row tiles
+
+    extern __shared__ uint8_t smem_raw[];
+    Smem<D> sh;
+    {
+        const uint32_t raw = smem_u32(smem_raw);
+        sh.base = (raw + 1023u) & ~1023u;
+        sh.ptr = smem_raw + (sh.base - raw);
+    }
+    if (threadIdx.x == 0) {
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(sh.bar(G::Q_READY + x), 4);
+            mbar_init(sh.bar(G::K_FULL + x), 4);
+            mbar_init(sh.bar(G::K_EMPTY + x), 1);
+            mbar_init(sh.bar(G::V_FULL + x), 4);
+            mbar_init(sh.bar(G::V_EMPTY + x), 1);
+            mbar_init(sh.bar(G::S_READY + x), 1);
+            mbar_init(sh.bar(G::P_PART + x), 4);
+            mbar_init(sh.bar(G::P_READY + x), 4);
+        }
+        mbar_init(sh.bar(G::DRAIN), 1);
+        *sh.abort_flag() = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        cp::tcgen05_alloc(cp::cta_group_1, sh.tmem_slot(), 512);
+        cp::tcgen05_relinquish_alloc_permit(cp::cta_group_1);
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *sh.tmem_slot();
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 0) {
+            // =========================== MMA issuer ===========================
+            constexpr uint64_t kHi = (uint64_t)tc::kDescHi << 32;
+            const uint64_t q_d = kHi | tc::desc_lo(sh.base + G::kOffQ, 16), k_d = kHi | tc::desc_lo(sh.base + G::kOffK, 16),
+                           v_d = kHi | tc::desc_lo(sh.base + G::kOffV, kHalfBytes);
+            auto issue_qk = [&](int x, int s) {  // S_x = Q_x K(s)^T
+                if (tc::elect_one()) {
+                    const uint64_t qd = q_d + (uint32_t)x * (G::kTileBytes >> 4), kd = k_d + (uint32_t)s * (G::kTileBytes >> 4);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
+                        tc::mma_ss(tmem + 128 * x, qd + off, kd + off, G::kIdescQK, k > 0 ? 1u : 0u);
+                    }
+                }
+                __syncwarp();
+            };
+            auto issue_pv = [&](int x, int s, bool acc, int k0, int k1) {  // O_x (+)= P_x[:, 16 k0 : 16 k1] V(s)[16 k0 : 16 k1, :]
+                if (tc::elect_one()) {
+                    const uint64_t vd = v_d + (uint32_t)s * (G::kTileBytes >> 4);
+#pragma unroll
+                    for (int k = 0; k < kBN / 16; ++k)
+                        if (k >= k0 && k < k1) tc::mma_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, (acc || k > 0) ? 1u : 0u);
+                }
+                __syncwarp();
+            };
+            bool ok = wait_warp<D>(sh, G::K_FULL, 0, p);
+            for (int x = 0; x < nx && ok; ++x) {
+                ok = wait_warp<D>(sh, G::Q_READY + x, 0, p);
+                if (!ok) break;
+                fence_after();
+                issue_qk(x, 0);
+                if (x == nx - 1) tc::mma_commit(sh.bar(G::K_EMPTY));
+                tc::mma_commit(sh.bar(G::S_READY + x));
+            }
+            for (int j = 0; j < n_tiles && ok; ++j) {
+                const int s = j & 1, s1 = s ^ 1;
+                const bool more = j + 1 < n_tiles;
+                ok = wait_warp<D>(sh, G::V_FULL + s, (uint32_t)((j >> 1) & 1), p);
+                for (int x = 0; x < nx && ok; ++x) {
+                    ok = wait_warp<D>(sh, G::P_PART + x, (uint32_t)(j & 1), p);
+                    if (!ok) break;
+                    fence_after();
+                    issue_pv(x, s, j > 0, 0, tc::kPartSteps);  // keys 0..95 while the softmax warps finish the rest
+                    ok = wait_warp<D>(sh, G::P_READY + x, (uint32_t)(j & 1), p);
+                    if (!ok) break;
+                    fence_after();
+                    issue_pv(x, s, true, tc::kPartSteps, kBN / 16);
+                    if (x == nx - 1) tc::mma_commit(sh.bar(G::V_EMPTY + s));
+                    if (more) {
+                        if (x == 0) ok = wait_warp<D>(sh, G::K_FULL + s1, (uint32_t)(((j + 1) >> 1) & 1), p);
+                        if (!ok) break;
+                        fence_after();
+                        issue_qk(x, s1);
+                        if (x == nx - 1) tc::mma_commit(sh.bar(G::K_EMPTY + s1));
+                    }
+                    tc::mma_commit(sh.bar(G::S_READY + x));  // the next scores, and O up to this tile
+                }
+            }
+            // every MMA this thread issued must be finished before TMEM is released
+            tc::mma_commit(sh.bar(G::DRAIN));
+            (void)wait_warp<D>(sh, G::DRAIN, 0, p);
+        }
+    } else if (warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        // =========================== converters ===========================
+        constexpr int kIts = D / 16;                  // 16-byte pieces of codes a thread takes of a tile
+        constexpr int kBlocksPerIt = 128 * 16 / (16 * D);  // blocks the 128 threads cover at once: 1, or 2 at head_dim 64
+        const int ct = threadIdx.x - 384;
+        const int in_block = ct % D;                  // 16 * D bytes of a block are D pieces
+        const int rowb = in_block / (D / 16), piece = in_block % (D / 16);
+        const long long live = *p.live;
+        const int *bt = p.block_tables + (size_t)req * p.max_blocks;
+        const uint8_t *src = pp.cache + (long long)g * (16 * D) + in_block * 16;
+        const long long v_off = (long long)p.num_kv_heads * (16 * D);
+        // lane l: id of block 8j + l % 8 of tile j (-1 past the end, -2 invalid)
+        auto load_id = [&](int j) {
+            int id = -1;
+            const int bi = 8 * j + (lane & 7);
+            if (bi < n_blocks) {
+                id = bt[bi];
+                if (id < 0 || (long long)id >= live) id = -2;
+            }
+            return id;
+        };
+        auto load_tile = [&](uint4 (&buf)[kIts], int ids, int kv) {
+#pragma unroll
+            for (int it = 0; it < kIts; ++it) {
+                const int id = __shfl_sync(0xffffffffu, ids, it * kBlocksPerIt + (kBlocksPerIt > 1 ? ct / D : 0));
+                buf[it] = id >= 0 ? __ldg(reinterpret_cast<const uint4 *>(src + id * pp.block_stride + (kv ? v_off : 0))) : make_uint4(0u, 0u, 0u, 0u);
+            }
+        };
+        auto load_scale = [&](int ids, int kv) { return ids >= 0 ? __ldg(pp.scales + ((long long)ids * 2 + kv) * p.num_kv_heads + g) : 0.f; };
+        // 16 codes of one row -> two 16-byte chunks of the 128-byte swizzled tile; lanes of the upper half tile store theirs in
+        // the other order, so that eight lanes never meet in a bank
+        const uint32_t half_off = (uint32_t)(piece >> 2) * kHalfBytes;
+        const int c0 = 2 * (piece & 3) + ((D == 128 && piece >= 4) ? 1 : 0);
+        auto store = [&](uint32_t tile_off, int row, const uint32_t (&w)[8]) {
+            uint8_t *at = sh.ptr + tile_off + half_off + row * 128;
+            const bool flip = c0 & 1;
+            *reinterpret_cast<uint4 *>(at + ((c0 ^ (row & 7)) << 4)) = flip ? make_uint4(w[4], w[5], w[6], w[7]) : make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4 *>(at + (((c0 ^ 1) ^ (row & 7)) << 4)) = flip ? make_uint4(w[0], w[1], w[2], w[3]) : make_uint4(w[4], w[5], w[6], w[7]);
+        };
+        auto block_of = [&](int it) { return it * kBlocksPerIt + (kBlocksPerIt > 1 ? ct / D : 0); };
+        auto publish = [&](int bar) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.bar(bar));
+        };
+        uint4 kb[kIts], vb[kIts];
+        int ids = load_id(0);
+        float ks = load_scale(ids, 0), vs = load_scale(ids, 1);
+        load_tile(kb, ids, 0);
+        bool ok = true;
+        for (int j = 0; j < n_tiles; ++j) {
+            const int s = j & 1;
+            const uint32_t ph = (uint32_t)(((j >> 1) - 1) & 1);
+            load_tile(vb, ids, 1);
+            const int ids_next = j + 1 < n_tiles ? load_id(j + 1) : -1;
+            // ---- K: f16, scales beside it
+            ok = j < kStages || wait_warp<D>(sh, G::K_EMPTY + s, ph, p);
+            if (!ok) break;
+            if (warp == 12) {
+                const unsigned bad = __ballot_sync(0xffffffffu, ids < 0) & 0xffu;  // invalid, or past the last visible key
+                const unsigned oob = __ballot_sync(0xffffffffu, ids == -2) & 0xffu;
+                if (lane < 8) sh.k_scale(j)[lane] = ks > 0.f ? ks : 1.f;
+                if (lane == 0) {
+                    *sh.bad_mask(j) = (int)bad;
+                    if (oob) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+                }
+            }
+#pragma unroll
+            for (int it = 0; it < kIts; ++it) {
+                const bool none = !(__shfl_sync(0xffffffffu, ks, block_of(it)) > 0.f);  // no scale: nothing was written, the values are 0
+                const uint32_t c[4] = {kb[it].x, kb[it].y, kb[it].z, kb[it].w};
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[2 * i] = none ? 0u : e4m3_lo(c[i]);
+                    w[2 * i + 1] = none ? 0u : e4m3_hi(c[i]);
+                }
+                store(G::kOffK + s * G::kTileBytes, block_of(it) * 16 + rowb, w);
+            }
+            publish(G::K_FULL + s);
+            float ks_next = 0.f, vs_next = 0.f;
+            if (j + 1 < n_tiles) {
+                load_tile(kb, ids_next, 0);
+                ks_next = load_scale(ids_next, 0);
+                vs_next = load_scale(ids_next, 1);
+            }
+            // ---- V: bf16 with the scale in it; zero rows past the last visible key
+            ok = j < kStages || wait_warp<D>(sh, G::V_EMPTY + s, ph, p);
+            if (!ok) break;
+#pragma unroll
+            for (int it = 0; it < kIts; ++it) {
+                const float scale = __shfl_sync(0xffffffffu, vs, block_of(it));
+                const int row = block_of(it) * 16 + rowb;
+                const bool none = j * kBN + row >= kv_end || !(scale > 0.f);
+                const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);
+                const uint32_t c[4] = {vb[it].x, vb[it].y, vb[it].z, vb[it].w};
+                uint32_t w[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 a = f16x2_to_float2(e4m3_lo(c[i])), b = f16x2_to_float2(e4m3_hi(c[i]));
+                    const __nv_bfloat162 x = __hmul2(__floats2bfloat162_rn(a.x, a.y), s2), y = __hmul2(__floats2bfloat162_rn(b.x, b.y), s2);
+                    w[2 * i] = none ? 0u : *reinterpret_cast<const uint32_t *>(&x);
+                    w[2 * i + 1] = none ? 0u : *reinterpret_cast<const uint32_t *>(&y);
+                }
+                store(G::kOffV + s * G::kTileBytes, row, w);
+            }
+            publish(G::V_FULL + s);
+            ids = ids_next;
+            ks = ks_next;
+            vs = vs_next;
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        // =========================== softmax + write-out ===========================
+        const int x = (warp - 4) >> 2;        // row tile
+        const int wrow0 = (warp & 3) << 5;    // TMEM lanes wrow0 .. +31 belong to this warp
+        const int row = wrow0 | lane;         // row of the tile = TMEM lane
+        const uint32_t t_s = tmem + ((uint32_t)wrow0 << 16) + 128 * x;
+        const uint32_t t_o = tmem + ((uint32_t)wrow0 << 16) + 256 + 128 * x;
+        if (x < nx) {
+            uint8_t *q_tile = sh.ptr + G::kOffQ + x * G::kTileBytes;
+            const int piece = lane % kPieces, sub = lane / kPieces;
+            // ---- Q rows of this warp: bf16 -> f16 with a row's largest magnitude in [2^13, 2^14), 128-byte swizzle
+#pragma unroll 4
+            for (int it = 0; it < 32 / kRowsPerInst; ++it) {
+                const int rr = wrow0 + kRowsPerInst * it + sub, in_item = x * kBM + rr;
+                const uint4 v = in_item < rows_here ? *reinterpret_cast<const uint4 *>(p.q + row_offset(in_item) + piece * 8) : make_uint4(0u, 0u, 0u, 0u);
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+                top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+                for (int o = kPieces / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                const float up = to_f16_range(__uint_as_float(top << 16));
+                const float f = up * pp.q_sign;
+                uint32_t h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __half2 y = __floats2half2_rn(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
+                    h[i] = *reinterpret_cast<const uint32_t *>(&y);
+                }
+                *reinterpret_cast<uint4 *>(q_tile + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                if (piece == 0) sh.q_inv()[in_item] = pow2_inverse(up);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.bar(G::Q_READY + x));
+            const float row_scale = p.scale_log2 * sh.q_inv()[x * kBM + row];
+
+            const int first_lim = prefix + (row0 + x * kBM) / group;                                  // last key the tile's first row may see
+            const int lim = prefix + (row0 + min(x * kBM + row, rows_here - 1)) / group;              // ... and this row
+            float m_run = -INFINITY, l_run = 0.f;
+            bool ok = true;
+            auto publish = [&](int bar) {  // this warp's 32 rows of P are in TMEM: one lane tells the MMA warp
+                cp::tcgen05_wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sh.bar(bar));
+            };
+            for (int j = 0; j < n_tiles; ++j) {
+                ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(j & 1), p);
+                if (!ok) break;
+                fence_after();
+                const int key0 = j * kBN;
+                const int bad = *sh.bad_mask(j);
+                // ---- the whole score row into registers (one TMEM read), masked entries become -inf
+                float sv[128];
+                {
+                    uint32_t(&r)[128] = reinterpret_cast<uint32_t(&)[128]>(sv);
+                    cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[0]), t_s);
+                    cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[32]), t_s + 32);
+                    cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[64]), t_s + 64);
+                    cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[96]), t_s + 96);
+                    cp::tcgen05_wait_ld();
+                }
+                float ks[8];
+                {
+                    const float4 a = *reinterpret_cast<const float4 *>(sh.k_scale(j)), b = *reinterpret_cast<const float4 *>(sh.k_scale(j) + 4);
+                    const float e[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ks[i] = fmaxf(e[i] * row_scale, 1.17549435e-38f);  // not 0: a masked score times it stays -inf
+                }
+                if (key0 + kBN - 1 > first_lim || bad != 0) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (key0 + i > lim || ((bad >> (i >> 4)) & 1)) sv[i] = -INFINITY;
+                }
+                float m_tile = -INFINITY;  // scaled: a block at a time
+#pragma unroll
+                for (int b = 0; b < 8; ++b) {
+                    float m0 = sv[16 * b], m1 = sv[16 * b + 1];
+#pragma unroll
+                    for (int i = 2; i < 16; i += 2) {
+                        m0 = fmaxf(m0, sv[16 * b + i]);
+                        m1 = fmaxf(m1, sv[16 * b + i + 1]);
+                    }
+                    m_tile = fmaxf(m_tile, fmaxf(m0, m1) * ks[b]);
+                }
+                // ---- lazy rescale: raise the reference max only when it is far behind
+                const bool raise = m_tile > m_run + tc::kRescaleThreshold;  // also true for the first finite tile
+                if (__any_sync(0xffffffffu, raise)) {
+                    const float m_new = raise ? m_tile : m_run;
+                    const float alpha = (raise && m_run > -INFINITY) ? fast_exp2(m_run - m_new) : (raise ? 0.f : 1.f);
+                    m_run = m_new;
+                    l_run *= alpha;
+                    if (j > 0) {  // O holds the sum over earlier tiles and no MMA touches it right now
+#pragma unroll
+                        for (int cc = 0; cc < D / 32; ++cc) {
+                            float ov[32];
+                            tc::tmem_ld32(ov, t_o + 32 * cc);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) ov[i] *= alpha;
+                            tc::tmem_st32(t_o + 32 * cc, ov);
+                        }
+                    }
+                }
+                const float m_use = m_run > -INFINITY ? m_run : 0.f;
+                // ---- P = exp2(S*scale - m) (a masked -inf gives 0), row sum, bf16 pairs into the S columns
+                float2 acc_a = make_float2(0.f, 0.f), acc_b = make_float2(0.f, 0.f);
+                const float2 nm2 = make_float2(-m_use, -m_use);
+#pragma unroll
+                for (int cc = 0; cc < 4; ++cc) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float2 sc2 = make_float2(ks[2 * cc + (i >> 4)], ks[2 * cc + (i >> 4)]);
+                        const float2 xa = __ffma2_rn(make_float2(sv[32 * cc + i], sv[32 * cc + i + 1]), sc2, nm2);
+                        const float2 xb = __ffma2_rn(make_float2(sv[32 * cc + i + 2], sv[32 * cc + i + 3]), sc2, nm2);
+                        const float2 pa = make_float2(fast_exp2(xa.x), fast_exp2(xa.y));
+                        const float2 pb = make_float2(fast_exp2(xb.x), fast_exp2(xb.y));
+                        acc_a = __fadd2_rn(acc_a, pa);
+                        acc_b = __fadd2_rn(acc_b, pb);
+                        pk[i >> 1] = pack_bf16x2(pa.x, pa.y);
+                        pk[(i >> 1) + 1] = pack_bf16x2(pb.x, pb.y);
+                    }
+                    cp::tcgen05_st_32x32b(t_s + 16 * cc, pk);
+                    if (cc == tc::kPartSteps / 2 - 1) publish(G::P_PART + x);  // 96 keys stored
+                }
+                l_run += (acc_a.x + acc_a.y) + (acc_b.x + acc_b.y);
+                publish(G::P_READY + x);
+            }
+
+            // ---- write-out: O / l -> bf16 -> the (now idle) Q tile in shared memory -> global, whole rows per instruction.
+            // Only the warp that wrote a row reads it: __syncwarp suffices.
+            if (ok) ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(n_tiles & 1), p);
+            if (ok) {
+                fence_after();  // every MMA that read this Q tile or wrote this O has completed (the commit covers all earlier ones)
+                const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+#pragma unroll
+                for (int cc = 0; cc < D / 32; ++cc) {
+                    float ov[32];
+                    tc::tmem_ld32(ov, t_o + 32 * cc);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8) {
+                        uint4 v;
+                        v.x = pack_bf16x2(ov[i] * inv, ov[i + 1] * inv);
+                        v.y = pack_bf16x2(ov[i + 2] * inv, ov[i + 3] * inv);
+                        v.z = pack_bf16x2(ov[i + 4] * inv, ov[i + 5] * inv);
+                        v.w = pack_bf16x2(ov[i + 6] * inv, ov[i + 7] * inv);
+                        const int c16 = cc * 4 + (i >> 3);
+                        *reinterpret_cast<uint4 *>(q_tile + row * (D * 2) + ((c16 ^ (row & (kPieces - 1))) << 4)) = v;
+                    }
+                }
+                __syncwarp();
+#pragma unroll 4
+                for (int it = 0; it < 32 / kRowsPerInst; ++it) {
+                    const int rr = wrow0 + kRowsPerInst * it + sub, in_item = x * kBM + rr;
+                    const uint4 v = *reinterpret_cast<const uint4 *>(q_tile + rr * (D * 2) + ((piece ^ (rr & (kPieces - 1))) << 4));
+                    if (in_item < rows_here) *reinterpret_cast<uint4 *>(p.out + row_offset(in_item) + piece * 8) = v;
+                }
+            }
+        }
+    }
+
+    // ---- teardown: everybody meets, TMEM goes back
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == 1) cp::tcgen05_dealloc(cp::cta_group_1, tmem, 512);
+}
+
+template <int D>
+static ekv_status_t launch_prefill8(ekv_pool *pool, const Params &pp, cudaStream_t stream) {
+    static bool attr_set[64] = {false};
+    const int dev = pool->desc.device;
+    if (dev >= 64 || !attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(prefill8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<D>::kSmemBytes);
+        if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: shared-memory attribute");
+        if (dev < 64) attr_set[dev] = true;
+    }
+    cudaError_t e = cudaMemsetAsync(pp.p.abort_word, 0, sizeof(int), stream);
+    if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: clear abort word");
+    prefill8_kernel<D><<<(unsigned)((long long)pp.p.q_tiles * pp.p.num_kv_heads), kThreads, Geo<D>::kSmemBytes, stream>>>(pp);
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: launch");
+    return EKV_OK;
+}
+
+}  // namespace tc8
+}  // namespace ekv

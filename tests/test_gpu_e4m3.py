@@ -365,6 +365,140 @@ def test_hoststep_runs_on_an_8_bit_pool():
         step.close()
 
 
+def check_prefill(c, chunks, scale=None, mag=1.0, tables=None, what=""):
+    """Request r's last chunks[r] tokens as its query rows."""
+    scale = 1 / math.sqrt(c.shape.head_dim) if scale is None else scale
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(chunks)]), dtype=torch.int32)
+    q = c.queries(int(cu[-1]), mag)
+    out = torch.full_like(q, 7.0).to(DEV)
+    c.pool.attn_prefill_chunk(0, q.to(DEV), c.d_tables if tables is None else tables, cu.to(DEV), cu, c.d_lens, scale, out=out)
+    for r, (n, L) in enumerate(zip(chunks, c.lengths)):
+        a, b = int(cu[r]), int(cu[r + 1])
+        if n > L:
+            assert (out[a:b] == 0).all(), what
+        elif n:
+            want, bound = M.attention(q[a:b].double(), c.K[r], c.V[r], torch.arange(L - n, L) + 1, scale)
+            M.assert_within(out[a:b], want, bound, f"{what} request {r}: {n} rows of {L}")
+    return q, cu, out
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_prefill_shapes(shape):
+    """Whole prompts, chunks over prefixes, single rows and empty requests; lengths around tiles of keys, items of rows and blocks."""
+    lengths = [1, 2, 16, 17, 0, 127, 128, 129, 300, 513, 40, 260, 255, 700]
+    chunks = [1, 1, 16, 17, 0, 127, 128, 129, 300, 200, 1, 256, 5, 33]
+    c = Case(shape, lengths, seed=71)
+    with c.pool:
+        q, cu, out = check_prefill(c, chunks)
+        again = c.pool.attn_prefill_chunk(0, q.to(DEV), c.d_tables, cu.to(DEV), cu, c.d_lens, 1 / math.sqrt(shape.head_dim))
+        assert torch.equal(out, again)
+        assert c.pool.poll_status() == ekv.Status.OK
+
+
+@pytest.mark.parametrize("shape", [I.TINY, I.LLAMA8B, I.Shape(28, 4, 128)], ids=str)
+def test_prefill_long_and_many(shape):
+    c = Case(shape, [3000], seed=81)
+    with c.pool:
+        for n in (3000, 1, 65, 777):
+            check_prefill(c, [n])
+    rng = np.random.default_rng(8)
+    lengths = rng.integers(1, 60, 300)  # more requests than the launch parameters hold offsets for
+    c = Case(shape, lengths, seed=82)
+    with c.pool:
+        check_prefill(c, [int(rng.integers(0, L + 1)) for L in lengths])
+        assert c.pool.poll_status() == ekv.Status.OK
+
+
+def test_prefill_magnitudes_and_scales():
+    shape = I.Shape(6, 2, 128)
+    c = Case(shape, [400, 40], seed=83)
+    with c.pool:
+        for mag, scale in ((1e-30, 0.1), (1e30, 1e-30), (300.0, 1e-3), (1.0, -0.1), (1.0, 0.0), (1e-38, 1e-3)):
+            check_prefill(c, [150, 40], scale, mag, what=f"queries x {mag}, scale {scale}")
+        n = c.pool.info.live_blocks
+        up = torch.from_numpy(c.rng.integers(-20, 21, (n, 2, 2))).to(DEV).float()
+        up[:, 0] = up[:, 0].clamp(-3, 1)
+        c.pool.layer_scales(0, 0, n).mul_(torch.exp2(up))
+        kk, vv = c.pool.read_kv(0, torch.cat(c.slots).to(DEV))
+        c.K, c.V = [kk[:400].double().cpu(), kk[400:].double().cpu()], [vv[:400].double().cpu(), vv[400:].double().cpu()]
+        check_prefill(c, [150, 40], 0.05, what="scales far apart")
+
+
+def test_prefill_invalid_blocks_and_requests():
+    shape = I.LLAMA8B
+    c = Case(shape, [300, 40, 16, 500, 3, 77], seed=84)
+    with c.pool:
+        t = c.d_tables.clone()
+        for b, j, bad in ((0, 3, -1), (0, 17, 1 << 30), (2, 0, -9), (3, 0, 1 << 20)):
+            t[b, j] = bad
+            c.K[b][16 * j:16 * j + 16] = float("nan")
+        q, cu, out = check_prefill(c, [300, 41, 16, 129, 9, 60], tables=t)  # the second and fifth have fewer keys than rows
+        assert (out[int(cu[2]):int(cu[3])] == 0).all()  # a request whose every key is skipped
+        assert c.pool.poll_status() == ekv.Status.ERR_BLOCK_OOB
+
+
+def test_prefill_never_written_blocks_read_as_zero():
+    """Scale 0: the values are 0, whatever the codes (here NaN)."""
+    shape = I.TINY
+    c = Case(shape, [64], seed=85)
+    with c.pool:
+        ids = c.tables[0, 1:3].long()
+        c.pool.layer_scales(0)[ids.to(DEV)] = 0.0
+        c.pool.layer_tensor(0).view(torch.uint8)[ids.to(DEV)] = 0x7F
+        c.K[0][16:48], c.V[0][16:48] = 0.0, 0.0
+        check_prefill(c, [64])
+
+
+def test_prefill_on_streams_and_in_a_replayed_graph():
+    shape = I.LLAMA8B
+    c = Case(shape, [700, 333, 90], seed=86)
+    with c.pool:
+        cu = torch.tensor([0, 200, 533, 560], dtype=torch.int32)
+        qs = [c.queries(560).to(DEV) for _ in range(4)]
+        dcu, want = cu.to(DEV), []
+        for q in qs:
+            want.append(c.pool.attn_prefill_chunk(0, q, c.d_tables, dcu, cu, c.d_lens, 0.09))
+        torch.cuda.synchronize()
+        streams, got = [torch.cuda.Stream() for _ in qs], [torch.empty_like(q) for q in qs]
+        for s, q, o in zip(streams, qs, got):
+            c.pool.attn_prefill_chunk(0, q, c.d_tables, dcu, cu, c.d_lens, 0.09, out=o, stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+        q, o = qs[0].clone(), torch.empty_like(qs[0])
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.pool.attn_prefill_chunk(0, q, c.d_tables, dcu, cu, c.d_lens, 0.09, out=o)
+        for a, b in zip(qs, want):
+            q.copy_(a)
+            g.replay()
+            assert torch.equal(o, b)
+
+
+def test_prompt_in_chunks_then_decode_steps():
+    """A run as it would be used: chunks written and attended to one after the other, then single tokens; every result against the
+    cache's own values, and the last decode step against the prefill of that one row."""
+    shape, rng = I.LLAMA8B, np.random.default_rng(87)
+    pool, _ = fresh(shape, 64)
+    with pool:
+        free, cursor = torch.from_numpy(rng.permutation(64).astype(np.int32)).to(DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        lens, tables = torch.zeros(1, dtype=torch.int32, device=DEV), torch.full((1, 40), -1, dtype=torch.int32, device=DEV)
+        for n in (100, 37, 250, 1, 1, 130, 1, 1):
+            slots, cu = torch.zeros(n, dtype=torch.int64, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+            pool.extend_tables(torch.tensor([n], dtype=torch.int32, device=DEV), lens, tables, free, cursor, slots, cu)
+            k, v = rows(rng, n, shape, 1.5).to(DEV), rows(rng, n, shape, 1.5).to(DEV)
+            pool.write_kv(0, k, v, slots)
+            q = torch.from_numpy(rng.standard_normal((n, 32, 128))).to(torch.bfloat16)
+            L = int(lens)
+            at = tables[0, torch.arange(L, device=DEV) // 16].long() * 16 + torch.arange(L, device=DEV) % 16
+            kk, vv = (x.double().cpu() for x in pool.read_kv(0, at))
+            want, bound = M.attention(q.double(), kk, vv, torch.arange(L - n, L) + 1, 0.09)
+            out = pool.attn_prefill_chunk(0, q.to(DEV), tables, cu, torch.tensor([0, n], dtype=torch.int32), lens, 0.09)
+            M.assert_within(out, want, bound, f"{n} rows of {L}")
+            if n == 1:
+                M.assert_within(pool.attn_decode(0, q.to(DEV), tables, lens, 0.09), want, bound, f"token {L}")
+        assert pool.poll_status() == ekv.Status.OK
+
+
 def test_a_view_keeps_its_pool():
     """The pool goes with its last name or view, whichever is later."""
     import weakref
