@@ -18,10 +18,15 @@
 //   warp 1        TMEM allocation; warps 2, 3 complete the warpgroup
 //   warps 4-7     rows 0-127: Q into shared memory, softmax (a thread a row), write-out
 //   warps 8-11    rows 128-255
-//   warps 12-15   converters: 16-byte loads of codes through the block table, one tile ahead in registers, conversion, swizzled
-//                 stores.  Keys past the item's last visible one become zero rows of V, so nothing a slot that was never
-//                 written holds can reach a sum (0 * NaN), and no code is needed for that elsewhere.
+//   warps 12-15   converters: codes come through the block table by 16-byte asynchronous copies into places of shared memory
+//                 that belong to the copying thread (so a thread waits for its own copies and for nobody), each place being
+//                 refilled for the next tile as soon as it has been read; conversion, swizzled stores.  Keys past the item's
+//                 last visible one become zero rows of V, so nothing a slot that was never written holds can reach a sum
+//                 (0 * NaN), and no code is needed for that elsewhere.
 // Softmax: online with lazy rescaling, as in the other tcgen05 kernels.  The sign of the scale is folded into Q.
+// The loops are kept rolled wherever that costs no registers: all roles of a quarter of the SM share an instruction cache
+// of about 32 KB (see ekv_prefill_tc.cuh), and with the converters' and the mask's loops unrolled (106 KB in all) every role ran at
+// 4 to 6 cycles an instruction.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -41,15 +46,16 @@ static constexpr int kThreads = 512;
 static constexpr int kHalfBytes = 128 * 128;  // [128 rows][64 16-bit channels], 128-byte swizzle
 static constexpr int kStages = 2;
 // setmaxnreg: warps 0-3 kRegsUtil, 4-11 kRegsSoftmax, 12-15 kRegsConv; the shares add up to what the CTA is launched with
-static constexpr int kLaunchRegs = 128, kRegsUtil = 40, kRegsSoftmax = 184, kRegsConv = 104;
+static constexpr int kLaunchRegs = 128, kRegsUtil = 40, kRegsSoftmax = 200, kRegsConv = 64;
 static_assert(128 * (kRegsUtil + kRegsConv) + 256 * kRegsSoftmax <= kLaunchRegs * kThreads, "setmaxnreg split exceeds the CTA's registers");
-static_assert(kRegsUtil == 40 && kRegsSoftmax == 184 && kRegsConv == 104, "the setmaxnreg instructions in the kernel carry these numbers as literals");
+static_assert(kRegsUtil == 40 && kRegsSoftmax == 200 && kRegsConv == 64, "the setmaxnreg instructions in the kernel carry these numbers as literals");
 
 struct Params {
     PrefillParams p;  // q_tiles, tile_prefix: in items of kItemRows rows per kv-head; scale_log2 >= 0
     const uint8_t *cache;
     const float *scales;
     long long block_stride;
+    unsigned group_magic;  // ceil(2^32 / group): a division by the group (2 or more) is one multiplication, exact below 2^29
     float q_sign;  // -1 for a negative scale; 0 for a scale of 0
 };
 
@@ -60,7 +66,9 @@ struct Geo {
     static constexpr int kOffQ = 0;
     static constexpr int kOffK = 2 * kTileBytes;
     static constexpr int kOffV = kOffK + kStages * kTileBytes;
-    static constexpr int kOffBar = kOffV + kStages * kTileBytes;
+    static constexpr int kRawBytes = 128 * D;  // a tile of codes
+    static constexpr int kOffRaw = kOffV + kStages * kTileBytes;  // one of K, one of V
+    static constexpr int kOffBar = kOffRaw + 2 * kRawBytes;
     enum Bar { Q_READY = 0, K_FULL = 2, K_EMPTY = 4, V_FULL = 6, V_EMPTY = 8, S_READY = 10, P_PART = 12, P_READY = 14, DRAIN = 16, NBAR = 17 };
     static constexpr int kOffFlags = kOffBar + 8 * NBAR;       // abort flag, TMEM address, 4 masks of invalid blocks
     static constexpr int kOffKScale = kOffBar + 192;           // [4 tiles][8 blocks] floats
@@ -86,30 +94,12 @@ struct Smem {
     __device__ __forceinline__ float *q_inv() const { return (float *)(ptr + Geo<D>::kOffQInv); }
 };
 
-// Bounded wait of a whole warp that also gives up as soon as another role has flagged an abort.
+// Bounded wait of a whole warp, as in the two-head kernel: one poll and a vote, then a polling loop of a dozen instructions that
+// gives up when another role has, or after tc::kPollLimit polls (it leaves 2 in the abort flag; the teardown reports it).
 template <int D>
-__device__ __forceinline__ bool wait_warp(const Smem<D> &sh, int bar, uint32_t parity, const PrefillParams &p) {
-    const uint32_t b = sh.bar(bar);
-    bool ok = mbar_try_wait(b, parity);
-    if (!ok) {
-        const uint64_t t0 = global_timer_ns();
-        for (uint32_t i = 1;; ++i) {
-            if (mbar_try_wait(b, parity)) {
-                ok = true;
-                break;
-            }
-            if ((i & 31u) == 0u) {
-                if (*sh.abort_flag()) break;
-                if (global_timer_ns() - t0 > 2000000000ull) {
-                    *sh.abort_flag() = 1;
-                    *(volatile int *)p.abort_word = 1;
-                    atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);
-                    break;
-                }
-            }
-        }
-    }
-    return __all_sync(0xffffffffu, ok);
+__device__ __forceinline__ bool wait_warp(const Smem<D> &sh, int bar, uint32_t parity) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(sh.bar(bar), parity))) return true;
+    return __all_sync(0xffffffffu, mbar_wait_polls(sh.bar(bar), parity, sh.base + Geo<D>::kOffFlags, tc::kPollLimit));
 }
 
 // Which request owns item `idx` (items of kItemRows (position, head) rows, requests in order)?
@@ -150,8 +140,9 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     const int prefix = L - c_r;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // element offset of a row of the item in q and out
+    auto position = [&](int r) { return group == 1 ? row0 + r : (int)__umulhi((unsigned)(row0 + r), pp.group_magic); };
     auto row_offset = [&](int r) {
-        const int pos = (row0 + r) / group, hg = row0 + r - pos * group;
+        const int pos = position(r), hg = row0 + r - pos * group;
         return ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D;
     };
 
@@ -161,7 +152,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             *reinterpret_cast<uint4 *>(p.out + row_offset(e / kPieces) + (e % kPieces) * 8) = make_uint4(0u, 0u, 0u, 0u);
         return;
     }
-    const int kv_end = min(L, prefix + (row0 + rows_here - 1) / group + 1);  // keys any row of the item may see
+    const int kv_end = min(L, prefix + position(rows_here - 1) + 1);  // keys any row of the item may see
     const int n_tiles = (kv_end + kBN - 1) / kBN;
     const int n_blocks = (kv_end + 15) >> 4;
     const int nx = rows_here > kBM ? 2 : 1;  // row tiles
@@ -181,8 +172,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             mbar_init(sh.bar(G::V_FULL + x), 4);
             mbar_init(sh.bar(G::V_EMPTY + x), 1);
             mbar_init(sh.bar(G::S_READY + x), 1);
-            mbar_init(sh.bar(G::P_PART + x), 4);
-            mbar_init(sh.bar(G::P_READY + x), 4);
+            mbar_init(sh.bar(G::P_PART + x), 128);
+            mbar_init(sh.bar(G::P_READY + x), 128);
         }
         mbar_init(sh.bar(G::DRAIN), 1);
         *sh.abort_flag() = 0;
@@ -204,75 +195,77 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             constexpr uint64_t kHi = (uint64_t)tc::kDescHi << 32;
             const uint64_t q_d = kHi | tc::desc_lo(sh.base + G::kOffQ, 16), k_d = kHi | tc::desc_lo(sh.base + G::kOffK, 16),
                            v_d = kHi | tc::desc_lo(sh.base + G::kOffV, kHalfBytes);
-            auto issue_qk = [&](int x, int s) {  // S_x = Q_x K(s)^T
-                if (tc::elect_one()) {
-                    const uint64_t qd = q_d + (uint32_t)x * (G::kTileBytes >> 4), kd = k_d + (uint32_t)s * (G::kTileBytes >> 4);
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
-                        tc::mma_ss(tmem + 128 * x, qd + off, kd + off, G::kIdescQK, k > 0 ? 1u : 0u);
-                    }
-                }
-                __syncwarp();
-            };
-            auto issue_pv = [&](int x, int s, bool acc, int k0, int k1) {  // O_x (+)= P_x[:, 16 k0 : 16 k1] V(s)[16 k0 : 16 k1, :]
-                if (tc::elect_one()) {
-                    const uint64_t vd = v_d + (uint32_t)s * (G::kTileBytes >> 4);
-#pragma unroll
-                    for (int k = 0; k < kBN / 16; ++k)
-                        if (k >= k0 && k < k1) tc::mma_ts(tmem + 256 + 128 * x, tmem + 128 * x + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, (acc || k > 0) ? 1u : 0u);
-                }
-                __syncwarp();
-            };
-            bool ok = wait_warp<D>(sh, G::K_FULL, 0, p);
-            for (int x = 0; x < nx && ok; ++x) {
-                ok = wait_warp<D>(sh, G::Q_READY + x, 0, p);
-                if (!ok) break;
-                fence_after();
-                issue_qk(x, 0);
-                if (x == nx - 1) tc::mma_commit(sh.bar(G::K_EMPTY));
-                tc::mma_commit(sh.bar(G::S_READY + x));
-            }
-            for (int j = 0; j < n_tiles && ok; ++j) {
+            bool ok = wait_warp<D>(sh, G::K_FULL, 0);
+            // Step j = -1 only brings the first scores.  One elected lane issues a step's run for a row tile in one go: the last
+            // quarter of PV, QK^T of the next key tile, the commits.
+#pragma unroll 1
+            for (int j = -1; j < n_tiles && ok; ++j) {
                 const int s = j & 1, s1 = s ^ 1;
-                const bool more = j + 1 < n_tiles;
-                ok = wait_warp<D>(sh, G::V_FULL + s, (uint32_t)((j >> 1) & 1), p);
+                int pv = j >= 0, more = j + 1 < n_tiles;
+                asm volatile("" : "+r"(pv), "+r"(more));  // one copy of the loop, not one for each combination
+                if (pv) ok = wait_warp<D>(sh, G::V_FULL + s, (uint32_t)((j >> 1) & 1));
+#pragma unroll 1
                 for (int x = 0; x < nx && ok; ++x) {
-                    ok = wait_warp<D>(sh, G::P_PART + x, (uint32_t)(j & 1), p);
-                    if (!ok) break;
-                    fence_after();
-                    issue_pv(x, s, j > 0, 0, tc::kPartSteps);  // keys 0..95 while the softmax warps finish the rest
-                    ok = wait_warp<D>(sh, G::P_READY + x, (uint32_t)(j & 1), p);
-                    if (!ok) break;
-                    fence_after();
-                    issue_pv(x, s, true, tc::kPartSteps, kBN / 16);
-                    if (x == nx - 1) tc::mma_commit(sh.bar(G::V_EMPTY + s));
-                    if (more) {
-                        if (x == 0) ok = wait_warp<D>(sh, G::K_FULL + s1, (uint32_t)(((j + 1) >> 1) & 1), p);
+                    const uint32_t t_s = tmem + 128 * x, t_o = tmem + 256 + 128 * x;
+                    const uint64_t vd = v_d + (uint32_t)s * (G::kTileBytes >> 4);
+                    if (pv) {
+                        ok = wait_warp<D>(sh, G::P_PART + x, (uint32_t)(j & 1));
                         if (!ok) break;
                         fence_after();
-                        issue_qk(x, s1);
-                        if (x == nx - 1) tc::mma_commit(sh.bar(G::K_EMPTY + s1));
+                        if (tc::elect_one()) {  // keys 0..95 while the softmax warps finish the rest
+#pragma unroll
+                            for (int k = 0; k < tc::kPartSteps; ++k)
+                                tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, (j > 0 || k > 0) ? 1u : 0u);
+                        }
+                        __syncwarp();
+                        ok = wait_warp<D>(sh, G::P_READY + x, (uint32_t)(j & 1));
+                    } else {
+                        ok = wait_warp<D>(sh, G::Q_READY + x, 0);
                     }
-                    tc::mma_commit(sh.bar(G::S_READY + x));  // the next scores, and O up to this tile
+                    if (ok && more && x == 0) ok = wait_warp<D>(sh, G::K_FULL + s1, (uint32_t)(((j + 1) >> 1) & 1));
+                    if (!ok) break;
+                    fence_after();
+                    if (tc::elect_one()) {
+                        if (pv) {
+#pragma unroll
+                            for (int k = tc::kPartSteps; k < kBN / 16; ++k) tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, 1u);
+                            if (x == nx - 1) tc::mma_commit_one(sh.bar(G::V_EMPTY + s));
+                        }
+                        if (more) {
+                            const uint64_t qd = q_d + (uint32_t)x * (G::kTileBytes >> 4), kd = k_d + (uint32_t)s1 * (G::kTileBytes >> 4);
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k) {
+                                const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
+                                tc::mma_ss(t_s, qd + off, kd + off, G::kIdescQK, k > 0 ? 1u : 0u);
+                            }
+                            if (x == nx - 1) tc::mma_commit_one(sh.bar(G::K_EMPTY + s1));
+                        }
+                        tc::mma_commit_one(sh.bar(G::S_READY + x));  // the next scores, and O up to this tile
+                    }
+                    __syncwarp();
                 }
             }
             // every MMA this thread issued must be finished before TMEM is released
             tc::mma_commit(sh.bar(G::DRAIN));
-            (void)wait_warp<D>(sh, G::DRAIN, 0, p);
+            (void)wait_warp<D>(sh, G::DRAIN, 0);
         }
     } else if (warp >= 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         // =========================== converters ===========================
-        constexpr int kIts = D / 16;                  // 16-byte pieces of codes a thread takes of a tile
+        constexpr int kIts = D / 16;                       // 16-byte pieces of codes a thread takes of a tile
         constexpr int kBlocksPerIt = 128 * 16 / (16 * D);  // blocks the 128 threads cover at once: 1, or 2 at head_dim 64
         const int ct = threadIdx.x - 384;
-        const int in_block = ct % D;                  // 16 * D bytes of a block are D pieces
-        const int rowb = in_block / (D / 16), piece = in_block % (D / 16);
+        // Which 16 bytes of a block: eight neighbouring lanes take four pieces of two rows, so that their stores into the
+        // 128-byte swizzled tile (two chunks a piece) never meet in a bank.
+        const int in_block = ct % D;                       // 16 * D bytes of a block are D pieces
+        const int rowb = D == 128 ? (in_block >> 5 << 2) | ((in_block >> 3) & 2) | ((in_block >> 2) & 1) : in_block >> 2;
+        const int piece = D == 128 ? ((in_block >> 1) & 4) | (in_block & 3) : in_block & 3;
+        const int first_block = kBlocksPerIt > 1 ? ct / D : 0;
         const long long live = *p.live;
         const int *bt = p.block_tables + (size_t)req * p.max_blocks;
-        const uint8_t *src = pp.cache + (long long)g * (16 * D) + in_block * 16;
+        const uint8_t *src = pp.cache + (long long)g * (16 * D) + rowb * D + piece * 16;
         const long long v_off = (long long)p.num_kv_heads * (16 * D);
+        const uint32_t raw = sh.base + G::kOffRaw + ct * 16;  // this thread's places: one every 2048 bytes
         // lane l: id of block 8j + l % 8 of tile j (-1 past the end, -2 invalid)
         auto load_id = [&](int j) {
             int id = -1;
@@ -283,42 +276,42 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             }
             return id;
         };
-        auto load_tile = [&](uint4 (&buf)[kIts], int ids, int kv) {
-#pragma unroll
-            for (int it = 0; it < kIts; ++it) {
-                const int id = __shfl_sync(0xffffffffu, ids, it * kBlocksPerIt + (kBlocksPerIt > 1 ? ct / D : 0));
-                buf[it] = id >= 0 ? __ldg(reinterpret_cast<const uint4 *>(src + id * pp.block_stride + (kv ? v_off : 0))) : make_uint4(0u, 0u, 0u, 0u);
-            }
-        };
         auto load_scale = [&](int ids, int kv) { return ids >= 0 ? __ldg(pp.scales + ((long long)ids * 2 + kv) * p.num_kv_heads + g) : 0.f; };
-        // 16 codes of one row -> two 16-byte chunks of the 128-byte swizzled tile; lanes of the upper half tile store theirs in
-        // the other order, so that eight lanes never meet in a bank
-        const uint32_t half_off = (uint32_t)(piece >> 2) * kHalfBytes;
-        const int c0 = 2 * (piece & 3) + ((D == 128 && piece >= 4) ? 1 : 0);
-        auto store = [&](uint32_t tile_off, int row, const uint32_t (&w)[8]) {
-            uint8_t *at = sh.ptr + tile_off + half_off + row * 128;
-            const bool flip = c0 & 1;
-            *reinterpret_cast<uint4 *>(at + ((c0 ^ (row & 7)) << 4)) = flip ? make_uint4(w[4], w[5], w[6], w[7]) : make_uint4(w[0], w[1], w[2], w[3]);
-            *reinterpret_cast<uint4 *>(at + (((c0 ^ 1) ^ (row & 7)) << 4)) = flip ? make_uint4(w[0], w[1], w[2], w[3]) : make_uint4(w[4], w[5], w[6], w[7]);
+        auto copy = [&](int it, int ids, int kv) {  // piece `it` of this thread; an invalid block's codes read as 0
+            const int id = __shfl_sync(0xffffffffu, ids, it * kBlocksPerIt + first_block);
+            cp_async_16(raw + kv * G::kRawBytes + it * 2048, src + (long long)max(id, 0) * pp.block_stride + (kv ? v_off : 0), id >= 0 ? 16u : 0u);
         };
-        auto block_of = [&](int it) { return it * kBlocksPerIt + (kBlocksPerIt > 1 ? ct / D : 0); };
+        // 16 values of one row -> two 16-byte chunks of the tile
+        auto store = [&](uint32_t tile_off, int row, const uint32_t (&w)[8]) {
+            uint8_t *at = sh.ptr + tile_off + (piece >> 2) * kHalfBytes + row * 128;
+            const int c = (2 * (piece & 3)) ^ (row & 7);
+            *reinterpret_cast<uint4 *>(at + (c << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4 *>(at + ((c ^ 1) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+        };
         auto publish = [&](int bar) {
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.bar(bar));
         };
-        uint4 kb[kIts], vb[kIts];
         int ids = load_id(0);
         float ks = load_scale(ids, 0), vs = load_scale(ids, 1);
-        load_tile(kb, ids, 0);
+#pragma unroll 1
+        for (int it = 0; it < kIts; ++it) copy(it, ids, 0);
+        cp_async_commit();
+#pragma unroll 1
+        for (int it = 0; it < kIts; ++it) copy(it, ids, 1);
+        cp_async_commit();
+        int ids_next = 1 < n_tiles ? load_id(1) : -1;
         bool ok = true;
+#pragma unroll 1
         for (int j = 0; j < n_tiles; ++j) {
             const int s = j & 1;
             const uint32_t ph = (uint32_t)(((j >> 1) - 1) & 1);
-            load_tile(vb, ids, 1);
-            const int ids_next = j + 1 < n_tiles ? load_id(j + 1) : -1;
+            const int ids_after = j + 2 < n_tiles ? load_id(j + 2) : -1;
+            const float ks_next = load_scale(ids_next, 0), vs_next = load_scale(ids_next, 1);
             // ---- K: f16, scales beside it
-            ok = j < kStages || wait_warp<D>(sh, G::K_EMPTY + s, ph, p);
+            cp_async_wait_1();
+            ok = j < kStages || wait_warp<D>(sh, G::K_EMPTY + s, ph);
             if (!ok) break;
             if (warp == 12) {
                 const unsigned bad = __ballot_sync(0xffffffffu, ids < 0) & 0xffu;  // invalid, or past the last visible key
@@ -329,52 +322,54 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     if (oob) atomicOr(p.status, EKV_DEV_FLAG_OOB);
                 }
             }
-#pragma unroll
+#pragma unroll 2
             for (int it = 0; it < kIts; ++it) {
-                const bool none = !(__shfl_sync(0xffffffffu, ks, block_of(it)) > 0.f);  // no scale: nothing was written, the values are 0
-                const uint32_t c[4] = {kb[it].x, kb[it].y, kb[it].z, kb[it].w};
-                uint32_t w[8];
+                const int blk = it * kBlocksPerIt + first_block;
+                const uint4 v = lds_16(raw + it * 2048);
+                copy(it, ids_next, 0);  // the place is free: the next tile's codes
+                uint32_t c[4] = {v.x, v.y, v.z, v.w}, w[8];
+                if (!(__shfl_sync(0xffffffffu, ks, blk) > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;  // no scale: nothing was written, the values are 0
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    w[2 * i] = none ? 0u : e4m3_lo(c[i]);
-                    w[2 * i + 1] = none ? 0u : e4m3_hi(c[i]);
+                    w[2 * i] = e4m3_lo(c[i]);
+                    w[2 * i + 1] = e4m3_hi(c[i]);
                 }
-                store(G::kOffK + s * G::kTileBytes, block_of(it) * 16 + rowb, w);
+                store(G::kOffK + s * G::kTileBytes, blk * 16 + rowb, w);
             }
+            cp_async_commit();
             publish(G::K_FULL + s);
-            float ks_next = 0.f, vs_next = 0.f;
-            if (j + 1 < n_tiles) {
-                load_tile(kb, ids_next, 0);
-                ks_next = load_scale(ids_next, 0);
-                vs_next = load_scale(ids_next, 1);
-            }
             // ---- V: bf16 with the scale in it; zero rows past the last visible key
-            ok = j < kStages || wait_warp<D>(sh, G::V_EMPTY + s, ph, p);
+            cp_async_wait_1();
+            ok = j < kStages || wait_warp<D>(sh, G::V_EMPTY + s, ph);
             if (!ok) break;
-#pragma unroll
+#pragma unroll 2
             for (int it = 0; it < kIts; ++it) {
-                const float scale = __shfl_sync(0xffffffffu, vs, block_of(it));
-                const int row = block_of(it) * 16 + rowb;
-                const bool none = j * kBN + row >= kv_end || !(scale > 0.f);
+                const int blk = it * kBlocksPerIt + first_block, row = blk * 16 + rowb;
+                const uint4 v = lds_16(raw + G::kRawBytes + it * 2048);
+                copy(it, ids_next, 1);
+                uint32_t c[4] = {v.x, v.y, v.z, v.w}, w[8];
+                const float scale = __shfl_sync(0xffffffffu, vs, blk);
+                if (j * kBN + row >= kv_end || !(scale > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;
                 const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);
-                const uint32_t c[4] = {vb[it].x, vb[it].y, vb[it].z, vb[it].w};
-                uint32_t w[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float2 a = f16x2_to_float2(e4m3_lo(c[i])), b = f16x2_to_float2(e4m3_hi(c[i]));
                     const __nv_bfloat162 x = __hmul2(__floats2bfloat162_rn(a.x, a.y), s2), y = __hmul2(__floats2bfloat162_rn(b.x, b.y), s2);
-                    w[2 * i] = none ? 0u : *reinterpret_cast<const uint32_t *>(&x);
-                    w[2 * i + 1] = none ? 0u : *reinterpret_cast<const uint32_t *>(&y);
+                    w[2 * i] = *reinterpret_cast<const uint32_t *>(&x);
+                    w[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&y);
                 }
                 store(G::kOffV + s * G::kTileBytes, row, w);
             }
+            cp_async_commit();
             publish(G::V_FULL + s);
             ids = ids_next;
+            ids_next = ids_after;
             ks = ks_next;
             vs = vs_next;
         }
+        cp_async_wait_all();  // what was started for a tile that does not come (or after a wait that was given up)
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // =========================== softmax + write-out ===========================
         const int x = (warp - 4) >> 2;        // row tile
         const int wrow0 = (warp & 3) << 5;    // TMEM lanes wrow0 .. +31 belong to this warp
@@ -384,11 +379,21 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         if (x < nx) {
             uint8_t *q_tile = sh.ptr + G::kOffQ + x * G::kTileBytes;
             const int piece = lane % kPieces, sub = lane / kPieces;
-            // ---- Q rows of this warp: bf16 -> f16 with a row's largest magnitude in [2^13, 2^14), 128-byte swizzle
-#pragma unroll 4
+            // ---- Q rows of this warp: all of them on their way at once, straight to where they belong in the 128-byte swizzled
+            // tile, then bf16 -> f16 in place with a row's largest magnitude in [2^13, 2^14); rows past the end are 0
+            auto q_place = [&](int rr) { return (uint32_t)(G::kOffQ + x * G::kTileBytes + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4)); };
+#pragma unroll 1
             for (int it = 0; it < 32 / kRowsPerInst; ++it) {
                 const int rr = wrow0 + kRowsPerInst * it + sub, in_item = x * kBM + rr;
-                const uint4 v = in_item < rows_here ? *reinterpret_cast<const uint4 *>(p.q + row_offset(in_item) + piece * 8) : make_uint4(0u, 0u, 0u, 0u);
+                const bool there = in_item < rows_here;
+                cp_async_16(sh.base + q_place(rr), p.q + row_offset(there ? in_item : 0) + piece * 8, there ? 16u : 0u);
+            }
+            cp_async_commit();
+            cp_async_wait_all();
+#pragma unroll 1
+            for (int it = 0; it < 32 / kRowsPerInst; ++it) {
+                const int rr = wrow0 + kRowsPerInst * it + sub;
+                const uint4 v = lds_16(sh.base + q_place(rr));
                 const uint32_t w[4] = {v.x, v.y, v.z, v.w};
                 uint32_t top = 0;
 #pragma unroll
@@ -404,31 +409,50 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     const __half2 y = __floats2half2_rn(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
                     h[i] = *reinterpret_cast<const uint32_t *>(&y);
                 }
-                *reinterpret_cast<uint4 *>(q_tile + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-                if (piece == 0) sh.q_inv()[in_item] = pow2_inverse(up);
+                *reinterpret_cast<uint4 *>(sh.ptr + q_place(rr)) = make_uint4(h[0], h[1], h[2], h[3]);
+                if (piece == 0) sh.q_inv()[x * kBM + rr] = pow2_inverse(up);
             }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.bar(G::Q_READY + x));
             const float row_scale = p.scale_log2 * sh.q_inv()[x * kBM + row];
 
-            const int first_lim = prefix + (row0 + x * kBM) / group;                                  // last key the tile's first row may see
-            const int lim = prefix + (row0 + min(x * kBM + row, rows_here - 1)) / group;              // ... and this row
+            const int first_lim = prefix + position(x * kBM);                              // last key the tile's first row may see
+            const int lim = prefix + position(min(x * kBM + row, rows_here - 1));          // ... and this row
             float m_run = -INFINITY, l_run = 0.f;
             bool ok = true;
-            auto publish = [&](int bar) {  // this warp's 32 rows of P are in TMEM: one lane tells the MMA warp
+            auto publish = [&](int bar) {  // this thread's row of P is in TMEM
                 cp::tcgen05_wait_st();
                 fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(sh.bar(bar));
+                mbar_arrive(sh.bar(bar));
             };
+#pragma unroll 1
             for (int j = 0; j < n_tiles; ++j) {
-                ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(j & 1), p);
+                ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(j & 1));
                 if (!ok) break;
                 fence_after();
                 const int key0 = j * kBN;
                 const int bad = *sh.bad_mask(j);
-                // ---- the whole score row into registers (one TMEM read), masked entries become -inf
+                // ---- a tile that the causal boundary cuts, or that holds a block the table does not name, first gets its hidden
+                // scores overwritten with -inf in TMEM, and then runs through the same code as every other one
+                if (key0 + kBN - 1 > first_lim || bad != 0) {
+                    const int rel = lim - key0;  // this row sees columns 0..rel
+                    const int rel_min = __reduce_min_sync(0xffffffffu, rel);
+#pragma unroll 1
+                    for (int cc = 0; cc < 4; ++cc) {
+                        const unsigned b2 = ((unsigned)bad >> (2 * cc)) & 3u;
+                        if (32 * cc + 31 <= rel_min && b2 == 0u) continue;
+                        const int r = rel - 32 * cc;
+                        const unsigned past = r >= 31 ? 0u : (r < 0 ? 0xffffffffu : 0xfffffffeu << r);
+                        const unsigned hid = past | ((b2 & 1u) ? 0x0000ffffu : 0u) | ((b2 & 2u) ? 0xffff0000u : 0u);
+                        float v[32];
+                        tc::tmem_ld32(v, t_s + 32 * cc);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = ((hid >> i) & 1u) ? -INFINITY : v[i];
+                        tc::tmem_st32(t_s + 32 * cc, v);
+                    }
+                    cp::tcgen05_wait_st();
+                }
                 float sv[128];
                 {
                     uint32_t(&r)[128] = reinterpret_cast<uint32_t(&)[128]>(sv);
@@ -444,11 +468,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     const float e[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
                     for (int i = 0; i < 8; ++i) ks[i] = fmaxf(e[i] * row_scale, 1.17549435e-38f);  // not 0: a masked score times it stays -inf
-                }
-                if (key0 + kBN - 1 > first_lim || bad != 0) {
-#pragma unroll
-                    for (int i = 0; i < 128; ++i)
-                        if (key0 + i > lim || ((bad >> (i >> 4)) & 1)) sv[i] = -INFINITY;
                 }
                 float m_tile = -INFINITY;  // scaled: a block at a time
 #pragma unroll
@@ -469,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     m_run = m_new;
                     l_run *= alpha;
                     if (j > 0) {  // O holds the sum over earlier tiles and no MMA touches it right now
-#pragma unroll
+#pragma unroll 1
                         for (int cc = 0; cc < D / 32; ++cc) {
                             float ov[32];
                             tc::tmem_ld32(ov, t_o + 32 * cc);
@@ -507,11 +526,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
 
             // ---- write-out: O / l -> bf16 -> the (now idle) Q tile in shared memory -> global, whole rows per instruction.
             // Only the warp that wrote a row reads it: __syncwarp suffices.
-            if (ok) ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(n_tiles & 1), p);
+            if (ok) ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(n_tiles & 1));
             if (ok) {
                 fence_after();  // every MMA that read this Q tile or wrote this O has completed (the commit covers all earlier ones)
                 const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-#pragma unroll
+#pragma unroll 1
                 for (int cc = 0; cc < D / 32; ++cc) {
                     float ov[32];
                     tc::tmem_ld32(ov, t_o + 32 * cc);
@@ -527,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     }
                 }
                 __syncwarp();
-#pragma unroll 4
+#pragma unroll 2
                 for (int it = 0; it < 32 / kRowsPerInst; ++it) {
                     const int rr = wrow0 + kRowsPerInst * it + sub, in_item = x * kBM + rr;
                     const uint4 v = *reinterpret_cast<const uint4 *>(q_tile + rr * (D * 2) + ((piece ^ (rr & (kPieces - 1))) << 4));
@@ -541,6 +560,10 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     fence_before();
     __syncthreads();
     fence_after();
+    if (threadIdx.x == 0 && *sh.abort_flag()) {  // a wait ran out: report it, and keep the launch's other CTAs from starting
+        *(volatile int *)p.abort_word = 1;
+        atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);
+    }
     if (warp == 1) cp::tcgen05_dealloc(cp::cta_group_1, tmem, 512);
 }
 
