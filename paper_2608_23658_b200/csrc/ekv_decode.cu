@@ -321,6 +321,7 @@ __global__ void __launch_bounds__(D) decode_combine_kernel(const DecodeParams p)
     const int bh = blockIdx.x;
     const int b = bh / p.num_q_heads;
     const int x = threadIdx.x;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // 8-bit pools launch this kernel early; else there is nothing to wait for
     int L = p.seq_lens[b];
     L = max(0, min(L, p.max_blocks * 16));
     const int ns = (L + p.chunk_tokens - 1) / p.chunk_tokens;
@@ -345,6 +346,13 @@ __global__ void __launch_bounds__(D) decode_combine_kernel(const DecodeParams p)
             const int n = min(D, ns - s0);
             const float *src = po + (size_t)s0 * D + x;
             int i = 0;
+            for (; i + 16 <= n; i += 16) {  // sixteen loads in flight, added in the same order as one by one
+                float o[16];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) o[u] = src[(size_t)(i + u) * D];
+#pragma unroll
+                for (int u = 0; u < 16; ++u) acc += w_tile[i + u] * o[u];
+            }
             for (; i + 4 <= n; i += 4) {
                 const float o0 = src[(size_t)i * D], o1 = src[(size_t)(i + 1) * D];
                 const float o2 = src[(size_t)(i + 2) * D], o3 = src[(size_t)(i + 3) * D];
@@ -458,7 +466,7 @@ static DecodeParams make_decode_params(const ekv_pool *pool, const DecodePlan &p
 
 template <int D>
 static ekv_status_t launch_decode8(ekv_pool *pool, int layer, const DecodeParams &p, int B, cudaStream_t stream) {
-    constexpr int kBytes = kDecodeWarps * kDecode8Stages * (2 * 16 * D + 8) + 1024;
+    constexpr int kBytes = kDecodeWarps * kDecode8Stages<D> * (2 * 16 * D + 8) + 1024;
     static bool attr_set[64] = {false};
     const int dev = pool->desc.device;
     if (dev >= 64 || !attr_set[dev]) {
@@ -471,8 +479,16 @@ static ekv_status_t launch_decode8(ekv_pool *pool, int layer, const DecodeParams
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_decode: split launch");
     if (p.nsplit == 1) return EKV_OK;  // the split kernel wrote the final rows itself
-    decode_combine_kernel<D><<<B * pool->desc.num_q_heads, D, 0, stream>>>(p);
-    e = cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};  // launched while the split pass runs out: its CTAs wait for that pass's end on the GPU
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((unsigned)(B * pool->desc.num_q_heads));
+    cfg.blockDim = dim3(D);
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, decode_combine_kernel<D>, p);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_decode: combine launch");
     return EKV_OK;
 }

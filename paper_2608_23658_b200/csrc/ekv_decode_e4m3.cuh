@@ -21,7 +21,13 @@
 
 namespace ekv {
 
-static constexpr int kDecode8Stages = 6;
+// Four CTAs share an SM, with rings of 4 to 8 KiB a warp (64 to 128 KiB in flight per SM).  The bf16 kernel's two CTAs with
+// rings three times as deep leave this kernel at 0.72 of the copy rate: converting makes a block's chain of instructions long,
+// and it takes four warps a scheduler to hide it (256 sequences of 2048..8192 keys, 32q/8kv: 2 CTAs x 6 stages 540 us, 3 x 4
+// 429, 4 x 3 416, 4 x 2 411, 5 x 2 427, 6 x 2 505 -- registers are spilled from 5 on).
+static constexpr int kDecode8Ctas = 4;
+template <int D>
+constexpr int kDecode8Stages = D == 128 ? 2 : 4;
 
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -37,8 +43,9 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(kDecodeWarps * 32, 2)
+__global__ void __launch_bounds__(kDecodeWarps * 32, kDecode8Ctas)
 decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodeParams p, const float *__restrict__ scales) {
+    constexpr int STAGES = kDecode8Stages<D>;
     constexpr int TILE_BYTES = 16 * D;  // 16 tokens of K (or V) of one head
     constexpr int STAGE_BYTES = 2 * TILE_BYTES;
     constexpr int KSTEPS = D / 16;
@@ -65,12 +72,12 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
     const uint32_t raw_u32 = smem_u32(smem_raw);
     const uint32_t base_u32 = (raw_u32 + 1023u) & ~1023u;
     uint8_t *base_ptr = smem_raw + (base_u32 - raw_u32);
-    const uint32_t my_stages = base_u32 + warp * kDecode8Stages * STAGE_BYTES;
-    const uint32_t my_bars = base_u32 + kDecodeWarps * kDecode8Stages * STAGE_BYTES + warp * kDecode8Stages * 8;
+    const uint32_t my_stages = base_u32 + warp * STAGES * STAGE_BYTES;
+    const uint32_t my_bars = base_u32 + kDecodeWarps * STAGES * STAGE_BYTES + warp * STAGES * 8;
 
     if (lane == 0) {
         prefetch_tensormap(&kvmap);
-        for (int s = 0; s < kDecode8Stages; ++s) mbar_init(my_bars + 8 * s, 1);
+        for (int s = 0; s < STAGES; ++s) mbar_init(my_bars + 8 * s, 1);
         mbar_fence_init();
     }
     __syncwarp();
@@ -87,7 +94,7 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
     auto issue = [&](int i) {
         const int id = __shfl_sync(FULL, my_id, i);
         if (lane == 0 && ((valid_mask >> i) & 1u)) {
-            const int stage = i % kDecode8Stages;
+            const int stage = i % STAGES;
             const uint32_t bar = my_bars + 8 * stage;
             const uint32_t dst = my_stages + stage * STAGE_BYTES;
             mbar_expect_tx(bar, STAGE_BYTES);
@@ -95,13 +102,15 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
             tma_load_3d_hint(dst + TILE_BYTES, &kvmap, 0, (p.num_kv_heads + g) * 16, id, bar, policy);
         }
     };
-    for (int s = 0; s < kDecode8Stages && s < nw; ++s) issue(s);
+    for (int s = 0; s < STAGES && s < nw; ++s) issue(s);
     float my_sk = 0.f, my_sv = 0.f;
     if (my_ok) {
         const float *at = scales + (size_t)my_id * 2 * p.num_kv_heads + g;
         my_sk = at[0];
         my_sv = at[p.num_kv_heads];
     }
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the combine pass may take its place on the SMs (and waits there)
 
     // Q fragments (A operand, f16): rows = heads of the group (r < group), zero above; channels in the order of K's codes.
     uint32_t qa[KSTEPS][2];
@@ -149,7 +158,7 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
     uint32_t stage_parity = 0;
     int i = 0;
     for (; i < nw; ++i) {
-        const int stage = i % kDecode8Stages;
+        const int stage = i % STAGES;
         if ((valid_mask >> i) & 1u) {
             const bool got = mbar_wait(my_bars + 8 * stage, (stage_parity >> stage) & 1u);
             stage_parity ^= 1u << stage;
@@ -228,17 +237,17 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
             }
         }
         __syncwarp();  // every lane is done reading the stage before it is refilled
-        if (i + kDecode8Stages < nw) issue(i + kDecode8Stages);
+        if (i + STAGES < nw) issue(i + STAGES);
     }
 
     if (failed) {
         // A copy barrier never completed.  Latch the error, give copies still in flight a bounded
         // chance to land (their destination must stay allocated), and contribute nothing.
         if (lane == 0) atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);
-        stage_parity ^= 1u << (i % kDecode8Stages);  // the wait that failed belongs to a copy still outstanding
-        for (int j = i; j < nw && j < i + kDecode8Stages; ++j)
+        stage_parity ^= 1u << (i % STAGES);  // the wait that failed belongs to a copy still outstanding
+        for (int j = i; j < nw && j < i + STAGES; ++j)
             if ((valid_mask >> j) & 1u)
-                (void)mbar_wait(my_bars + 8 * (j % kDecode8Stages), (stage_parity >> (j % kDecode8Stages)) & 1u, 200000000ull);
+                (void)mbar_wait(my_bars + 8 * (j % STAGES), (stage_parity >> (j % STAGES)) & 1u, 200000000ull);
         m_run = -INFINITY;
         l_run = 0.f;
 #pragma unroll
@@ -249,9 +258,9 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
     l_run += __shfl_xor_sync(FULL, l_run, 2);
 
     // Merge the 4 warps through shared memory (each warp reuses its own, now idle, stages).
-    float *wo = reinterpret_cast<float *>(base_ptr + warp * kDecode8Stages * STAGE_BYTES);  // [8][D]
+    float *wo = reinterpret_cast<float *>(base_ptr + warp * STAGES * STAGE_BYTES);  // [8][D]
     float *wm = wo + 8 * D;                                                                 // [8] m, [8] l
-    static_assert((8 * D + 16) * 4 <= kDecode8Stages * STAGE_BYTES, "merge area");
+    static_assert((8 * D + 16) * 4 <= STAGES * STAGE_BYTES, "merge area");
 #pragma unroll
     for (int mt = 0; mt < KSTEPS; ++mt) {  // row r of the fragment is channel 2r of the sixteen, row r+8 channel 2r+1
         *reinterpret_cast<float2 *>(wo + (2 * c) * D + 16 * mt + 2 * r) = make_float2(o[mt][0], o[mt][2]);
@@ -268,14 +277,14 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
         float mw[kDecodeWarps], mstar = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kDecodeWarps; ++w) {
-            mw[w] = reinterpret_cast<const float *>(base_ptr + w * kDecode8Stages * STAGE_BYTES)[8 * D + h];
+            mw[w] = reinterpret_cast<const float *>(base_ptr + w * STAGES * STAGE_BYTES)[8 * D + h];
             mstar = fmaxf(mstar, mw[w]);
         }
         float acc = 0.f, lsum = 0.f;
         if (mstar > -INFINITY) {
 #pragma unroll
             for (int w = 0; w < kDecodeWarps; ++w) {
-                const float *src = reinterpret_cast<const float *>(base_ptr + w * kDecode8Stages * STAGE_BYTES);
+                const float *src = reinterpret_cast<const float *>(base_ptr + w * STAGES * STAGE_BYTES);
                 const float wgt = (mw[w] > -INFINITY) ? fast_exp2(mw[w] - mstar) : 0.f;
                 acc += wgt * src[h * D + x];
                 lsum += wgt * src[8 * D + 8 + h];
