@@ -68,7 +68,7 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
     }
     if (p.n_prefix && q_tiles <= 0x7fffffffLL) p.tile_prefix[R] = (int)q_tiles;
     if (q_tiles == 0) return EKV_OK;
-    if (q_tiles > 0x7fffffffLL || (e4m3 && (q_tiles * pool->desc.num_kv_heads > 0x7fffffffLL || (long long)cu_q_lens_host[R] * group >= (1LL << 29)))) {
+    if (q_tiles > 0x7fffffffLL || (e4m3 && (q_tiles * pool->desc.num_kv_heads * tc8::kMaxCluster > 0x7fffffffLL || (long long)cu_q_lens_host[R] * group >= (1LL << 29)))) {
         set_error("ekv_attn_prefill_chunk: too many query tiles");
         return EKV_ERR_INVALID;
     }
@@ -98,6 +98,7 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
         pp.cache = (const uint8_t *)pool->layer_base(layer);
         pp.scales = pool->layer_scales(layer);
         pp.block_stride = (long long)pool->block_stride;
+        pp.cluster = tc8::plan_cluster(q_tiles * pool->desc.num_kv_heads, max_blocks_per_seq, pool->sm_count);
         pp.group_magic = group > 1 ? (unsigned)(((1ull << 32) + group - 1) / group) : 0u;
         return d128 ? tc8::launch_prefill8<128>(pool, pp, (cudaStream_t)stream) : tc8::launch_prefill8<64>(pool, pp, (cudaStream_t)stream);
     }

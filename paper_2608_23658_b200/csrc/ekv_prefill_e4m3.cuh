@@ -8,7 +8,12 @@
 //   - A work item is 256 rows of ONE kv-head: rows are (position, head of the group) pairs in that order, so all query heads
 //     that share the kv-head read the converted tile, whatever their number (groups of seven as well as of eight), and a
 //     few drafted tokens of a request fill a tile that would be 128 times one head's few rows otherwise.
-//   - The rows are two tiles of 128 (TMEM lanes) that take turns: the softmax of one runs beside the MMAs of the other.
+//   - The CTA has two slots (S and O in TMEM, a softmax warpgroup) that take turns: the softmax of one runs beside the MMAs of
+//     the other.  More than 128 rows: a slot for each half, both on every key tile.  Fewer: both slots hold the SAME rows and
+//     take every other key tile, so that a few rows do not run at the latency of one slot's chain.
+//   - A call with too few items to fill the machine evenly cuts each item's keys into 2 .. 16 ranges, one for each CTA of a
+//     cluster.  Slots and CTAs that share rows leave (m, l, O) in shared memory when they are through, and the CTAs of the
+//     cluster merge a share of the rows each, out of all their shared memories.  No workspace, and the same bits every time.
 //   - K goes to f16: one conversion instruction for two codes and nothing else, as its scale is applied to the scores, where
 //     a multiplication by the softmax scale stands anyway.  Q becomes f16 with each row brought to a maximum in
 //     [2^13, 2^14) by a power of two, as in decode (what f16 then drops lies 2^-37 below the row's largest element).
@@ -42,6 +47,7 @@ using tc::fence_before;
 
 static constexpr int kBM = 128, kBN = 128;
 static constexpr int kItemRows = 2 * kBM;
+static constexpr int kMaxCluster = 16;
 static constexpr int kThreads = 512;
 static constexpr int kHalfBytes = 128 * 128;  // [128 rows][64 16-bit channels], 128-byte swizzle
 static constexpr int kStages = 2;
@@ -56,6 +62,7 @@ struct Params {
     const float *scales;
     long long block_stride;
     unsigned group_magic;  // ceil(2^32 / group): a division by the group (2 or more) is one multiplication, exact below 2^29
+    int cluster;   // CTAs that share an item's keys
     float q_sign;  // -1 for a negative scale; 0 for a scale of 0
 };
 
@@ -73,6 +80,10 @@ struct Geo {
     static constexpr int kOffFlags = kOffBar + 8 * NBAR;       // abort flag, TMEM address, 4 masks of invalid blocks
     static constexpr int kOffKScale = kOffBar + 192;           // [4 tiles][8 blocks] floats
     static constexpr int kOffQInv = kOffKScale + 128;          // [256 rows] floats
+    static constexpr int kOffPart = 0;                         // merge: O of [2 slots][128 rows][D] floats, over the tiles ...
+    static constexpr int kOffPartML = 2 * kBM * D * 4;         // ... and (m, l) of [2][128]
+    static constexpr int kOffPartW = kOffPartML + 2 * kBM * 8;  // the CTA's own weights of its rows' partials: at most 512
+    static_assert(kOffPartW + 512 * 4 <= kOffRaw, "merge area");
     static constexpr int kSmemBytes = kOffQInv + 1024 + 1024;  // + alignment slack
     static_assert(kOffFlags + 24 <= kOffKScale && kSmemBytes <= 232448, "shared memory");
     // kind::f16 instruction descriptors, D = f32, M = 128: QK with f16 operands, PV with bf16 ones and V MN-major
@@ -125,10 +136,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     const PrefillParams &p = pp.p;
     constexpr int kPieces = D / 8;              // 16-byte pieces of a row of Q / O
     constexpr int kRowsPerInst = 32 / kPieces;  // rows one warp-wide 16-byte access covers
-    if (*(volatile int *)p.abort_word) return;  // an earlier CTA of this launch timed out
+    const int cluster = pp.cluster, part = blockIdx.x % cluster;  // CTAs that share an item's keys; which of them this is
+    // an earlier CTA of this launch timed out (a cluster has to stay together: its CTAs give up at their own waits)
+    if (cluster == 1 && *(volatile int *)p.abort_word) return;
 
     // ---- which (request, rows, kv-head)?  Heaviest (latest) items first, all kv-heads of one next to each other.
-    const int rank = blockIdx.x / p.num_kv_heads, g = blockIdx.x - rank * p.num_kv_heads;
+    const int item = blockIdx.x / cluster;
+    const int rank = item / p.num_kv_heads, g = item - rank * p.num_kv_heads;
     const int idx = p.q_tiles - 1 - rank;
     int req = 0, first = 0, c_r = 0, q0 = 0;
     if (!find_item(p, idx, req, first, q0, c_r)) return;
@@ -148,14 +162,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
 
     if (prefix < 0) {  // malformed request: zero rows, latch
         if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
-        for (int e = threadIdx.x; e < rows_here * kPieces; e += kThreads)
+        for (int e = threadIdx.x; e < rows_here * kPieces && part == 0; e += kThreads)
             *reinterpret_cast<uint4 *>(p.out + row_offset(e / kPieces) + (e % kPieces) * 8) = make_uint4(0u, 0u, 0u, 0u);
         return;
     }
     const int kv_end = min(L, prefix + position(rows_here - 1) + 1);  // keys any row of the item may see
-    const int n_tiles = (kv_end + kBN - 1) / kBN;
+    const int all_tiles = (kv_end + kBN - 1) / kBN;
+    const int tile0 = (int)((long long)all_tiles * part / cluster);  // this CTA's key tiles: tile0 .. tile0 + n_tiles - 1 (possibly none)
+    const int n_tiles = (int)((long long)all_tiles * (part + 1) / cluster) - tile0;
     const int n_blocks = (kv_end + 15) >> 4;
-    const int nx = rows_here > kBM ? 2 : 1;  // row tiles
+    // by_rows: slot x holds rows 128 x .. and sees every key tile j.  Else both hold rows 0 .. and slot x sees tiles x, x + 2, ...
+    const bool by_rows = rows_here > kBM;
+    const bool merge = cluster > 1 || !by_rows;
 
     extern __shared__ uint8_t smem_raw[];
     Smem<D> sh;
@@ -188,6 +206,20 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     fence_after();
     const uint32_t tmem = *sh.tmem_slot();
 
+    // The merge: all roles meet when the CTA's tiles are no longer needed, again when the partial results of the cluster are in
+    // place, and (clusters) once more when they have been read.  Hardware barriers; every role comes here, given up or not.
+    auto meet_all = [&]() { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+    auto meet_cluster = [&]() {
+        if (cluster > 1) cluster_barrier();
+        else meet_all();
+    };
+    auto merge_barriers = [&]() {
+        __syncwarp();
+        meet_all();
+        meet_cluster();
+        if (cluster > 1) cluster_barrier();
+    };
+
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
         if (warp == 0) {
@@ -195,60 +227,63 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             constexpr uint64_t kHi = (uint64_t)tc::kDescHi << 32;
             const uint64_t q_d = kHi | tc::desc_lo(sh.base + G::kOffQ, 16), k_d = kHi | tc::desc_lo(sh.base + G::kOffK, 16),
                            v_d = kHi | tc::desc_lo(sh.base + G::kOffV, kHalfBytes);
-            bool ok = wait_warp<D>(sh, G::K_FULL, 0);
-            // Step j = -1 only brings the first scores.  One elected lane issues a step's run for a row tile in one go: the last
-            // quarter of PV, QK^T of the next key tile, the commits.
+            // Steps alternate between the slots: step u is P V of slot x = u & 1 on its key tile number i = u >> 1, and Q K^T for the
+            // slot's next one; steps -2 and -1 only bring the first scores.  One elected lane issues a step in one go: the last
+            // quarter of PV, QK^T, the commits.
+            bool ok = true;
+            const int steps = by_rows ? 2 * n_tiles : n_tiles, step_max = n_tiles > 0 ? steps : -2;
 #pragma unroll 1
-            for (int j = -1; j < n_tiles && ok; ++j) {
-                const int s = j & 1, s1 = s ^ 1;
-                int pv = j >= 0, more = j + 1 < n_tiles;
+            for (int u = -2; u < step_max && ok; ++u) {
+                const int x = u & 1, i = u >> 1;
+                const int j = by_rows ? i : u, jn = by_rows ? i + 1 : u + 2;  // the CTA's key tiles of the two
+                const int s = j & 1, s1 = jn & 1;
+                const bool closes = !by_rows || x == 1;  // the last slot to read these stages
+                int pv = u >= 0, more = jn < n_tiles;
                 asm volatile("" : "+r"(pv), "+r"(more));  // one copy of the loop, not one for each combination
-                if (pv) ok = wait_warp<D>(sh, G::V_FULL + s, (uint32_t)((j >> 1) & 1));
-#pragma unroll 1
-                for (int x = 0; x < nx && ok; ++x) {
-                    const uint32_t t_s = tmem + 128 * x, t_o = tmem + 256 + 128 * x;
-                    const uint64_t vd = v_d + (uint32_t)s * (G::kTileBytes >> 4);
-                    if (pv) {
-                        ok = wait_warp<D>(sh, G::P_PART + x, (uint32_t)(j & 1));
-                        if (!ok) break;
-                        fence_after();
-                        if (tc::elect_one()) {  // keys 0..95 while the softmax warps finish the rest
-#pragma unroll
-                            for (int k = 0; k < tc::kPartSteps; ++k)
-                                tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, (j > 0 || k > 0) ? 1u : 0u);
-                        }
-                        __syncwarp();
-                        ok = wait_warp<D>(sh, G::P_READY + x, (uint32_t)(j & 1));
-                    } else {
-                        ok = wait_warp<D>(sh, G::Q_READY + x, 0);
-                    }
-                    if (ok && more && x == 0) ok = wait_warp<D>(sh, G::K_FULL + s1, (uint32_t)(((j + 1) >> 1) & 1));
+                const uint32_t t_s = tmem + 128 * x, t_o = tmem + 256 + 128 * x;
+                const uint64_t vd = v_d + (uint32_t)s * (G::kTileBytes >> 4);
+                if (pv) {
+                    ok = wait_warp<D>(sh, G::V_FULL + s, (uint32_t)((j >> 1) & 1));
+                    if (ok) ok = wait_warp<D>(sh, G::P_PART + x, (uint32_t)(i & 1));
                     if (!ok) break;
                     fence_after();
-                    if (tc::elect_one()) {
-                        if (pv) {
+                    if (tc::elect_one()) {  // keys 0..95 while the softmax warps finish the rest
 #pragma unroll
-                            for (int k = tc::kPartSteps; k < kBN / 16; ++k) tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, 1u);
-                            if (x == nx - 1) tc::mma_commit_one(sh.bar(G::V_EMPTY + s));
-                        }
-                        if (more) {
-                            const uint64_t qd = q_d + (uint32_t)x * (G::kTileBytes >> 4), kd = k_d + (uint32_t)s1 * (G::kTileBytes >> 4);
-#pragma unroll
-                            for (int k = 0; k < D / 16; ++k) {
-                                const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
-                                tc::mma_ss(t_s, qd + off, kd + off, G::kIdescQK, k > 0 ? 1u : 0u);
-                            }
-                            if (x == nx - 1) tc::mma_commit_one(sh.bar(G::K_EMPTY + s1));
-                        }
-                        tc::mma_commit_one(sh.bar(G::S_READY + x));  // the next scores, and O up to this tile
+                        for (int k = 0; k < tc::kPartSteps; ++k)
+                            tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, (i > 0 || k > 0) ? 1u : 0u);
                     }
                     __syncwarp();
+                    ok = wait_warp<D>(sh, G::P_READY + x, (uint32_t)(i & 1));
+                } else {
+                    ok = wait_warp<D>(sh, G::Q_READY + (by_rows ? x : 0), 0);
                 }
+                if (ok && more) ok = wait_warp<D>(sh, G::K_FULL + s1, (uint32_t)((jn >> 1) & 1));
+                if (!ok) break;
+                fence_after();
+                if (tc::elect_one()) {
+                    if (pv) {
+#pragma unroll
+                        for (int k = tc::kPartSteps; k < kBN / 16; ++k) tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, 1u);
+                        if (closes) tc::mma_commit_one(sh.bar(G::V_EMPTY + s));
+                    }
+                    if (more) {
+                        const uint64_t qd = q_d + (uint32_t)(by_rows ? x : 0) * (G::kTileBytes >> 4), kd = k_d + (uint32_t)s1 * (G::kTileBytes >> 4);
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
+                            tc::mma_ss(t_s, qd + off, kd + off, G::kIdescQK, k > 0 ? 1u : 0u);
+                        }
+                        if (closes) tc::mma_commit_one(sh.bar(G::K_EMPTY + s1));
+                    }
+                    tc::mma_commit_one(sh.bar(G::S_READY + x));  // the slot's next scores, and its O up to this tile
+                }
+                __syncwarp();
             }
             // every MMA this thread issued must be finished before TMEM is released
             tc::mma_commit(sh.bar(G::DRAIN));
             (void)wait_warp<D>(sh, G::DRAIN, 0);
         }
+        if (merge) merge_barriers();
     } else if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         // =========================== converters ===========================
@@ -269,8 +304,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         // lane l: id of block 8j + l % 8 of tile j (-1 past the end, -2 invalid)
         auto load_id = [&](int j) {
             int id = -1;
-            const int bi = 8 * j + (lane & 7);
-            if (bi < n_blocks) {
+            const int bi = 8 * (tile0 + j) + (lane & 7);
+            if (j < n_tiles && bi < n_blocks) {
                 id = bt[bi];
                 if (id < 0 || (long long)id >= live) id = -2;
             }
@@ -301,13 +336,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
 #pragma unroll 1
         for (int it = 0; it < kIts; ++it) copy(it, ids, 1);
         cp_async_commit();
-        int ids_next = 1 < n_tiles ? load_id(1) : -1;
+        int ids_next = load_id(1);
         bool ok = true;
 #pragma unroll 1
         for (int j = 0; j < n_tiles; ++j) {
             const int s = j & 1;
             const uint32_t ph = (uint32_t)(((j >> 1) - 1) & 1);
-            const int ids_after = j + 2 < n_tiles ? load_id(j + 2) : -1;
+            const int ids_after = load_id(j + 2);
             const float ks_next = load_scale(ids_next, 0), vs_next = load_scale(ids_next, 1);
             // ---- K: f16, scales beside it
             cp_async_wait_1();
@@ -349,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 copy(it, ids_next, 1);
                 uint32_t c[4] = {v.x, v.y, v.z, v.w}, w[8];
                 const float scale = __shfl_sync(0xffffffffu, vs, blk);
-                if (j * kBN + row >= kv_end || !(scale > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;
+                if ((tile0 + j) * kBN + row >= kv_end || !(scale > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;
                 const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -368,17 +403,20 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             vs = vs_next;
         }
         cp_async_wait_all();  // what was started for a tile that does not come (or after a wait that was given up)
+        if (merge) merge_barriers();
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // =========================== softmax + write-out ===========================
-        const int x = (warp - 4) >> 2;        // row tile
+        const int x = (warp - 4) >> 2;        // slot
+        const int rx = by_rows ? x : 0;       // its row tile
+        const int n_it = by_rows ? n_tiles : (n_tiles - x + 1) >> 1;  // its key tiles
         const int wrow0 = (warp & 3) << 5;    // TMEM lanes wrow0 .. +31 belong to this warp
         const int row = wrow0 | lane;         // row of the tile = TMEM lane
         const uint32_t t_s = tmem + ((uint32_t)wrow0 << 16) + 128 * x;
         const uint32_t t_o = tmem + ((uint32_t)wrow0 << 16) + 256 + 128 * x;
-        if (x < nx) {
-            uint8_t *q_tile = sh.ptr + G::kOffQ + x * G::kTileBytes;
-            const int piece = lane % kPieces, sub = lane / kPieces;
+        uint8_t *q_tile = sh.ptr + G::kOffQ + rx * G::kTileBytes;
+        const int piece = lane % kPieces, sub = lane / kPieces;
+        if (by_rows || x == 0) {
             // ---- Q rows of this warp: all of them on their way at once, straight to where they belong in the 128-byte swizzled
             // tile, then bf16 -> f16 in place with a row's largest magnitude in [2^13, 2^14); rows past the end are 0
             auto q_place = [&](int rr) { return (uint32_t)(G::kOffQ + x * G::kTileBytes + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4)); };
@@ -415,120 +453,124 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.bar(G::Q_READY + x));
-            const float row_scale = p.scale_log2 * sh.q_inv()[x * kBM + row];
+        }
+        bool ok = true;
+        if (!by_rows && x == 1 && n_it > 0) ok = wait_warp<D>(sh, G::S_READY + 1, 0);  // the other slot's warps have been through Q
+        const float row_scale = p.scale_log2 * (n_it > 0 ? sh.q_inv()[rx * kBM + row] : 1.f);
 
-            const int first_lim = prefix + position(x * kBM);                              // last key the tile's first row may see
-            const int lim = prefix + position(min(x * kBM + row, rows_here - 1));          // ... and this row
-            float m_run = -INFINITY, l_run = 0.f;
-            bool ok = true;
-            auto publish = [&](int bar) {  // this thread's row of P is in TMEM
-                cp::tcgen05_wait_st();
-                fence_before();
-                mbar_arrive(sh.bar(bar));
-            };
+        const int first_lim = prefix + position(rx * kBM);                          // last key the tile's first row may see
+        const int lim = prefix + position(min(rx * kBM + row, rows_here - 1));      // ... and this row
+        float m_run = -INFINITY, l_run = 0.f;
+        auto publish = [&](int bar) {  // this thread's row of P is in TMEM
+            cp::tcgen05_wait_st();
+            fence_before();
+            mbar_arrive(sh.bar(bar));
+        };
 #pragma unroll 1
-            for (int j = 0; j < n_tiles; ++j) {
-                ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(j & 1));
-                if (!ok) break;
-                fence_after();
-                const int key0 = j * kBN;
-                const int bad = *sh.bad_mask(j);
-                // ---- a tile that the causal boundary cuts, or that holds a block the table does not name, first gets its hidden
-                // scores overwritten with -inf in TMEM, and then runs through the same code as every other one
-                if (key0 + kBN - 1 > first_lim || bad != 0) {
-                    const int rel = lim - key0;  // this row sees columns 0..rel
-                    const int rel_min = __reduce_min_sync(0xffffffffu, rel);
+        for (int i = 0; i < n_it && ok; ++i) {
+            ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(i & 1));
+            if (!ok) break;
+            fence_after();
+            const int j = by_rows ? i : 2 * i + x;  // the CTA's key tile
+            const int key0 = (tile0 + j) * kBN;
+            const int bad = *sh.bad_mask(j);
+            // ---- a tile that the causal boundary cuts, or that holds a block the table does not name, first gets its hidden
+            // scores overwritten with -inf in TMEM, and then runs through the same code as every other one
+            if (key0 + kBN - 1 > first_lim || bad != 0) {
+                const int rel = lim - key0;  // this row sees columns 0..rel
+                const int rel_min = __reduce_min_sync(0xffffffffu, rel);
 #pragma unroll 1
-                    for (int cc = 0; cc < 4; ++cc) {
-                        const unsigned b2 = ((unsigned)bad >> (2 * cc)) & 3u;
-                        if (32 * cc + 31 <= rel_min && b2 == 0u) continue;
-                        const int r = rel - 32 * cc;
-                        const unsigned past = r >= 31 ? 0u : (r < 0 ? 0xffffffffu : 0xfffffffeu << r);
-                        const unsigned hid = past | ((b2 & 1u) ? 0x0000ffffu : 0u) | ((b2 & 2u) ? 0xffff0000u : 0u);
-                        float v[32];
-                        tc::tmem_ld32(v, t_s + 32 * cc);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = ((hid >> i) & 1u) ? -INFINITY : v[i];
-                        tc::tmem_st32(t_s + 32 * cc, v);
-                    }
-                    cp::tcgen05_wait_st();
-                }
-                float sv[128];
-                {
-                    uint32_t(&r)[128] = reinterpret_cast<uint32_t(&)[128]>(sv);
-                    cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[0]), t_s);
-                    cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[32]), t_s + 32);
-                    cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[64]), t_s + 64);
-                    cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[96]), t_s + 96);
-                    cp::tcgen05_wait_ld();
-                }
-                float ks[8];
-                {
-                    const float4 a = *reinterpret_cast<const float4 *>(sh.k_scale(j)), b = *reinterpret_cast<const float4 *>(sh.k_scale(j) + 4);
-                    const float e[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) ks[i] = fmaxf(e[i] * row_scale, 1.17549435e-38f);  // not 0: a masked score times it stays -inf
-                }
-                float m_tile = -INFINITY;  // scaled: a block at a time
-#pragma unroll
-                for (int b = 0; b < 8; ++b) {
-                    float m0 = sv[16 * b], m1 = sv[16 * b + 1];
-#pragma unroll
-                    for (int i = 2; i < 16; i += 2) {
-                        m0 = fmaxf(m0, sv[16 * b + i]);
-                        m1 = fmaxf(m1, sv[16 * b + i + 1]);
-                    }
-                    m_tile = fmaxf(m_tile, fmaxf(m0, m1) * ks[b]);
-                }
-                // ---- lazy rescale: raise the reference max only when it is far behind
-                const bool raise = m_tile > m_run + tc::kRescaleThreshold;  // also true for the first finite tile
-                if (__any_sync(0xffffffffu, raise)) {
-                    const float m_new = raise ? m_tile : m_run;
-                    const float alpha = (raise && m_run > -INFINITY) ? fast_exp2(m_run - m_new) : (raise ? 0.f : 1.f);
-                    m_run = m_new;
-                    l_run *= alpha;
-                    if (j > 0) {  // O holds the sum over earlier tiles and no MMA touches it right now
-#pragma unroll 1
-                        for (int cc = 0; cc < D / 32; ++cc) {
-                            float ov[32];
-                            tc::tmem_ld32(ov, t_o + 32 * cc);
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) ov[i] *= alpha;
-                            tc::tmem_st32(t_o + 32 * cc, ov);
-                        }
-                    }
-                }
-                const float m_use = m_run > -INFINITY ? m_run : 0.f;
-                // ---- P = exp2(S*scale - m) (a masked -inf gives 0), row sum, bf16 pairs into the S columns
-                float2 acc_a = make_float2(0.f, 0.f), acc_b = make_float2(0.f, 0.f);
-                const float2 nm2 = make_float2(-m_use, -m_use);
-#pragma unroll
                 for (int cc = 0; cc < 4; ++cc) {
-                    uint32_t pk[16];
+                    const unsigned b2 = ((unsigned)bad >> (2 * cc)) & 3u;
+                    if (32 * cc + 31 <= rel_min && b2 == 0u) continue;
+                    const int r = rel - 32 * cc;
+                    const unsigned past = r >= 31 ? 0u : (r < 0 ? 0xffffffffu : 0xfffffffeu << r);
+                    const unsigned hid = past | ((b2 & 1u) ? 0x0000ffffu : 0u) | ((b2 & 2u) ? 0xffff0000u : 0u);
+                    float v[32];
+                    tc::tmem_ld32(v, t_s + 32 * cc);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float2 sc2 = make_float2(ks[2 * cc + (i >> 4)], ks[2 * cc + (i >> 4)]);
-                        const float2 xa = __ffma2_rn(make_float2(sv[32 * cc + i], sv[32 * cc + i + 1]), sc2, nm2);
-                        const float2 xb = __ffma2_rn(make_float2(sv[32 * cc + i + 2], sv[32 * cc + i + 3]), sc2, nm2);
-                        const float2 pa = make_float2(fast_exp2(xa.x), fast_exp2(xa.y));
-                        const float2 pb = make_float2(fast_exp2(xb.x), fast_exp2(xb.y));
-                        acc_a = __fadd2_rn(acc_a, pa);
-                        acc_b = __fadd2_rn(acc_b, pb);
-                        pk[i >> 1] = pack_bf16x2(pa.x, pa.y);
-                        pk[(i >> 1) + 1] = pack_bf16x2(pb.x, pb.y);
-                    }
-                    cp::tcgen05_st_32x32b(t_s + 16 * cc, pk);
-                    if (cc == tc::kPartSteps / 2 - 1) publish(G::P_PART + x);  // 96 keys stored
+                    for (int i = 0; i < 32; ++i) v[i] = ((hid >> i) & 1u) ? -INFINITY : v[i];
+                    tc::tmem_st32(t_s + 32 * cc, v);
                 }
-                l_run += (acc_a.x + acc_a.y) + (acc_b.x + acc_b.y);
-                publish(G::P_READY + x);
+                cp::tcgen05_wait_st();
             }
+            float sv[128];
+            {
+                uint32_t(&r)[128] = reinterpret_cast<uint32_t(&)[128]>(sv);
+                cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[0]), t_s);
+                cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[32]), t_s + 32);
+                cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[64]), t_s + 64);
+                cp::tcgen05_ld_32x32b(reinterpret_cast<uint32_t(&)[32]>(r[96]), t_s + 96);
+                cp::tcgen05_wait_ld();
+            }
+            float ks[8];
+            {
+                const float4 a = *reinterpret_cast<const float4 *>(sh.k_scale(j)), b = *reinterpret_cast<const float4 *>(sh.k_scale(j) + 4);
+                const float e[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ks[i] = fmaxf(e[i] * row_scale, 1.17549435e-38f);  // not 0: a masked score times it stays -inf
+            }
+            float m_tile = -INFINITY;  // scaled: a block at a time
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                float m0 = sv[16 * b], m1 = sv[16 * b + 1];
+#pragma unroll
+                for (int i = 2; i < 16; i += 2) {
+                    m0 = fmaxf(m0, sv[16 * b + i]);
+                    m1 = fmaxf(m1, sv[16 * b + i + 1]);
+                }
+                m_tile = fmaxf(m_tile, fmaxf(m0, m1) * ks[b]);
+            }
+            // ---- lazy rescale: raise the reference max only when it is far behind
+            const bool raise = m_tile > m_run + tc::kRescaleThreshold;  // also true for the first finite tile
+            if (__any_sync(0xffffffffu, raise)) {
+                const float m_new = raise ? m_tile : m_run;
+                const float alpha = (raise && m_run > -INFINITY) ? fast_exp2(m_run - m_new) : (raise ? 0.f : 1.f);
+                m_run = m_new;
+                l_run *= alpha;
+                if (i > 0) {  // O holds the sum over earlier tiles and no MMA touches it right now
+#pragma unroll 1
+                    for (int cc = 0; cc < D / 32; ++cc) {
+                        float ov[32];
+                        tc::tmem_ld32(ov, t_o + 32 * cc);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) ov[c] *= alpha;
+                        tc::tmem_st32(t_o + 32 * cc, ov);
+                    }
+                }
+            }
+            const float m_use = m_run > -INFINITY ? m_run : 0.f;
+            // ---- P = exp2(S*scale - m) (a masked -inf gives 0), row sum, bf16 pairs into the S columns
+            float2 acc_a = make_float2(0.f, 0.f), acc_b = make_float2(0.f, 0.f);
+            const float2 nm2 = make_float2(-m_use, -m_use);
+#pragma unroll
+            for (int cc = 0; cc < 4; ++cc) {
+                uint32_t pk[16];
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const float2 sc2 = make_float2(ks[2 * cc + (i >> 4)], ks[2 * cc + (i >> 4)]);
+                    const float2 xa = __ffma2_rn(make_float2(sv[32 * cc + i], sv[32 * cc + i + 1]), sc2, nm2);
+                    const float2 xb = __ffma2_rn(make_float2(sv[32 * cc + i + 2], sv[32 * cc + i + 3]), sc2, nm2);
+                    const float2 pa = make_float2(fast_exp2(xa.x), fast_exp2(xa.y));
+                    const float2 pb = make_float2(fast_exp2(xb.x), fast_exp2(xb.y));
+                    acc_a = __fadd2_rn(acc_a, pa);
+                    acc_b = __fadd2_rn(acc_b, pb);
+                    pk[i >> 1] = pack_bf16x2(pa.x, pa.y);
+                    pk[(i >> 1) + 1] = pack_bf16x2(pb.x, pb.y);
+                }
+                cp::tcgen05_st_32x32b(t_s + 16 * cc, pk);
+                if (cc == tc::kPartSteps / 2 - 1) publish(G::P_PART + x);  // 96 keys stored
+            }
+            l_run += (acc_a.x + acc_a.y) + (acc_b.x + acc_b.y);
+            publish(G::P_READY + x);
+        }
 
+        if (ok && n_it > 0) ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(n_it & 1));
+        fence_after();  // every MMA that read the slot's Q tile or wrote its O has completed (the commit covers all earlier ones)
+        if (!merge) {
             // ---- write-out: O / l -> bf16 -> the (now idle) Q tile in shared memory -> global, whole rows per instruction.
             // Only the warp that wrote a row reads it: __syncwarp suffices.
-            if (ok) ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(n_tiles & 1));
             if (ok) {
-                fence_after();  // every MMA that read this Q tile or wrote this O has completed (the commit covers all earlier ones)
                 const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
 #pragma unroll 1
                 for (int cc = 0; cc < D / 32; ++cc) {
@@ -548,11 +590,90 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 __syncwarp();
 #pragma unroll 2
                 for (int it = 0; it < 32 / kRowsPerInst; ++it) {
-                    const int rr = wrow0 + kRowsPerInst * it + sub, in_item = x * kBM + rr;
+                    const int rr = wrow0 + kRowsPerInst * it + sub, in_item = rx * kBM + rr;
                     const uint4 v = *reinterpret_cast<const uint4 *>(q_tile + rr * (D * 2) + ((piece ^ (rr & (kPieces - 1))) << 4));
                     if (in_item < rows_here) *reinterpret_cast<uint4 *>(p.out + row_offset(in_item) + piece * 8) = v;
                 }
             }
+        } else {
+            // ---- partial results into shared memory, in place of the tiles, once every role is through with those.  Chunks of 16
+            // bytes are XORed with the row, so that the 32 rows of a warp do not meet in a bank.
+            constexpr int kChunks = D / 4;
+            meet_all();
+            const bool none = !ok || n_it == 0;
+            if (rx * kBM + wrow0 < rows_here) {
+#pragma unroll 1
+                for (int cc = 0; cc < D / 32; ++cc) {
+                    float ov[32];
+                    tc::tmem_ld32(ov, t_o + 32 * cc);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float4 v = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(ov[4 * c], ov[4 * c + 1], ov[4 * c + 2], ov[4 * c + 3]);
+                        *reinterpret_cast<float4 *>(sh.ptr + G::kOffPart + ((x * kBM + row) * kChunks + ((8 * cc + c) ^ (row & (kChunks - 1)))) * 16) = v;
+                    }
+                }
+                *reinterpret_cast<float2 *>(sh.ptr + G::kOffPartML + (x * kBM + row) * 8) = none ? make_float2(-INFINITY, 0.f) : make_float2(m_run, l_run);
+            }
+            meet_cluster();
+            // ---- this CTA's share of the rows (part, part + cluster, ...), out of the shared memories of all of the cluster.  A read
+            // of another SM's shared memory takes most of a microsecond, so it is done wide: first a thread a row for the weights,
+            // then a warp for four rows (kChunks lanes a row) at a time.
+            const int parts = by_rows ? cluster : 2 * cluster;
+            const int n_rows = (rows_here - part + cluster - 1) / cluster;
+            float *weights = (float *)(sh.ptr + G::kOffPartW);
+            auto source = [&](int i, int r, uint32_t &slot_row) {  // partial i of row r: a CTA's, or a CTA's slot's
+                slot_row = (uint32_t)((by_rows ? r >> 7 : i & 1) * kBM + (r & (kBM - 1)));
+                return cluster > 1 ? map_to_cta(sh.base, by_rows ? i : i >> 1) : sh.base;
+            };
+            for (int k = threadIdx.x - 128; k < n_rows; k += 256) {
+                float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+                for (int i = 0; i < parts; ++i) {
+                    uint32_t sr;
+                    const uint32_t base = source(i, part + cluster * k, sr);
+                    const float2 v = ld_cluster_f2(base + G::kOffPartML + sr * 8);
+                    const float m_new = fmaxf(m, v.x);
+                    if (m_new > -INFINITY) l = l * fast_exp2(m - m_new) + v.y * fast_exp2(v.x - m_new);
+                    m = m_new;
+                }
+                const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll 4
+                for (int i = 0; i < parts; ++i) {
+                    uint32_t sr;
+                    const uint32_t base = source(i, part + cluster * k, sr);
+                    const float mi = ld_cluster_f2(base + G::kOffPartML + sr * 8).x;
+                    weights[k * parts + i] = mi > -INFINITY ? fast_exp2(mi - m) * inv : 0.f;
+                }
+            }
+            asm volatile("bar.sync 2, 256;" ::: "memory");
+            constexpr int kRowsAtOnce = 4, kRowsPerWarp = 32 / kChunks;
+            const int chunk = lane & (kChunks - 1);
+#pragma unroll 1
+            for (int k0 = (warp - 4) * kRowsPerWarp * kRowsAtOnce + lane / kChunks; k0 < n_rows; k0 += 8 * kRowsPerWarp * kRowsAtOnce) {
+                float4 acc[kRowsAtOnce];
+#pragma unroll
+                for (int u = 0; u < kRowsAtOnce; ++u) acc[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+                for (int i = 0; i < parts; ++i) {
+#pragma unroll
+                    for (int u = 0; u < kRowsAtOnce; ++u) {
+                        const int k = min(k0 + u * kRowsPerWarp, n_rows - 1), r = part + cluster * k;
+                        uint32_t sr;
+                        const uint32_t base = source(i, r, sr);
+                        const float4 o = ld_cluster_f4(base + G::kOffPart + (sr * kChunks + (chunk ^ (r & (kChunks - 1)))) * 16);
+                        const float w = weights[k * parts + i];
+                        acc[u].x += w * o.x, acc[u].y += w * o.y, acc[u].z += w * o.z, acc[u].w += w * o.w;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kRowsAtOnce; ++u) {
+                    const int k = k0 + u * kRowsPerWarp;
+                    if (k < n_rows)
+                        *reinterpret_cast<uint2 *>(p.out + row_offset(part + cluster * k) + chunk * 4) =
+                            make_uint2(pack_bf16x2(acc[u].x, acc[u].y), pack_bf16x2(acc[u].z, acc[u].w));
+                }
+            }
+            if (cluster > 1) cluster_barrier();  // nobody leaves while another may read its shared memory
         }
     }
 
@@ -568,20 +689,49 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
 }
 
 template <int D>
-static ekv_status_t launch_prefill8(ekv_pool *pool, const Params &pp, cudaStream_t stream) {
-    static bool attr_set[64] = {false};
+static ekv_status_t launch_prefill8(ekv_pool *pool, Params &pp, cudaStream_t stream) {
+    static int max_cluster[64] = {0};  // 0: not asked yet
     const int dev = pool->desc.device;
-    if (dev >= 64 || !attr_set[dev]) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Geo<D>::kSmemBytes;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int most = dev < 64 ? max_cluster[dev] : 0;
+    if (most == 0) {
         cudaError_t e = cudaFuncSetAttribute(prefill8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<D>::kSmemBytes);
-        if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: shared-memory attribute");
-        if (dev < 64) attr_set[dev] = true;
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill8_kernel<D>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: kernel attributes");
+        for (most = kMaxCluster; most > 8; most /= 2) {  // more than 8 is for the device to allow
+            int fit = 0;
+            attr.val.clusterDim.x = (unsigned)most;
+            cfg.gridDim = dim3((unsigned)most);
+            if (cudaOccupancyMaxActiveClusters(&fit, prefill8_kernel<D>, &cfg) == cudaSuccess && fit > 0) break;
+            (void)cudaGetLastError();
+        }
+        if (dev < 64) max_cluster[dev] = most;
     }
+    if (pp.cluster > most) pp.cluster = most;
     cudaError_t e = cudaMemsetAsync(pp.p.abort_word, 0, sizeof(int), stream);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: clear abort word");
-    prefill8_kernel<D><<<(unsigned)((long long)pp.p.q_tiles * pp.p.num_kv_heads), kThreads, Geo<D>::kSmemBytes, stream>>>(pp);
-    e = cudaGetLastError();
+    attr.val.clusterDim.x = (unsigned)pp.cluster;
+    cfg.gridDim = dim3((unsigned)((long long)pp.p.q_tiles * pp.p.num_kv_heads * pp.cluster));
+    cfg.stream = stream;
+    e = cudaLaunchKernelEx(&cfg, prefill8_kernel<D>, pp);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: launch");
     return EKV_OK;
+}
+
+// CTAs an item's keys are cut over: until the launch has about four items' parts for every SM (an even finish), while a part keeps
+// two key tiles of the longest sequence that the table can hold.  Depends on the call's shape arguments alone.
+static int plan_cluster(long long items, int max_blocks, int sm_count) {
+    const long long max_tiles = ((long long)max_blocks * 16 + kBN - 1) / kBN;
+    int c = 1;
+    while (c < kMaxCluster && items * c < 4ll * sm_count && 2 * c * 2 <= max_tiles) c *= 2;
+    return c;
 }
 
 }  // namespace tc8

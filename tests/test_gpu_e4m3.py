@@ -409,6 +409,22 @@ def test_prefill_long_and_many(shape):
         assert c.pool.poll_status() == ekv.Status.OK
 
 
+@pytest.mark.parametrize("shape", [I.TINY, I.LLAMA8B, I.Shape(5, 1, 64)], ids=str)
+def test_prefill_few_rows_over_long_and_wide_tables(shape):
+    """Few rows (both slots on the same ones), keys cut over clusters of every size, and tables so much wider than the
+    sequences that some of a cluster's CTAs have no keys."""
+    for lengths, chunks, width in (([5000], [3], 0), ([2600, 1, 900], [4, 1, 130], 0), ([130, 5, 300, 256], [40, 5, 2, 256], 700),
+                                   ([700] * 40, [5] * 40, 0), ([1500] * 9, [100] * 9, 300)):
+        c = Case(shape, lengths, seed=sum(lengths))
+        with c.pool:
+            if width:
+                wide = torch.full((len(lengths), width), 1 << 30, dtype=torch.int32, device=DEV)
+                wide[:, :c.d_tables.shape[1]] = c.d_tables
+                c.d_tables = wide
+            _, cu, out = check_prefill(c, chunks, what=f"{lengths[:4]}, {chunks[:4]}")
+            assert c.pool.poll_status() == ekv.Status.OK
+
+
 def test_prefill_magnitudes_and_scales():
     shape = I.Shape(6, 2, 128)
     c = Case(shape, [400, 40], seed=83)
