@@ -136,45 +136,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     const PrefillParams &p = pp.p;
     constexpr int kPieces = D / 8;              // 16-byte pieces of a row of Q / O
     constexpr int kRowsPerInst = 32 / kPieces;  // rows one warp-wide 16-byte access covers
-    const int cluster = pp.cluster, part = blockIdx.x % cluster;  // CTAs that share an item's keys; which of them this is
-    // an earlier CTA of this launch timed out (a cluster has to stay together: its CTAs give up at their own waits)
-    if (cluster == 1 && *(volatile int *)p.abort_word) return;
-
-    // ---- which (request, rows, kv-head)?  Heaviest (latest) items first, all kv-heads of one next to each other.
-    const int item = blockIdx.x / cluster;
-    const int rank = item / p.num_kv_heads, g = item - rank * p.num_kv_heads;
-    const int idx = p.q_tiles - 1 - rank;
-    int req = 0, first = 0, c_r = 0, q0 = 0;
-    if (!find_item(p, idx, req, first, q0, c_r)) return;
-    const int group = p.group;
-    const int row0 = (idx - first) * kItemRows;               // first of the request's c_r * group rows
-    const int rows_here = min(kItemRows, c_r * group - row0);
-    if (rows_here <= 0) return;  // the device's offsets say less than the host's
-    const int L = min(p.seq_lens[req], p.max_blocks * 16);
-    const int prefix = L - c_r;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    // element offset of a row of the item in q and out
-    auto position = [&](int r) { return group == 1 ? row0 + r : (int)__umulhi((unsigned)(row0 + r), pp.group_magic); };
-    auto row_offset = [&](int r) {
-        const int pos = position(r), hg = row0 + r - pos * group;
-        return ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D;
-    };
-
-    if (prefix < 0) {  // malformed request: zero rows, latch
-        if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
-        for (int e = threadIdx.x; e < rows_here * kPieces && part == 0; e += kThreads)
-            *reinterpret_cast<uint4 *>(p.out + row_offset(e / kPieces) + (e % kPieces) * 8) = make_uint4(0u, 0u, 0u, 0u);
-        return;
-    }
-    const int kv_end = min(L, prefix + position(rows_here - 1) + 1);  // keys any row of the item may see
-    const int all_tiles = (kv_end + kBN - 1) / kBN;
-    const int tile0 = (int)((long long)all_tiles * part / cluster);  // this CTA's key tiles: tile0 .. tile0 + n_tiles - 1 (possibly none)
-    const int n_tiles = (int)((long long)all_tiles * (part + 1) / cluster) - tile0;
-    const int n_blocks = (kv_end + 15) >> 4;
-    // by_rows: slot x holds rows 128 x .. and sees every key tile j.  Else both hold rows 0 .. and slot x sees tiles x, x + 2, ...
-    const bool by_rows = rows_here > kBM;
-    const bool merge = cluster > 1 || !by_rows;
-
     extern __shared__ uint8_t smem_raw[];
     Smem<D> sh;
     {
@@ -182,6 +143,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         sh.base = (raw + 1023u) & ~1023u;
         sh.ptr = smem_raw + (sh.base - raw);
     }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int cluster = pp.cluster, part = blockIdx.x % cluster;  // CTAs that share an item's keys; which of them this is
+
+    // ---- which (request, rows, kv-head)?  Heaviest (latest) items first, all kv-heads of one next to each other.  The reads of
+    // device memory are under way while barriers and TMEM are set up.
+    const int item = blockIdx.x / cluster;
+    const int rank = item / p.num_kv_heads, g = item - rank * p.num_kv_heads;
+    const int idx = p.q_tiles - 1 - rank;
+    int req = 0, first = 0, c_r = 0, q0 = 0;
+    bool work = find_item(p, idx, req, first, q0, c_r);
+    const int given_up = *(volatile int *)p.abort_word;  // an earlier CTA of this launch timed out
+    const int seq_len = work ? p.seq_lens[req] : 0;
     if (threadIdx.x == 0) {
         for (int x = 0; x < 2; ++x) {
             mbar_init(sh.bar(G::Q_READY + x), 4);
@@ -201,10 +174,44 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         cp::tcgen05_alloc(cp::cta_group_1, sh.tmem_slot(), 512);
         cp::tcgen05_relinquish_alloc_permit(cp::cta_group_1);
     }
+
+    const int group = p.group;
+    const int row0 = (idx - first) * kItemRows;               // first of the request's c_r * group rows
+    const int rows_here = min(kItemRows, c_r * group - row0);
+    const int L = min(seq_len, p.max_blocks * 16);
+    const int prefix = L - c_r;
+    // element offset of a row of the item in q and out
+    auto position = [&](int r) { return group == 1 ? row0 + r : (int)__umulhi((unsigned)(row0 + r), pp.group_magic); };
+    auto row_offset = [&](int r) {
+        const int pos = position(r), hg = row0 + r - pos * group;
+        return ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D;
+    };
+    // no rows: the device's offsets say less than the host's.  (A cluster has to stay together: all but the last reason are the same
+    // for its CTAs, and for that one they go by their own waits.)
+    work = work && rows_here > 0 && !(cluster == 1 && given_up);
+    if (work && prefix < 0) {  // malformed request: zero rows, latch
+        if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+        for (int e = threadIdx.x; e < rows_here * kPieces && part == 0; e += kThreads)
+            *reinterpret_cast<uint4 *>(p.out + row_offset(e / kPieces) + (e % kPieces) * 8) = make_uint4(0u, 0u, 0u, 0u);
+        work = false;
+    }
+    // the address of TMEM is there, and (it does not matter who is first) so is what a CTA without work gives back
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = *sh.tmem_slot();
+    if (!work) {
+        if (warp == 1) cp::tcgen05_dealloc(cp::cta_group_1, tmem, 512);
+        return;
+    }
+    const int kv_end = min(L, prefix + position(rows_here - 1) + 1);  // keys any row of the item may see
+    const int all_tiles = (kv_end + kBN - 1) / kBN;
+    const int tile0 = (int)((long long)all_tiles * part / cluster);  // this CTA's key tiles: tile0 .. tile0 + n_tiles - 1 (possibly none)
+    const int n_tiles = (int)((long long)all_tiles * (part + 1) / cluster) - tile0;
+    const int n_blocks = (kv_end + 15) >> 4;
+    // by_rows: slot x holds rows 128 x .. and sees every key tile j.  Else both hold rows 0 .. and slot x sees tiles x, x + 2, ...
+    const bool by_rows = rows_here > kBM;
+    const bool merge = cluster > 1 || !by_rows;
 
     // The merge: all roles meet when the CTA's tiles are no longer needed, again when the partial results of the cluster are in
     // place, and (clusters) once more when they have been read.  Hardware barriers; every role comes here, given up or not.
@@ -357,19 +364,25 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     if (oob) atomicOr(p.status, EKV_DEV_FLAG_OOB);
                 }
             }
-#pragma unroll 2
-            for (int it = 0; it < kIts; ++it) {
-                const int blk = it * kBlocksPerIt + first_block;
-                const uint4 v = lds_16(raw + it * 2048);
-                copy(it, ids_next, 0);  // the place is free: the next tile's codes
-                uint32_t c[4] = {v.x, v.y, v.z, v.w}, w[8];
-                if (!(__shfl_sync(0xffffffffu, ks, blk) > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;  // no scale: nothing was written, the values are 0
+#pragma unroll 1
+            for (int it = 0; it < kIts; it += 4) {  // four pieces side by side: one alone is a chain of some 180 cycles
+                uint4 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[2 * i] = e4m3_lo(c[i]);
-                    w[2 * i + 1] = e4m3_hi(c[i]);
+                for (int u = 0; u < 4; ++u) v[u] = lds_16(raw + (it + u) * 2048);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) copy(it + u, ids_next, 0);  // the places are free: the next tile's codes
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int blk = (it + u) * kBlocksPerIt + first_block;
+                    uint32_t c[4] = {v[u].x, v[u].y, v[u].z, v[u].w}, w[8];
+                    if (!(__shfl_sync(0xffffffffu, ks, blk) > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;  // no scale: nothing was written, the values are 0
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        w[2 * i] = e4m3_lo(c[i]);
+                        w[2 * i + 1] = e4m3_hi(c[i]);
+                    }
+                    store(G::kOffK + s * G::kTileBytes, blk * 16 + rowb, w);
                 }
-                store(G::kOffK + s * G::kTileBytes, blk * 16 + rowb, w);
             }
             cp_async_commit();
             publish(G::K_FULL + s);
@@ -377,23 +390,29 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             cp_async_wait_1();
             ok = j < kStages || wait_warp<D>(sh, G::V_EMPTY + s, ph);
             if (!ok) break;
-#pragma unroll 2
-            for (int it = 0; it < kIts; ++it) {
-                const int blk = it * kBlocksPerIt + first_block, row = blk * 16 + rowb;
-                const uint4 v = lds_16(raw + G::kRawBytes + it * 2048);
-                copy(it, ids_next, 1);
-                uint32_t c[4] = {v.x, v.y, v.z, v.w}, w[8];
-                const float scale = __shfl_sync(0xffffffffu, vs, blk);
-                if ((tile0 + j) * kBN + row >= kv_end || !(scale > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;
-                const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);
+#pragma unroll 1
+            for (int it = 0; it < kIts; it += 4) {
+                uint4 v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 a = f16x2_to_float2(e4m3_lo(c[i])), b = f16x2_to_float2(e4m3_hi(c[i]));
-                    const __nv_bfloat162 x = __hmul2(__floats2bfloat162_rn(a.x, a.y), s2), y = __hmul2(__floats2bfloat162_rn(b.x, b.y), s2);
-                    w[2 * i] = *reinterpret_cast<const uint32_t *>(&x);
-                    w[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&y);
+                for (int u = 0; u < 4; ++u) v[u] = lds_16(raw + G::kRawBytes + (it + u) * 2048);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) copy(it + u, ids_next, 1);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int blk = (it + u) * kBlocksPerIt + first_block, row = blk * 16 + rowb;
+                    uint32_t c[4] = {v[u].x, v[u].y, v[u].z, v[u].w}, w[8];
+                    const float scale = __shfl_sync(0xffffffffu, vs, blk);
+                    if ((tile0 + j) * kBN + row >= kv_end || !(scale > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;
+                    const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 a = f16x2_to_float2(e4m3_lo(c[i])), b = f16x2_to_float2(e4m3_hi(c[i]));
+                        const __nv_bfloat162 x = __hmul2(__floats2bfloat162_rn(a.x, a.y), s2), y = __hmul2(__floats2bfloat162_rn(b.x, b.y), s2);
+                        w[2 * i] = *reinterpret_cast<const uint32_t *>(&x);
+                        w[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&y);
+                    }
+                    store(G::kOffV + s * G::kTileBytes, row, w);
                 }
-                store(G::kOffV + s * G::kTileBytes, row, w);
             }
             cp_async_commit();
             publish(G::V_FULL + s);
@@ -420,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             // ---- Q rows of this warp: all of them on their way at once, straight to where they belong in the 128-byte swizzled
             // tile, then bf16 -> f16 in place with a row's largest magnitude in [2^13, 2^14); rows past the end are 0
             auto q_place = [&](int rr) { return (uint32_t)(G::kOffQ + x * G::kTileBytes + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4)); };
-#pragma unroll 1
+#pragma unroll 2
             for (int it = 0; it < 32 / kRowsPerInst; ++it) {
                 const int rr = wrow0 + kRowsPerInst * it + sub, in_item = x * kBM + rr;
                 const bool there = in_item < rows_here;
@@ -429,26 +448,35 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             cp_async_commit();
             cp_async_wait_all();
 #pragma unroll 1
-            for (int it = 0; it < 32 / kRowsPerInst; ++it) {
-                const int rr = wrow0 + kRowsPerInst * it + sub;
-                const uint4 v = lds_16(sh.base + q_place(rr));
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-                uint32_t top = 0;
+            for (int it = 0; it < 32 / kRowsPerInst; it += 4) {  // four pieces side by side: one is a chain of some 300 cycles
+                uint4 v[4];
+                uint32_t top[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
-                top = max(top & 0xffffu, top >> 16);
+                for (int u = 0; u < 4; ++u) v[u] = lds_16(sh.base + q_place(wrow0 + kRowsPerInst * (it + u) + sub));
 #pragma unroll
-                for (int o = kPieces / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const float up = to_f16_range(__uint_as_float(top << 16));
-                const float f = up * pp.q_sign;
-                uint32_t h[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const __half2 y = __floats2half2_rn(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
-                    h[i] = *reinterpret_cast<const uint32_t *>(&y);
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t t2 = __vmaxu2(__vmaxu2(v[u].x & 0x7fff7fffu, v[u].y & 0x7fff7fffu), __vmaxu2(v[u].z & 0x7fff7fffu, v[u].w & 0x7fff7fffu));
+                    top[u] = max(t2 & 0xffffu, t2 >> 16);
                 }
-                *reinterpret_cast<uint4 *>(sh.ptr + q_place(rr)) = make_uint4(h[0], h[1], h[2], h[3]);
-                if (piece == 0) sh.q_inv()[x * kBM + rr] = pow2_inverse(up);
+#pragma unroll
+                for (int o = kPieces / 2; o > 0; o >>= 1)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) top[u] = max(top[u], __shfl_xor_sync(0xffffffffu, top[u], o));
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int rr = wrow0 + kRowsPerInst * (it + u) + sub;
+                    const float up = to_f16_range(__uint_as_float(top[u] << 16));
+                    const float f = up * pp.q_sign;
+                    const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+                    uint32_t h[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const __half2 y = __floats2half2_rn(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
+                        h[i] = *reinterpret_cast<const uint32_t *>(&y);
+                    }
+                    *reinterpret_cast<uint4 *>(sh.ptr + q_place(rr)) = make_uint4(h[0], h[1], h[2], h[3]);
+                    if (piece == 0) sh.q_inv()[x * kBM + rr] = pow2_inverse(up);
+                }
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -725,12 +753,15 @@ static ekv_status_t launch_prefill8(ekv_pool *pool, Params &pp, cudaStream_t str
     return EKV_OK;
 }
 
-// CTAs an item's keys are cut over: until the launch has about four items' parts for every SM (an even finish), while a part keeps
-// two key tiles of the longest sequence that the table can hold.  Depends on the call's shape arguments alone.
+// CTAs an item's keys are cut over: as many as fit beside each other, while a part keeps two key tiles of the longest sequence that
+// the table can hold.  Never more than one round of the machine: a part costs 10 to 15 us beyond its tiles (a cold start and the
+// merge), and clusters leave some SMs without a place.  Measured, 32q/8kv: 4 rows over 30000 keys (8 items) 429 us with one CTA an
+// item, 222 / 120 / 77 with 2 / 4 / 8; 512 rows over 8000 (64 items) 144, 86 with 2, 100 with 4; 2048 over 14001 (256 items) 478,
+// 516 with 2, 585 with 4.  Depends on the call's shape arguments alone.
 static int plan_cluster(long long items, int max_blocks, int sm_count) {
     const long long max_tiles = ((long long)max_blocks * 16 + kBN - 1) / kBN;
     int c = 1;
-    while (c < kMaxCluster && items * c < 4ll * sm_count && 2 * c * 2 <= max_tiles) c *= 2;
+    while (c < kMaxCluster && items * c * 2 <= sm_count && 2 * c * 2 <= max_tiles) c *= 2;
     return c;
 }
 
