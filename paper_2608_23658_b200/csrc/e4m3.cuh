@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
+#include "ptx.cuh"
+
 namespace ekv {
 
 static constexpr int kScaleMinExp = -112, kScaleMaxExp = 120;
@@ -46,6 +48,12 @@ __device__ __forceinline__ float to_f16_range(float a) {
     if (e == 0xff || a == 0.f) return 1.f;
     const int k = 13 - (e - 127);
     return __uint_as_float((uint32_t)(min(k, 126) + 127) << 23);
+}
+
+// two f16 that codes became -> two bf16 (exact: codes have four significant bits)
+__device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) {
+    const float2 f = f16x2_to_float2(h);
+    return pack_bf16x2(f.x, f.y);
 }
 
 }  // namespace ekv

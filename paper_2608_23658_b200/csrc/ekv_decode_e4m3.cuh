@@ -36,12 +36,6 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// two codes -> two bf16
-__device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) {
-    const float2 f = f16x2_to_float2(h);
-    return pack_bf16x2(f.x, f.y);
-}
-
 template <int D>
 __global__ void __launch_bounds__(kDecodeWarps * 32, kDecode8Ctas)
 decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodeParams p, const float *__restrict__ scales) {

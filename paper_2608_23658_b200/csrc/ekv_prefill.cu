@@ -5,6 +5,7 @@
 #include "ekv_prefill_tc.cuh"
 #include "ekv_prefill_tc1.cuh"
 #include "ekv_prefill_e4m3.cuh"
+#include "ekv_prefill_e4m3_few.cuh"
 #include "ekv_prefill_tcs.cuh"
 
 using namespace ekv;
@@ -53,6 +54,9 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
     // An 8-bit pool has one kernel, whose items are rows of all heads of a group (ekv_prefill_e4m3.cuh).
     const bool e4m3 = pool->e4m3();
     const int bm = e4m3 ? tc8::kItemRows : kernel == K_WARP_MMA ? kPmBM : tc::kBM;
+    // Of an 8-bit pool's requests those with few rows go to a kernel of their own (ekv_prefill_e4m3_few.cuh): one launch each if a
+    // call has both kinds.
+    long long few = 0, few_most = 0;  // such requests, and the most rows of one
     PrefillParams p;
     p.n_prefix = R <= kPrefixMax ? 1 : 0;
     long long q_tiles = 0;
@@ -63,12 +67,17 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
             return EKV_ERR_INVALID;
         }
         if (p.n_prefix) p.tile_prefix[r] = (int)q_tiles;
+        if (e4m3 && c <= few8::kMaxRows) {
+            if (c > 0) ++few;
+            if (c > few_most) few_most = c;
+            continue;
+        }
         q_tiles += (c + bm - 1) / bm;
         if (q_tiles > 0x7fffffffLL) break;
     }
     if (p.n_prefix && q_tiles <= 0x7fffffffLL) p.tile_prefix[R] = (int)q_tiles;
-    if (q_tiles == 0) return EKV_OK;
-    if (q_tiles > 0x7fffffffLL || (e4m3 && (q_tiles * pool->desc.num_kv_heads * tc8::kMaxCluster > 0x7fffffffLL || (long long)cu_q_lens_host[R] * group >= (1LL << 29)))) {
+    if (q_tiles == 0 && few == 0) return EKV_OK;
+    if (q_tiles > 0x7fffffffLL || (e4m3 && ((q_tiles + R) * pool->desc.num_kv_heads * tc8::kMaxCluster > 0x7fffffffLL || (long long)cu_q_lens_host[R] * group >= (1LL << 29)))) {
         set_error("ekv_attn_prefill_chunk: too many query tiles");
         return EKV_ERR_INVALID;
     }
@@ -98,9 +107,26 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
         pp.cache = (const uint8_t *)pool->layer_base(layer);
         pp.scales = pool->layer_scales(layer);
         pp.block_stride = (long long)pool->block_stride;
+        pp.few_rows = few8::kMaxRows;
         pp.cluster = tc8::plan_cluster(q_tiles * pool->desc.num_kv_heads, max_blocks_per_seq, pool->sm_count);
         pp.group_magic = group > 1 ? (unsigned)(((1ull << 32) + group - 1) / group) : 0u;
-        return d128 ? tc8::launch_prefill8<128>(pool, pp, (cudaStream_t)stream) : tc8::launch_prefill8<64>(pool, pp, (cudaStream_t)stream);
+        if (q_tiles > 0) {
+            st = d128 ? tc8::launch_prefill8<128>(pool, pp, (cudaStream_t)stream) : tc8::launch_prefill8<64>(pool, pp, (cudaStream_t)stream);
+            if (st != EKV_OK) return st;
+        }
+        if (few > 0) {
+            const int items = R * pool->desc.num_kv_heads;  // the others leave at once
+            const cudaStream_t str = (cudaStream_t)stream;
+            if (d128)
+                st = few_most <= 16   ? few8::launch<128, 1>(pool, layer, pp, items, str)
+                     : few_most <= 32 ? few8::launch<128, 2>(pool, layer, pp, items, str)
+                                      : few8::launch<128, 4>(pool, layer, pp, items, str);
+            else
+                st = few_most <= 16   ? few8::launch<64, 1>(pool, layer, pp, items, str)
+                     : few_most <= 32 ? few8::launch<64, 2>(pool, layer, pp, items, str)
+                                      : few8::launch<64, 4>(pool, layer, pp, items, str);
+        }
+        return st;
     }
     if (kernel == K_TWO_HEAD) return tc::launch_prefill_tc(pool, layer, p, q, out, cu_q_lens_host[R], (cudaStream_t)stream);
     if (kernel == K_ONE_HEAD)

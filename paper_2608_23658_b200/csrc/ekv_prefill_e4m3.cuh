@@ -62,6 +62,7 @@ struct Params {
     const float *scales;
     long long block_stride;
     unsigned group_magic;  // ceil(2^32 / group): a division by the group (2 or more) is one multiplication, exact below 2^29
+    int few_rows;  // requests of at most this many rows are another kernel's (ekv_prefill_e4m3_few.cuh)
     int cluster;   // CTAs that share an item's keys
     float q_sign;  // -1 for a negative scale; 0 for a scale of 0
 };
@@ -114,13 +115,13 @@ __device__ __forceinline__ bool wait_warp(const Smem<D> &sh, int bar, uint32_t p
 }
 
 // Which request owns item `idx` (items of kItemRows (position, head) rows, requests in order)?
-__device__ __forceinline__ bool find_item(const PrefillParams &p, int idx, int &req, int &first, int &q0, int &c_r) {
+__device__ __forceinline__ bool find_item(const PrefillParams &p, int few_rows, int idx, int &req, int &first, int &q0, int &c_r) {
     if (p.n_prefix) return find_request(p, idx, kItemRows, req, first, q0, c_r);
     int acc = 0;
     for (req = 0; req < p.R; ++req) {
         q0 = p.cu_q_lens[req];
         c_r = p.cu_q_lens[req + 1] - q0;
-        const int n = (int)(((long long)c_r * p.group + kItemRows - 1) / kItemRows);
+        const int n = (long long)c_r * p.group > few_rows ? (int)(((long long)c_r * p.group + kItemRows - 1) / kItemRows) : 0;
         if (idx < acc + n) {
             first = acc;
             return true;
@@ -152,7 +153,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     const int rank = item / p.num_kv_heads, g = item - rank * p.num_kv_heads;
     const int idx = p.q_tiles - 1 - rank;
     int req = 0, first = 0, c_r = 0, q0 = 0;
-    bool work = find_item(p, idx, req, first, q0, c_r);
+    bool work = find_item(p, pp.few_rows, idx, req, first, q0, c_r);
     const int given_up = *(volatile int *)p.abort_word;  // an earlier CTA of this launch timed out
     const int seq_len = work ? p.seq_lens[req] : 0;
     if (threadIdx.x == 0) {
