@@ -1,6 +1,7 @@
 // Conversions of e4m3 codes (sm_100a has them as instructions on pairs) and the power-of-two scales of an 8-bit pool.
 #pragma once
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <stdint.h>
 
 #include "ptx.cuh"
@@ -54,6 +55,40 @@ __device__ __forceinline__ float to_f16_range(float a) {
 __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) {
     const float2 f = f16x2_to_float2(h);
     return pack_bf16x2(f.x, f.y);
+}
+
+// ---- what decode and the few-rows kernel share: P V with both operands in f16 -----------------------------------
+// V's codes are exact in f16, so one conversion instruction makes an operand of them, if V's scale 2^e_V goes elsewhere.  It goes
+// into P, and so that f16's range does not matter, a row keeps two references: m for its scores x (log2), which its sum of
+// weights p = 2^(x - m) is relative to, and M for x + e_V, i.e. for its contributions to O, which P = 2^(x + e_V - M + kPUp) =
+// p * 2^(e_V + m - M + kPUp) is relative to: one more exponential a block and row, none a score.  P then has 11 bits while a
+// contribution is within 2^-20 of the row's largest one, and an absolute error of 2^-31 of that below (bf16 would have 8 bits at
+// any distance, and V would need three instructions more for two codes).
+//   kPUp    against f16's small end; P is at most 2^(kPUp + kLazy) = 2^14
+//   kLazy   how far (log2) a score may lie above a reference before the reference is raised and l, O scaled
+//   kNoRef  references of a row without a score yet; no finite score is below
+static constexpr float kPUp = 6.f, kLazy = 8.f, kNoRef = -3.0e38f;
+
+struct RowRef {
+    float m, M, l;
+    // 2^(e + m - M + kPUp), kept finite: beyond 2^120 the weights it goes with are below 2^-106 (P is at most 2^14)
+    __device__ __forceinline__ float p_factor(float e) const { return fast_exp2(fminf((m - M) + (e + kPUp), 120.f)); }
+    // what O is to be multiplied by to be relative to m, like l
+    __device__ __forceinline__ float o_factor() const { return fast_exp2((M - m) - kPUp); }
+};
+// e_V of a V scale (a power of two; -127 for a scale of 0, whose codes the kernels take as 0)
+__device__ __forceinline__ float scale_exponent(float scale) { return (float)((int)((__float_as_uint(scale) >> 23) & 0xffu) - 127); }
+
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+// D(16x8, f32) += A(16x16, f16, row) * B(16x8, f16, col)
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
 }  // namespace ekv

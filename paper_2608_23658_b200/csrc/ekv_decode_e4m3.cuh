@@ -1,6 +1,6 @@
 // ekv_attn_decode's split pass over an 8-bit pool (the combine pass is the bf16 pool's).
 //
-//   S[head, t] = s_K(block of t) * (Q . code_K[t]),   O^T[d, head] += code_V[t, d] * (P[head, t] * s_V(block of t))
+//   S[head, t] = s_K(block of t) * (Q . code_K[t]),   O^T[d, head] += code_V[t, d] * P[head, t],   P = 2^(scale log2(e) S + e_V(block of t) - M)
 //
 // The plan, the key ranges, the four warps with rings of TMA stages and the merge are those of decode_split_kernel; a block's
 // K and V tiles are 16 x head_dim BYTES here.  What differs is the way from a code to a tensor operand:
@@ -12,8 +12,7 @@
 //   - Codes convert in pairs to f16, exactly, and K is used as f16.  Q becomes f16 too: a row is first brought to a
 //     maximum in [2^13, 2^14) by a power of two (undone with the scale of the scores), so bf16's 8 bits fit, and
 //     what falls below 2^-24 there is 2^-37 of the row's largest element, less than the fp32 sum resolves.
-//   - V goes on to bf16 (exact as well): P takes the block's s_V before its rounding, and only bf16 has the range for
-//     that.  Scaling by a power of two does not change what P's rounding loses.
+//   - V is used as f16 as well, and its scale goes into the exponent of P (e4m3.cuh has how, and what f16 keeps of P).
 #pragma once
 #include "e4m3.cuh"
 #include "ekv_internal.h"
@@ -28,13 +27,6 @@ namespace ekv {
 static constexpr int kDecode8Ctas = 4;
 template <int D>
 constexpr int kDecode8Stages = D == 128 ? 2 : 4;
-
-__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 
 template <int D>
 __global__ void __launch_bounds__(kDecodeWarps * 32, kDecode8Ctas)
@@ -107,7 +99,7 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the combine pass may take its place on the SMs (and waits there)
 
     // Q fragments (A operand, f16): rows = heads of the group (r < group), zero above; channels in the order of K's codes.
-    uint32_t qa[KSTEPS][2];
+    uint32_t qa[KSTEPS][4];
     float score_scale;
     {
         const uint2 *qrow = reinterpret_cast<const uint2 *>(p.q + ((size_t)b * p.num_q_heads + (size_t)g * p.group + r) * D);
@@ -128,29 +120,27 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
             const __half2 lo = __floats2half2_rn(__uint_as_float(raw[ks].x << 16) * up, __uint_as_float(raw[ks].x & 0xffff0000u) * up);
             const __half2 hi = __floats2half2_rn(__uint_as_float(raw[ks].y << 16) * up, __uint_as_float(raw[ks].y & 0xffff0000u) * up);
             qa[ks][0] = *reinterpret_cast<const uint32_t *>(&lo);
-            qa[ks][1] = *reinterpret_cast<const uint32_t *>(&hi);
+            qa[ks][2] = *reinterpret_cast<const uint32_t *>(&hi);
+            qa[ks][1] = qa[ks][3] = 0u;  // rows 8-15
         }
     }
 
-    // ldmatrix lane addressing: matrix mi = lane/8 is (tokens 8*(mi>>1)..+7) x (16-byte chunk 2*step + (mi&1)), row rr = lane%8
-    const int mi = lane >> 3, rr = lane & 7;
-    const int lane_row = 8 * (mi >> 1) + rr;
-    const int lane_par = mi & 1;
-    auto chunk_addr = [&](uint32_t tile, int chunk) {  // the TMA swizzle spans one row: 128 bytes, or 64
-        if (D == 128) return tile + lane_row * 128 + ((chunk ^ (lane_row & 7)) << 4);
-        return tile + lane_row * 64 + ((chunk ^ ((lane_row >> 1) & 3)) << 4);
-    };
+    // ldmatrix lane addressing (matrix mi = lane / 8: tokens 8 (mi >> 1) .. + 7, 16-byte chunk step + (mi & 1); the TMA swizzle
+    // spans one row, 128 bytes or 64): chunk `step` of a tile is at (tile + lane_at) ^ (step << 4) for even steps
+    const int mi = lane >> 3, lane_row = 8 * (mi >> 1) + (lane & 7);
+    const uint32_t lane_at = D == 128 ? lane_row * 128 + (((mi & 1) ^ (lane_row & 7)) << 4) : lane_row * 64 + (((mi & 1) ^ ((lane_row >> 1) & 3)) << 4);
 
     float o[KSTEPS][4];
 #pragma unroll
     for (int mt = 0; mt < KSTEPS; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
+    RowRef ref = {kNoRef, kNoRef, 0.f};  // of head r
     bool failed = false;
 
     // Phase parity per stage.  A skipped (invalid) block neither issues a copy nor waits, so the parity of a
     // stage advances only with the copies that really went through it, not with the iteration count.
     uint32_t stage_parity = 0;
     int i = 0;
+#pragma unroll 1
     for (; i < nw; ++i) {
         const int stage = i % STAGES;
         if ((valid_mask >> i) & 1u) {
@@ -160,45 +150,45 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
                 failed = true;
                 break;
             }
-            const uint32_t kbase = my_stages + stage * STAGE_BYTES;
-            const uint32_t vbase = kbase + TILE_BYTES;
+            const uint32_t kbase = my_stages + stage * STAGE_BYTES + lane_at, vbase = kbase + TILE_BYTES;
             const int tok0 = t_begin + (warp + kDecodeWarps * i) * 16;
             const bool partial = tok0 + 16 > L;
-            const float xs = score_scale * __shfl_sync(FULL, my_sk, i);
-            const float sv = __shfl_sync(FULL, my_sv, i);
+            const float xs = __shfl_sync(FULL, my_sk, i), sv = __shfl_sync(FULL, my_sv, i);
+            const float e_v = scale_exponent(sv);
 
             float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KSTEPS; ks += 2) {
                 uint32_t k0, k1, k2, k3;  // tokens 0-7: steps ks, ks+1; tokens 8-15: steps ks, ks+1
-                ldmatrix_x4(chunk_addr(kbase, ks + lane_par), k0, k1, k2, k3);
-                mma_f16_16816(s0, qa[ks][0], 0u, qa[ks][1], 0u, e4m3_lo(k0), e4m3_hi(k0));
-                mma_f16_16816(s1, qa[ks][0], 0u, qa[ks][1], 0u, e4m3_lo(k2), e4m3_hi(k2));
-                mma_f16_16816(s0, qa[ks + 1][0], 0u, qa[ks + 1][1], 0u, e4m3_lo(k1), e4m3_hi(k1));
-                mma_f16_16816(s1, qa[ks + 1][0], 0u, qa[ks + 1][1], 0u, e4m3_lo(k3), e4m3_hi(k3));
+                ldmatrix_x4(kbase ^ (ks << 4), k0, k1, k2, k3);
+                mma_f16(s0, qa[ks], e4m3_lo(k0), e4m3_hi(k0));
+                mma_f16(s1, qa[ks], e4m3_lo(k2), e4m3_hi(k2));
+                mma_f16(s0, qa[ks + 1], e4m3_lo(k1), e4m3_hi(k1));
+                mma_f16(s1, qa[ks + 1], e4m3_lo(k3), e4m3_hi(k3));
             }
-            float x0 = s0[0] * xs, x1 = s0[1] * xs;
-            float x2 = s1[0] * xs, x3 = s1[1] * xs;
-            uint32_t mask_lo = 0xffffffffu, mask_hi = 0xffffffffu;
+            if (!(xs > 0.f)) s0[0] = s0[1] = s1[0] = s1[1] = 0.f;  // never written: the keys are 0, whatever the codes
+            const float f = score_scale * xs;
+            float x0 = s0[0] * f, x1 = s0[1] * f, x2 = s1[0] * f, x3 = s1[1] * f;
+            uint32_t keep_lo = sv > 0.f ? 0xffffffffu : 0u, keep_hi = keep_lo;  // bytes of codes that count: tokens 2c in bytes 0 and 2, 2c + 1 in 1 and 3
             if (partial) {
                 const int t = tok0 + 2 * c;
                 if (t >= L) x0 = -INFINITY;
                 if (t + 1 >= L) x1 = -INFINITY;
                 if (t + 8 >= L) x2 = -INFINITY;
                 if (t + 9 >= L) x3 = -INFINITY;
-                mask_lo = (t < L ? 0x0000ffffu : 0u) | (t + 1 < L ? 0xffff0000u : 0u);
-                mask_hi = (t + 8 < L ? 0x0000ffffu : 0u) | (t + 9 < L ? 0xffff0000u : 0u);
+                // slots not written may hold NaN codes: 0 * NaN must not reach O
+                keep_lo &= (t < L ? 0x00ff00ffu : 0u) | (t + 1 < L ? 0xff00ff00u : 0u);
+                keep_hi &= (t + 8 < L ? 0x00ff00ffu : 0u) | (t + 9 < L ? 0xff00ff00u : 0u);
             }
-            float mx = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
-            mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, 2));
-            const float m_new = fmaxf(m_run, mx);  // finite: token tok0 < L is never masked
-            const float alpha = fast_exp2(m_run - m_new);
-            const float p0 = fast_exp2(x0 - m_new), p1 = fast_exp2(x1 - m_new);
-            const float p2 = fast_exp2(x2 - m_new), p3 = fast_exp2(x3 - m_new);
-            l_run = l_run * alpha + ((p0 + p1) + (p2 + p3));
-            m_run = m_new;
-            if (__any_sync(FULL, alpha != 1.f)) {
+            // the references are raised only when a score is 2^8 above one of them: most blocks take no vote but this one
+            float top = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
+            if (__any_sync(FULL, top > fminf(ref.m, ref.M - e_v) + kLazy)) {
+                top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
+                const float m_new = fmaxf(ref.m, top), M_new = fmaxf(ref.M, top + e_v), alpha = fast_exp2(ref.M - M_new);
+                ref.l *= fast_exp2(ref.m - m_new);
+                ref.m = m_new;
+                ref.M = M_new;
                 const float a_lo = __shfl_sync(FULL, alpha, 8 * c);
                 const float a_hi = __shfl_sync(FULL, alpha, 8 * c + 4);
 #pragma unroll
@@ -209,24 +199,21 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
                     o[mt][3] *= a_hi;
                 }
             }
-            const uint32_t pb0 = pack_bf16x2(p0 * sv, p1 * sv), pb1 = pack_bf16x2(p2 * sv, p3 * sv);
+            const float up = ref.p_factor(e_v);
+            const float p0 = fast_exp2(x0 - ref.m), p1 = fast_exp2(x1 - ref.m), p2 = fast_exp2(x2 - ref.m), p3 = fast_exp2(x3 - ref.m);
+            ref.l += (p0 + p1) + (p2 + p3);
+            const uint32_t pb0 = pack_f16x2(p0 * up, p1 * up), pb1 = pack_f16x2(p2 * up, p3 * up);
 #pragma unroll
             for (int mt = 0; mt < KSTEPS; mt += 2) {
                 uint32_t w[4];  // chunk mt: tokens 0-7, chunk mt+1: tokens 0-7, and tokens 8-15 of both
-                ldmatrix_x4_trans(chunk_addr(vbase, mt + lane_par), w[0], w[1], w[2], w[3]);
+                ldmatrix_x4_trans(vbase ^ (mt << 4), w[0], w[1], w[2], w[3]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[j] = __byte_perm(w[j], 0, 0x3120);  // (d 2r: tokens 2c, 2c+1), (d 2r+1: ...)
+                w[0] &= keep_lo, w[1] &= keep_lo, w[2] &= keep_hi, w[3] &= keep_hi;
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    uint32_t v0 = f16x2_to_bf16x2(e4m3_lo(w[j])), v1 = f16x2_to_bf16x2(e4m3_hi(w[j]));
-                    uint32_t v2 = f16x2_to_bf16x2(e4m3_lo(w[j + 2])), v3 = f16x2_to_bf16x2(e4m3_hi(w[j + 2]));
-                    if (partial) {  // slots not written may hold NaN codes: 0 * NaN must not reach O
-                        v0 &= mask_lo;
-                        v1 &= mask_lo;
-                        v2 &= mask_hi;
-                        v3 &= mask_hi;
-                    }
-                    mma_bf16_16816(o[mt + j], v0, v1, v2, v3, pb0, pb1);
+                    const uint32_t va[4] = {e4m3_lo(w[j]), e4m3_hi(w[j]), e4m3_lo(w[j + 2]), e4m3_hi(w[j + 2])};
+                    mma_f16(o[mt + j], va, pb0, pb1);
                 }
             }
         }
@@ -242,14 +229,14 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
         for (int j = i; j < nw && j < i + STAGES; ++j)
             if ((valid_mask >> j) & 1u)
                 (void)mbar_wait(my_bars + 8 * (j % STAGES), (stage_parity >> (j % STAGES)) & 1u, 200000000ull);
-        m_run = -INFINITY;
-        l_run = 0.f;
+        ref = {kNoRef, kNoRef, 0.f};
 #pragma unroll
         for (int mt = 0; mt < KSTEPS; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
     }
 
-    l_run += __shfl_xor_sync(FULL, l_run, 1);
-    l_run += __shfl_xor_sync(FULL, l_run, 2);
+    ref.l += __shfl_xor_sync(FULL, ref.l, 1);
+    ref.l += __shfl_xor_sync(FULL, ref.l, 2);
+    const float f = ref.o_factor(), f_lo = __shfl_sync(FULL, f, 8 * c), f_hi = __shfl_sync(FULL, f, 8 * c + 4);
 
     // Merge the 4 warps through shared memory (each warp reuses its own, now idle, stages).
     float *wo = reinterpret_cast<float *>(base_ptr + warp * STAGES * STAGE_BYTES);  // [8][D]
@@ -257,12 +244,12 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
     static_assert((8 * D + 16) * 4 <= STAGES * STAGE_BYTES, "merge area");
 #pragma unroll
     for (int mt = 0; mt < KSTEPS; ++mt) {  // row r of the fragment is channel 2r of the sixteen, row r+8 channel 2r+1
-        *reinterpret_cast<float2 *>(wo + (2 * c) * D + 16 * mt + 2 * r) = make_float2(o[mt][0], o[mt][2]);
-        *reinterpret_cast<float2 *>(wo + (2 * c + 1) * D + 16 * mt + 2 * r) = make_float2(o[mt][1], o[mt][3]);
+        *reinterpret_cast<float2 *>(wo + (2 * c) * D + 16 * mt + 2 * r) = make_float2(o[mt][0] * f_lo, o[mt][2] * f_lo);
+        *reinterpret_cast<float2 *>(wo + (2 * c + 1) * D + 16 * mt + 2 * r) = make_float2(o[mt][1] * f_hi, o[mt][3] * f_hi);
     }
     if (c == 0) {
-        wm[r] = m_run;
-        wm[8 + r] = l_run;
+        wm[r] = ref.m;
+        wm[8 + r] = ref.l;
     }
     __syncthreads();
 

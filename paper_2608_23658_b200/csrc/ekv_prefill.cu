@@ -56,7 +56,7 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
     const int bm = e4m3 ? tc8::kItemRows : kernel == K_WARP_MMA ? kPmBM : tc::kBM;
     // Of an 8-bit pool's requests those with few rows go to a kernel of their own (ekv_prefill_e4m3_few.cuh): one launch each if a
     // call has both kinds.
-    long long few = 0, few_most = 0;  // such requests, and the most rows of one
+    long long few = 0;
     PrefillParams p;
     p.n_prefix = R <= kPrefixMax ? 1 : 0;
     long long q_tiles = 0;
@@ -69,7 +69,6 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
         if (p.n_prefix) p.tile_prefix[r] = (int)q_tiles;
         if (e4m3 && c <= few8::kMaxRows) {
             if (c > 0) ++few;
-            if (c > few_most) few_most = c;
             continue;
         }
         q_tiles += (c + bm - 1) / bm;
@@ -116,15 +115,7 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
         }
         if (few > 0) {
             const int items = R * pool->desc.num_kv_heads;  // the others leave at once
-            const cudaStream_t str = (cudaStream_t)stream;
-            if (d128)
-                st = few_most <= 16   ? few8::launch<128, 1>(pool, layer, pp, items, str)
-                     : few_most <= 32 ? few8::launch<128, 2>(pool, layer, pp, items, str)
-                                      : few8::launch<128, 4>(pool, layer, pp, items, str);
-            else
-                st = few_most <= 16   ? few8::launch<64, 1>(pool, layer, pp, items, str)
-                     : few_most <= 32 ? few8::launch<64, 2>(pool, layer, pp, items, str)
-                                      : few8::launch<64, 4>(pool, layer, pp, items, str);
+            st = d128 ? few8::launch<128>(pool, layer, pp, items, (cudaStream_t)stream) : few8::launch<64>(pool, layer, pp, items, (cudaStream_t)stream);
         }
         return st;
     }

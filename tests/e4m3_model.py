@@ -87,9 +87,9 @@ class Cache:
         return x[:, 0], x[:, 1]
 
 
-def attention(q, K, V, limits, scale):
+def attention(q, K, V, limits, scale, sv=None):
     """q [c, Hq, D], K and V [L, Hk, D] float64; row i sees keys j < limits[i] with `valid` rows (NaN rows of K stand for keys
-    that are skipped).  Returns (out, bound): bound is how far a bf16 result may be off (see below)."""
+    that are skipped).  sv: V's scale of each key and head [L, Hk], for the bound.  Returns (out, bound): bound is how far a bf16 result may be off (see below)."""
     q, K, V = (torch.as_tensor(x, dtype=torch.float64) for x in (q, K, V))
     c, Hq, D = q.shape
     L, Hk, _ = K.shape
@@ -115,7 +115,11 @@ def attention(q, K, V, limits, scale):
         size = p @ V[:, h // G].abs()
         reach = (q[:, h].abs() @ K[:, h // G].abs().T * abs(scale)).where(seen, torch.zeros(()).double()).amax(1, keepdim=True)
         d = (D + 4) * 2.0 ** -23 * reach + 2.0 ** -21
-        bound[:, h] = 2.0 ** -8 * (size + out[:, h].abs()) + (2 * d + (L + 200) * 2.0 ** -24) * size + 1e-30
+        # P in f16 (decode, few rows): 2^-11 of it, less than the above, down to 2^-14, and half of f16's smallest step, 2^-25, below.
+        # P is exp2 of the score with V's exponent on top, scaled so that a row's largest is 2^6 at least: 2^-31 of the largest
+        # p_j s_j at most for each key, times its code, which is 448 at most.
+        floor = 0.0 if sv is None else 2.0 ** -31 * 448 * seen.sum(1, keepdim=True) * (p * torch.as_tensor(sv, dtype=torch.float64)[:, h // G]).amax(1, keepdim=True)
+        bound[:, h] = floor + 2.0 ** -8 * (size + out[:, h].abs()) + (2 * d + (L + 200) * 2.0 ** -24) * size + 1e-30
     return out, bound
 
 

@@ -246,9 +246,14 @@ class Case:
             self.K.append(kk[at:at + L])
             self.V.append(vv[at:at + L])
             at += L
+        self.V_ids = [s // 16 for s in self.slots]
         self.d_tables = self.tables.to(torch.int32).to(DEV)
         self.d_lens = torch.tensor(self.lengths, dtype=torch.int32, device=DEV)
         self.rng = rng
+
+    def sv(self, b, L=None):
+        """V's scale of every key of a sequence, as the pool has it now."""
+        return self.pool.layer_scales(0)[self.V_ids[b][:L].to(DEV), 1].double().cpu()
 
     def queries(self, n, mag=1.0):
         s = self.shape
@@ -256,7 +261,7 @@ class Case:
 
     def check_decode(self, q, out, scale, what=""):
         for b, L in enumerate(self.lengths):
-            want, bound = M.attention(q[b:b + 1].double(), self.K[b], self.V[b], [L], scale)
+            want, bound = M.attention(q[b:b + 1].double(), self.K[b], self.V[b], [L], scale, self.sv(b))
             M.assert_within(out[b:b + 1], want, bound, f"{what} sequence {b} of {L}")
 
 
@@ -344,7 +349,7 @@ def test_decode_over_long_offsets_on_a_stream_in_a_graph():
             q.copy_(c.queries(2))
             g.replay()
             for b, L in enumerate(lens):
-                want, bound = M.attention(q[b:b + 1].double().cpu(), c.K[b][:L], c.V[b][:L], [L], 0.09)
+                want, bound = M.attention(q[b:b + 1].double().cpu(), c.K[b][:L], c.V[b][:L], [L], 0.09, c.sv(b, L))
                 M.assert_within(out[b:b + 1], want, bound)
 
 
@@ -377,7 +382,7 @@ def check_prefill(c, chunks, scale=None, mag=1.0, tables=None, what=""):
         if n > L:
             assert (out[a:b] == 0).all(), what
         elif n:
-            want, bound = M.attention(q[a:b].double(), c.K[r], c.V[r], torch.arange(L - n, L) + 1, scale)
+            want, bound = M.attention(q[a:b].double(), c.K[r], c.V[r], torch.arange(L - n, L) + 1, scale, c.sv(r))
             M.assert_within(out[a:b], want, bound, f"{what} request {r}: {n} rows of {L}")
     return q, cu, out
 
@@ -453,16 +458,26 @@ def test_prefill_invalid_blocks_and_requests():
         assert c.pool.poll_status() == ekv.Status.ERR_BLOCK_OOB
 
 
-def test_prefill_never_written_blocks_read_as_zero():
-    """Scale 0: the values are 0, whatever the codes (here NaN)."""
+def test_never_written_blocks_read_as_zero():
+    """Scale 0: the values are 0, whatever the codes (here NaN); and V blocks of zeros, whose scale is the smallest there is."""
     shape = I.TINY
-    c = Case(shape, [64], seed=85)
+    c = Case(shape, [64, 100], seed=85)
     with c.pool:
         ids = c.tables[0, 1:3].long()
         c.pool.layer_scales(0)[ids.to(DEV)] = 0.0
         c.pool.layer_tensor(0).view(torch.uint8)[ids.to(DEV)] = 0x7F
         c.K[0][16:48], c.V[0][16:48] = 0.0, 0.0
-        check_prefill(c, [64])
+        # many keys whose values are 0 and whose scores are not the lowest: their weights count
+        zero = torch.zeros(80, 2, 64, dtype=torch.bfloat16)
+        k = rows(c.rng, 80, shape, 1.0)
+        c.pool.write_kv(0, k.to(DEV), zero.to(DEV), c.slots[1][:80].to(DEV))
+        kk, vv = c.pool.read_kv(0, c.slots[1].to(DEV))
+        c.K[1], c.V[1] = kk.double().cpu(), vv.double().cpu()
+        assert float(c.pool.layer_scales(0)[int(c.tables[1, 0]), 1].max()) == 2.0 ** -112
+        for chunks in ([64, 100], [3, 2], [20, 9], [0, 40]):
+            check_prefill(c, chunks)
+        q = c.queries(2)
+        c.check_decode(q, c.pool.attn_decode(0, q.to(DEV), c.d_tables, c.d_lens, 0.125), 0.125)
 
 
 def test_prefill_on_streams_and_in_a_replayed_graph():
@@ -507,7 +522,7 @@ def test_prompt_in_chunks_then_decode_steps():
             L = int(lens)
             at = tables[0, torch.arange(L, device=DEV) // 16].long() * 16 + torch.arange(L, device=DEV) % 16
             kk, vv = (x.double().cpu() for x in pool.read_kv(0, at))
-            want, bound = M.attention(q.double(), kk, vv, torch.arange(L - n, L) + 1, 0.09)
+            want, bound = M.attention(q.double(), kk, vv, torch.arange(L - n, L) + 1, 0.09, pool.layer_scales(0)[at // 16, 1].double().cpu())
             out = pool.attn_prefill_chunk(0, q.to(DEV), tables, cu, torch.tensor([0, n], dtype=torch.int32), lens, 0.09)
             M.assert_within(out, want, bound, f"{n} rows of {L}")
             if n == 1:

@@ -203,7 +203,8 @@ def test_decode_steps_in_one_replayed_graph(dtype):
                     hist = torch.stack(history_k[r]).double()
                     step_of = hist.abs().max() * 2.0 ** -4 if dtype == ekv.EKV_E4M3 else 0.0
                     assert ((kk.double().cpu() - hist).abs() <= step_of).all()
-                    want, bound = M.attention(hq[r:r + 1].double(), kk.double().cpu(), vv.double().cpu(), [L], 1 / math.sqrt(D))
+                    sv = pool.layer_scales(0)[at // 16, 1].double().cpu() if dtype == ekv.EKV_E4M3 else None
+                    want, bound = M.attention(hq[r:r + 1].double(), kk.double().cpu(), vv.double().cpu(), [L], 1 / math.sqrt(D), sv)
                     M.assert_within(out[r:r + 1], want, bound, f"step {step} request {r}")
         assert int(cursor) == sum(-(-len(h) // 16) for h in history_k)
         assert pool.poll_status() == ekv.Status.OK
