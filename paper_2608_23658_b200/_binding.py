@@ -169,10 +169,20 @@ def _dptr(t):
     return t.data_ptr()
 
 
+_current_raw_stream = None
+
+
 def _stream(stream):
+    """Address of a stream; None = torch's current stream on the current device.  (Asked for by its raw address: building the
+    Stream object costs more than the rest of a small call.)"""
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        global _current_raw_stream
+        if _current_raw_stream is None:
+            import torch
+            raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+            torch.cuda.current_stream()  # initialises CUDA
+            _current_raw_stream = (lambda: raw(device())) if raw and device else (lambda: torch.cuda.current_stream().cuda_stream)
+        return _current_raw_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -256,9 +266,9 @@ def ekv_extend_tables(pool: int, new_tokens, seq_lens, block_tables, free_ids, f
     out = seq_lens if seq_lens_out is None else seq_lens_out
     cursor_out = free_cursor if free_cursor_out is None else free_cursor_out
     assert out.shape[0] == R and free_cursor.numel() == 1 and cursor_out.numel() == 1
-    for t in (new_tokens, seq_lens, block_tables, free_ids, free_cursor, cu_q_lens, out, cursor_out):
-        assert t.element_size() == 4, "lengths, tables, ids and offsets are int32"
-    assert slot_mapping.element_size() == 8, "the slot mapping is int64"
+    assert new_tokens.itemsize == seq_lens.itemsize == block_tables.itemsize == free_ids.itemsize == free_cursor.itemsize == \
+        cu_q_lens.itemsize == out.itemsize == cursor_out.itemsize == 4, "lengths, tables, ids and offsets are int32"
+    assert slot_mapping.itemsize == 8, "the slot mapping is int64"
     _check(load_library().ekv_extend_tables(pool, _dptr(new_tokens), _dptr(seq_lens), R, _dptr(block_tables), max_blocks,
                                             _dptr(free_ids), int(free_ids.shape[0]), _dptr(free_cursor), _dptr(slot_mapping),
                                             int(slot_mapping.shape[0]), _dptr(cu_q_lens), _dptr(out), _dptr(cursor_out),

@@ -111,11 +111,10 @@ class Pool:
     def read_kv(self, layer, slot_mapping, k_out=None, v_out=None, stream=None):
         """Values stored in the slots as bf16 rows (k, v), each [T, Hkv, head_dim].  Rows of negative slots are left as they
         were: hand in tensors of your own if the mapping has any."""
-        shape = (int(slot_mapping.shape[0]), self.num_kv_heads, self.head_dim)
         if k_out is None:
-            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            k_out = torch.empty((slot_mapping.shape[0], self.num_kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
         if v_out is None:
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            v_out = torch.empty_like(k_out)
         B.ekv_read_kv(self.handle, layer, k_out, v_out, slot_mapping, stream)
         return k_out, v_out
 
