@@ -20,6 +20,7 @@ namespace ekv {
 
 static constexpr int kW8Threads = 256;
 static constexpr int kW8Warps = kW8Threads / 32;
+static constexpr int kW8ClaimedThreads = 512;  // a warp for each (K|V, head) of a block with 8 kv-heads: all its rows are on their way at once
 static constexpr int kW8TokensPerCta = 16;
 static constexpr int kScanTokens = 1024;
 
@@ -161,6 +162,7 @@ __global__ void __launch_bounds__(kW8Threads) write8_scan_kernel(const Write8Par
 // claims[n] = {T - first token, last token + 1} of block n, both by atomic maximum over zeros
 __global__ void __launch_bounds__(256) write8_claim_kernel(const Write8Params p) {
     const int t = blockIdx.x * 256 + threadIdx.x;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (t >= p.T) return;
     const long long s = p.slots[t];
     if (s < 0) return;
@@ -173,46 +175,46 @@ __global__ void __launch_bounds__(256) write8_claim_kernel(const Write8Params p)
     atomicMax(&p.claims[n].y, t + 1);
 }
 
+// A CTA takes the blocks that begin in its 16 tokens; its warps share out their (block, K|V, head) tasks.  Everything a warp needs
+// to know it works out itself, from the caches: the only meeting is the one after which the claims may go.
 template <int D>
-__global__ void __launch_bounds__(kW8Threads) write8_claimed_kernel(const Write8Params p) {
-    __shared__ int tok[16];
-    __shared__ int todo[kW8TokensPerCta], last_of[kW8TokensPerCta];
-    __shared__ int count;
-    const int t0 = blockIdx.x * kW8TokensPerCta;
-    if (threadIdx.x < 32) {
-        const int t = t0 + (int)threadIdx.x;
-        bool mine = false;
-        int last = 0;
-        if (threadIdx.x < kW8TokensPerCta && t < p.T) {
-            const long long s = p.slots[t];
-            if (s >= 0 && (s >> 4) < *p.live) {
-                const volatile int2 *c = p.claims + (s >> 4);
-                mine = c->x == p.T - t;  // first token of its block; a block done already reads 0, which no token is
-                last = c->y - 1;
-            }
+__global__ void __launch_bounds__(kW8ClaimedThreads, 2) write8_claimed_kernel(const Write8Params p) {
+    __shared__ int tok_of[kW8ClaimedThreads / 32][16];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int t0 = blockIdx.x * kW8TokensPerCta, t = t0 + lane;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // the claims are complete (this launch's CTAs come up beside the last of them)
+    bool mine = false;
+    int last = 0;
+    long long n = -1;
+    if (lane < kW8TokensPerCta && t < p.T) {
+        const long long s = p.slots[t];
+        if (s >= 0 && (s >> 4) < *p.live) {
+            n = s >> 4;
+            const volatile int2 *c = p.claims + n;
+            mine = c->x == p.T - t;  // first token of its block; a block done already reads 0, which no token is
+            last = c->y - 1;
         }
-        const unsigned mask = __ballot_sync(0xffffffffu, mine);
-        if (mine) {
-            const int at = __popc(mask & ((1u << threadIdx.x) - 1u));
-            todo[at] = t;
-            last_of[at] = last;
-        }
-        if (threadIdx.x == 0) count = __popc(mask);
     }
+    const unsigned mask = __ballot_sync(0xffffffffu, mine);
     __syncthreads();
-    for (int b = 0; b < count; ++b) {
-        const int first = todo[b], last = last_of[b];
-        const long long n = p.slots[first] >> 4;
-        if (threadIdx.x < 16) tok[threadIdx.x] = 0;
-        if (threadIdx.x == 0) p.claims[n] = make_int2(0, 0);
-        __syncthreads();
-        for (int i = first + threadIdx.x; i <= last; i += kW8Threads) {
-            const long long o = p.slots[i];
-            if (o >= 0 && (o >> 4) == n) atomicMax(&tok[(int)(o & 15)], i + 1);
+    if (warp == 0 && mine) p.claims[n] = make_int2(0, 0);
+    const int per_block = 2 * p.num_kv_heads, tasks = __popc(mask) * per_block;
+    int *tok = tok_of[warp];
+    for (int i = warp; i < tasks; i += kW8ClaimedThreads / 32) {
+        const int b = i / per_block, pair = i - b * per_block;
+        const int lead = (int)__fns(mask, 0, b + 1);  // lane of the b-th block's first token
+        const long long block = __shfl_sync(0xffffffffu, n, lead);
+        const int to = __shfl_sync(0xffffffffu, last, lead);
+        __syncwarp();
+        if (lane < 16) tok[lane] = 0;
+        __syncwarp();
+        for (int k = t0 + lead + lane; k <= to; k += 32) {
+            const long long o = p.slots[k];
+            if (o >= 0 && (o >> 4) == block) atomicMax(&tok[(int)(o & 15)], k + 1);  // of duplicate slots the last one
         }
-        __syncthreads();
-        write8_block<D>(p, n, tok);
-        __syncthreads();  // tok is used again
+        __syncwarp();
+        const int kv = pair >= p.num_kv_heads;
+        write8_task<D>(p, block, kv, pair - kv * p.num_kv_heads, tok, lane);
     }
 }
 
@@ -224,7 +226,17 @@ static ekv_status_t launch_write8(ekv_pool *pool, const Write8Params &p, cudaStr
         write8_claim_kernel<<<(unsigned)(((long long)p.T + 255) / 256), 256, 0, stream>>>(p);
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return cuda_fail(e, "ekv_write_kv: claim launch");
-        write8_claimed_kernel<D><<<(unsigned)(((long long)p.T + kW8TokensPerCta - 1) / kW8TokensPerCta), kW8Threads, 0, stream>>>(p);
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cfg.gridDim = dim3((unsigned)(((long long)p.T + kW8TokensPerCta - 1) / kW8TokensPerCta));
+        cfg.blockDim = dim3(kW8ClaimedThreads);
+        cfg.stream = stream;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, write8_claimed_kernel<D>, p);
+        if (e != cudaSuccess) return cuda_fail(e, "ekv_write_kv launch");
     }
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, "ekv_write_kv launch");

@@ -67,42 +67,70 @@ __global__ void __launch_bounds__(kWriteThreads) write_kv_kernel(uint4 *__restri
     }
 }
 
-// ekv_read_kv: a thread takes 8 channels of one row -- 16 bytes of bf16, or 8 codes and their scale -- and stores 16 bytes.
-// Bound by memory; a code times a power of two needs 4 significant bits, so the bf16 is exact.
+// ekv_read_kv: a thread takes kReadUnroll pieces of 16 channels of one row each -- 32 bytes of bf16, or 16 codes and their scale --
+// and has the loads of all of them on their way before it stores.  Bound by memory; a code times a power of two needs 4 significant
+// bits, so the bf16 is exact.
+static constexpr int kReadUnroll = 4;
+
 template <bool kE4m3>
 __global__ void __launch_bounds__(256) read_kv_kernel(const uint8_t *__restrict__ cache, const float *__restrict__ scales,
                                                       uint4 *__restrict__ k, uint4 *__restrict__ v, const long long *__restrict__ slot_mapping,
-                                                      int T, int tokens_per_cta, int num_kv_heads, int pieces_per_row,
+                                                      long long pieces, int num_kv_heads, int pieces_per_row, int token_shift,
                                                       long long block_stride, const long long *__restrict__ live_ptr, unsigned *status) {
     const long long live = *live_ptr;
     const int row_pieces = num_kv_heads * pieces_per_row, token_pieces = 2 * row_pieces;
-    const long long first = (long long)blockIdx.x * tokens_per_cta;
-    const int tokens = (int)min((long long)tokens_per_cta, (long long)T - first);
-    for (int i = threadIdx.x; i < tokens * token_pieces; i += 256) {
-        const int dt = i / token_pieces, rem = i - dt * token_pieces;
-        const int kv = rem >= row_pieces, hp = rem - kv * row_pieces;
+    long long to[kReadUnroll];  // piece of k_out or v_out (16 channels); -1: none
+    int rem[kReadUnroll];
+    const uint8_t *src[kReadUnroll];
+    const float *sc[kReadUnroll];
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        const long long i = ((long long)blockIdx.x * kReadUnroll + u) * 256 + threadIdx.x;
+        to[u] = -1;
+        if (i >= pieces) continue;
+        const long long t = token_shift >= 0 ? i >> token_shift : i / token_pieces;
+        rem[u] = (int)(i - t * token_pieces);
+        const int kv = rem[u] >= row_pieces, hp = rem[u] - kv * row_pieces;
         const int h = hp / pieces_per_row, c = hp - h * pieces_per_row;
-        const long long t = first + dt, s = slot_mapping[t];
+        const long long s = slot_mapping[t];
         if (s < 0) continue;
         const long long n = s >> 4;
         if (n >= live) {
-            if (rem == 0) atomicOr(status, EKV_DEV_FLAG_OOB);
+            if (rem[u] == 0) atomicOr(status, EKV_DEV_FLAG_OOB);
             continue;
         }
         const int row = (kv * num_kv_heads + h) * 16 + (int)(s & 15);
-        const uint8_t *src = cache + n * block_stride + ((long long)row * pieces_per_row + c) * (kE4m3 ? 8 : 16);
-        uint4 out;
+        src[u] = cache + n * block_stride + ((long long)row * pieces_per_row + c) * (kE4m3 ? 16 : 32);
+        if (kE4m3) sc[u] = scales + (n * 2 + kv) * num_kv_heads + h;
+        to[u] = t * row_pieces + hp;
+    }
+    uint4 a[kReadUnroll], b[kReadUnroll];
+    float scale[kReadUnroll];
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        if (to[u] < 0) continue;
+        a[u] = *reinterpret_cast<const uint4 *>(src[u]);
+        if (kE4m3) scale[u] = *sc[u];
+        else b[u] = *reinterpret_cast<const uint4 *>(src[u] + 16);
+    }
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        if (to[u] < 0) continue;
         if (kE4m3) {
-            const uint2 w = *reinterpret_cast<const uint2 *>(src);
-            const float sc = scales[(n * 2 + kv) * num_kv_heads + h];
-            const float2 a = f16x2_to_float2(e4m3_lo(w.x)), b = f16x2_to_float2(e4m3_hi(w.x));
-            const float2 e = f16x2_to_float2(e4m3_lo(w.y)), f = f16x2_to_float2(e4m3_hi(w.y));
-            out = make_uint4(pack_bf16x2(a.x * sc, a.y * sc), pack_bf16x2(b.x * sc, b.y * sc), pack_bf16x2(e.x * sc, e.y * sc),
-                             pack_bf16x2(f.x * sc, f.y * sc));
-        } else {
-            out = *reinterpret_cast<const uint4 *>(src);
+            const uint32_t w[4] = {a[u].x, a[u].y, a[u].z, a[u].w};
+            uint32_t o[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 lo = f16x2_to_float2(e4m3_lo(w[j])), hi = f16x2_to_float2(e4m3_hi(w[j]));
+                o[2 * j] = pack_bf16x2(lo.x * scale[u], lo.y * scale[u]);
+                o[2 * j + 1] = pack_bf16x2(hi.x * scale[u], hi.y * scale[u]);
+            }
+            a[u] = make_uint4(o[0], o[1], o[2], o[3]);
+            b[u] = make_uint4(o[4], o[5], o[6], o[7]);
         }
-        (kv ? v : k)[t * row_pieces + hp] = out;
+        uint4 *dst = (rem[u] >= row_pieces ? v : k) + 2 * to[u];
+        dst[0] = a[u];
+        dst[1] = b[u];
     }
 }
 
@@ -119,14 +147,20 @@ extern "C" ekv_status_t ekv_read_kv(ekv_pool_t *pool, int32_t layer, void *k_out
         return EKV_ERR_INVALID;
     }
     if (T == 0) return EKV_OK;
-    const int pieces_per_row = pool->desc.head_dim / 8, token_pieces = 2 * pool->desc.num_kv_heads * pieces_per_row;
-    const int tokens_per_cta = token_pieces >= 1024 ? 1 : 1024 / token_pieces;  // about four pieces a thread
-    const unsigned grid = (unsigned)(((long long)T + tokens_per_cta - 1) / tokens_per_cta);
+    const int pieces_per_row = pool->desc.head_dim / 16, token_pieces = 2 * pool->desc.num_kv_heads * pieces_per_row;
+    int token_shift = -1;
+    if ((token_pieces & (token_pieces - 1)) == 0)
+        for (token_shift = 0; (1 << token_shift) < token_pieces;) ++token_shift;
+    const long long pieces = (long long)T * token_pieces, per_cta = 256 * kReadUnroll;
+    if ((pieces + per_cta - 1) / per_cta > 0x7fffffffLL) {
+        set_error("ekv_read_kv: too many rows (T=%d)", T);
+        return EKV_ERR_INVALID;
+    }
     const auto kernel = pool->e4m3() ? read_kv_kernel<true> : read_kv_kernel<false>;
-    kernel<<<grid, 256, 0, (cudaStream_t)stream>>>((const uint8_t *)pool->layer_base(layer), pool->e4m3() ? pool->layer_scales(layer) : nullptr,
-                                                   (uint4 *)k_out, (uint4 *)v_out, (const long long *)slot_mapping, T, tokens_per_cta,
-                                                   pool->desc.num_kv_heads, pieces_per_row, (long long)pool->block_stride, pool->d_live,
-                                                   pool->d_status);
+    kernel<<<(unsigned)((pieces + per_cta - 1) / per_cta), 256, 0, (cudaStream_t)stream>>>(
+        (const uint8_t *)pool->layer_base(layer), pool->e4m3() ? pool->layer_scales(layer) : nullptr, (uint4 *)k_out, (uint4 *)v_out,
+        (const long long *)slot_mapping, pieces, pool->desc.num_kv_heads, pieces_per_row, token_shift, (long long)pool->block_stride, pool->d_live,
+        pool->d_status);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail(e, "ekv_read_kv launch");
     return EKV_OK;
