@@ -20,7 +20,8 @@
 //   - V goes to bf16 with its scale multiplied in (exact, a power of two), since only bf16 has the scales' range; P is bf16.
 //
 //   warp 0        MMA issuer: S = Q K^T (both from shared memory) and O += P V (P from TMEM, V MN-major)
-//   warp 1        TMEM allocation; warps 2, 3 complete the warpgroup
+//   warp 1        TMEM allocation; warp 2: item scheduler (the kernel is persistent, a CTA an SM: set-up and instruction caches
+//                 are paid for once, and the next item is decoded beside the current one); warp 3 completes the warpgroup
 //   warps 4-7     rows 0-127: Q into shared memory, softmax (a thread a row), write-out
 //   warps 8-11    rows 128-255
 //   warps 12-15   converters: codes come through the block table by 16-byte asynchronous copies into places of shared memory
@@ -78,6 +79,9 @@ struct Geo {
     static constexpr int kOffRaw = kOffV + kStages * kTileBytes;  // one of K, one of V
     static constexpr int kOffBar = kOffRaw + 2 * kRawBytes;
     enum Bar { Q_READY = 0, K_FULL = 2, K_EMPTY = 4, V_FULL = 6, V_EMPTY = 8, S_READY = 10, P_PART = 12, P_READY = 14, DRAIN = 16, NBAR = 17 };
+    __device__ static __forceinline__ uint32_t arrivals(int bar) {  // warps for Q, K and V tiles, threads for P, a commit for the others
+        return bar >= P_PART && bar < DRAIN ? 128u : (bar < K_EMPTY || (bar >= V_FULL && bar < V_EMPTY)) ? 4u : 1u;
+    }
     static constexpr int kOffFlags = kOffBar + 8 * NBAR;       // abort flag, TMEM address, 4 masks of invalid blocks
     static constexpr int kOffKScale = kOffBar + 192;           // [4 tiles][8 blocks] floats
     static constexpr int kOffQInv = kOffKScale + 128;          // [256 rows] floats
@@ -85,7 +89,8 @@ struct Geo {
     static constexpr int kOffPartML = 2 * kBM * D * 4;         // ... and (m, l) of [2][128]
     static constexpr int kOffPartW = kOffPartML + 2 * kBM * 8;  // the CTA's own weights of its rows' partials: at most 512
     static_assert(kOffPartW + 512 * 4 <= kOffRaw, "merge area");
-    static constexpr int kSmemBytes = kOffQInv + 1024 + 1024;  // + alignment slack
+    static constexpr int kOffItem = kOffQInv + 1024;           // two slots of the scheduler: state and seven numbers
+    static constexpr int kSmemBytes = kOffItem + 128 + 1024;    // + alignment slack
     static_assert(kOffFlags + 24 <= kOffKScale && kSmemBytes <= 232448, "shared memory");
     // kind::f16 instruction descriptors, D = f32, M = 128: QK with f16 operands, PV with bf16 ones and V MN-major
     static constexpr uint32_t kIdescQK = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
@@ -103,6 +108,8 @@ struct Smem {
     // softmax of tile j has read its entry
     __device__ __forceinline__ volatile int *bad_mask(int tile) const { return (volatile int *)(ptr + Geo<D>::kOffFlags + 8 + 4 * (tile & 3)); }
     __device__ __forceinline__ float *k_scale(int tile) const { return (float *)(ptr + Geo<D>::kOffKScale) + 8 * (tile & 3); }
+    __device__ __forceinline__ volatile int *progress() const { return (volatile int *)(ptr + Geo<D>::kOffItem + 64); }  // tile that the converters are at
+    __device__ __forceinline__ int *item(int n) const { return (int *)(ptr + Geo<D>::kOffItem) + 8 * (n & 1); }
     __device__ __forceinline__ float *q_inv() const { return (float *)(ptr + Geo<D>::kOffQInv); }
 };
 
@@ -147,72 +154,97 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cluster = pp.cluster, part = blockIdx.x % cluster;  // CTAs that share an item's keys; which of them this is
 
-    // ---- which (request, rows, kv-head)?  Heaviest (latest) items first, all kv-heads of one next to each other.  The reads of
-    // device memory are under way while barriers and TMEM are set up.
-    const int item = blockIdx.x / cluster;
-    const int rank = item / p.num_kv_heads, g = item - rank * p.num_kv_heads;
-    const int idx = p.q_tiles - 1 - rank;
-    int req = 0, first = 0, c_r = 0, q0 = 0;
-    bool work = find_item(p, pp.few_rows, idx, req, first, q0, c_r);
-    const int given_up = *(volatile int *)p.abort_word;  // an earlier CTA of this launch timed out
-    const int seq_len = work ? p.seq_lens[req] : 0;
-    if (threadIdx.x == 0) {
-        for (int x = 0; x < 2; ++x) {
-            mbar_init(sh.bar(G::Q_READY + x), 4);
-            mbar_init(sh.bar(G::K_FULL + x), 4);
-            mbar_init(sh.bar(G::K_EMPTY + x), 1);
-            mbar_init(sh.bar(G::V_FULL + x), 4);
-            mbar_init(sh.bar(G::V_EMPTY + x), 1);
-            mbar_init(sh.bar(G::S_READY + x), 1);
-            mbar_init(sh.bar(G::P_PART + x), 128);
-            mbar_init(sh.bar(G::P_READY + x), 128);
+    // One thread sets up the barriers, for every item anew, so that all phases of an item count from 0.
+    auto set_barriers = [&]() {
+#pragma unroll 1
+        for (int i = 0; i < G::NBAR; ++i) {
+            mbar_inval(sh.bar(i));
+            mbar_init(sh.bar(i), G::arrivals(i));
         }
-        mbar_init(sh.bar(G::DRAIN), 1);
-        *sh.abort_flag() = 0;
         mbar_fence_init();
+    };
+    if (threadIdx.x == 64) {
+#pragma unroll 1
+        for (int i = 0; i < G::NBAR; ++i) mbar_init(sh.bar(i), G::arrivals(i));
+        mbar_fence_init();
+        *sh.abort_flag() = 0;
     }
     if (warp == 1) {
         cp::tcgen05_alloc(cp::cta_group_1, sh.tmem_slot(), 512);
         cp::tcgen05_relinquish_alloc_permit(cp::cta_group_1);
     }
-
     const int group = p.group;
-    const int row0 = (idx - first) * kItemRows;               // first of the request's c_r * group rows
-    const int rows_here = min(kItemRows, c_r * group - row0);
-    const int L = min(seq_len, p.max_blocks * 16);
-    const int prefix = L - c_r;
-    // element offset of a row of the item in q and out
-    auto position = [&](int r) { return group == 1 ? row0 + r : (int)__umulhi((unsigned)(row0 + r), pp.group_magic); };
-    auto row_offset = [&](int r) {
-        const int pos = position(r), hg = row0 + r - pos * group;
-        return ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D;
+    auto by_group = [&](int r) { return group == 1 ? r : (int)__umulhi((unsigned)r, pp.group_magic); };
+
+    // ---- the scheduler (warp 2): which (request, rows, kv-head) is next?  Items are listed heaviest (latest) first, all kv-heads of
+    // one next to each other; a CTA starts with the one of its own number and draws the others from a counter, each while the CTA
+    // works on the one before.  Rows that have no keys to see are dealt with here.  (The CTAs of a cluster have one item.)
+    auto post = [&](int item, int n) {
+        const int n_items = p.q_tiles * p.num_kv_heads;
+        int *slot = sh.item(n);
+        for (;; item = -1) {
+            if (item < 0) {
+                if (cluster == 1 && lane == 0) item = (int)gridDim.x + atomicAdd(p.abort_word + 1, 1);
+                item = cluster == 1 ? __shfl_sync(0xffffffffu, item, 0) : n_items;
+            }
+            // past the end, or (not for a cluster, whose CTAs have to stay together) another CTA of this launch timed out
+            const bool over = item >= n_items || (cluster == 1 && *(volatile int *)p.abort_word);
+            const int rank = item / p.num_kv_heads, g = item - rank * p.num_kv_heads, idx = p.q_tiles - 1 - rank;
+            int req = 0, first = 0, c_r = 0, q0 = 0;
+            if (!over && !find_item(p, pp.few_rows, idx, req, first, q0, c_r)) continue;
+            const int row0 = (idx - first) * kItemRows;  // first of the request's c_r * group rows
+            const int rows_here = min(kItemRows, c_r * group - row0);
+            const int L = over ? 0 : min(p.seq_lens[req], p.max_blocks * 16);
+            if (!over && rows_here <= 0) continue;  // the device's offsets say less than the host's
+            if (!over && L < c_r) {  // malformed request: zero rows, latch
+                if (lane == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+                for (int r = 0; r < rows_here && part == 0; ++r) {
+                    const int pos = by_group(row0 + r), hg = row0 + r - pos * group;
+                    if (lane < kPieces) reinterpret_cast<uint4 *>(p.out + ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D)[lane] = make_uint4(0u, 0u, 0u, 0u);
+                }
+                continue;
+            }
+            if (lane == 0) slot[0] = over ? 0 : 1, slot[1] = req, slot[2] = g, slot[3] = row0, slot[4] = rows_here, slot[5] = q0, slot[6] = L, slot[7] = L - c_r;
+            break;
+        }
+        __syncwarp();
     };
-    // no rows: the device's offsets say less than the host's.  (A cluster has to stay together: all but the last reason are the same
-    // for its CTAs, and for that one they go by their own waits.)
-    work = work && rows_here > 0 && !(cluster == 1 && given_up);
-    if (work && prefix < 0) {  // malformed request: zero rows, latch
-        if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
-        for (int e = threadIdx.x; e < rows_here * kPieces && part == 0; e += kThreads)
-            *reinterpret_cast<uint4 *>(p.out + row_offset(e / kPieces) + (e % kPieces) * 8) = make_uint4(0u, 0u, 0u, 0u);
-        work = false;
-    }
-    // the address of TMEM is there, and (it does not matter who is first) so is what a CTA without work gives back
     fence_before();
     __syncthreads();
     fence_after();
     const uint32_t tmem = *sh.tmem_slot();
-    if (!work) {
-        if (warp == 1) cp::tcgen05_dealloc(cp::cta_group_1, tmem, 512);
-        return;
-    }
-    const int kv_end = min(L, prefix + position(rows_here - 1) + 1);  // keys any row of the item may see
-    const int all_tiles = (kv_end + kBN - 1) / kBN;
-    const int tile0 = (int)((long long)all_tiles * part / cluster);  // this CTA's key tiles: tile0 .. tile0 + n_tiles - 1 (possibly none)
-    const int n_tiles = (int)((long long)all_tiles * (part + 1) / cluster) - tile0;
-    const int n_blocks = (kv_end + 15) >> 4;
-    // by_rows: slot x holds rows 128 x .. and sees every key tile j.  Else both hold rows 0 .. and slot x sees tiles x, x + 2, ...
-    const bool by_rows = rows_here > kBM;
-    const bool merge = cluster > 1 || !by_rows;
+
+    // ---- the current item, as each role reads it from the scheduler's slot
+    int req, g, row0, rows_here, q0, prefix, kv_end, tile0, n_tiles, n_blocks;
+    bool by_rows, merge;
+    auto position = [&](int r) { return by_group(row0 + r); };
+    // element offset of a row of the item in q and out
+    auto row_offset = [&](int r) {
+        const int pos = position(r), hg = row0 + r - pos * group;
+        return ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D;
+    };
+    auto next_item = [&](int n) {
+        __syncwarp();
+        asm volatile("bar.sync 3, 512;" ::: "memory");  // slot and barriers are ready
+        const volatile int *slot = sh.item(n);
+        if (slot[0] == 0 || *sh.abort_flag()) return false;
+        req = slot[1], g = slot[2], row0 = slot[3], rows_here = slot[4], q0 = slot[5], prefix = slot[7];
+        kv_end = min(slot[6], prefix + position(rows_here - 1) + 1);  // keys any row of the item may see
+        const int all_tiles = (kv_end + kBN - 1) / kBN;
+        tile0 = (int)((long long)all_tiles * part / cluster);  // this CTA's key tiles: tile0 .. tile0 + n_tiles - 1 (possibly none)
+        n_tiles = (int)((long long)all_tiles * (part + 1) / cluster) - tile0;
+        n_blocks = (kv_end + 15) >> 4;
+        // by_rows: slot x holds rows 128 x .. and sees every key tile j.  Else both hold rows 0 .. and slot x sees tiles x, x + 2, ...
+        by_rows = rows_here > kBM;
+        merge = cluster > 1 || !by_rows;
+        return true;
+    };
+    auto leave_item = [&]() {  // every role is through with the item's shared memory, TMEM and barriers
+        fence_before();
+        __syncwarp();
+        asm volatile("bar.sync 4, 512;" ::: "memory");
+        fence_after();
+    };
 
     // The merge: all roles meet when the CTA's tiles are no longer needed, again when the partial results of the cluster are in
     // place, and (clusters) once more when they have been read.  Hardware barriers; every role comes here, given up or not.
@@ -230,6 +262,34 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 2) {
+            // =========================== item scheduler ===========================
+            int item = blockIdx.x / cluster;
+#pragma unroll 1
+            for (int n = 0;; ++n) {
+                if (n > 0 && cluster == 1) {
+                    // Not before the converters have come to the item's last tile, some 6000 cycles from its end: an item drawn at the
+                    // start of the one before would wait for this CTA while another stands idle.  (A plain word, since a phase parity
+                    // cannot tell "not yet" from "two phases ago"; bounded like every wait.)
+                    const uint64_t t0 = global_timer_ns();
+                    while (*sh.progress() < n_tiles - 1 && !*sh.abort_flag()) {
+                        __nanosleep(200);
+                        if (global_timer_ns() - t0 > 2000000000ull) *sh.abort_flag() = 2;
+                    }
+                }
+                post(item, n);  // beside the end of the work on item n - 1
+                item = -1;
+                if (n > 0) {
+                    if (merge) merge_barriers();
+                    leave_item();
+                    if (lane == 0) set_barriers();
+                }
+                if (lane == 0) *sh.progress() = -1;
+                if (!next_item(n)) break;
+            }
+        } else {
+#pragma unroll 1
+        for (int n = 0; next_item(n); ++n) {
         if (warp == 0) {
             // =========================== MMA issuer ===========================
             constexpr uint64_t kHi = (uint64_t)tc::kDescHi << 32;
@@ -239,15 +299,16 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             // slot's next one; steps -2 and -1 only bring the first scores.  One elected lane issues a step in one go: the last
             // quarter of PV, QK^T, the commits.
             bool ok = true;
-            const int steps = by_rows ? 2 * n_tiles : n_tiles, step_max = n_tiles > 0 ? steps : -2;
+            int sh2 = by_rows ? 1 : 0;  // (through an empty asm, here and below: one copy of the loop, not one for each case)
+            asm volatile("" : "+r"(sh2));
+            const int step_max = n_tiles > 0 ? n_tiles << sh2 : -2;
 #pragma unroll 1
             for (int u = -2; u < step_max && ok; ++u) {
                 const int x = u & 1, i = u >> 1;
-                const int j = by_rows ? i : u, jn = by_rows ? i + 1 : u + 2;  // the CTA's key tiles of the two
+                const int j = u >> sh2, jn = (u + 2) >> sh2;  // the CTA's key tiles of the two
                 const int s = j & 1, s1 = jn & 1;
-                const bool closes = !by_rows || x == 1;  // the last slot to read these stages
-                int pv = u >= 0, more = jn < n_tiles;
-                asm volatile("" : "+r"(pv), "+r"(more));  // one copy of the loop, not one for each combination
+                int pv = u >= 0, more = jn < n_tiles, closes = x >= sh2;  // closes: the last slot to read these stages
+                asm volatile("" : "+r"(pv), "+r"(more), "+r"(closes));
                 const uint32_t t_s = tmem + 128 * x, t_o = tmem + 256 + 128 * x;
                 const uint64_t vd = v_d + (uint32_t)s * (G::kTileBytes >> 4);
                 if (pv) {
@@ -263,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     __syncwarp();
                     ok = wait_warp<D>(sh, G::P_READY + x, (uint32_t)(i & 1));
                 } else {
-                    ok = wait_warp<D>(sh, G::Q_READY + (by_rows ? x : 0), 0);
+                    ok = wait_warp<D>(sh, G::Q_READY + (x & sh2), 0);
                 }
                 if (ok && more) ok = wait_warp<D>(sh, G::K_FULL + s1, (uint32_t)((jn >> 1) & 1));
                 if (!ok) break;
@@ -275,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                         if (closes) tc::mma_commit_one(sh.bar(G::V_EMPTY + s));
                     }
                     if (more) {
-                        const uint64_t qd = q_d + (uint32_t)(by_rows ? x : 0) * (G::kTileBytes >> 4), kd = k_d + (uint32_t)s1 * (G::kTileBytes >> 4);
+                        const uint64_t qd = q_d + (uint32_t)(x & sh2) * (G::kTileBytes >> 4), kd = k_d + (uint32_t)s1 * (G::kTileBytes >> 4);
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k) {
                             const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
@@ -292,9 +353,14 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             (void)wait_warp<D>(sh, G::DRAIN, 0);
         }
         if (merge) merge_barriers();
+        leave_item();
+        }
+        }
     } else if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         // =========================== converters ===========================
+#pragma unroll 1
+        for (int n = 0; next_item(n); ++n) {
         constexpr int kIts = D / 16;                       // 16-byte pieces of codes a thread takes of a tile
         constexpr int kBlocksPerIt = 128 * 16 / (16 * D);  // blocks the 128 threads cover at once: 1, or 2 at head_dim 64
         const int ct = threadIdx.x - 384;
@@ -352,6 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             const uint32_t ph = (uint32_t)(((j >> 1) - 1) & 1);
             const int ids_after = load_id(j + 2);
             const float ks_next = load_scale(ids_next, 0), vs_next = load_scale(ids_next, 1);
+            if (threadIdx.x == 384) *sh.progress() = j;
             // ---- K: f16, scales beside it
             cp_async_wait_1();
             ok = j < kStages || wait_warp<D>(sh, G::K_EMPTY + s, ph);
@@ -424,9 +491,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         }
         cp_async_wait_all();  // what was started for a tile that does not come (or after a wait that was given up)
         if (merge) merge_barriers();
+        leave_item();
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // =========================== softmax + write-out ===========================
+#pragma unroll 1
+        for (int n = 0; next_item(n); ++n) {
         const int x = (warp - 4) >> 2;        // slot
         const int rx = by_rows ? x : 0;       // its row tile
         const int n_it = by_rows ? n_tiles : (n_tiles - x + 1) >> 1;  // its key tiles
@@ -489,6 +560,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
 
         const int first_lim = prefix + position(rx * kBM);                          // last key the tile's first row may see
         const int lim = prefix + position(min(rx * kBM + row, rows_here - 1));      // ... and this row
+        int dj = by_rows ? 0 : 1, j0 = by_rows ? 0 : x;
+        asm volatile("" : "+r"(dj), "+r"(j0));
         float m_run = -INFINITY, l_run = 0.f;
         auto publish = [&](int bar) {  // this thread's row of P is in TMEM
             cp::tcgen05_wait_st();
@@ -500,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(i & 1));
             if (!ok) break;
             fence_after();
-            const int j = by_rows ? i : 2 * i + x;  // the CTA's key tile
+            const int j = (i << dj) + j0;  // the CTA's key tile
             const int key0 = (tile0 + j) * kBN;
             const int bad = *sh.bad_mask(j);
             // ---- a tile that the causal boundary cuts, or that holds a block the table does not name, first gets its hidden
@@ -704,6 +777,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             }
             if (cluster > 1) cluster_barrier();  // nobody leaves while another may read its shared memory
         }
+        leave_item();
+        }
     }
 
     // ---- teardown: everybody meets, TMEM goes back
@@ -744,10 +819,11 @@ static ekv_status_t launch_prefill8(ekv_pool *pool, Params &pp, cudaStream_t str
         if (dev < 64) max_cluster[dev] = most;
     }
     if (pp.cluster > most) pp.cluster = most;
-    cudaError_t e = cudaMemsetAsync(pp.p.abort_word, 0, sizeof(int), stream);
+    cudaError_t e = cudaMemsetAsync(pp.p.abort_word, 0, 2 * sizeof(int), stream);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: clear abort word");
     attr.val.clusterDim.x = (unsigned)pp.cluster;
-    cfg.gridDim = dim3((unsigned)((long long)pp.p.q_tiles * pp.p.num_kv_heads * pp.cluster));
+    const long long items = (long long)pp.p.q_tiles * pp.p.num_kv_heads;
+    cfg.gridDim = dim3((unsigned)(pp.cluster > 1 ? items * pp.cluster : items < pool->sm_count ? items : pool->sm_count));
     cfg.stream = stream;
     e = cudaLaunchKernelEx(&cfg, prefill8_kernel<D>, pp);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: launch");
