@@ -46,9 +46,8 @@ __device__ __forceinline__ float scale_of_bf16_bits(uint32_t a) {
 // 2^k that brings a positive finite magnitude a into [2^13, 2^14); 1 for 0 and for what is not finite
 __device__ __forceinline__ float to_f16_range(float a) {
     const int e = (int)(__float_as_uint(a) >> 23) & 0xff;
-    if (e == 0xff || a == 0.f) return 1.f;
-    const int k = 13 - (e - 127);
-    return __uint_as_float((uint32_t)(min(k, 126) + 127) << 23);
+    const int k = (e == 0xff || a == 0.f) ? 0 : min(13 - (e - 127), 126);
+    return __uint_as_float((uint32_t)(k + 127) << 23);
 }
 
 // two f16 that codes became -> two bf16 (exact: codes have four significant bits)

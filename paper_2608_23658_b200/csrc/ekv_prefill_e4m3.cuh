@@ -53,9 +53,9 @@ static constexpr int kThreads = 512;
 static constexpr int kHalfBytes = 128 * 128;  // [128 rows][64 16-bit channels], 128-byte swizzle
 static constexpr int kStages = 2;
 // setmaxnreg: warps 0-3 kRegsUtil, 4-11 kRegsSoftmax, 12-15 kRegsConv; the shares add up to what the CTA is launched with
-static constexpr int kLaunchRegs = 128, kRegsUtil = 40, kRegsSoftmax = 200, kRegsConv = 64;
+static constexpr int kLaunchRegs = 128, kRegsUtil = 40, kRegsSoftmax = 200, kRegsConv = 72;
 static_assert(128 * (kRegsUtil + kRegsConv) + 256 * kRegsSoftmax <= kLaunchRegs * kThreads, "setmaxnreg split exceeds the CTA's registers");
-static_assert(kRegsUtil == 40 && kRegsSoftmax == 200 && kRegsConv == 64, "the setmaxnreg instructions in the kernel carry these numbers as literals");
+static_assert(kRegsUtil == 40 && kRegsSoftmax == 200 && kRegsConv == 72, "the setmaxnreg instructions in the kernel carry these numbers as literals");
 
 struct Params {
     PrefillParams p;  // q_tiles, tile_prefix: in items of kItemRows rows per kv-head; scale_log2 >= 0
@@ -154,15 +154,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cluster = pp.cluster, part = blockIdx.x % cluster;  // CTAs that share an item's keys; which of them this is
 
-    // One thread sets up the barriers, for every item anew, so that all phases of an item count from 0.
-    auto set_barriers = [&]() {
-#pragma unroll 1
-        for (int i = 0; i < G::NBAR; ++i) {
-            mbar_inval(sh.bar(i));
-            mbar_init(sh.bar(i), G::arrivals(i));
-        }
-        mbar_fence_init();
-    };
     if (threadIdx.x == 64) {
 #pragma unroll 1
         for (int i = 0; i < G::NBAR; ++i) mbar_init(sh.bar(i), G::arrivals(i));
@@ -223,9 +214,26 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         const int pos = position(r), hg = row0 + r - pos * group;
         return ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D;
     };
+    // Barriers live as long as the CTA; an item's waits count phases from 0, on top of what earlier items left in bit `bar` of this.
+    uint32_t phases = 0;
+    auto wait = [&](int bar, uint32_t parity) { return wait_warp<D>(sh, bar, (parity ^ (phases >> bar)) & 1u); };
+    // All roles are through with the item before (its shared memory and TMEM), and the slot of this one is posted.
     auto next_item = [&](int n) {
+        if (n > 0) {  // completions of the item before, by barrier
+            const uint32_t t[2] = {(uint32_t)(n_tiles + 1) >> 1, (uint32_t)n_tiles >> 1};
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t of_slot = by_rows ? (uint32_t)n_tiles : t[x];
+                phases ^= (x == 0 || by_rows ? 1u : 0u) << (G::Q_READY + x);
+                phases ^= (t[x] & 1u) * (1u << (G::K_FULL + x) | 1u << (G::K_EMPTY + x) | 1u << (G::V_FULL + x) | 1u << (G::V_EMPTY + x));
+                phases ^= (of_slot & 1u) * (1u << (G::P_PART + x) | 1u << (G::P_READY + x)) ^ ((of_slot + 1u) & 1u) << (G::S_READY + x);
+            }
+            phases ^= 1u << G::DRAIN;
+        }
+        fence_before();
         __syncwarp();
-        asm volatile("bar.sync 3, 512;" ::: "memory");  // slot and barriers are ready
+        asm volatile("bar.sync 3, 512;" ::: "memory");
+        fence_after();
         const volatile int *slot = sh.item(n);
         if (slot[0] == 0 || *sh.abort_flag()) return false;
         req = slot[1], g = slot[2], row0 = slot[3], rows_here = slot[4], q0 = slot[5], prefix = slot[7];
@@ -238,12 +246,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         by_rows = rows_here > kBM;
         merge = cluster > 1 || !by_rows;
         return true;
-    };
-    auto leave_item = [&]() {  // every role is through with the item's shared memory, TMEM and barriers
-        fence_before();
-        __syncwarp();
-        asm volatile("bar.sync 4, 512;" ::: "memory");
-        fence_after();
     };
 
     // The merge: all roles meet when the CTA's tiles are no longer needed, again when the partial results of the cluster are in
@@ -279,11 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 }
                 post(item, n);  // beside the end of the work on item n - 1
                 item = -1;
-                if (n > 0) {
-                    if (merge) merge_barriers();
-                    leave_item();
-                    if (lane == 0) set_barriers();
-                }
+                if (n > 0 && merge) merge_barriers();
                 if (lane == 0) *sh.progress() = -1;
                 if (!next_item(n)) break;
             }
@@ -312,8 +310,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 const uint32_t t_s = tmem + 128 * x, t_o = tmem + 256 + 128 * x;
                 const uint64_t vd = v_d + (uint32_t)s * (G::kTileBytes >> 4);
                 if (pv) {
-                    ok = wait_warp<D>(sh, G::V_FULL + s, (uint32_t)((j >> 1) & 1));
-                    if (ok) ok = wait_warp<D>(sh, G::P_PART + x, (uint32_t)(i & 1));
+                    ok = wait(G::V_FULL + s, (uint32_t)((j >> 1) & 1));
+                    if (ok) ok = wait(G::P_PART + x, (uint32_t)(i & 1));
                     if (!ok) break;
                     fence_after();
                     if (tc::elect_one()) {  // keys 0..95 while the softmax warps finish the rest
@@ -322,11 +320,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                             tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, (i > 0 || k > 0) ? 1u : 0u);
                     }
                     __syncwarp();
-                    ok = wait_warp<D>(sh, G::P_READY + x, (uint32_t)(i & 1));
+                    ok = wait(G::P_READY + x, (uint32_t)(i & 1));
                 } else {
-                    ok = wait_warp<D>(sh, G::Q_READY + (x & sh2), 0);
+                    ok = wait(G::Q_READY + (x & sh2), 0);
                 }
-                if (ok && more) ok = wait_warp<D>(sh, G::K_FULL + s1, (uint32_t)((jn >> 1) & 1));
+                if (ok && more) ok = wait(G::K_FULL + s1, (uint32_t)((jn >> 1) & 1));
                 if (!ok) break;
                 fence_after();
                 if (tc::elect_one()) {
@@ -350,14 +348,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             }
             // every MMA this thread issued must be finished before TMEM is released
             tc::mma_commit(sh.bar(G::DRAIN));
-            (void)wait_warp<D>(sh, G::DRAIN, 0);
+            (void)wait(G::DRAIN, 0);
         }
         if (merge) merge_barriers();
-        leave_item();
         }
         }
     } else if (warp >= 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // =========================== converters ===========================
 #pragma unroll 1
         for (int n = 0; next_item(n); ++n) {
@@ -390,13 +387,38 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             const int id = __shfl_sync(0xffffffffu, ids, it * kBlocksPerIt + first_block);
             cp_async_16(raw + kv * G::kRawBytes + it * 2048, src + (long long)max(id, 0) * pp.block_stride + (kv ? v_off : 0), id >= 0 ? 16u : 0u);
         };
-        // 16 values of one row -> two 16-byte chunks of the tile
-        auto store = [&](uint32_t tile_off, int row, const uint32_t (&w)[8]) {
-            uint8_t *at = sh.ptr + tile_off + (piece >> 2) * kHalfBytes + row * 128;
-            const int c = (2 * (piece & 3)) ^ (row & 7);
-            *reinterpret_cast<uint4 *>(at + (c << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-            *reinterpret_cast<uint4 *>(at + ((c ^ 1) << 4)) = make_uint4(w[4], w[5], w[6], w[7]);
+        // 16 values of one row -> two 16-byte chunks of the tile.  The place inside a block's 16 rows is the same for every block.
+        uint8_t *const store_at = sh.ptr + (piece >> 2) * kHalfBytes + (first_block * 16 + rowb) * 128;
+        const int c0 = ((2 * (piece & 3)) ^ (rowb & 7)) << 4, c1 = c0 ^ 16;
+        auto store = [&](uint32_t tile_off, int it, const uint32_t (&w)[8]) {
+            uint8_t *to = store_at + tile_off + it * (kBlocksPerIt * 2048);
+            *reinterpret_cast<uint4 *>(to + c0) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4 *>(to + c1) = make_uint4(w[4], w[5], w[6], w[7]);
         };
+        auto put_k = [&](int s, int it, const uint4 &v) {  // f16
+            const uint32_t c[4] = {v.x, v.y, v.z, v.w};
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[2 * i] = e4m3_lo(c[i]);
+                w[2 * i + 1] = e4m3_hi(c[i]);
+            }
+            store(G::kOffK + s * G::kTileBytes, it, w);
+        };
+        auto put_v = [&](int s, int it, const uint4 &v, float scale) {  // bf16 with the scale in it
+            const uint32_t c[4] = {v.x, v.y, v.z, v.w};
+            const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 a = f16x2_to_float2(e4m3_lo(c[i])), b = f16x2_to_float2(e4m3_hi(c[i]));
+                const __nv_bfloat162 x = __hmul2(__floats2bfloat162_rn(a.x, a.y), s2), y = __hmul2(__floats2bfloat162_rn(b.x, b.y), s2);
+                w[2 * i] = *reinterpret_cast<const uint32_t *>(&x);
+                w[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&y);
+            }
+            store(G::kOffV + s * G::kTileBytes, it, w);
+        };
+        const uint4 zeros = make_uint4(0u, 0u, 0u, 0u);
         auto publish = [&](int bar) {
             fence_proxy_async_smem();
             __syncwarp();
@@ -405,11 +427,11 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         int ids = load_id(0);
         float ks = load_scale(ids, 0), vs = load_scale(ids, 1);
 #pragma unroll 1
-        for (int it = 0; it < kIts; ++it) copy(it, ids, 0);
-        cp_async_commit();
-#pragma unroll 1
-        for (int it = 0; it < kIts; ++it) copy(it, ids, 1);
-        cp_async_commit();
+        for (int kv = 0; kv < 2; ++kv) {
+#pragma unroll 2
+            for (int it = 0; it < kIts; ++it) copy(it, ids, kv);
+            cp_async_commit();
+        }
         int ids_next = load_id(1);
         bool ok = true;
 #pragma unroll 1
@@ -418,12 +440,17 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             const uint32_t ph = (uint32_t)(((j >> 1) - 1) & 1);
             const int ids_after = load_id(j + 2);
             const float ks_next = load_scale(ids_next, 0), vs_next = load_scale(ids_next, 1);
-            if (threadIdx.x == 384) *sh.progress() = j;
-            // ---- K: f16, scales beside it
+            int reports = warp == 12;  // for all four warps
+            asm volatile("" : "+r"(reports));  // (one copy of the loop)
+            if (reports && lane == 0) *sh.progress() = j;
+            // Rows that are to be 0 whatever their codes: of blocks that were never written (no scale) or do not exist, and V's past
+            // the last visible key.  A tile without any takes no notice.
+            const bool some_zero = __any_sync(0xffffffffu, !(ks > 0.f) || !(vs > 0.f)) || (tile0 + j + 1) * kBN > kv_end;
+            // ---- K, with its scales beside it
             cp_async_wait_1();
-            ok = j < kStages || wait_warp<D>(sh, G::K_EMPTY + s, ph);
+            ok = j < kStages || wait(G::K_EMPTY + s, ph);
             if (!ok) break;
-            if (warp == 12) {
+            if (reports) {
                 const unsigned bad = __ballot_sync(0xffffffffu, ids < 0) & 0xffu;  // invalid, or past the last visible key
                 const unsigned oob = __ballot_sync(0xffffffffu, ids == -2) & 0xffu;
                 if (lane < 8) sh.k_scale(j)[lane] = ks > 0.f ? ks : 1.f;
@@ -432,54 +459,53 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     if (oob) atomicOr(p.status, EKV_DEV_FLAG_OOB);
                 }
             }
+            if (some_zero) {
 #pragma unroll 1
-            for (int it = 0; it < kIts; it += 4) {  // four pieces side by side: one alone is a chain of some 180 cycles
-                uint4 v[4];
+                for (int it = 0; it < kIts; ++it) {
+                    const uint4 v = lds_16(raw + it * 2048);
+                    copy(it, ids_next, 0);
+                    put_k(s, it, __shfl_sync(0xffffffffu, ks, it * kBlocksPerIt + first_block) > 0.f ? v : zeros);
+                }
+            } else {
+#pragma unroll 1
+                for (int it = 0; it < kIts; it += 4) {  // four pieces side by side: one alone is a chain of some 180 cycles
+                    uint4 v[4];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = lds_16(raw + (it + u) * 2048);
+                    for (int u = 0; u < 4; ++u) v[u] = lds_16(raw + (it + u) * 2048);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) copy(it + u, ids_next, 0);  // the places are free: the next tile's codes
+                    for (int u = 0; u < 4; ++u) copy(it + u, ids_next, 0);  // the places are free: the next tile's codes
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int blk = (it + u) * kBlocksPerIt + first_block;
-                    uint32_t c[4] = {v[u].x, v[u].y, v[u].z, v[u].w}, w[8];
-                    if (!(__shfl_sync(0xffffffffu, ks, blk) > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;  // no scale: nothing was written, the values are 0
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        w[2 * i] = e4m3_lo(c[i]);
-                        w[2 * i + 1] = e4m3_hi(c[i]);
-                    }
-                    store(G::kOffK + s * G::kTileBytes, blk * 16 + rowb, w);
+                    for (int u = 0; u < 4; ++u) put_k(s, it + u, v[u]);
                 }
             }
             cp_async_commit();
             publish(G::K_FULL + s);
-            // ---- V: bf16 with the scale in it; zero rows past the last visible key
+            // ---- V
             cp_async_wait_1();
-            ok = j < kStages || wait_warp<D>(sh, G::V_EMPTY + s, ph);
+            ok = j < kStages || wait(G::V_EMPTY + s, ph);
             if (!ok) break;
+            if (some_zero) {
 #pragma unroll 1
-            for (int it = 0; it < kIts; it += 4) {
-                uint4 v[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = lds_16(raw + G::kRawBytes + (it + u) * 2048);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) copy(it + u, ids_next, 1);
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int blk = (it + u) * kBlocksPerIt + first_block, row = blk * 16 + rowb;
-                    uint32_t c[4] = {v[u].x, v[u].y, v[u].z, v[u].w}, w[8];
+                for (int it = 0; it < kIts; ++it) {
+                    const uint4 v = lds_16(raw + G::kRawBytes + it * 2048);
+                    copy(it, ids_next, 1);
+                    const int blk = it * kBlocksPerIt + first_block;
                     const float scale = __shfl_sync(0xffffffffu, vs, blk);
-                    if ((tile0 + j) * kBN + row >= kv_end || !(scale > 0.f)) c[0] = c[1] = c[2] = c[3] = 0u;
-                    const __nv_bfloat162 s2 = __float2bfloat162_rn(scale);
+                    put_v(s, it, scale > 0.f && (tile0 + j) * kBN + blk * 16 + rowb < kv_end ? v : zeros, scale);
+                }
+            } else {
+#pragma unroll 1
+                for (int it = 0; it < kIts; it += 4) {
+                    uint4 v[4];
+                    float scale[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 a = f16x2_to_float2(e4m3_lo(c[i])), b = f16x2_to_float2(e4m3_hi(c[i]));
-                        const __nv_bfloat162 x = __hmul2(__floats2bfloat162_rn(a.x, a.y), s2), y = __hmul2(__floats2bfloat162_rn(b.x, b.y), s2);
-                        w[2 * i] = *reinterpret_cast<const uint32_t *>(&x);
-                        w[2 * i + 1] = *reinterpret_cast<const uint32_t *>(&y);
-                    }
-                    store(G::kOffV + s * G::kTileBytes, row, w);
+                    for (int u = 0; u < 4; ++u) v[u] = lds_16(raw + G::kRawBytes + (it + u) * 2048);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) copy(it + u, ids_next, 1);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) scale[u] = __shfl_sync(0xffffffffu, vs, (it + u) * kBlocksPerIt + first_block);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) put_v(s, it + u, v[u], scale[u]);
                 }
             }
             cp_async_commit();
@@ -491,7 +517,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         }
         cp_async_wait_all();  // what was started for a tile that does not come (or after a wait that was given up)
         if (merge) merge_barriers();
-        leave_item();
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
@@ -509,45 +534,54 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         const int piece = lane % kPieces, sub = lane / kPieces;
         if (by_rows || x == 0) {
             // ---- Q rows of this warp: all of them on their way at once, straight to where they belong in the 128-byte swizzled
-            // tile, then bf16 -> f16 in place with a row's largest magnitude in [2^13, 2^14); rows past the end are 0
-            auto q_place = [&](int rr) { return (uint32_t)(G::kOffQ + x * G::kTileBytes + (piece >> 3) * kHalfBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4)); };
-#pragma unroll 2
-            for (int it = 0; it < 32 / kRowsPerInst; ++it) {
-                const int rr = wrow0 + kRowsPerInst * it + sub, in_item = x * kBM + rr;
-                const bool there = in_item < rows_here;
-                cp_async_16(sh.base + q_place(rr), p.q + row_offset(there ? in_item : 0) + piece * 8, there ? 16u : 0u);
+            // tile, then bf16 -> f16 in place with a row's largest magnitude in [2^13, 2^14); rows past the end are 0.  A warp-wide
+            // access covers kRowsPerInst rows; four of them come back to the same place of the swizzle.
+            constexpr int kBatch = 4, kBatchRows = kBatch * kRowsPerInst;
+            static_assert(kBatchRows % 8 == 0, "swizzle period");
+            uint32_t place[kBatch];  // of this lane's piece in the rows of a batch
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const int r = kRowsPerInst * u + sub;
+                place[u] = G::kOffQ + x * G::kTileBytes + (piece >> 3) * kHalfBytes + (wrow0 + r) * 128 + (((piece & 7) ^ (r & 7)) << 4);
+            }
+            const __nv_bfloat16 *q_src = p.q + piece * 8;
+            const int first_row = x * kBM + wrow0 + sub;
+#pragma unroll 1
+            for (int b = 0; b < 32 / kBatchRows; ++b) {
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    const int in_item = first_row + b * kBatchRows + kRowsPerInst * u;
+                    const bool there = in_item < rows_here;
+                    cp_async_16(sh.base + place[u] + b * (kBatchRows * 128), q_src + row_offset(there ? in_item : 0), there ? 16u : 0u);
+                }
             }
             cp_async_commit();
             cp_async_wait_all();
 #pragma unroll 1
-            for (int it = 0; it < 32 / kRowsPerInst; it += 4) {  // four pieces side by side: one is a chain of some 300 cycles
-                uint4 v[4];
-                uint32_t top[4];
+            for (int b = 0; b < 32 / kBatchRows; ++b) {  // four pieces side by side: one is a chain of some 300 cycles
+                uint4 v[kBatch];
+                uint32_t top[kBatch];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) v[u] = lds_16(sh.base + q_place(wrow0 + kRowsPerInst * (it + u) + sub));
+                for (int u = 0; u < kBatch; ++u) v[u] = lds_16(sh.base + place[u] + b * (kBatchRows * 128));
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
+                for (int u = 0; u < kBatch; ++u) {
                     const uint32_t t2 = __vmaxu2(__vmaxu2(v[u].x & 0x7fff7fffu, v[u].y & 0x7fff7fffu), __vmaxu2(v[u].z & 0x7fff7fffu, v[u].w & 0x7fff7fffu));
                     top[u] = max(t2 & 0xffffu, t2 >> 16);
                 }
 #pragma unroll
                 for (int o = kPieces / 2; o > 0; o >>= 1)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) top[u] = max(top[u], __shfl_xor_sync(0xffffffffu, top[u], o));
+                    for (int u = 0; u < kBatch; ++u) top[u] = max(top[u], __shfl_xor_sync(0xffffffffu, top[u], o));
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int rr = wrow0 + kRowsPerInst * (it + u) + sub;
+                for (int u = 0; u < kBatch; ++u) {
                     const float up = to_f16_range(__uint_as_float(top[u] << 16));
                     const float f = up * pp.q_sign;
                     const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
                     uint32_t h[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const __half2 y = __floats2half2_rn(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
-                        h[i] = *reinterpret_cast<const uint32_t *>(&y);
-                    }
-                    *reinterpret_cast<uint4 *>(sh.ptr + q_place(rr)) = make_uint4(h[0], h[1], h[2], h[3]);
-                    if (piece == 0) sh.q_inv()[x * kBM + rr] = pow2_inverse(up);
+                    for (int i = 0; i < 4; ++i) h[i] = pack_f16x2(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
+                    *reinterpret_cast<uint4 *>(sh.ptr + place[u] + b * (kBatchRows * 128)) = make_uint4(h[0], h[1], h[2], h[3]);
+                    if (piece == 0) sh.q_inv()[first_row + b * kBatchRows + kRowsPerInst * u] = pow2_inverse(up);
                 }
             }
             fence_proxy_async_smem();
@@ -555,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             if (lane == 0) mbar_arrive(sh.bar(G::Q_READY + x));
         }
         bool ok = true;
-        if (!by_rows && x == 1 && n_it > 0) ok = wait_warp<D>(sh, G::S_READY + 1, 0);  // the other slot's warps have been through Q
+        if (!by_rows && x == 1 && n_it > 0) ok = wait(G::S_READY + 1, 0);  // the other slot's warps have been through Q
         const float row_scale = p.scale_log2 * (n_it > 0 ? sh.q_inv()[rx * kBM + row] : 1.f);
 
         const int first_lim = prefix + position(rx * kBM);                          // last key the tile's first row may see
@@ -570,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         };
 #pragma unroll 1
         for (int i = 0; i < n_it && ok; ++i) {
-            ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(i & 1));
+            ok = wait(G::S_READY + x, (uint32_t)(i & 1));
             if (!ok) break;
             fence_after();
             const int j = (i << dj) + j0;  // the CTA's key tile
@@ -667,7 +701,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             publish(G::P_READY + x);
         }
 
-        if (ok && n_it > 0) ok = wait_warp<D>(sh, G::S_READY + x, (uint32_t)(n_it & 1));
+        if (ok && n_it > 0) ok = wait(G::S_READY + x, (uint32_t)(n_it & 1));
         fence_after();  // every MMA that read the slot's Q tile or wrote its O has completed (the commit covers all earlier ones)
         if (!merge) {
             // ---- write-out: O / l -> bf16 -> the (now idle) Q tile in shared memory -> global, whole rows per instruction.
@@ -777,7 +811,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             }
             if (cluster > 1) cluster_barrier();  // nobody leaves while another may read its shared memory
         }
-        leave_item();
         }
     }
 
