@@ -107,7 +107,7 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
         pp.scales = pool->layer_scales(layer);
         pp.block_stride = (long long)pool->block_stride;
         pp.few_rows = few8::kMaxRows;
-        pp.cluster = tc8::plan_cluster(q_tiles * pool->desc.num_kv_heads, max_blocks_per_seq, pool->sm_count);
+        pp.cluster = 1;  // the launchers choose
         pp.group_magic = group > 1 ? (unsigned)(((1ull << 32) + group - 1) / group) : 0u;
         if (q_tiles > 0) {
             st = d128 ? tc8::launch_prefill8<128>(pool, pp, (cudaStream_t)stream) : tc8::launch_prefill8<64>(pool, pp, (cudaStream_t)stream);

@@ -48,7 +48,7 @@ using tc::fence_before;
 
 static constexpr int kBM = 128, kBN = 128;
 static constexpr int kItemRows = 2 * kBM;
-static constexpr int kMaxCluster = 16;
+static constexpr int kMaxClusterLog = 4, kMaxCluster = 1 << kMaxClusterLog;
 static constexpr int kThreads = 512;
 static constexpr int kHalfBytes = 128 * 128;  // [128 rows][64 16-bit channels], 128-byte swizzle
 static constexpr int kStages = 2;
@@ -825,9 +825,41 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     if (warp == 1) cp::tcgen05_dealloc(cp::cta_group_1, tmem, 512);
 }
 
+// fit[i] = clusters of 2^i CTAs of the kernel that run at the same time on the current device (0: none do)
+static void clusters_that_fit(const void *kernel, cudaLaunchConfig_t cfg, int *fit) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    for (int i = kMaxClusterLog; i >= 0; --i) {
+        attr.val.clusterDim.x = 1u << i;
+        cfg.gridDim = dim3(1u << i);
+        if (cudaOccupancyMaxActiveClusters(&fit[i], kernel, &cfg) != cudaSuccess) {
+            fit[i] = 0;
+            (void)cudaGetLastError();
+        }
+    }
+    if (fit[0] < 1) fit[0] = 1;  // asked
+}
+
+// log2 of the CTAs that an item's keys are cut over: as many as let all items run at the same time, while a part keeps two key
+// tiles of the longest sequence that the table can hold.  fit[i]: clusters of 2^i CTAs that run at the same time.  Never more than
+// one round of the machine: a part costs 10 to 15 us beyond its tiles (a cold start and the merge).  Measured, 32q/8kv, us with 1 / 2
+// / 4 / 8 / 16 CTAs an item: 64 positions over 30000 keys (8 items) 460 243 134 81 104; 128 over 8000 (16) 136 80 50 70 89; 512 over
+// 8000 (64) 143 85 100 176 296; 1024 over 8000 (128) 151 163 198 319 566.  (Clusters stay inside a GPC: of a B200's 148 SMs, 7
+// clusters of 16, 15 of 8, 33 of 4 run at a time.)
+// Depends on the call's shape arguments alone.
+static int plan_cluster(long long items, int max_blocks, const int *fit) {
+    const long long max_tiles = ((long long)max_blocks * 16 + kBN - 1) / kBN;
+    int c = 0;
+    while (c < kMaxClusterLog && items <= fit[c + 1] && (4ll << c) <= max_tiles) ++c;
+    return c;
+}
+
 template <int D>
 static ekv_status_t launch_prefill8(ekv_pool *pool, Params &pp, cudaStream_t stream) {
-    static int max_cluster[64] = {0};  // 0: not asked yet
+    static int fits[64][kMaxClusterLog + 1] = {};  // per device: clusters of 2^i CTAs that run at the same time; [..][0] 0: not asked yet
     const int dev = pool->desc.device;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr;
@@ -837,42 +869,23 @@ static ekv_status_t launch_prefill8(ekv_pool *pool, Params &pp, cudaStream_t str
     cfg.dynamicSmemBytes = Geo<D>::kSmemBytes;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    int most = dev < 64 ? max_cluster[dev] : 0;
-    if (most == 0) {
+    int asked[kMaxClusterLog + 1] = {}, *fit = dev < 64 ? fits[dev] : asked;
+    if (fit[0] == 0) {
         cudaError_t e = cudaFuncSetAttribute(prefill8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<D>::kSmemBytes);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(prefill8_kernel<D>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: kernel attributes");
-        for (most = kMaxCluster; most > 8; most /= 2) {  // more than 8 is for the device to allow
-            int fit = 0;
-            attr.val.clusterDim.x = (unsigned)most;
-            cfg.gridDim = dim3((unsigned)most);
-            if (cudaOccupancyMaxActiveClusters(&fit, prefill8_kernel<D>, &cfg) == cudaSuccess && fit > 0) break;
-            (void)cudaGetLastError();
-        }
-        if (dev < 64) max_cluster[dev] = most;
+        clusters_that_fit((const void *)prefill8_kernel<D>, cfg, fit);
     }
-    if (pp.cluster > most) pp.cluster = most;
+    const long long items = (long long)pp.p.q_tiles * pp.p.num_kv_heads;
+    pp.cluster = 1 << plan_cluster(items, pp.p.max_blocks, fit);
     cudaError_t e = cudaMemsetAsync(pp.p.abort_word, 0, 2 * sizeof(int), stream);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: clear abort word");
     attr.val.clusterDim.x = (unsigned)pp.cluster;
-    const long long items = (long long)pp.p.q_tiles * pp.p.num_kv_heads;
     cfg.gridDim = dim3((unsigned)(pp.cluster > 1 ? items * pp.cluster : items < pool->sm_count ? items : pool->sm_count));
     cfg.stream = stream;
     e = cudaLaunchKernelEx(&cfg, prefill8_kernel<D>, pp);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: launch");
     return EKV_OK;
-}
-
-// CTAs an item's keys are cut over: as many as fit beside each other, while a part keeps two key tiles of the longest sequence that
-// the table can hold.  Never more than one round of the machine: a part costs 10 to 15 us beyond its tiles (a cold start and the
-// merge), and clusters leave some SMs without a place.  Measured, 32q/8kv: 4 rows over 30000 keys (8 items) 429 us with one CTA an
-// item, 222 / 120 / 77 with 2 / 4 / 8; 512 rows over 8000 (64 items) 144, 86 with 2, 100 with 4; 2048 over 14001 (256 items) 478,
-// 516 with 2, 585 with 4.  Depends on the call's shape arguments alone.
-static int plan_cluster(long long items, int max_blocks, int sm_count) {
-    const long long max_tiles = ((long long)max_blocks * 16 + kBN - 1) / kBN;
-    int c = 1;
-    while (c < kMaxCluster && items * c * 2 <= sm_count && 2 * c * 2 <= max_tiles) c *= 2;
-    return c;
 }
 
 }  // namespace tc8

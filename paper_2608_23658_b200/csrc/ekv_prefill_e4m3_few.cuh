@@ -24,7 +24,7 @@ namespace few8 {
 static constexpr int kWarps = 8;
 static constexpr int kThreads = 32 * kWarps;
 static constexpr int kMaxRows = 32;
-static constexpr int kMaxCluster = 16;
+static constexpr int kMaxClusterLog = tc8::kMaxClusterLog;
 
 template <int D>
 struct Geo {
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 2) few8_kernel(const __grid_constant
 template <int D>
 static ekv_status_t launch(ekv_pool *pool, int layer, tc8::Params &pp, int items, cudaStream_t stream) {
     using G = Geo<D>;
-    static int max_cluster[64] = {0};  // 0: not asked yet
+    static int fits[64][kMaxClusterLog + 1] = {};  // per device: clusters of 2^i CTAs that run at the same time; [..][0] 0: not asked yet
     const int dev = pool->desc.device;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr;
@@ -369,24 +369,23 @@ static ekv_status_t launch(ekv_pool *pool, int layer, tc8::Params &pp, int items
     cfg.dynamicSmemBytes = G::kSmemBytes;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    int most = dev < 64 ? max_cluster[dev] : 0;
-    if (most == 0) {
+    int asked[kMaxClusterLog + 1] = {}, *fit = dev < 64 ? fits[dev] : asked;
+    if (fit[0] == 0) {
         cudaError_t e = cudaFuncSetAttribute(few8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmemBytes);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(few8_kernel<D>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: kernel attributes");
-        for (most = kMaxCluster; most > 8; most /= 2) {  // more than 8 is for the device to allow
-            int fit = 0;
-            attr.val.clusterDim.x = (unsigned)most;
-            cfg.gridDim = dim3((unsigned)most);
-            if (cudaOccupancyMaxActiveClusters(&fit, few8_kernel<D>, &cfg) == cudaSuccess && fit > 0) break;
-            (void)cudaGetLastError();
-        }
-        if (dev < 64) max_cluster[dev] = most;
+        tc8::clusters_that_fit((const void *)few8_kernel<D>, cfg, fit);
     }
-    // Parts: about one round of two CTAs an SM, while a ring keeps two blocks of the longest sequence that the table can hold.  Depends
-    // on the call's shape arguments alone.
-    pp.cluster = 1;
-    while (pp.cluster < most && (long long)items * pp.cluster < 2ll * pool->sm_count && pp.p.max_blocks / (2 * pp.cluster) >= 2 * kWarps) pp.cluster *= 2;
+    // Parts: as many as let the items run at the same time, or nearly so (slack[i] quarters of that for 2^i CTAs), while a part has
+    // eight blocks, one a ring, of the longest sequence that the table can hold -- 64 if the items take turns, as a cluster takes
+    // longer to start than a CTA.  Measured, requests of 16 rows, us with 1 / 2 / 4 / 8 / 16 CTAs an item: one over 30000 keys (8
+    // items) 292 152 83 47 38; over 1000..8000 keys 2 requests 50 31 21 20 29; 4: 65 39 25 22 42; 10: 83 48 37 48 83; 16: 83 50 59
+    // 72 129; 20: 85 58 64 85 157; 64: 168 159 180 265 498; over 400 keys 1: 13 13 11 11 15, 8: 13 13 15 24 57, 32: 17 28 44 84 193.
+    // (14 clusters of 16 run at a time, 33 of 8, 71 of 4, 148 of 2.)  Depends on the call's shape arguments alone.
+    static constexpr int slack[kMaxClusterLog + 1] = {0, 8, 5, 5, 4};
+    int c = 0;
+    while (c < kMaxClusterLog && 4ll * items <= (long long)slack[c + 1] * fit[c + 1] && pp.p.max_blocks >= (items <= fit[c + 1] ? 8ll : 64ll) << (c + 1)) ++c;
+    pp.cluster = 1 << c;
     attr.val.clusterDim.x = (unsigned)pp.cluster;
     cfg.gridDim = dim3((unsigned)((long long)items * pp.cluster));
     cfg.stream = stream;
