@@ -40,7 +40,7 @@
  * block_bytes is half of the bf16 pool's -- holding an e4m3 code c, and beside the range an fp32 array
  * scales[n][kv][h] per layer (ekv_layer_scales; plain device memory for base and elastic ids, 8*num_kv_heads bytes a
  * block).  The element's value is c * scales[n][kv][h].  A scale is a power of two 2^e with -112 <= e <= 120, or 0
- * while nothing was written: e4m3 is a floating-point format, so a finer scale would buy no precision, and with powers
+ * while nothing was written (the values are 0 then, whatever the codes): e4m3 is a floating-point format, so a finer scale would buy no precision, and with powers
  * of two applying a scale is exact and raising one loses only bits below the code's smallest step.
  * ekv_write_kv quantises (see there); decode and prefill read codes and scales, accumulate in fp32 and give what they
  * would give on a bf16 pool that held the same values.  Grow, shrink, EKV_FUSED_RANGE, ekv_move_blocks and
@@ -382,8 +382,9 @@ EKV_API ekv_status_t ekv_hoststep_flush(ekv_hoststep_t *step, void *stream);
  * cu_q_lens_host: HOST copy of the same R+1 values (used to size the launch without a sync).
  * Requests with seq_lens[r] < c_r are invalid (rows produce zeros, EKV_ERR_BLOCK_OOB is latched).
  * Needs no workspace.  Calls on one pool may run at the same time on different streams; each call in flight
- * holds one of 64 per-pool launch words (work counter of the persistent kernel), so more than 64 calls of one
- * pool in flight at once are not supported.
+ * over an EKV_BF16 pool holds one of 64 per-pool launch words (work counter of the persistent kernel), so more than
+ * 64 calls of one such pool in flight at once are not supported (a captured call holds the same word in every replay).
+ * Over an EKV_E4M3 pool calls share nothing, in any number, captured or not.
  */
 EKV_API ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, const void *q, void *out,
                                     const int32_t *block_tables, int32_t max_blocks_per_seq,

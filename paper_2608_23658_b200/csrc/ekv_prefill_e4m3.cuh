@@ -78,7 +78,7 @@ struct Geo {
     static constexpr int kRawBytes = 128 * D;  // a tile of codes
     static constexpr int kOffRaw = kOffV + kStages * kTileBytes;  // one of K, one of V
     static constexpr int kOffBar = kOffRaw + 2 * kRawBytes;
-    enum Bar { Q_READY = 0, K_FULL = 2, K_EMPTY = 4, V_FULL = 6, V_EMPTY = 8, S_READY = 10, P_PART = 12, P_READY = 14, DRAIN = 16, NBAR = 17 };
+    enum Bar { Q_READY = 0, K_FULL = 2, K_EMPTY = 4, V_FULL = 6, V_EMPTY = 8, S_READY = 10, P_PART = 12, P_READY = 14, DRAIN = 16, NEXT = 17, NBAR = 18 };
     __device__ static __forceinline__ uint32_t arrivals(int bar) {  // warps for Q, K and V tiles, threads for P, a commit for the others
         return bar >= P_PART && bar < DRAIN ? 128u : (bar < K_EMPTY || (bar >= V_FULL && bar < V_EMPTY)) ? 4u : 1u;
     }
@@ -89,9 +89,9 @@ struct Geo {
     static constexpr int kOffPartML = 2 * kBM * D * 4;         // ... and (m, l) of [2][128]
     static constexpr int kOffPartW = kOffPartML + 2 * kBM * 8;  // the CTA's own weights of its rows' partials: at most 512
     static_assert(kOffPartW + 512 * 4 <= kOffRaw, "merge area");
-    static constexpr int kOffItem = kOffQInv + 1024;           // two slots of the scheduler: state and seven numbers
+    static constexpr int kOffItem = kOffQInv + 1024;           // two slots of the scheduler: state and seven numbers; then progress, response
     static constexpr int kSmemBytes = kOffItem + 128 + 1024;    // + alignment slack
-    static_assert(kOffFlags + 24 <= kOffKScale && kSmemBytes <= 232448, "shared memory");
+    static_assert(kOffFlags + 24 <= kOffKScale && kOffItem % 16 == 0 && kSmemBytes <= 232448, "shared memory");
     // kind::f16 instruction descriptors, D = f32, M = 128: QK with f16 operands, PV with bf16 ones and V MN-major
     static constexpr uint32_t kIdescQK = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
     static constexpr uint32_t kIdescPV = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
@@ -109,6 +109,7 @@ struct Smem {
     __device__ __forceinline__ volatile int *bad_mask(int tile) const { return (volatile int *)(ptr + Geo<D>::kOffFlags + 8 + 4 * (tile & 3)); }
     __device__ __forceinline__ float *k_scale(int tile) const { return (float *)(ptr + Geo<D>::kOffKScale) + 8 * (tile & 3); }
     __device__ __forceinline__ volatile int *progress() const { return (volatile int *)(ptr + Geo<D>::kOffItem + 64); }  // tile that the converters are at
+    __device__ __forceinline__ uint4 *response() const { return (uint4 *)(ptr + Geo<D>::kOffItem + 80); }  // the launch's next CTA, if any
     __device__ __forceinline__ int *item(int n) const { return (int *)(ptr + Geo<D>::kOffItem) + 8 * (n & 1); }
     __device__ __forceinline__ float *q_inv() const { return (float *)(ptr + Geo<D>::kOffQInv); }
 };
@@ -168,18 +169,35 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     auto by_group = [&](int r) { return group == 1 ? r : (int)__umulhi((unsigned)r, pp.group_magic); };
 
     // ---- the scheduler (warp 2): which (request, rows, kv-head) is next?  Items are listed heaviest (latest) first, all kv-heads of
-    // one next to each other; a CTA starts with the one of its own number and draws the others from a counter, each while the CTA
-    // works on the one before.  Rows that have no keys to see are dealt with here.  (The CTAs of a cluster have one item.)
+    // one next to each other, and the launch has a CTA for each.  A CTA starts with the one of its own number and then takes the
+    // place of CTAs that have not started (cluster launch control), each while it works on the item before: no word of device memory
+    // that two launches, or two replays of captured ones, could share.  Rows that have no keys to see are dealt with here.  (The CTAs of a cluster have one item.)
+    bool may_draw = cluster == 1;
+    uint32_t draws = 0;
+    auto draw = [&]() {  // number of a CTA that will not start now, or -1
+        if (!may_draw) return -1;
+        if (lane == 0) {
+            mbar_expect_tx(sh.bar(G::NEXT), 16);
+            cp::clusterlaunchcontrol_try_cancel(sh.response(), (uint64_t *)(sh.ptr + G::kOffBar + 8 * G::NEXT));
+        }
+        __syncwarp();
+        // (given up or not: an answer under way must not land in the shared memory of a CTA that has left)
+        if (!__all_sync(0xffffffffu, mbar_wait(sh.bar(G::NEXT), draws++ & 1u))) {
+            *sh.abort_flag() = 2;
+            may_draw = false;
+            return -1;
+        }
+        const uint4 response = *sh.response();
+        fence_proxy_async_smem();  // read before the next answer is written there
+        __syncwarp();
+        may_draw = cp::clusterlaunchcontrol_query_cancel_is_canceled(response);  // nothing left: no further question is allowed
+        return may_draw ? cp::clusterlaunchcontrol_query_cancel_get_first_ctaid_x<int>(response) : -1;
+    };
     auto post = [&](int item, int n) {
-        const int n_items = p.q_tiles * p.num_kv_heads;
         int *slot = sh.item(n);
         for (;; item = -1) {
-            if (item < 0) {
-                if (cluster == 1 && lane == 0) item = (int)gridDim.x + atomicAdd(p.abort_word + 1, 1);
-                item = cluster == 1 ? __shfl_sync(0xffffffffu, item, 0) : n_items;
-            }
-            // past the end, or (not for a cluster, whose CTAs have to stay together) another CTA of this launch timed out
-            const bool over = item >= n_items || (cluster == 1 && *(volatile int *)p.abort_word);
+            if (item < 0) item = draw();
+            const bool over = item < 0;
             const int rank = item / p.num_kv_heads, g = item - rank * p.num_kv_heads, idx = p.q_tiles - 1 - rank;
             int req = 0, first = 0, c_r = 0, q0 = 0;
             if (!over && !find_item(p, pp.few_rows, idx, req, first, q0, c_r)) continue;
@@ -285,6 +303,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 if (lane == 0) *sh.progress() = -1;
                 if (!next_item(n)) break;
             }
+            if (*sh.abort_flag())  // a wait ran out: the CTAs that have not started, and would wait as long, are not to
+                while (draw() >= 0) {}
         } else {
 #pragma unroll 1
         for (int n = 0; next_item(n); ++n) {
@@ -818,10 +838,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     fence_before();
     __syncthreads();
     fence_after();
-    if (threadIdx.x == 0 && *sh.abort_flag()) {  // a wait ran out: report it, and keep the launch's other CTAs from starting
-        *(volatile int *)p.abort_word = 1;
-        atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);
-    }
+    if (threadIdx.x == 0 && *sh.abort_flag()) atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);  // a wait ran out
     if (warp == 1) cp::tcgen05_dealloc(cp::cta_group_1, tmem, 512);
 }
 
@@ -878,12 +895,10 @@ static ekv_status_t launch_prefill8(ekv_pool *pool, Params &pp, cudaStream_t str
     }
     const long long items = (long long)pp.p.q_tiles * pp.p.num_kv_heads;
     pp.cluster = 1 << plan_cluster(items, pp.p.max_blocks, fit);
-    cudaError_t e = cudaMemsetAsync(pp.p.abort_word, 0, 2 * sizeof(int), stream);
-    if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: clear abort word");
     attr.val.clusterDim.x = (unsigned)pp.cluster;
-    cfg.gridDim = dim3((unsigned)(pp.cluster > 1 ? items * pp.cluster : items < pool->sm_count ? items : pool->sm_count));
+    cfg.gridDim = dim3((unsigned)(items * pp.cluster));
     cfg.stream = stream;
-    e = cudaLaunchKernelEx(&cfg, prefill8_kernel<D>, pp);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, prefill8_kernel<D>, pp);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: launch");
     return EKV_OK;
 }

@@ -117,6 +117,7 @@ __global__ void __launch_bounds__(256) read_kv_kernel(const uint8_t *__restrict_
     for (int u = 0; u < kReadUnroll; ++u) {
         if (to[u] < 0) continue;
         if (kE4m3) {
+            if (!(scale[u] > 0.f)) a[u] = make_uint4(0u, 0u, 0u, 0u);  // never written: 0, as attention reads it, whatever the codes
             const uint32_t w[4] = {a[u].x, a[u].y, a[u].z, a[u].w};
             uint32_t o[8];
 #pragma unroll

@@ -81,9 +81,10 @@ class Cache:
         return CODE_VALUE[self.codes] * self.scales[..., None, None]
 
     def rows(self, slots):
-        """(k, v) float64 [T, Hk, D] of valid slots."""
+        """(k, v) float64 [T, Hk, D] of valid slots; a tile that was never written is 0."""
         slots = np.asarray(slots)
-        x = CODE_VALUE[self.codes[slots // 16, :, :, slots % 16]] * self.scales[slots // 16][..., None]
+        scales = self.scales[slots // 16][..., None]
+        x = np.where(scales > 0, CODE_VALUE[self.codes[slots // 16, :, :, slots % 16]] * scales, 0.0)
         return x[:, 0], x[:, 1]
 
 

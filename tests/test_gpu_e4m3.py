@@ -467,6 +467,8 @@ def test_never_written_blocks_read_as_zero():
         c.pool.layer_scales(0)[ids.to(DEV)] = 0.0
         c.pool.layer_tensor(0).view(torch.uint8)[ids.to(DEV)] = 0x7F
         c.K[0][16:48], c.V[0][16:48] = 0.0, 0.0
+        for x in c.pool.read_kv(0, c.slots[0][16:48].to(DEV)):
+            assert (x == 0).all()
         # many keys whose values are 0 and whose scores are not the lowest: their weights count
         zero = torch.zeros(80, 2, 64, dtype=torch.bfloat16)
         k = rows(c.rng, 80, shape, 1.0)
@@ -503,6 +505,37 @@ def test_prefill_on_streams_and_in_a_replayed_graph():
             q.copy_(a)
             g.replay()
             assert torch.equal(o, b)
+
+
+def test_captured_prefills_replayed_side_by_side():
+    """Two captured calls of more items than the GPU has SMs, captured any number of calls apart, share no state."""
+    shape = I.LLAMA8B
+    c = Case(shape, [257, 300, 280, 266] * 3, seed=88)
+    with c.pool:
+        cu = torch.tensor([0, *np.cumsum([257, 200, 280, 66] * 3)], dtype=torch.int32)
+        dcu, n = cu.to(DEV), int(cu[-1])
+        qs = [c.queries(n).to(DEV) for _ in range(2)]
+        want = [c.pool.attn_prefill_chunk(0, q, c.d_tables, dcu, cu, c.d_lens, 0.09) for q in qs]
+        outs, graphs, streams = [torch.empty_like(q) for q in qs], [], [torch.cuda.Stream() for _ in qs]
+        few = torch.tensor([0, 16] + [16] * 11, dtype=torch.int32)
+        d_few = few.to(DEV)
+        for q, o in zip(qs, outs):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                c.pool.attn_prefill_chunk(0, q, c.d_tables, dcu, cu, c.d_lens, 0.09, out=o)
+            graphs.append(g)
+            for _ in range(63):
+                c.pool.attn_prefill_chunk(0, q[:16], c.d_tables, d_few, few, c.d_lens, 0.09)
+        for _ in range(20):
+            for o in outs:
+                o.zero_()
+            torch.cuda.synchronize()
+            for g, s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, outs))
+        assert c.pool.poll_status() == ekv.Status.OK
 
 
 def test_prompt_in_chunks_then_decode_steps():
