@@ -261,17 +261,17 @@ def ekv_extend_tables(pool: int, new_tokens, seq_lens, block_tables, free_ids, f
                       seq_lens_out=None, free_cursor_out=None, stream=None):
     """Block tables, slot mapping, offsets and lengths of a step, on the GPU.  seq_lens and free_cursor are updated in
     place unless seq_lens_out / free_cursor_out are given."""
-    R, max_blocks = int(seq_lens.shape[0]), int(block_tables.shape[1])
-    assert new_tokens.shape[0] == R and block_tables.shape[0] == R and cu_q_lens.numel() == R + 1
+    R, max_blocks = block_tables.shape
     out = seq_lens if seq_lens_out is None else seq_lens_out
     cursor_out = free_cursor if free_cursor_out is None else free_cursor_out
-    assert out.shape[0] == R and free_cursor.numel() == 1 and cursor_out.numel() == 1
+    assert new_tokens.numel() == seq_lens.numel() == out.numel() == R and cu_q_lens.numel() == R + 1
+    assert free_cursor.numel() == cursor_out.numel() == 1
     assert new_tokens.itemsize == seq_lens.itemsize == block_tables.itemsize == free_ids.itemsize == free_cursor.itemsize == \
         cu_q_lens.itemsize == out.itemsize == cursor_out.itemsize == 4, "lengths, tables, ids and offsets are int32"
     assert slot_mapping.itemsize == 8, "the slot mapping is int64"
     _check(load_library().ekv_extend_tables(pool, _dptr(new_tokens), _dptr(seq_lens), R, _dptr(block_tables), max_blocks,
-                                            _dptr(free_ids), int(free_ids.shape[0]), _dptr(free_cursor), _dptr(slot_mapping),
-                                            int(slot_mapping.shape[0]), _dptr(cu_q_lens), _dptr(out), _dptr(cursor_out),
+                                            _dptr(free_ids), free_ids.numel(), _dptr(free_cursor), _dptr(slot_mapping),
+                                            slot_mapping.numel(), _dptr(cu_q_lens), _dptr(out), _dptr(cursor_out),
                                             _stream(stream)))
 
 

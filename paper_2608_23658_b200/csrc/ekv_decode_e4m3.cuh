@@ -21,9 +21,10 @@
 namespace ekv {
 
 // Four CTAs share an SM, with rings of 4 to 8 KiB a warp (64 to 128 KiB in flight per SM).  The bf16 kernel's two CTAs with
-// rings three times as deep leave this kernel at 0.72 of the copy rate: converting makes a block's chain of instructions long,
-// and it takes four warps a scheduler to hide it (256 sequences of 2048..8192 keys, 32q/8kv: 2 CTAs x 6 stages 540 us, 3 x 4
-// 429, 4 x 3 416, 4 x 2 411, 5 x 2 427, 6 x 2 505 -- registers are spilled from 5 on).
+// rings three times as deep leave this kernel at 0.87 of the copy rate: converting makes a block's chain of instructions long,
+// and it takes three or four warps a scheduler to hide it.  Measured, us: 256 sequences of 2048..8192 keys, 32q/8kv, d128 (2.68 GB; at
+// the copy rate 411) 2 CTAs x 6 stages 458, 3 x 4 399, 4 x 3 400, 4 x 2 399 = 6.7 TB/s, 5 x 2 416 (registers are spilled from 5 on);
+// 64 sequences of 8000..30000, 16q/2kv, d64 (0.33 GB) 101, 83, 92, 77, 83.
 static constexpr int kDecode8Ctas = 4;
 template <int D>
 constexpr int kDecode8Stages = D == 128 ? 2 : 4;

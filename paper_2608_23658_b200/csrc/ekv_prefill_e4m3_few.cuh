@@ -11,8 +11,9 @@
 //   CTA          8 warps = 8 or 4 rings; ring k takes every 8th or 4th block of the CTA's key range
 //   cluster      up to 16 CTAs share a (request, kv-head)'s keys and merge (m, l, O) through distributed shared memory: the call
 //                has no workspace.  Rings first, then CTAs, each in a fixed order: the same bits every time.
-// More rows than 32 are better off on the tensor instruction: 128 requests over 2000..8000 keys, 32q/8kv: 8 positions each (32
-// rows) 566 us here and 628 there, 16 positions (with rings of four warps) 1117 and 647.
+// Measured, 32q/8kv, d128, us here and on the tensor instruction's kernel: 128 requests over 2000..8000 keys, 16 rows 282 (4.6 TB/s)
+// and 613, 32 rows 569 and 615; one of 32 rows over 30000 62 and 97; 32 of 32 rows over 500 35 and 34.  More than 32 rows would take
+// four warps a ring, each converting what it reads: half the rate again, and slower than the 615.
 // Rows differ in the last key they see, so a block can be hidden from a row altogether: its references may stay at the value that
 // stands for none.
 #pragma once

@@ -237,6 +237,7 @@ extern "C" ekv_status_t ekv_extend_tables(ekv_pool_t *pool, const int32_t *new_t
     // a token a thread of one CTA, then a cluster
     const int ctas = T_cap > kTabThreads ? widest : 1;
     attr.val.clusterDim.x = (unsigned)ctas;
+    cfg.numAttrs = ctas > 1 ? 1 : 0;
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(kTabThreads);
     cfg.dynamicSmemBytes = 3 * (size_t)R * sizeof(int);

@@ -69,10 +69,12 @@ __global__ void __launch_bounds__(kWriteThreads) write_kv_kernel(uint4 *__restri
 
 // ekv_read_kv: a thread takes kReadUnroll pieces of 16 channels of one row each -- 32 bytes of bf16, or 16 codes and their scale --
 // and has the loads of all of them on their way before it stores.  Bound by memory; a code times a power of two needs 4 significant
-// bits, so the bf16 is exact.
+// bits, so the bf16 is exact.  Outputs on 32-byte boundaries are stored 32 bytes at a time (kWhole).  Measured, 8 kv-heads of 128:
+// 16384 tokens from an 8-bit pool (101 MB) 22.3 us = 4.5 TB/s, with two stores of 16 bytes 24.2; 2048 tokens 3.9 and 5.3; from a
+// bf16 pool (134 MB) 24.0 = 5.6 TB/s and 26.1.
 static constexpr int kReadUnroll = 4;
 
-template <bool kE4m3>
+template <bool kE4m3, bool kWhole>
 __global__ void __launch_bounds__(256) read_kv_kernel(const uint8_t *__restrict__ cache, const float *__restrict__ scales,
                                                       uint4 *__restrict__ k, uint4 *__restrict__ v, const long long *__restrict__ slot_mapping,
                                                       long long pieces, int num_kv_heads, int pieces_per_row, int token_shift,
@@ -130,8 +132,12 @@ __global__ void __launch_bounds__(256) read_kv_kernel(const uint8_t *__restrict_
             b[u] = make_uint4(o[4], o[5], o[6], o[7]);
         }
         uint4 *dst = (rem[u] >= row_pieces ? v : k) + 2 * to[u];
-        dst[0] = a[u];
-        dst[1] = b[u];
+        if (kWhole) {
+            st_global_32(dst, a[u], b[u]);
+        } else {
+            dst[0] = a[u];
+            dst[1] = b[u];
+        }
     }
 }
 
@@ -157,7 +163,9 @@ extern "C" ekv_status_t ekv_read_kv(ekv_pool_t *pool, int32_t layer, void *k_out
         set_error("ekv_read_kv: too many rows (T=%d)", T);
         return EKV_ERR_INVALID;
     }
-    const auto kernel = pool->e4m3() ? read_kv_kernel<true> : read_kv_kernel<false>;
+    const bool whole = (((uintptr_t)k_out | (uintptr_t)v_out) & 31) == 0;
+    const auto kernel = pool->e4m3() ? (whole ? read_kv_kernel<true, true> : read_kv_kernel<true, false>)
+                                     : (whole ? read_kv_kernel<false, true> : read_kv_kernel<false, false>);
     kernel<<<(unsigned)((pieces + per_cta - 1) / per_cta), 256, 0, (cudaStream_t)stream>>>(
         (const uint8_t *)pool->layer_base(layer), pool->e4m3() ? pool->layer_scales(layer) : nullptr, (uint4 *)k_out, (uint4 *)v_out,
         (const long long *)slot_mapping, pieces, pool->desc.num_kv_heads, pieces_per_row, token_shift, (long long)pool->block_stride, pool->d_live,

@@ -184,6 +184,23 @@ def test_layers_elastic_blocks_and_moves(fused):
         assert pool.poll_status() == ekv.Status.OK
 
 
+@pytest.mark.parametrize("dtype", [ekv.EKV_BF16, ekv.EKV_E4M3])
+@pytest.mark.parametrize("k_at,v_at", [(8, 0), (0, 8), (8, 8)])  # elements: 16 bytes past a 32-byte boundary
+def test_read_kv_into_outputs_on_16_byte_boundaries(dtype, k_at, v_at):
+    rng = np.random.default_rng(6)
+    with ekv.Pool(num_q_heads=4, num_kv_heads=2, head_dim=64, base_blocks=64, dtype=dtype) as pool:
+        n = 37 * 2 * 64
+        pool.write_kv(0, rows(rng, 37, I.TINY).to(DEV), rows(rng, 37, I.TINY).to(DEV), torch.arange(37).to(DEV))
+        at = torch.from_numpy(rng.permutation(37)).to(DEV)
+        want = pool.read_kv(0, at)
+        flat = [torch.full((n + 32,), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        got = [f[s:s + n].view(37, 2, 64) for f, s in zip(flat, (k_at, v_at))]
+        pool.read_kv(0, at, *got)
+        for f, s, g, w in zip(flat, (k_at, v_at), got, want):
+            assert torch.equal(g, w) and (f[:s] == 7).all() and (f[s + n:] == 7).all()
+
+
+
 def test_write_on_streams_and_in_a_replayed_graph():
     shape, rng = I.TINY, np.random.default_rng(12)
     pool, cache = fresh(shape, 400, num_layers=2)
