@@ -68,7 +68,7 @@ struct Params {
     long long block_stride;
     unsigned group_magic;  // ceil(2^32 / group): a division by the group (2 or more) is one multiplication, exact below 2^29
     int few_rows;  // requests of at most this many rows are another kernel's (ekv_prefill_e4m3_few.cuh)
-    int cluster;   // CTAs that share an item's keys
+    int cluster, cluster_log;  // CTAs that share an item's keys: 2^cluster_log
     float q_sign;  // -1 for a negative scale; 0 for a scale of 0
 };
 
@@ -230,17 +230,15 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     // ---- the current item, as each role reads it from the scheduler's slot
     int req, g, row0, rows_here, q0, prefix, kv_end, tile0, n_tiles, n_blocks;
     bool by_rows, merge;
-    auto position = [&](int r) { return by_group(row0 + r); };
-    // element offset of a row of the item in q and out
-    auto row_offset = [&](int r) {
-        const int pos = position(r), hg = row0 + r - pos * group;
-        return ((size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + hg)) * D;
-    };
+    int pos0, head0;    // the item's first row: its position in the request and its head of the group
+    size_t first_head;  // offset in q and out of the first head of the group, at that position
+    auto position = [&](int r) { return pos0 + by_group(head0 + r); };
+    // offset of a row of the item behind that: 32 bits hold it (256 rows)
+    auto row_offset = [&](int r) { return (by_group(head0 + r) * (p.num_q_heads - group) + head0 + r) * D; };
     // Barriers live as long as the CTA; an item's waits count phases from 0, on top of what earlier items left in bit `bar` of this.
     uint32_t phases = 0;
     auto wait = [&](int bar, uint32_t parity) { return wait_warp<D>(sh, bar, (parity ^ (phases >> bar)) & 1u); };
-    // All roles are through with the item before (its shared memory and TMEM), and the slot of this one is posted.
-    auto next_item = [&](int n) {
+    auto count_phases = [&](int n) {
         if (n > 0) {  // completions of the item before, by barrier
             const uint32_t t[2] = {(uint32_t)(n_tiles + 1) >> 1, (uint32_t)n_tiles >> 1};
 #pragma unroll
@@ -252,22 +250,34 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             }
             phases ^= 1u << G::DRAIN;
         }
+    };
+    auto meet_items = [&]() {  // all roles are through with the item before (its shared memory and TMEM), and the next one's slot is posted
         fence_before();
         __syncwarp();
         asm volatile("bar.sync 3, 512;" ::: "memory");
         fence_after();
+    };
+    auto read_item = [&](int n) {
         const volatile int *slot = sh.item(n);
-        if (slot[0] == 0 || *sh.abort_flag()) return false;
+        if (slot[0] == 0) return false;
         req = slot[1], g = slot[2], row0 = slot[3], rows_here = slot[4], q0 = slot[5], prefix = slot[7];
+        pos0 = by_group(row0);
+        head0 = row0 - pos0 * group;
+        first_head = ((size_t)(q0 + pos0) * p.num_q_heads + (size_t)g * group) * D;
         kv_end = min(slot[6], prefix + position(rows_here - 1) + 1);  // keys any row of the item may see
         const int all_tiles = (kv_end + kBN - 1) / kBN;
-        tile0 = (int)((long long)all_tiles * part / cluster);  // this CTA's key tiles: tile0 .. tile0 + n_tiles - 1 (possibly none)
-        n_tiles = (int)((long long)all_tiles * (part + 1) / cluster) - tile0;
+        tile0 = (all_tiles * part) >> pp.cluster_log;  // this CTA's key tiles: tile0 .. tile0 + n_tiles - 1 (possibly none)
+        n_tiles = ((all_tiles * (part + 1)) >> pp.cluster_log) - tile0;
         n_blocks = (kv_end + 15) >> 4;
         // by_rows: slot x holds rows 128 x .. and sees every key tile j.  Else both hold rows 0 .. and slot x sees tiles x, x + 2, ...
         by_rows = rows_here > kBM;
         merge = cluster > 1 || !by_rows;
         return true;
+    };
+    auto next_item = [&](int n) {
+        count_phases(n);
+        meet_items();
+        return !*sh.abort_flag() && read_item(n);
     };
 
     // The merge: all roles meet when the CTA's tiles are no longer needed, again when the partial results of the cluster are in
@@ -302,6 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     }
                 }
                 post(item, n);  // beside the end of the work on item n - 1
+                asm volatile("bar.arrive 4, 160;" ::: "memory");  // the converters may look at it
                 item = -1;
                 if (n > 0 && merge) merge_barriers();
                 if (lane == 0) *sh.progress() = -1;
@@ -380,8 +391,6 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     } else if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // =========================== converters ===========================
-#pragma unroll 1
-        for (int n = 0; next_item(n); ++n) {
         constexpr int kIts = D / 16;                       // 16-byte pieces of codes a thread takes of a tile
         constexpr int kBlocksPerIt = 128 * 16 / (16 * D);  // blocks the 128 threads cover at once: 1, or 2 at head_dim 64
         const int ct = threadIdx.x - 384;
@@ -392,8 +401,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         const int piece = D == 128 ? ((in_block >> 1) & 4) | (in_block & 3) : in_block & 3;
         const int first_block = kBlocksPerIt > 1 ? ct / D : 0;
         const long long live = *p.live;
-        const int *bt = p.block_tables + (size_t)req * p.max_blocks;
-        const uint8_t *src = pp.cache + (long long)g * (16 * D) + rowb * D + piece * 16;
+        const int *bt;
+        const uint8_t *src;
         const long long v_off = (long long)p.num_kv_heads * (16 * D);
         const uint32_t raw = sh.base + G::kOffRaw + ct * 16;  // this thread's places: one every 2048 bytes
         // lane l: id of block 8j + l % 8 of tile j (-1 past the end, -2 invalid)
@@ -448,15 +457,29 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.bar(bar));
         };
-        int ids = load_id(0);
-        float ks = load_scale(ids, 0), vs = load_scale(ids, 1);
+        // An item's first tile of codes is on its way before the item before is finished by the other roles: the places are free.
+        int ids, ids_next;
+        float ks, vs;
+        auto start_item = [&](int n) {
+            asm volatile("bar.sync 4, 160;" ::: "memory");  // posted
+            if (!read_item(n)) return false;
+            bt = p.block_tables + (size_t)req * p.max_blocks;
+            src = pp.cache + (long long)g * (16 * D) + rowb * D + piece * 16;
+            ids = load_id(0);
+            ks = load_scale(ids, 0), vs = load_scale(ids, 1);
 #pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv) {
+            for (int kv = 0; kv < 2; ++kv) {
 #pragma unroll 2
-            for (int it = 0; it < kIts; ++it) copy(it, ids, kv);
-            cp_async_commit();
-        }
-        int ids_next = load_id(1);
+                for (int it = 0; it < kIts; ++it) copy(it, ids, kv);
+                cp_async_commit();
+            }
+            ids_next = load_id(1);
+            return true;
+        };
+        bool more = start_item(0);
+        meet_items();
+#pragma unroll 1
+        for (int n = 0; more && !*sh.abort_flag(); ++n) {
         bool ok = true;
 #pragma unroll 1
         for (int j = 0; j < n_tiles; ++j) {
@@ -540,8 +563,13 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             vs = vs_next;
         }
         cp_async_wait_all();  // what was started for a tile that does not come (or after a wait that was given up)
-        if (merge) merge_barriers();
+        const bool merges = merge;
+        count_phases(n + 1);
+        more = start_item(n + 1);
+        if (merges) merge_barriers();
+        meet_items();
         }
+        cp_async_wait_all();
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // =========================== softmax + write-out ===========================
@@ -568,7 +596,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 const int r = kRowsPerInst * u + sub;
                 place[u] = G::kOffQ + x * G::kTileBytes + (piece >> 3) * kHalfBytes + (wrow0 + r) * 128 + (((piece & 7) ^ (r & 7)) << 4);
             }
-            const __nv_bfloat16 *q_src = p.q + piece * 8;
+            const __nv_bfloat16 *q_src = p.q + first_head + piece * 8;
             const int first_row = x * kBM + wrow0 + sub;
 #pragma unroll 1
             for (int b = 0; b < 32 / kBatchRows; ++b) {
@@ -748,11 +776,20 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                     }
                 }
                 __syncwarp();
-#pragma unroll 2
-                for (int it = 0; it < 32 / kRowsPerInst; ++it) {
-                    const int rr = wrow0 + kRowsPerInst * it + sub, in_item = rx * kBM + rr;
-                    const uint4 v = *reinterpret_cast<const uint4 *>(q_tile + rr * (D * 2) + ((piece ^ (rr & (kPieces - 1))) << 4));
-                    if (in_item < rows_here) *reinterpret_cast<uint4 *>(p.out + row_offset(in_item) + piece * 8) = v;
+                __nv_bfloat16 *to = p.out + first_head + piece * 8;
+#pragma unroll 1
+                for (int it = 0; it < 32 / kRowsPerInst; it += 4) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int rr = wrow0 + kRowsPerInst * (it + u) + sub;
+                        v[u] = *reinterpret_cast<const uint4 *>(q_tile + rr * (D * 2) + ((piece ^ (rr & (kPieces - 1))) << 4));
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int in_item = rx * kBM + wrow0 + kRowsPerInst * (it + u) + sub;
+                        if (in_item < rows_here) *reinterpret_cast<uint4 *>(to + row_offset(in_item)) = v[u];
+                    }
                 }
             }
         } else {
@@ -829,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 for (int u = 0; u < kRowsAtOnce; ++u) {
                     const int k = k0 + u * kRowsPerWarp;
                     if (k < n_rows)
-                        *reinterpret_cast<uint2 *>(p.out + row_offset(part + cluster * k) + chunk * 4) =
+                        *reinterpret_cast<uint2 *>(p.out + first_head + row_offset(part + cluster * k) + chunk * 4) =
                             make_uint2(pack_bf16x2(acc[u].x, acc[u].y), pack_bf16x2(acc[u].z, acc[u].w));
                 }
             }
@@ -898,7 +935,8 @@ static ekv_status_t launch_prefill8(ekv_pool *pool, Params &pp, cudaStream_t str
         clusters_that_fit((const void *)prefill8_kernel<D>, cfg, fit);
     }
     const long long items = (long long)pp.p.q_tiles * pp.p.num_kv_heads;
-    pp.cluster = 1 << plan_cluster(items, pp.p.max_blocks, fit);
+    pp.cluster_log = plan_cluster(items, pp.p.max_blocks, fit);
+    pp.cluster = 1 << pp.cluster_log;
     attr.val.clusterDim.x = (unsigned)pp.cluster;
     cfg.gridDim = dim3((unsigned)(items * pp.cluster));
     cfg.stream = stream;

@@ -68,7 +68,7 @@ __device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::P
         return;
     }
     const int all_blocks = (L + 15) >> 4;
-    const int blk0 = (int)((long long)all_blocks * part / cluster), blk1 = (int)((long long)all_blocks * (part + 1) / cluster);
+    const int blk0 = (int)((long long)all_blocks * part >> pp.cluster_log), blk1 = (int)((long long)all_blocks * (part + 1) >> pp.cluster_log);
     const int nw = max(0, (blk1 - blk0 - ring + rings - 1) / rings);  // blocks of this ring
     const bool busy = 16 * tile < rows;  // a warp without rows only keeps step
 
@@ -386,6 +386,7 @@ static ekv_status_t launch(ekv_pool *pool, int layer, tc8::Params &pp, int items
     static constexpr int slack[kMaxClusterLog + 1] = {0, 8, 5, 5, 4};
     int c = 0;
     while (c < kMaxClusterLog && 4ll * items <= (long long)slack[c + 1] * fit[c + 1] && pp.p.max_blocks >= (items <= fit[c + 1] ? 8ll : 64ll) << (c + 1)) ++c;
+    pp.cluster_log = c;
     pp.cluster = 1 << c;
     attr.val.clusterDim.x = (unsigned)pp.cluster;
     cfg.gridDim = dim3((unsigned)((long long)items * pp.cluster));
