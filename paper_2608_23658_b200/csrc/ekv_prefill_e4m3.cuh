@@ -313,6 +313,18 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 }
                 post(item, n);  // beside the end of the work on item n - 1
                 asm volatile("bar.arrive 4, 160;" ::: "memory");  // the converters may look at it
+                if (n > 0 && cluster == 1) {  // its Q rows into L2, while the item before takes its time
+                    const volatile int *slot = sh.item(n);
+                    if (slot[0]) {
+                        const int at = slot[3] - by_group(slot[3]) * group, lines = slot[4] * (D / 64);
+                        const __nv_bfloat16 *from = p.q + ((size_t)(slot[5] + by_group(slot[3])) * p.num_q_heads + (size_t)slot[2] * group) * D;
+#pragma unroll 1
+                        for (int i = lane; i < lines; i += 32) {
+                            const int r = at + i / (D / 64);
+                            asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (by_group(r) * (p.num_q_heads - group) + r) * D + i % (D / 64) * 64));
+                        }
+                    }
+                }
                 item = -1;
                 if (n > 0 && merge) merge_barriers();
                 if (lane == 0) *sh.progress() = -1;
