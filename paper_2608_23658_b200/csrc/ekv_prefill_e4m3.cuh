@@ -621,31 +621,34 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             }
             cp_async_commit();
             cp_async_wait_all();
+            __syncwarp();
+            // a thread a row from here: the maximum takes no shuffles, and eight rows' chunks at the same place lie in all banks
+            uint8_t *const mine = sh.ptr + G::kOffQ + x * G::kTileBytes + row * 128;
+            auto chunk = [&](int c) { return mine + (c >> 3) * kHalfBytes + (((c ^ row) & 7) << 4); };
+            uint32_t top = 0;
 #pragma unroll 1
-            for (int b = 0; b < 32 / kBatchRows; ++b) {  // four pieces side by side: one is a chain of some 300 cycles
-                uint4 v[kBatch];
-                uint32_t top[kBatch];
+            for (int c = 0; c < kPieces; c += 4) {
+                uint4 v[4];
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) v[u] = lds_16(sh.base + place[u] + b * (kBatchRows * 128));
+                for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const uint4 *>(chunk(c + u));
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    const uint32_t t2 = __vmaxu2(__vmaxu2(v[u].x & 0x7fff7fffu, v[u].y & 0x7fff7fffu), __vmaxu2(v[u].z & 0x7fff7fffu, v[u].w & 0x7fff7fffu));
-                    top[u] = max(t2 & 0xffffu, t2 >> 16);
-                }
+                for (int u = 0; u < 4; ++u)
+                    top = __vmaxu2(top, __vmaxu2(__vmaxu2(v[u].x & 0x7fff7fffu, v[u].y & 0x7fff7fffu), __vmaxu2(v[u].z & 0x7fff7fffu, v[u].w & 0x7fff7fffu)));
+            }
+            const float up = to_f16_range(__uint_as_float(max(top & 0xffffu, top >> 16) << 16)), f = up * pp.q_sign;
+            sh.q_inv()[x * kBM + row] = pow2_inverse(up);
+#pragma unroll 1
+            for (int c = 0; c < kPieces; c += 4) {
+                uint4 v[4];
 #pragma unroll
-                for (int o = kPieces / 2; o > 0; o >>= 1)
+                for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const uint4 *>(chunk(c + u));
 #pragma unroll
-                    for (int u = 0; u < kBatch; ++u) top[u] = max(top[u], __shfl_xor_sync(0xffffffffu, top[u], o));
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) {
-                    const float up = to_f16_range(__uint_as_float(top[u] << 16));
-                    const float f = up * pp.q_sign;
+                for (int u = 0; u < 4; ++u) {
                     const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
                     uint32_t h[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) h[i] = pack_f16x2(__uint_as_float(w[i] << 16) * f, __uint_as_float(w[i] & 0xffff0000u) * f);
-                    *reinterpret_cast<uint4 *>(sh.ptr + place[u] + b * (kBatchRows * 128)) = make_uint4(h[0], h[1], h[2], h[3]);
-                    if (piece == 0) sh.q_inv()[first_row + b * kBatchRows + kRowsPerInst * u] = pow2_inverse(up);
+                    *reinterpret_cast<uint4 *>(chunk(c + u)) = make_uint4(h[0], h[1], h[2], h[3]);
                 }
             }
             fence_proxy_async_smem();
