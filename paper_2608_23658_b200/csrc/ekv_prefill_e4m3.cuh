@@ -19,9 +19,10 @@
 //     [2^13, 2^14) by a power of two, as in decode (what f16 then drops lies 2^-37 below the row's largest element).
 //   - V goes to bf16 with its scale multiplied in (exact, a power of two), since only bf16 has the scales' range; P is bf16.
 // Measured, 32q/8kv, d128: 2048 positions over 14001 keys 469 us = 1075 TFLOP/s, 0.67 of cuBLAS' burst; a prompt of 8192 493 us =
-// 1114; 64 prompts of 512 335 us, 256 of 128 255 us.  What bounds it: a key tile's chain through one head's scores, softmax and P V (3500
+// 1114; 64 prompts of 512 303 us, 256 of 128 218 us.  What bounds it: a key tile's chain through one head's scores, softmax and P V (3500
 // cycles a pair of tiles, as in the other tcgen05 kernels) plus a tenth for the conversion; 256 items on 148 SMs are two rounds for
-// 1.73; and an item costs 10 to 13 thousand cycles besides its tiles, which is most of a short prompt.
+// 1.73; and an item costs some 9000 cycles besides its tiles, which is most of a short prompt: Q on its way and to f16, the first scores,
+// the write-out (whose rows go through the idle Q tile: straight from the registers, a thread a row, they took 224 us for 218).
 //
 //   warp 0        MMA issuer: S = Q K^T (both from shared memory) and O += P V (P from TMEM, V MN-major)
 //   warp 1        TMEM allocation; warp 2: item scheduler (the kernel is persistent, a CTA an SM: set-up and instruction caches
