@@ -50,12 +50,6 @@ __device__ __forceinline__ float to_f16_range(float a) {
     return __uint_as_float((uint32_t)(k + 127) << 23);
 }
 
-// two f16 that codes became -> two bf16 (exact: codes have four significant bits)
-__device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) {
-    const float2 f = f16x2_to_float2(h);
-    return pack_bf16x2(f.x, f.y);
-}
-
 // ---- what decode and the few-rows kernel share: P V with both operands in f16 -----------------------------------
 // V's codes are exact in f16, so one conversion instruction makes an operand of them, if V's scale 2^e_V goes elsewhere.  It goes
 // into P, and so that f16's range does not matter, a row keeps two references: m for its scores x (log2), which its sum of
