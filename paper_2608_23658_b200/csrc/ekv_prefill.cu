@@ -55,7 +55,8 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
     const bool e4m3 = pool->e4m3();
     const int bm = e4m3 ? tc8::kItemRows : kernel == K_WARP_MMA ? kPmBM : tc::kBM;
     // Of an 8-bit pool's requests those with few rows go to a kernel of their own (ekv_prefill_e4m3_few.cuh): one launch each if a
-    // call has both kinds.
+    // call has both kinds, the second in the tail of the first (a chunk of 2048 over 8000 keys and 128 single rows 425 -> 400 us, 100
+    // tokens over 500 keys and 8 requests of 4 31 -> 22).
     long long few = 0;
     PrefillParams p;
     p.n_prefix = R <= kPrefixMax ? 1 : 0;
@@ -113,10 +114,8 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, 
             st = d128 ? tc8::launch_prefill8<128>(pool, pp, (cudaStream_t)stream) : tc8::launch_prefill8<64>(pool, pp, (cudaStream_t)stream);
             if (st != EKV_OK) return st;
         }
-        if (few > 0) {
-            const int items = R * pool->desc.num_kv_heads;  // the others leave at once
-            st = d128 ? few8::launch<128>(pool, layer, pp, items, (cudaStream_t)stream) : few8::launch<64>(pool, layer, pp, items, (cudaStream_t)stream);
-        }
+        if (few > 0)
+            st = d128 ? few8::launch<128>(pool, layer, pp, few, q_tiles > 0, (cudaStream_t)stream) : few8::launch<64>(pool, layer, pp, few, q_tiles > 0, (cudaStream_t)stream);
         return st;
     }
     if (kernel == K_TWO_HEAD) return tc::launch_prefill_tc(pool, layer, p, q, out, cu_q_lens_host[R], (cudaStream_t)stream);

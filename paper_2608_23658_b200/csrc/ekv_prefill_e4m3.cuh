@@ -160,6 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cluster = pp.cluster, part = blockIdx.x % cluster;  // CTAs that share an item's keys; which of them this is
 
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the call's other kernel, if it has one, may use what falls free
     if (threadIdx.x == 64) {
 #pragma unroll 1
         for (int i = 0; i < G::NBAR; ++i) mbar_init(sh.bar(i), G::arrivals(i));

@@ -352,24 +352,27 @@ __global__ void __launch_bounds__(kThreads, 2) few8_kernel(const __grid_constant
     const int req = blockIdx.x / pp.cluster / pp.p.num_kv_heads;
     const long long rows = (long long)(pp.p.cu_q_lens[req + 1] - pp.p.cu_q_lens[req]) * pp.p.group;
     // Every reason to leave, here and in few8_item, is the same for all CTAs of a cluster.
-    if (rows <= 0 || rows > kMaxRows) return;  // not one of this kernel's requests
-    if (rows > 16) few8_item<D, 1>(kvmap, pp);
+    if (rows <= 0 || rows > kMaxRows) {}  // not one of this kernel's requests
+    else if (rows > 16) few8_item<D, 1>(kvmap, pp);
     else few8_item<D, 0>(kvmap, pp);
+    // Beside the other kernel of the call, which it shares nothing with, but not through before it: what follows on the stream
+    // waits for this launch alone.
+    if (blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 template <int D>
-static ekv_status_t launch(ekv_pool *pool, int layer, tc8::Params &pp, int items, cudaStream_t stream) {
+static ekv_status_t launch(ekv_pool *pool, int layer, tc8::Params &pp, long long few, bool beside, cudaStream_t stream) {
     using G = Geo<D>;
     static int fits[64][kMaxClusterLog + 1] = {};  // per device: clusters of 2^i CTAs that run at the same time; [..][0] 0: not asked yet
     const int dev = pool->desc.device;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // from the tail of the launch before on, if that is the call's own
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = G::kSmemBytes;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
     int asked[kMaxClusterLog + 1] = {}, *fit = dev < 64 ? fits[dev] : asked;
     if (fit[0] == 0) {
         cudaError_t e = cudaFuncSetAttribute(few8_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kSmemBytes);
@@ -383,13 +386,16 @@ static ekv_status_t launch(ekv_pool *pool, int layer, tc8::Params &pp, int items
     // items) 292 152 83 47 38; over 1000..8000 keys 2 requests 50 31 21 20 29; 4: 65 39 25 22 42; 10: 83 48 37 48 83; 16: 83 50 59
     // 72 129; 20: 85 58 64 85 157; 64: 168 159 180 265 498; over 400 keys 1: 13 13 11 11 15, 8: 13 13 15 24 57, 32: 17 28 44 84 193.
     // (14 clusters of 16 run at a time, 33 of 8, 71 of 4, 148 of 2.)  Depends on the call's shape arguments alone.
+    const long long items = few * pool->desc.num_kv_heads;  // (those of the other requests leave at once)
     static constexpr int slack[kMaxClusterLog + 1] = {0, 8, 5, 5, 4};
     int c = 0;
     while (c < kMaxClusterLog && 4ll * items <= (long long)slack[c + 1] * fit[c + 1] && pp.p.max_blocks >= (items <= fit[c + 1] ? 8ll : 64ll) << (c + 1)) ++c;
     pp.cluster_log = c;
     pp.cluster = 1 << c;
-    attr.val.clusterDim.x = (unsigned)pp.cluster;
-    cfg.gridDim = dim3((unsigned)((long long)items * pp.cluster));
+    attr[0].val.clusterDim.x = (unsigned)pp.cluster;
+    cfg.attrs = attr;
+    cfg.numAttrs = beside ? 2 : 1;
+    cfg.gridDim = dim3((unsigned)((long long)pp.p.R * pool->desc.num_kv_heads * pp.cluster));
     cfg.stream = stream;
     cudaError_t e = cudaLaunchKernelEx(&cfg, few8_kernel<D>, pool->kv_map[layer], (const tc8::Params &)pp);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_attn_prefill_chunk: launch");

@@ -555,6 +555,31 @@ def test_captured_prefills_replayed_side_by_side():
         assert c.pool.poll_status() == ekv.Status.OK
 
 
+def test_mixed_call_is_through_before_what_follows():
+    """A long chunk and a single row are two launches side by side: the next operation on the stream finds both results."""
+    shape = I.LLAMA8B
+    c = Case(shape, [3000, 20], seed=90)
+    with c.pool:
+        cu = torch.tensor([0, 1500, 1501], dtype=torch.int32)
+        q, dcu = c.queries(1501).to(DEV), cu.to(DEV)
+        want = c.pool.attn_prefill_chunk(0, q, c.d_tables, dcu, cu, c.d_lens, 0.09)
+        torch.cuda.synchronize()
+        out = torch.empty_like(want)
+        for _ in range(10):
+            out.fill_(7.0)
+            c.pool.attn_prefill_chunk(0, q, c.d_tables, dcu, cu, c.d_lens, 0.09, out=out)
+            assert torch.equal(out.clone(), want)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out.fill_(7.0)
+            c.pool.attn_prefill_chunk(0, q, c.d_tables, dcu, cu, c.d_lens, 0.09, out=out)
+            copy = out.clone()
+        for _ in range(10):
+            g.replay()
+            assert torch.equal(copy, want)
+        assert c.pool.poll_status() == ekv.Status.OK
+
+
 def test_prompt_in_chunks_then_decode_steps():
     """A run as it would be used: chunks written and attended to one after the other, then single tokens; every result against the
     cache's own values, and the last decode step against the prefill of that one row."""
