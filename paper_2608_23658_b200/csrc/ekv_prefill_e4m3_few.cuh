@@ -381,15 +381,20 @@ static ekv_status_t launch(ekv_pool *pool, int layer, tc8::Params &pp, long long
         tc8::clusters_that_fit((const void *)few8_kernel<D>, cfg, fit);
     }
     // Parts: as many as let the items run at the same time, or nearly so (slack[i] quarters of that for 2^i CTAs), while a part has
-    // eight blocks, one a ring, of the longest sequence that the table can hold -- 64 if the items take turns, as a cluster takes
-    // longer to start than a CTA.  Measured, requests of 16 rows, us with 1 / 2 / 4 / 8 / 16 CTAs an item: one over 30000 keys (8
-    // items) 292 152 83 47 38; over 1000..8000 keys 2 requests 50 31 21 20 29; 4: 65 39 25 22 42; 10: 83 48 37 48 83; 16: 83 50 59
-    // 72 129; 20: 85 58 64 85 157; 64: 168 159 180 265 498; over 400 keys 1: 13 13 11 11 15, 8: 13 13 15 24 57, 32: 17 28 44 84 193.
-    // (14 clusters of 16 run at a time, 33 of 8, 71 of 4, 148 of 2.)  Depends on the call's shape arguments alone.
+    // eight blocks, one a ring, of the longest sequence that the table can hold -- 64 if the items take turns, as a cluster takes longer
+    // to start than a CTA, and 128 if they take more than two.  Measured, requests of 16 rows, us with 1 / 2 / 4 / 8 / 16 CTAs an item: one
+    // over 30000 keys (8 items) 292 152 83 47 38; over 1000..8000 keys 2 requests 50 31 21 20 29; 4: 65 39 25 22 42; 10: 83 48 37 48 83;
+    // 16: 83 50 59 72 129; 20: 85 58 64 85 157; 48: 131 119; 64: 169 159 180 265 498; 72: 171 175; 64 over 1200..2100 67 81; 32 of 4 to 20
+    // rows over 1000..4100 101 75 83 119 219; over 400 keys 1: 13 13 11 11 15, 8: 13 13 15 24 57, 32: 17 28 44 84 193.  (14 clusters of 16
+    // run at a time, 33 of 8, 71 of 4, 148 of 2.)  Depends on the call's shape arguments alone.
     const long long items = few * pool->desc.num_kv_heads;  // (those of the other requests leave at once)
-    static constexpr int slack[kMaxClusterLog + 1] = {0, 8, 5, 5, 4};
+    static constexpr int slack[kMaxClusterLog + 1] = {0, 14, 5, 5, 4};
     int c = 0;
-    while (c < kMaxClusterLog && 4ll * items <= (long long)slack[c + 1] * fit[c + 1] && pp.p.max_blocks >= (items <= fit[c + 1] ? 8ll : 64ll) << (c + 1)) ++c;
+    while (c < kMaxClusterLog && 4ll * items <= (long long)slack[c + 1] * fit[c + 1]) {
+        const long long part_blocks = items <= fit[c + 1] ? 8 : items <= 2ll * fit[c + 1] ? 64 : 128;
+        if (pp.p.max_blocks < part_blocks << (c + 1)) break;
+        ++c;
+    }
     pp.cluster_log = c;
     pp.cluster = 1 << c;
     attr[0].val.clusterDim.x = (unsigned)pp.cluster;
