@@ -285,6 +285,8 @@ EKV_API ekv_status_t ekv_attn_decode_plan(const ekv_pool_t *pool, int32_t B, int
  * Two passes: a split pass over fixed-size key ranges writing fp32 partials, and a combine pass.
  * The split plan depends only on (B, max_blocks_per_seq), so results are bitwise reproducible and
  * independent of which physical blocks hold the data.
+ * A NaN in the query of a head, or in a key that it sees, makes the head's row NaN; a row is 0 only when it
+ * has no key, or none whose block is valid.
  */
 EKV_API ekv_status_t ekv_attn_decode(ekv_pool_t *pool, int32_t layer, const void *q, void *out,
                              const int32_t *block_tables, int32_t max_blocks_per_seq,

@@ -48,6 +48,10 @@ struct DecodeParams {
     long long total_blocks;         // two-tensor variant only: ids at or above this are invalid
 };
 
+// A row's result.  0 stands for a row without any weight (no keys, or all of them skipped) and for nothing else: a NaN sum has to
+// come out as NaN, not as a row of plausible zeros.
+__device__ __forceinline__ float finish_row(float acc, float l) { return l == 0.f ? 0.f : acc / l; }
+
 // kTwo = false: the paper's arrangement, one tensor map over the layer's single virtual range.
 // kTwo = true: the alternative the paper rejected (two tensors, the kernel reads both): ids at or above
 // p.first_tensor_blocks address a second, separately allocated tensor through kvmap2.
@@ -268,18 +272,16 @@ decode_split_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_cons
             mstar = fmaxf(mstar, mw[w]);
         }
         float acc = 0.f, lsum = 0.f;
-        if (mstar > -INFINITY) {
 #pragma unroll
-            for (int w = 0; w < kDecodeWarps; ++w) {
-                const float *src = reinterpret_cast<const float *>(base_ptr + w * kDecodeStages * STAGE_BYTES);
-                const float wgt = (mw[w] > -INFINITY) ? fast_exp2(mw[w] - mstar) : 0.f;
-                acc += wgt * src[h * D + x];
-                lsum += wgt * src[8 * D + 8 + h];
-            }
+        for (int w = 0; w < kDecodeWarps; ++w) {  // (a warp without a maximum holds zeros, or NaN if its scores were NaN: either counts)
+            const float *src = reinterpret_cast<const float *>(base_ptr + w * kDecodeStages * STAGE_BYTES);
+            const float wgt = (mw[w] > -INFINITY) ? fast_exp2(mw[w] - mstar) : 0.f;
+            acc += wgt * src[h * D + x];
+            lsum += wgt * src[8 * D + 8 + h];
         }
         const size_t slot = ((size_t)b * p.num_q_heads + (size_t)g * p.group + h) * p.nsplit + split;
         if (p.nsplit == 1) {  // the only split of every sequence: finish here, no partials, no combine pass
-            p.out[slot * D + x] = __float2bfloat16_rn(lsum > 0.f ? acc / lsum : 0.f);
+            p.out[slot * D + x] = __float2bfloat16_rn(finish_row(acc, lsum));
         } else {
             p.part_o[slot * D + x] = acc;
             if (x == 0) p.part_ml[slot] = make_float2(mstar, lsum);
@@ -331,41 +333,39 @@ __global__ void __launch_bounds__(D) decode_combine_kernel(const DecodeParams p)
     for (int s = x; s < ns; s += D) mloc = fmaxf(mloc, ml[s].x);
     const float mstar = block_reduce<D, true>(mloc, scratch);
     float acc = 0.f, lloc = 0.f;
-    if (mstar > -INFINITY) {  // block-uniform
-        for (int s0 = 0; s0 < ns; s0 += D) {
-            const int s = s0 + x;
-            float w = 0.f;
-            if (s < ns) {
-                const float2 v = ml[s];
-                w = (v.x > -INFINITY) ? fast_exp2(v.x - mstar) : 0.f;
-                lloc += w * v.y;
-            }
-            __syncthreads();  // the previous tile's weights are no longer needed
-            w_tile[x] = w;
-            __syncthreads();
-            const int n = min(D, ns - s0);
-            const float *src = po + (size_t)s0 * D + x;
-            int i = 0;
-            for (; i + 16 <= n; i += 16) {  // sixteen loads in flight, added in the same order as one by one
-                float o[16];
-#pragma unroll
-                for (int u = 0; u < 16; ++u) o[u] = src[(size_t)(i + u) * D];
-#pragma unroll
-                for (int u = 0; u < 16; ++u) acc += w_tile[i + u] * o[u];
-            }
-            for (; i + 4 <= n; i += 4) {
-                const float o0 = src[(size_t)i * D], o1 = src[(size_t)(i + 1) * D];
-                const float o2 = src[(size_t)(i + 2) * D], o3 = src[(size_t)(i + 3) * D];
-                acc += w_tile[i] * o0;
-                acc += w_tile[i + 1] * o1;
-                acc += w_tile[i + 2] * o2;
-                acc += w_tile[i + 3] * o3;
-            }
-            for (; i < n; ++i) acc += w_tile[i] * src[(size_t)i * D];
+    for (int s0 = 0; s0 < ns; s0 += D) {
+        const int s = s0 + x;
+        float w = 0.f;
+        if (s < ns) {
+            const float2 v = ml[s];
+            w = (v.x > -INFINITY) ? fast_exp2(v.x - mstar) : 0.f;
+            lloc += w * v.y;
         }
+        __syncthreads();  // the previous tile's weights are no longer needed
+        w_tile[x] = w;
+        __syncthreads();
+        const int n = min(D, ns - s0);
+        const float *src = po + (size_t)s0 * D + x;
+        int i = 0;
+        for (; i + 16 <= n; i += 16) {  // sixteen loads in flight, added in the same order as one by one
+            float o[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) o[u] = src[(size_t)(i + u) * D];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) acc += w_tile[i + u] * o[u];
+        }
+        for (; i + 4 <= n; i += 4) {
+            const float o0 = src[(size_t)i * D], o1 = src[(size_t)(i + 1) * D];
+            const float o2 = src[(size_t)(i + 2) * D], o3 = src[(size_t)(i + 3) * D];
+            acc += w_tile[i] * o0;
+            acc += w_tile[i + 1] * o1;
+            acc += w_tile[i + 2] * o2;
+            acc += w_tile[i + 3] * o3;
+        }
+        for (; i < n; ++i) acc += w_tile[i] * src[(size_t)i * D];
     }
     const float lsum = block_reduce<D, false>(lloc, scratch);
-    p.out[(size_t)bh * D + x] = __float2bfloat16_rn(lsum > 0.f ? acc / lsum : 0.f);
+    p.out[(size_t)bh * D + x] = __float2bfloat16_rn(finish_row(acc, lsum));
 }
 
 static constexpr int kChunkMin = 256;  // 4 blocks per warp: below that the fixed cost of a CTA dominates

@@ -263,18 +263,16 @@ decode8_split_kernel(const __grid_constant__ CUtensorMap kvmap, const DecodePara
             mstar = fmaxf(mstar, mw[w]);
         }
         float acc = 0.f, lsum = 0.f;
-        if (mstar > -INFINITY) {
 #pragma unroll
-            for (int w = 0; w < kDecodeWarps; ++w) {
-                const float *src = reinterpret_cast<const float *>(base_ptr + w * STAGES * STAGE_BYTES);
-                const float wgt = (mw[w] > -INFINITY) ? fast_exp2(mw[w] - mstar) : 0.f;
-                acc += wgt * src[h * D + x];
-                lsum += wgt * src[8 * D + 8 + h];
-            }
+        for (int w = 0; w < kDecodeWarps; ++w) {  // (a warp without keys has kNoRef and zeros)
+            const float *src = reinterpret_cast<const float *>(base_ptr + w * STAGES * STAGE_BYTES);
+            const float wgt = fast_exp2(mw[w] - mstar);
+            acc += wgt * src[h * D + x];
+            lsum += wgt * src[8 * D + 8 + h];
         }
         const size_t slot = ((size_t)b * p.num_q_heads + (size_t)g * p.group + h) * p.nsplit + split;
         if (p.nsplit == 1) {  // the only split of every sequence: finish here, no partials, no combine pass
-            p.out[slot * D + x] = __float2bfloat16_rn(lsum > 0.f ? acc / lsum : 0.f);
+            p.out[slot * D + x] = __float2bfloat16_rn(finish_row(acc, lsum));
         } else {
             p.part_o[slot * D + x] = acc;
             if (x == 0) p.part_ml[slot] = make_float2(mstar, lsum);
