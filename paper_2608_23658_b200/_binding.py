@@ -159,6 +159,17 @@ def _check(st: int):
         raise EkvError(st, ekv_last_error())
 
 
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
 def _dptr(t):
     """Device (or host) address of a torch tensor / raw int / None."""
     if t is None:
@@ -251,28 +262,57 @@ def ekv_write_kv(pool: int, layer: int, k, v, slot_mapping, stream=None):
     _check(load_library().ekv_write_kv(pool, layer, _dptr(k), _dptr(v), _dptr(slot_mapping), T, _stream(stream)))
 
 
+def _refuse(call, name, t, want):
+    got = f"{t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous")
+    raise ValueError(f"{call}: {name} has to be {want}, not {got}")
+
+
 def ekv_read_kv(pool: int, layer: int, k_out, v_out, slot_mapping, stream=None):
-    """Values stored in the slots -> bf16 rows (the inverse of ekv_write_kv); rows of negative slots stay as they were."""
-    T = int(slot_mapping.shape[0])
-    _check(load_library().ekv_read_kv(pool, layer, _dptr(k_out), _dptr(v_out), _dptr(slot_mapping), T, _stream(stream)))
+    """Values stored in the slots -> bf16 rows (the inverse of ekv_write_kv); rows of negative slots stay as they were.
+    slot_mapping: int64 [T]; k_out, v_out: bf16, T rows of num_kv_heads * head_dim (Pool.read_kv checks these two; the binding
+    knows a pool by its handle alone), or plain addresses; all contiguous on one CUDA device."""
+    torch, dev, T = _torch(), slot_mapping.get_device(), slot_mapping.shape[0]
+    if slot_mapping.dtype is not torch.int64 or slot_mapping.dim() != 1 or dev < 0 or not slot_mapping.is_contiguous():
+        _refuse("ekv_read_kv", "slot_mapping", slot_mapping, "contiguous int64 [T] on a CUDA device")
+    at = []
+    for t in (k_out, v_out):
+        if isinstance(t, int):
+            at.append(t)
+        elif t.dtype is torch.bfloat16 and t.shape[0] == T and t.get_device() == dev and t.is_contiguous():
+            at.append(t.data_ptr())
+        else:
+            _refuse("ekv_read_kv", "k_out" if t is k_out else "v_out", t, f"contiguous bfloat16 with {T} rows, on the slot mapping's device")
+    _check(load_library().ekv_read_kv(pool, layer, at[0], at[1], slot_mapping.data_ptr(), T, _stream(stream)))
 
 
 def ekv_extend_tables(pool: int, new_tokens, seq_lens, block_tables, free_ids, free_cursor, slot_mapping, cu_q_lens,
                       seq_lens_out=None, free_cursor_out=None, stream=None):
     """Block tables, slot mapping, offsets and lengths of a step, on the GPU.  seq_lens and free_cursor are updated in
-    place unless seq_lens_out / free_cursor_out are given."""
+    place unless seq_lens_out / free_cursor_out are given.  int32 (slot_mapping: int64), contiguous, on one CUDA device."""
+    if block_tables.dim() != 2:
+        _refuse("ekv_extend_tables", "block_tables", block_tables, "int32 [R, max_blocks_per_seq]")
     R, max_blocks = block_tables.shape
     out = seq_lens if seq_lens_out is None else seq_lens_out
     cursor_out = free_cursor if free_cursor_out is None else free_cursor_out
-    assert new_tokens.numel() == seq_lens.numel() == out.numel() == R and cu_q_lens.numel() == R + 1
-    assert free_cursor.numel() == cursor_out.numel() == 1
-    assert new_tokens.itemsize == seq_lens.itemsize == block_tables.itemsize == free_ids.itemsize == free_cursor.itemsize == \
-        cu_q_lens.itemsize == out.itemsize == cursor_out.itemsize == 4, "lengths, tables, ids and offsets are int32"
-    assert slot_mapping.itemsize == 8, "the slot mapping is int64"
-    _check(load_library().ekv_extend_tables(pool, _dptr(new_tokens), _dptr(seq_lens), R, _dptr(block_tables), max_blocks,
-                                            _dptr(free_ids), free_ids.numel(), _dptr(free_cursor), _dptr(slot_mapping),
-                                            slot_mapping.numel(), _dptr(cu_q_lens), _dptr(out), _dptr(cursor_out),
-                                            _stream(stream)))
+    torch, dev, n_free, T_cap = _torch(), block_tables.get_device(), free_ids.numel(), slot_mapping.numel()
+    i32 = torch.int32
+    if not (new_tokens.dtype is seq_lens.dtype is block_tables.dtype is free_ids.dtype is free_cursor.dtype is cu_q_lens.dtype is i32
+            and out.dtype is cursor_out.dtype is i32 and slot_mapping.dtype is torch.int64
+            and new_tokens.numel() == seq_lens.numel() == out.numel() == R and cu_q_lens.numel() == R + 1
+            and free_cursor.numel() == cursor_out.numel() == 1
+            and new_tokens.get_device() == seq_lens.get_device() == free_ids.get_device() == free_cursor.get_device() == dev >= 0
+            and slot_mapping.get_device() == cu_q_lens.get_device() == out.get_device() == cursor_out.get_device() == dev
+            and new_tokens.is_contiguous() and seq_lens.is_contiguous() and block_tables.is_contiguous() and free_ids.is_contiguous()
+            and slot_mapping.is_contiguous() and cu_q_lens.is_contiguous() and out.is_contiguous()):
+        for name, t, n in (("new_tokens", new_tokens, R), ("seq_lens", seq_lens, R), ("block_tables", block_tables, R * max_blocks),
+                           ("free_ids", free_ids, n_free), ("free_cursor", free_cursor, 1), ("slot_mapping", slot_mapping, T_cap),
+                           ("cu_q_lens", cu_q_lens, R + 1), ("seq_lens_out", out, R), ("free_cursor_out", cursor_out, 1)):
+            dtype = torch.int64 if name == "slot_mapping" else i32
+            if t.dtype is not dtype or t.numel() != n or t.get_device() != dev or dev < 0 or not t.is_contiguous():
+                _refuse("ekv_extend_tables", name, t, f"contiguous {dtype} with {n} elements, on the tables' CUDA device")
+    _check(load_library().ekv_extend_tables(pool, new_tokens.data_ptr(), seq_lens.data_ptr(), R, block_tables.data_ptr(), max_blocks,
+                                            free_ids.data_ptr(), n_free, free_cursor.data_ptr(), slot_mapping.data_ptr(), T_cap,
+                                            cu_q_lens.data_ptr(), out.data_ptr(), cursor_out.data_ptr(), _stream(stream)))
 
 
 def ekv_attn_workspace_bytes(pool: int, max_batch: int, max_seq_len: int) -> int:

@@ -111,15 +111,28 @@ class Pool:
     def read_kv(self, layer, slot_mapping, k_out=None, v_out=None, stream=None):
         """Values stored in the slots as bf16 rows (k, v), each [T, Hkv, head_dim].  Rows of negative slots are left as they
         were: hand in tensors of your own if the mapping has any."""
+        self._on_device(slot_mapping)
+        shape = (slot_mapping.shape[0], self.num_kv_heads, self.head_dim)
+        k_at, v_at = k_out, v_out  # outputs made here need no checks
         if k_out is None:
-            k_out = torch.empty((slot_mapping.shape[0], self.num_kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            k_at = k_out.data_ptr()
         if v_out is None:
-            v_out = torch.empty_like(k_out)
-        B.ekv_read_kv(self.handle, layer, k_out, v_out, slot_mapping, stream)
+            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            v_at = v_out.data_ptr()
+        for t in (k_out, v_out):
+            if t.numel() != shape[0] * shape[1] * shape[2]:
+                raise ValueError(f"read_kv: k_out and v_out have to be {shape}, not {tuple(t.shape)}")
+        B.ekv_read_kv(self.handle, layer, k_at, v_at, slot_mapping, stream)
         return k_out, v_out
+
+    def _on_device(self, t):
+        if t.get_device() != self.device.index:
+            raise ValueError(f"a tensor on {t.device} for a pool on {self.device}")
 
     def extend_tables(self, new_tokens, seq_lens, block_tables, free_ids, free_cursor, slot_mapping, cu_q_lens,
                       seq_lens_out=None, free_cursor_out=None, stream=None):
+        self._on_device(block_tables)
         B.ekv_extend_tables(self.handle, new_tokens, seq_lens, block_tables, free_ids, free_cursor, slot_mapping, cu_q_lens,
                             seq_lens_out, free_cursor_out, stream)
 
