@@ -387,6 +387,9 @@ EKV_API ekv_status_t ekv_hoststep_flush(ekv_hoststep_t *step, void *stream);
  * over an EKV_BF16 pool holds one of 64 per-pool launch words (work counter of the persistent kernel), so more than
  * 64 calls of one such pool in flight at once are not supported (a captured call holds the same word in every replay).
  * Over an EKV_E4M3 pool calls share nothing, in any number, captured or not.
+ * A NaN in a row's query or in a key that it sees makes the row NaN; a NaN value makes its channel NaN in the rows that
+ * see it.  Over an EKV_E4M3 pool it reaches no other row.  Over an EKV_BF16 pool a value that is not finite may also reach
+ * earlier rows of the same chunk (their weight for it is 0, and 0 * NaN is NaN).
  */
 EKV_API ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, const void *q, void *out,
                                     const int32_t *block_tables, int32_t max_blocks_per_seq,

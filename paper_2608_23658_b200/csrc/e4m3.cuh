@@ -33,6 +33,14 @@ __device__ __forceinline__ uint32_t floats_to_e4m3x2(float lo, float hi) {
     return r;
 }
 
+// bit 7 of each byte that is a NaN code (magnitude 0x7f)
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// the same codes with 0 in place of NaN
+__device__ __forceinline__ uint32_t without_nan_codes(uint32_t w) { return w & ~((nan_codes(w) >> 7) * 0xffu); }
+__device__ __forceinline__ uint4 without_nan_codes(const uint4 &v) {
+    return make_uint4(without_nan_codes(v.x), without_nan_codes(v.y), without_nan_codes(v.z), without_nan_codes(v.w));
+}
+
 // 2^-e for a scale 2^e (a normal power of two): by its bits, no reciprocal
 __device__ __forceinline__ float pow2_inverse(float s) { return __uint_as_float((254u << 23) - (__float_as_uint(s) & 0x7f800000u)); }
 

@@ -34,6 +34,10 @@
 //                 refilled for the next tile as soon as it has been read; conversion, swizzled stores.  Keys past the item's
 //                 last visible one become zero rows of V, so nothing a slot that was never written holds can reach a sum
 //                 (0 * NaN), and no code is needed for that elsewhere.
+// NaN codes of V at keys that some rows of the item see and others do not (the tiles that the causal boundary cuts) must reach the
+// former and not the latter, whose weight of 0 does not stop them.  The converters look for them in those tiles alone (no time that
+// could be measured), put zeros in their place and leave word; the CTA then takes no further item, and gives the rows their NaN from the
+// codes themselves when all is written.
 // Softmax: online with lazy rescaling, as in the other tcgen05 kernels.  The sign of the scale is folded into Q.
 // The loops are kept rolled wherever that costs no registers: all roles of a quarter of the SM share an instruction cache
 // of about 32 KB (see ekv_prefill_tc.cuh), and with the converters' and the mask's loops unrolled (106 KB in all) every role ran at
@@ -94,7 +98,7 @@ struct Geo {
     static constexpr int kOffPartML = 2 * kBM * D * 4;         // ... and (m, l) of [2][128]
     static constexpr int kOffPartW = kOffPartML + 2 * kBM * 8;  // the CTA's own weights of its rows' partials: at most 512
     static_assert(kOffPartW + 512 * 4 <= kOffRaw, "merge area");
-    static constexpr int kOffItem = kOffQInv + 1024;           // two slots of the scheduler: state and seven numbers; then progress, response
+    static constexpr int kOffItem = kOffQInv + 1024;           // two slots of the scheduler: state and seven numbers; then progress, response, nan_seen
     static constexpr int kSmemBytes = kOffItem + 128 + 1024;    // + alignment slack
     static_assert(kOffFlags + 24 <= kOffKScale && kOffItem % 16 == 0 && kSmemBytes <= 232448, "shared memory");
     // kind::f16 instruction descriptors, D = f32, M = 128: QK with f16 operands, PV with bf16 ones and V MN-major
@@ -115,6 +119,7 @@ struct Smem {
     __device__ __forceinline__ float *k_scale(int tile) const { return (float *)(ptr + Geo<D>::kOffKScale) + 8 * (tile & 3); }
     __device__ __forceinline__ volatile int *progress() const { return (volatile int *)(ptr + Geo<D>::kOffItem + 64); }  // tile that the converters are at
     __device__ __forceinline__ uint4 *response() const { return (uint4 *)(ptr + Geo<D>::kOffItem + 80); }  // the launch's next CTA, if any
+    __device__ __forceinline__ volatile int *nan_seen(int n) const { return (volatile int *)(ptr + Geo<D>::kOffItem + 96) + (n & 1); }  // by item
     __device__ __forceinline__ int *item(int n) const { return (int *)(ptr + Geo<D>::kOffItem) + 8 * (n & 1); }
     __device__ __forceinline__ float *q_inv() const { return (float *)(ptr + Geo<D>::kOffQInv); }
 };
@@ -144,6 +149,35 @@ __device__ __forceinline__ bool find_item(const PrefillParams &p, int few_rows, 
     return false;
 }
 
+// A warp gives rows from, from + step, ... < to their NaN: channels of V that are NaN in a key from `key0` on up to the last one that the
+// row sees (keys before have had theirs from the sum).  row(r, lim, at): that key and where the row is in `out`.
+template <int D, typename Row>
+__device__ __forceinline__ void nan_values(const Params &pp, int g, const int *bt, int key0, int kv_end, int from, int to, int step, Row row) {
+    const int c0 = 4 * (threadIdx.x & 31), num_kv_heads = pp.p.num_kv_heads;  // four channels a lane
+    if (c0 >= D) return;
+    const long long live = *pp.p.live;
+    int first[4] = {kv_end, kv_end, kv_end, kv_end};  // the first key of which a channel is NaN
+#pragma unroll 1
+    for (int t = key0; t < kv_end; ++t) {
+        const int id = bt[t >> 4];
+        if (id < 0 || (long long)id >= live || !(pp.scales[((long long)id * 2 + 1) * num_kv_heads + g] > 0.f)) continue;
+        const uint32_t nan = nan_codes(*reinterpret_cast<const uint32_t *>(
+            pp.cache + (long long)id * pp.block_stride + (long long)(num_kv_heads + g) * (16 * D) + (t & 15) * D + c0));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if ((nan >> (8 * i)) & 0x80u) first[i] = min(first[i], t);
+    }
+#pragma unroll 1
+    for (int r = from; r < to; r += step) {
+        int lim;
+        __nv_bfloat16 *at;
+        row(r, lim, at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (first[i] <= lim && first[i] < kv_end) at[c0 + i] = __ushort_as_bfloat16(0x7fff);
+    }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_constant__ Params pp) {
     using G = Geo<D>;
@@ -166,6 +200,7 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
         for (int i = 0; i < G::NBAR; ++i) mbar_init(sh.bar(i), G::arrivals(i));
         mbar_fence_init();
         *sh.abort_flag() = 0;
+        *sh.nan_seen(0) = *sh.nan_seen(1) = 0;
     }
     if (warp == 1) {
         cp::tcgen05_alloc(cp::cta_group_1, sh.tmem_slot(), 512);
@@ -202,7 +237,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     auto post = [&](int item, int n) {
         int *slot = sh.item(n);
         for (;; item = -1) {
-            if (item < 0) item = draw();
+            // (the last item for a CTA that has NaN values to give: the slots keep the numbers of two items)
+            if (item < 0) item = __any_sync(0xffffffffu, *sh.nan_seen(0) | *sh.nan_seen(1)) ? -1 : draw();
             const bool over = item < 0;
             const int rank = item / p.num_kv_heads, g = item - rank * p.num_kv_heads, idx = p.q_tiles - 1 - rank;
             int req = 0, first = 0, c_r = 0, q0 = 0;
@@ -219,7 +255,8 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
                 }
                 continue;
             }
-            if (lane == 0) slot[0] = over ? 0 : 1, slot[1] = req, slot[2] = g, slot[3] = row0, slot[4] = rows_here, slot[5] = q0, slot[6] = L, slot[7] = L - c_r;
+            if (lane == 0) slot[0] = over ? 0 : 1;  // (the numbers of the item there before may still be needed)
+            if (lane == 0 && !over) slot[1] = req, slot[2] = g, slot[3] = row0, slot[4] = rows_here, slot[5] = q0, slot[6] = L, slot[7] = L - c_r;
             break;
         }
         __syncwarp();
@@ -543,6 +580,29 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
             publish(G::K_FULL + s);
             // ---- V
             cp_async_wait_1();
+            if ((tile0 + j + 1) * kBN > prefix + pos0 + 1) {  // not every row sees all of the tile: no NaN codes into it
+#pragma unroll 1
+                for (int it = 0; it < kIts; it += 4) {
+                    const uint32_t at = raw + G::kRawBytes + it * 2048;
+                    uint4 v[4];
+                    uint32_t any = 0;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[u] = lds_16(at + u * 2048);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) any |= nan_codes(v[u].x) | nan_codes(v[u].y) | nan_codes(v[u].z) | nan_codes(v[u].w);
+                    if (any) {
+#pragma unroll 1
+                        for (int u = 0; u < 4; ++u) {
+                            const uint4 w = lds_16(at + u * 2048), clean = without_nan_codes(w);
+                            sts_16(at + u * 2048, clean);
+                            // (those past the last visible key, slots not written yet, are nobody's)
+                            if ((w.x != clean.x || w.y != clean.y || w.z != clean.z || w.w != clean.w) &&
+                                (tile0 + j) * kBN + ((it + u) * kBlocksPerIt + first_block) * 16 + rowb < kv_end)
+                                *sh.nan_seen(n) = 1;
+                        }
+                    }
+                }
+            }
             ok = j < kStages || wait(G::V_EMPTY + s, ph);
             if (!ok) break;
             if (some_zero) {
@@ -898,6 +958,22 @@ __global__ void __launch_bounds__(kThreads, 1) prefill8_kernel(const __grid_cons
     fence_after();
     if (threadIdx.x == 0 && *sh.abort_flag()) atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);  // a wait ran out
     if (warp == 1) cp::tcgen05_dealloc(cp::cta_group_1, tmem, 512);
+
+    // ---- NaN values: of the last item or the one before it, whose rows have been written and whose numbers are still in their slots.  (By
+    // warps that have the registers; behind everything else, since in any other place this code cost calls without NaN up to 4 %.)
+    if (warp < 4 || warp >= 12 || *sh.abort_flag()) return;
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {
+        if (!*sh.nan_seen(k)) continue;
+        const volatile int *slot = sh.item(k);
+        const int kv_head = slot[2], from = slot[3], q_first = slot[5], before = slot[7];
+        nan_values<D>(pp, kv_head, p.block_tables + (size_t)slot[1] * p.max_blocks, (before + by_group(from) + 1) / kBN * kBN,
+                      min(slot[6], before + by_group(from + slot[4] - 1) + 1), warp - 4, slot[4], 8, [&](int r, int &last, __nv_bfloat16 *&at) {
+                          const int pos = by_group(from + r);
+                          last = before + pos;
+                          at = p.out + ((size_t)(q_first + pos) * p.num_q_heads + (size_t)(kv_head * group + from + r - pos * group)) * D;
+                      });
+    }
 }
 
 // fit[i] = clusters of 2^i CTAs of the kernel that run at the same time on the current device (0: none do)

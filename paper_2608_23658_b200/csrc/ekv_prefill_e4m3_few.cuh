@@ -16,6 +16,11 @@
 // four warps a ring, each converting what it reads: half the rate again, and slower than the 615.
 // Rows differ in the last key they see, so a block can be hidden from a row altogether: its references may stay at the value that
 // stands for none.
+// NaN codes of V at keys that some rows see and others do not must reach the former and not the latter, whose weight of 0 does not
+// stop them.  Those keys lie in the last three blocks at most; their codes come into shared memory beside the loop and are looked at behind
+// it.  If there are any, the item is done again by a second instantiation, which takes NaN codes out of its tiles, and its rows get
+// their NaN after the write-out (tc8::nan_values).  (The same in the one loop, however it was put, cost calls without NaN 2 to 7 %: the loop
+// has no register left.)
 #pragma once
 #include "ekv_prefill_e4m3.cuh"
 
@@ -34,14 +39,17 @@ struct Geo {
     static constexpr int kStages = D == 128 ? 2 : 4;                  // of a ring of one warp; one of two warps has twice as many
     static constexpr int kOffBar = kWarps * kStages * kStageBytes;    // in front: the rings, later O of each ring's rows
     static constexpr int kOffML = kOffBar + 8 * kWarps * kStages;     // (m, l) of each ring's rows (8 x 16 or 4 x 32), then of the CTA's
-    static constexpr int kSmemBytes = kOffML + (kWarps * 16 + kMaxRows) * 8 + 1024;
+    static constexpr int kCutBlocks = 3;                              // blocks that some rows see and others do not: of at most 31 keys
+    static constexpr int kOffCut = kOffML + (kWarps * 16 + kMaxRows) * 8;
+    static constexpr int kOffBarAgain = kOffCut + kCutBlocks * kTileBytes;
+    static constexpr int kSmemBytes = kOffBarAgain + 8 * kWarps * kStages + 1024;
     static_assert(kWarps * 16 * D * 4 <= kOffBar, "merge area");
     static_assert(2 * (kSmemBytes + 1024) <= 233472, "two CTAs an SM");
 };
 
-// kTwo: 1 for rings of two warps
-template <int D, int kTwo>
-__device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::Params &pp) {
+// kTwo: 1 for rings of two warps.  kClean: the item's second time, with NaN codes taken out.  Returns whether there has to be one.
+template <int D, int kTwo, bool kClean>
+__device__ __forceinline__ bool few8_item(const CUtensorMap &kvmap, const tc8::Params &pp) {
     using G = Geo<D>;
     const PrefillParams &p = pp.p;
     constexpr int KSTEPS = D / 16;
@@ -65,7 +73,7 @@ __device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::P
         if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
         for (int e = threadIdx.x; e < rows * (D / 8) && part == 0; e += kThreads)
             *reinterpret_cast<uint4 *>(p.out + row_offset(e / (D / 8)) + (e % (D / 8)) * 8) = make_uint4(0u, 0u, 0u, 0u);
-        return;
+        return false;
     }
     const int all_blocks = (L + 15) >> 4;
     const int blk0 = (int)((long long)all_blocks * part >> pp.cluster_log), blk1 = (int)((long long)all_blocks * (part + 1) >> pp.cluster_log);
@@ -77,7 +85,7 @@ __device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::P
     const uint32_t base = (raw_u32 + 1023u) & ~1023u;
     uint8_t *ptr = smem_raw + (base - raw_u32);
     const uint32_t my_stages = base + ring * stages * G::kStageBytes;
-    const uint32_t my_bars = base + G::kOffBar + ring * stages * 8;
+    const uint32_t my_bars = base + (kClean ? G::kOffBarAgain : G::kOffBar) + ring * stages * 8;
     const bool leads = tile == 0;  // ... the ring's other warps and issues its copies
     auto ring_sync = [&]() {
         if (kTwo) asm volatile("bar.sync %0, 64;" ::"r"(1 + ring) : "memory");
@@ -125,6 +133,15 @@ __device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::P
         }
     };
     for (int s = 0; s < stages && s < nw; ++s) issue(s, 0);
+    const int cut = (prefix + 1) >> 4;  // the first block that not every row sees all of
+    const bool looks = !kClean && warp < G::kCutBlocks && 16 * (cut + warp) < L && c_r > 1;
+    const int cut_id = looks ? p.block_tables[(size_t)req * p.max_blocks + cut + warp] : -1;
+    if (looks) {  // (invalid: zeros)
+        const bool valid = cut_id >= 0 && (long long)cut_id < live;
+        const uint8_t *codes = pp.cache + (long long)(valid ? cut_id : 0) * pp.block_stride + (long long)(p.num_kv_heads + g) * G::kTileBytes;
+#pragma unroll 1
+        for (int at = lane * 16; at < G::kTileBytes; at += 512) cp_async_16(base + G::kOffCut + warp * G::kTileBytes + at, codes + at, valid ? 16u : 0u);
+    }
 
     // Q fragments: rows r and r + 8 of the warp's tile, f16 with the row's largest magnitude in [2^13, 2^14)
     uint32_t qa[KSTEPS][4];
@@ -186,6 +203,15 @@ __device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::P
             const bool got = mbar_wait(my_bars + 8 * stage, (stage_parity >> stage) & 1u, failed ? 1000000ull : 2000000000ull);
             stage_parity ^= 1u << stage;
             if (__any_sync(FULL, !got)) failed = true;  // goes on in step with the ring's other warps, but computes no more
+            if (kClean && tok0 + 15 > prefix) {  // (a ring's two warps both do this, each before it reads: what they write is the same)
+#pragma unroll 1
+                for (int at = lane * 16; at < G::kTileBytes; at += 512) {
+                    const uint32_t to = my_stages + stage * G::kStageBytes + G::kTileBytes + at;
+                    sts_16(to, without_nan_codes(lds_16(to)));
+                }
+                fence_proxy_async_smem();  // before the stage's next copy
+                __syncwarp();
+            }
         }
         if (busy && !failed && __shfl_sync(FULL, id_a, i - i0) >= 0) {
             const uint32_t kbase = my_stages + stage * G::kStageBytes + lane_at, vbase = kbase + G::kTileBytes;
@@ -284,7 +310,21 @@ __device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::P
     // ---- rings: (m, l, O) of each into shared memory (over the stages, once all are through), then one set for the CTA
     float2 *ml = reinterpret_cast<float2 *>(ptr + G::kOffML);  // [ring][row], then [row] of the CTA
     float *ow = reinterpret_cast<float *>(ptr);                // [ring][row][D]
-    __syncthreads();
+    if (kClean) {
+        __syncthreads();
+    } else {  // all CTAs of a cluster look at the same codes, so they go on the same way
+        cp_async_wait_all();
+        __syncthreads();
+        uint32_t nan = 0;
+#pragma unroll 1
+        for (int at = threadIdx.x * 16; at < G::kCutBlocks * G::kTileBytes; at += kThreads * 16) {
+            const int t = 16 * cut + at / D;
+            if (t <= prefix || t >= L) continue;
+            const uint4 v = lds_16(base + G::kOffCut + at);
+            nan |= nan_codes(v.x) | nan_codes(v.y) | nan_codes(v.z) | nan_codes(v.w);
+        }
+        if (__syncthreads_or((int)(nan != 0u))) return true;
+    }
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
         float l = ref[n].l;
@@ -323,11 +363,9 @@ __device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::P
             if (x == 0) ml[rings * ring_rows + row] = make_float2(m, l);
         }
     }
-    if (cluster == 1) return;
-
     // ---- CTAs: each merges a share of the elements out of the shared memories of all of the cluster
-    cluster_barrier();
-    for (int e = part * kThreads + threadIdx.x; e < rows * kQuads; e += cluster * kThreads) {
+    if (cluster > 1) cluster_barrier();
+    for (int e = part * kThreads + threadIdx.x; e < rows * kQuads && cluster > 1; e += cluster * kThreads) {
         const int row = e / kQuads, x = e % kQuads;
         const uint32_t ml_at = base + G::kOffML + (rings * ring_rows + row) * 8, o_at = base + (row * kQuads + x) * 16;
         float m = kNoRef, l = 0.f;
@@ -344,7 +382,15 @@ __device__ __forceinline__ void few8_item(const CUtensorMap &kvmap, const tc8::P
         const float inv = l > 0.f ? 1.f / l : 0.f;
         *reinterpret_cast<uint2 *>(p.out + row_offset(row) + 4 * x) = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     }
-    cluster_barrier();  // nobody leaves while another may read its shared memory
+    if (cluster > 1) cluster_barrier();  // nobody leaves while another may read its shared memory
+    if (kClean) {
+        if (cluster == 1) __syncthreads();
+        tc8::nan_values<D>(pp, g, p.block_tables + (size_t)req * p.max_blocks, 16 * cut, L, warp, part == 0 ? rows : 0, kWarps, [&](int i, int &last, __nv_bfloat16 *&at) {
+            last = prefix + i / group;
+            at = p.out + row_offset(i);
+        });
+    }
+    return false;
 }
 
 template <int D>
@@ -353,8 +399,7 @@ __global__ void __launch_bounds__(kThreads, 2) few8_kernel(const __grid_constant
     const long long rows = (long long)(pp.p.cu_q_lens[req + 1] - pp.p.cu_q_lens[req]) * pp.p.group;
     // Every reason to leave, here and in few8_item, is the same for all CTAs of a cluster.
     if (rows <= 0 || rows > kMaxRows) {}  // not one of this kernel's requests
-    else if (rows > 16) few8_item<D, 1>(kvmap, pp);
-    else few8_item<D, 0>(kvmap, pp);
+    else if (rows > 16 ? few8_item<D, 1, false>(kvmap, pp) : few8_item<D, 0, false>(kvmap, pp)) (void)few8_item<D, 1, true>(kvmap, pp);
     // Beside the other kernel of the call, which it shares nothing with, but not through before it: what follows on the stream
     // waits for this launch alone.
     if (blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");

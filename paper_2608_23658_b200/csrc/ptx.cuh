@@ -152,6 +152,9 @@ __device__ __forceinline__ uint4 lds_16(uint32_t addr) {
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ void sts_16(uint32_t addr, const uint4 &v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 
 // ---- clusters: another CTA's shared memory, and the barrier of all threads of the cluster ------------------
 __device__ __forceinline__ uint32_t map_to_cta(uint32_t addr, int rank) {
