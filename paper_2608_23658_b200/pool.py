@@ -111,20 +111,24 @@ class Pool:
     def read_kv(self, layer, slot_mapping, k_out=None, v_out=None, stream=None):
         """Values stored in the slots as bf16 rows (k, v), each [T, Hkv, head_dim].  Rows of negative slots are left as they
         were: hand in tensors of your own if the mapping has any."""
-        self._on_device(slot_mapping)
-        shape = (slot_mapping.shape[0], self.num_kv_heads, self.head_dim)
-        k_at, v_at = k_out, v_out  # outputs made here need no checks
+        T, = slot_mapping.shape
+        if slot_mapping.dtype is not torch.int64 or slot_mapping.get_device() != self.device.index or not slot_mapping.is_contiguous():
+            B._refuse("read_kv", "slot_mapping", slot_mapping, f"contiguous int64 on {self.device}")
+        shape = (T, self.num_kv_heads, self.head_dim)
         if k_out is None:
             k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-            k_at = k_out.data_ptr()
+        else:
+            self._check_rows("k_out", k_out, shape)
         if v_out is None:
             v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-            v_at = v_out.data_ptr()
-        for t in (k_out, v_out):
-            if t.numel() != shape[0] * shape[1] * shape[2]:
-                raise ValueError(f"read_kv: k_out and v_out have to be {shape}, not {tuple(t.shape)}")
-        B.ekv_read_kv(self.handle, layer, k_at, v_at, slot_mapping, stream)
+        else:
+            self._check_rows("v_out", v_out, shape)
+        B._check(B.load_library().ekv_read_kv(self.handle, layer, k_out.data_ptr(), v_out.data_ptr(), slot_mapping.data_ptr(), T, B._stream(stream)))
         return k_out, v_out
+
+    def _check_rows(self, name, t, shape):
+        if t.dtype is not torch.bfloat16 or t.shape[:1] != shape[:1] or t.numel() != shape[0] * shape[1] * shape[2] or t.get_device() != self.device.index or not t.is_contiguous():
+            B._refuse("read_kv", name, t, f"contiguous bfloat16 {shape} on {self.device}")
 
     def _on_device(self, t):
         if t.get_device() != self.device.index:
