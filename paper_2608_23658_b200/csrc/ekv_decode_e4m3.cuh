@@ -22,7 +22,8 @@ namespace ekv {
 
 // Four CTAs share an SM, with rings of 4 to 8 KiB a warp (64 to 128 KiB in flight per SM).  The bf16 kernel's two CTAs with
 // rings three times as deep leave this kernel at 0.87 of the copy rate: converting makes a block's chain of instructions long,
-// and it takes three or four warps a scheduler to hide it.  Measured, us: 256 sequences of 2048..8192 keys, 32q/8kv, d128 (2.68 GB; at
+// and it takes three or four warps a scheduler to hide it.  Measured on one machine and one set of inputs (others: 404 to 449 for
+// the 399), us: 256 sequences of 2048..8192 keys, 32q/8kv, d128 (2.68 GB; at
 // the copy rate 411) 2 CTAs x 6 stages 458, 3 x 4 399, 4 x 3 400, 4 x 2 399 = 6.7 TB/s, 5 x 2 416 (registers are spilled from 5 on);
 // 64 sequences of 8000..30000, 16q/2kv, d64 (0.33 GB) 101, 83, 92, 77, 83.
 static constexpr int kDecode8Ctas = 4;

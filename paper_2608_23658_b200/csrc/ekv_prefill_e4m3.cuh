@@ -18,8 +18,8 @@
 //     a multiplication by the softmax scale stands anyway.  Q becomes f16 with each row brought to a maximum in
 //     [2^13, 2^14) by a power of two, as in decode (what f16 then drops lies 2^-37 below the row's largest element).
 //   - V goes to bf16 with its scale multiplied in (exact, a power of two), since only bf16 has the scales' range; P is bf16.
-// Measured, 32q/8kv, d128: 2048 positions over 14001 keys 469 us = 1075 TFLOP/s, 0.67 of cuBLAS' burst; a prompt of 8192 493 us =
-// 1114; 64 prompts of 512 303 us, 256 of 128 218 us.  What bounds it: a key tile's chain through one head's scores, softmax and P V (3500
+// Measured, 32q/8kv, d128: 2048 positions over 14001 keys 480 to 523 us by how far the part is at its power cap, 965 to 1050 TFLOP/s,
+// 0.60 to 0.65 of cuBLAS' burst (469 at best); a prompt of 8192 484 to 493 us, 1114 to 1136; 64 prompts of 512 304 us, 256 of 128 220 us.  What bounds it: a key tile's chain through one head's scores, softmax and P V (3500
 // cycles a pair of tiles, as in the other tcgen05 kernels) plus a tenth for the conversion; 256 items on 148 SMs are two rounds for
 // 1.73; and an item costs some 9000 cycles besides its tiles, which is most of a short prompt: Q on its way and to f16, the first scores,
 // the write-out (whose rows go through the idle Q tile: straight from the registers, a thread a row, they took 224 us for 218).
@@ -132,7 +132,8 @@ __device__ __forceinline__ bool wait_warp(const Smem<D> &sh, int bar, uint32_t p
     return __all_sync(0xffffffffu, mbar_wait_polls(sh.bar(bar), parity, sh.base + Geo<D>::kOffFlags, tc::kPollLimit));
 }
 
-// Which request owns item `idx` (items of kItemRows (position, head) rows, requests in order)?
+// Which request owns item `idx` (items of kItemRows (position, head) rows, requests in order)?  Beyond the offsets that the launch carries, a
+// walk from the first request on, in every item: 257 prompts of 128 take 514 us for the 219 of 256, 1024 take 6.5 ms.
 __device__ __forceinline__ bool find_item(const PrefillParams &p, int few_rows, int idx, int &req, int &first, int &q0, int &c_r) {
     if (p.n_prefix) return find_request(p, idx, kItemRows, req, first, q0, c_r);
     int acc = 0;

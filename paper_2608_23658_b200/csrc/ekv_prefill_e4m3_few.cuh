@@ -393,6 +393,8 @@ __device__ __forceinline__ bool few8_item(const CUtensorMap &kvmap, const tc8::P
     return false;
 }
 
+// Two CTAs an SM leave 128 registers a thread, and at head_dim 128 that is not enough: 420 bytes are spilled by the three instantiations of
+// the item together (one CTA an SM would not spill, with half the warps to hide a block's chain).
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2) few8_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ tc8::Params pp) {
     const int req = blockIdx.x / pp.cluster / pp.p.num_kv_heads;

@@ -12,9 +12,12 @@
 //                      (atomic maxima: no order matters), the second takes 16 tokens a CTA, does the blocks that begin
 //                      there and puts their words back to zero
 // Measured, 8 kv-heads of 128, write and read_kv together, us: 1024 tokens in a row 11.6 by the first form and 13.0 by the second, one
-// token a block 23 and 43; 2048 in a row 16.6 and 14.1, one token a block 46 and 58.  So the second form is for long prompts.
-// Bound by memory: 4 bytes in and 2 out a channel pair of K and V, scales and mapping beside it.  16384 tokens (101 MB) take 28.3 us =
-// 3.6 TB/s, 4.7 of it the claims; 256 tokens 5.8 us, a launch and four loads that wait for one another (slot, mapping, row and
+// token a block 23 and 43; 2048 in a row 16.6 and 14.1, one token a block 46 and 58.  So the second form is for long prompts.  Its tasks each
+// look through the mapping from their block's first token to its last: nothing for runs, T squared for blocks whose tokens are spread
+// over the call (16384 shuffled tokens, 8 kv-heads of 128: 0.97 ms for 31 us with the call's launches).
+// 16384 tokens (101 MB: 4 bytes in and 2 out a channel pair of K and V, scales and mapping beside it) take 28.3 us = 3.6 TB/s, 4.7 of it the
+// claims.  Not bound by memory (device memory is 29 % busy): a warp's chain of mapping, claim, row, maximum and store, gone through
+// once, with half the issue slots taken.  256 tokens 5.8 us, a launch and four loads that wait for one another (slot, mapping, row and
 // scale, then the rounding).
 #pragma once
 #include "e4m3.cuh"

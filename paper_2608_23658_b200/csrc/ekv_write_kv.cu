@@ -68,8 +68,8 @@ __global__ void __launch_bounds__(kWriteThreads) write_kv_kernel(uint4 *__restri
 }
 
 // ekv_read_kv: a thread takes kReadUnroll pieces of 16 channels of one row each -- 32 bytes of bf16, or 16 codes and their scale --
-// and has the loads of all of them on their way before it stores.  Bound by memory; a code times a power of two needs 4 significant
-// bits, so the bf16 is exact.  Outputs on 32-byte boundaries are stored 32 bytes at a time (kWhole).  Measured, 8 kv-heads of 128:
+// and has the loads of all of them on their way before it stores.  A code times a power of two needs 4 significant bits, so the bf16 is
+// exact.  Bound by the chain of mapping, codes and scale, gone through once a thread (device memory is 25 % busy on an 8-bit pool).  Outputs on 32-byte boundaries are stored 32 bytes at a time (kWhole).  Measured, 8 kv-heads of 128:
 // 16384 tokens from an 8-bit pool (101 MB) 22.3 us = 4.5 TB/s, with two stores of 16 bytes 24.2; 2048 tokens 3.9 and 5.3; from a
 // bf16 pool (134 MB) 24.0 = 5.6 TB/s and 26.1.
 static constexpr int kReadUnroll = 4;
