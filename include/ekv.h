@@ -226,6 +226,43 @@ EKV_API ekv_status_t ekv_write_kv(ekv_pool_t *pool, int32_t layer, const void *k
                           const int64_t *slot_mapping, int32_t T, void *stream);
 
 /*
+ * ekv_rope_write_kv -- what a model does to a projection's rows before attention, and the KV write, in one pass: queries
+ * and keys are normed by head and turned by their positions, the queries go to q_out, keys and values into the cache.  With
+ * D = head_dim, for each row x of D channels of a query or key head:
+ *   if the row's weight w is given:  x <- x / sqrt(mean(x^2) + eps) * (weight_offset + w);
+ *   for every pair i < rotary_dim/2 of channels (a, b) -- channels (i, i + rotary_dim/2), or (2i, 2i + 1) with EKV_ROPE_ADJACENT --
+ *     t = positions[pair_axis[i]][token] * inv_freq[i],  (a, b) <- factor * (a cos t - b sin t, b cos t + a sin t);
+ *   channels from rotary_dim on are not turned.  fp32, the angle in 64 bits; rounded to bf16 (nearest even) once.  The sum of
+ *   squares is taken in fp32: a row of elements of some 10^18 and more overflows it.
+ * Values go to the cache as they are.  EKV_E4M3 pools: the finished keys go to k_out first, as bf16, and what ekv_write_kv does with
+ * k_out and v follows (two or three launches).
+ * rope: HOST; its pointers are marked there.  q: DEVICE bf16, token t's heads at q + t*q_stride elements, [num_q_heads, D] contiguous;
+ * k, v: the same with [num_kv_heads, D] -- so the three may be parts of one fused projection's rows.  q_out: likewise, and may be q
+ * itself with the same stride.  Addresses on 16-byte boundaries, strides multiples of 8.
+ * k_out: EKV_E4M3 pools: DEVICE bf16 [T, num_kv_heads, D] contiguous; NULL on others.
+ * slot_mapping: DEVICE int64 [T], as ekv_write_kv takes it: a negative slot writes nothing to the cache, a slot outside the live
+ * range neither and latches EKV_ERR_BLOCK_OOB; the queries of such tokens are written all the same.
+ * Duplicate slots: as in ekv_write_kv.  T == 0 is a no-op.
+ */
+enum { EKV_ROPE_ADJACENT = 1u << 0 };
+typedef struct ekv_rope {
+    int32_t rotary_dim;       /* even, 0 (no rotation) .. head_dim */
+    int32_t num_axes;         /* 1 .. 4 axes of positions (time, height, width, ..) */
+    uint32_t flags;           /* EKV_ROPE_ADJACENT or 0 */
+    float factor;             /* 1 but for models that scale their sines and cosines */
+    float eps;                /* >= 0 */
+    float weight_offset;      /* 0, or 1 where a model stores its weights around 0 */
+    const float *inv_freq;    /* DEVICE [rotary_dim/2] */
+    const int32_t *positions; /* DEVICE [num_axes, T] */
+    const uint8_t *pair_axis; /* HOST [rotary_dim/2], the axis of each pair; NULL if num_axes is 1 */
+    const void *q_weight;     /* DEVICE bf16 [head_dim], or NULL: queries are not normed */
+    const void *k_weight;     /* DEVICE bf16 [head_dim], or NULL: keys are not normed */
+} ekv_rope_t;
+EKV_API ekv_status_t ekv_rope_write_kv(ekv_pool_t *pool, int32_t layer, const ekv_rope_t *rope, const void *q, int64_t q_stride,
+                               const void *k, int64_t k_stride, const void *v, int64_t v_stride, void *q_out, int64_t q_out_stride,
+                               void *k_out, const int64_t *slot_mapping, int32_t T, void *stream);
+
+/*
  * ekv_read_kv -- the inverse of ekv_write_kv: row i of k_out and v_out receives the values stored in slot
  * slot_mapping[i] of `layer` as bf16 (a bf16 pool's bit patterns; an EKV_E4M3 pool's code * scale, which bf16 holds
  * exactly), for a host that exports, moves or inspects a request's keys and values.

@@ -17,6 +17,7 @@ EKV_FUSED_RANGE = 4
 EKV_PREFILL_WARP_MMA = 8
 EKV_PREFILL_ONE_HEAD = 16
 EKV_PREFILL_TWO_HEAD = 32
+EKV_ROPE_ADJACENT = 1
 
 
 class Status(enum.IntEnum):
@@ -41,6 +42,12 @@ class PoolDesc(ctypes.Structure):
                 ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block_size", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("base_blocks", ctypes.c_int64),
                 ("elastic_blocks", ctypes.c_int64)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("flags", ctypes.c_uint32), ("factor", ctypes.c_float),
+                ("eps", ctypes.c_float), ("weight_offset", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("pair_axis", ctypes.c_char_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
 
 
 class BlockPoolStats(ctypes.Structure):
@@ -115,6 +122,7 @@ def load_library():
         "ekv_grow": (i32, [vp, vp, u32, dblp]),
         "ekv_shrink": (i32, [vp, vp, u32, dblp]),
         "ekv_write_kv": (i32, [vp, i32, vp, vp, vp, i32, vp]),
+        "ekv_rope_write_kv": (i32, [vp, i32, ctypes.POINTER(Rope), vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i32, vp]),
         "ekv_read_kv": (i32, [vp, i32, vp, vp, vp, i32, vp]),
         "ekv_extend_tables": (i32, [vp, vp, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, vp]),
         "ekv_attn_workspace_bytes": (sz, [vp, i32, i32]),
@@ -260,6 +268,14 @@ def ekv_shrink(pool: int, stream=None, flags: int = 0, host_only: bool = False):
 def ekv_write_kv(pool: int, layer: int, k, v, slot_mapping, stream=None):
     T = int(slot_mapping.shape[0])
     _check(load_library().ekv_write_kv(pool, layer, _dptr(k), _dptr(v), _dptr(slot_mapping), T, _stream(stream)))
+
+
+def ekv_rope_write_kv(pool: int, layer: int, rope: Rope, q: int, q_stride: int, k: int, k_stride: int, v: int, v_stride: int,
+                      q_out: int, q_out_stride: int, k_out: int | None, slot_mapping: int, T: int, stream=None):
+    """Norm, rotation and KV write of T tokens' rows.  Plain addresses and strides in elements: Pool.rope_write_kv takes tensors
+    and checks them."""
+    _check(load_library().ekv_rope_write_kv(pool, layer, ctypes.byref(rope), q, q_stride, k, k_stride, v, v_stride, q_out, q_out_stride,
+                                            k_out, slot_mapping, T, _stream(stream)))
 
 
 def _refuse(call, name, t, want):

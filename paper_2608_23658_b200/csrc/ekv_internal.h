@@ -79,6 +79,10 @@ DecodePlan plan_decode(const ekv_pool *pool, int B, int max_blocks_per_seq);
 
 ekv_status_t launch_set_live(ekv_pool *pool, long long value, cudaStream_t stream);
 
+// The quantising write of an EKV_E4M3 pool (ekv_write_kv) from rows k_stride / v_stride elements apart.
+ekv_status_t write_kv8(ekv_pool *pool, int layer, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int64_t *slot_mapping,
+                       int T, cudaStream_t stream);
+
 // Tensor map over a KV tensor of `blocks` blocks that are `block_stride` bytes apart, each laid out
 // (K|V, kv-head, token, channel): dims (channel, row in block, block), box 64 x block_size x 1, 128-byte swizzle.
 ekv_status_t encode_kv_map(void *base, uint64_t blocks, uint64_t block_stride, int num_kv_heads, int head_dim, int block_size,

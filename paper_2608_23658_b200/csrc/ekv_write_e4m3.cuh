@@ -40,6 +40,7 @@ struct Write8Params {
     const long long *live;
     unsigned *status;
     long long block_stride;
+    long long k_row, v_row;  // 16-byte pieces between a token's row and the next one's
     int T, num_kv_heads;
 };
 
@@ -51,7 +52,7 @@ __device__ __forceinline__ void write8_task(const Write8Params &p, long long n, 
     constexpr int kIts = 16 / kRows;
     const int sub = lane / kLanesPerRow, piece = lane % kLanesPerRow;
     const uint4 *src = (kv ? p.v : p.k) + (long long)h * kLanesPerRow + piece;
-    const long long row_pieces = (long long)p.num_kv_heads * kLanesPerRow;
+    const long long row_pieces = kv ? p.v_row : p.k_row;
     float *scale_at = p.scales + (n * 2 + kv) * p.num_kv_heads + h;
     const float old = tok[0] ? 0.f : *scale_at;
     uint4 x[kIts];

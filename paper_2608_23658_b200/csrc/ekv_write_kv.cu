@@ -141,6 +141,25 @@ __global__ void __launch_bounds__(256) read_kv_kernel(const uint8_t *__restrict_
     }
 }
 
+ekv_status_t write_kv8(ekv_pool *pool, int layer, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int64_t *slot_mapping,
+                       int T, cudaStream_t stream) {
+    Write8Params p;
+    p.cache = (uint8_t *)pool->layer_base(layer);
+    p.scales = pool->layer_scales(layer);
+    p.claims = pool->d_claims + (size_t)layer * pool->total_blocks();
+    p.k = (const uint4 *)k;
+    p.v = (const uint4 *)v;
+    p.k_row = k_stride / 8;
+    p.v_row = v_stride / 8;
+    p.slots = (const long long *)slot_mapping;
+    p.live = pool->d_live;
+    p.status = pool->d_status;
+    p.block_stride = (long long)pool->block_stride;
+    p.T = T;
+    p.num_kv_heads = pool->desc.num_kv_heads;
+    return pool->desc.head_dim == 128 ? launch_write8<128>(pool, p, stream) : launch_write8<64>(pool, p, stream);
+}
+
 }  // namespace ekv
 
 using namespace ekv;
@@ -185,19 +204,8 @@ extern "C" ekv_status_t ekv_write_kv(ekv_pool_t *pool, int32_t layer, const void
     }
     if (T == 0) return EKV_OK;
     if (pool->e4m3()) {
-        Write8Params p;
-        p.cache = (uint8_t *)pool->layer_base(layer);
-        p.scales = pool->layer_scales(layer);
-        p.claims = pool->d_claims + (size_t)layer * pool->total_blocks();
-        p.k = (const uint4 *)k;
-        p.v = (const uint4 *)v;
-        p.slots = (const long long *)slot_mapping;
-        p.live = pool->d_live;
-        p.status = pool->d_status;
-        p.block_stride = (long long)pool->block_stride;
-        p.T = T;
-        p.num_kv_heads = pool->desc.num_kv_heads;
-        return pool->desc.head_dim == 128 ? launch_write8<128>(pool, p, (cudaStream_t)stream) : launch_write8<64>(pool, p, (cudaStream_t)stream);
+        const int64_t row = (int64_t)pool->desc.num_kv_heads * pool->desc.head_dim;
+        return write_kv8(pool, layer, k, row, v, row, slot_mapping, T, (cudaStream_t)stream);
     }
     const int pieces_per_row = pool->desc.head_dim * 2 / 16;
     int block_shift = 0, row_shift = 0, token_shift = -1;

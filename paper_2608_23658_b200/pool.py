@@ -134,6 +134,57 @@ class Pool:
         if t.get_device() != self.device.index:
             raise ValueError(f"a tensor on {t.device} for a pool on {self.device}")
 
+    def _current(self, stream):
+        """The given stream, or the current one of the pool's own device."""
+        return torch.cuda.current_stream(self.device) if stream is None and torch.cuda.current_device() != self.device.index else stream
+
+    def _want(self, call, name, t, dtype, shape):
+        if t.dtype is not dtype or tuple(t.shape) != shape or t.get_device() != self.device.index or not t.is_contiguous():
+            B._refuse(call, name, t, f"contiguous {dtype} {shape} on {self.device}")
+
+    def _want_heads(self, call, name, t, T, heads):
+        """bf16 [T, heads, head_dim] whose tokens may stand apart (a part of a wider row)."""
+        if (t.dtype is not torch.bfloat16 or tuple(t.shape) != (T, heads, self.head_dim) or t.get_device() != self.device.index
+                or t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.head_dim)
+                or (T > 1 and (t.stride(0) % 8 or t.stride(0) < heads * self.head_dim)) or t.data_ptr() % 16):
+            B._refuse(call, name, t, f"bfloat16 {(T, heads, self.head_dim)} on {self.device}, a token's heads side by side, tokens a multiple of 8 elements apart, on 16 bytes")
+
+    def rope_write_kv(self, layer, q, k, v, positions, inv_freq, slot_mapping, q_weight=None, k_weight=None, eps=1e-6, weight_offset=0.0,
+                      factor=1.0, interleaved=False, axes=None, q_out=None, k_out=None, stream=None):
+        """Norms (where a weight is given) and turns queries [T, Hq, D] and keys [T, Hkv, D] by their positions, writes keys and values
+        into the slots, returns the queries.  q, k, v may be parts of one projection's rows.  positions: int32 [T], or [axes, T] with
+        `axes` naming the axis of each pair of channels; inv_freq: float32 [rotary_dim / 2]; interleaved: pairs are neighbours.  q_out may be q.  8-bit pools: k_out
+        receives the finished keys as bf16 before they are quantised (one is made if none is given)."""
+        call, (T,) = "rope_write_kv", slot_mapping.shape
+        self._want(call, "slot_mapping", slot_mapping, torch.int64, (T,))
+        self._want_heads(call, "q", q, T, self.num_q_heads)
+        self._want_heads(call, "k", k, T, self.num_kv_heads)
+        self._want_heads(call, "v", v, T, self.num_kv_heads)
+        pairs = inv_freq.numel()
+        self._want(call, "inv_freq", inv_freq, torch.float32, (pairs,))
+        num_axes = 1 if positions.dim() == 1 else positions.shape[0]
+        self._want(call, "positions", positions, torch.int32, (T,) if positions.dim() == 1 else (num_axes, T))
+        if num_axes > 1 and (axes is None or len(axes) != pairs):
+            raise ValueError(f"rope_write_kv: axes has to name the axis of each of the {pairs} pairs")
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None:
+                self._want(call, name, w, torch.bfloat16, (self.head_dim,))
+        if q_out is None:
+            q_out = torch.empty((T, self.num_q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+        else:
+            self._want_heads(call, "q_out", q_out, T, self.num_q_heads)
+        if k_out is not None:
+            self._want(call, "k_out", k_out, torch.bfloat16, (T, self.num_kv_heads, self.head_dim))
+        elif self.dtype == B.EKV_E4M3:
+            k_out = torch.empty((T, self.num_kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+        rope = B.Rope(2 * pairs, num_axes, B.EKV_ROPE_ADJACENT if interleaved else 0, factor, eps, weight_offset, inv_freq.data_ptr() or None,
+                      positions.data_ptr() or None, bytes(axes) if num_axes > 1 else None, q_weight.data_ptr() if q_weight is not None else None,
+                      k_weight.data_ptr() if k_weight is not None else None)
+        B.ekv_rope_write_kv(self.handle, layer, rope, q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+                            q_out.data_ptr(), q_out.stride(0), k_out.data_ptr() if k_out is not None else None, slot_mapping.data_ptr(), T,
+                            self._current(stream))
+        return q_out
+
     def extend_tables(self, new_tokens, seq_lens, block_tables, free_ids, free_cursor, slot_mapping, cu_q_lens,
                       seq_lens_out=None, free_cursor_out=None, stream=None):
         self._on_device(block_tables)
