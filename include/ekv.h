@@ -445,6 +445,61 @@ EKV_API ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, con
                                     const int32_t *seq_lens, int32_t R, float scale, void *stream);
 
 /*
+ * ---- Scores that are capped, biased by distance, windowed or open over a prefix -----------------------------------------
+ * The attention of models whose layers modify their scores or masks.  For a row at position p of its sequence, query head h,
+ * and the key at position j < seq_len:
+ *   x = scale * q.k;   x = cap * tanh(x / cap) if cap > 0;   x = x - slopes[h] * |p - j| if slopes is given;
+ *   the row sees the key if  p - window < j <= p  (j <= p if window is 0),  or if  j < prefix_lens[r];
+ *   out = sum_j softmax(x)_j v_j  over the keys it sees.
+ * prefix_lens[r] makes the first keys of request r visible to all its rows, also to rows before them (a prompt's image part, a
+ * prefix language model) and to rows whose window has moved on (tokens that stay in sight); values are clamped to 0 .. seq_len.
+ * Keys of a chunk's later rows below prefix_lens must be in the cache already, and a prompt that is cut into chunks must not be cut inside its prefix.
+ * Only keys that some row sees are read.  EKV_BF16 pools only.
+ */
+typedef struct ekv_scores {
+    float cap;                  /* 0: none */
+    int32_t window;             /* 0: none; else >= 1 */
+    const float *slopes;        /* DEVICE [num_q_heads], or NULL: no bias */
+    const int32_t *prefix_lens; /* DEVICE [B] or [R], or NULL: none */
+} ekv_scores_t;
+
+/* ekv_attn_decode with such scores; p = seq_lens[b] - 1.  scores: HOST.  The other arguments, the workspace's size too
+ * (ekv_attn_workspace_bytes), are those of ekv_attn_decode; any scale.  A NaN or an infinity in a key or value that the row does not see does not reach it. */
+EKV_API ekv_status_t ekv_attn_decode_scored(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
+                                    int32_t max_blocks_per_seq, const int32_t *seq_lens, int32_t B, float scale,
+                                    const ekv_scores_t *scores, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ekv_attn_prefill_chunk with such scores (tcgen05; any group, head_dim 64 or 128, any scale; calls share nothing but what they are
+ * given).  workspace: DEVICE, 256-byte aligned, ekv_attn_prefill_scored_workspace_bytes(pool) bytes cover every call of the
+ * pool; calls that share it must be stream-ordered.  Only a call of few rows over many keys uses it (its keys are cut into parts); one that does and has not enough is refused with EKV_ERR_WORKSPACE.
+ * A NaN or an infinity in a key or value reaches the rows that see it and no others. */
+EKV_API size_t ekv_attn_prefill_scored_workspace_bytes(const ekv_pool_t *pool);
+EKV_API ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
+                                           int32_t max_blocks_per_seq, const int32_t *cu_q_lens, const int32_t *cu_q_lens_host,
+                                           const int32_t *seq_lens, int32_t R, float scale, const ekv_scores_t *scores,
+                                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * ekv_attn_decode_shared -- ekv_attn_decode for a batch whose requests share prefixes (a system prompt, samples of one prompt, questions
+ * about one document): the result is ekv_attn_decode's within rounding, but the shared keys are read once for a group instead of once for each request.
+ * Group g is the requests group_starts[g] .. group_starts[g+1]-1; their first shared_lens[g] tokens are the same, i.e. the first
+ * shared_lens[g]/block_size entries of their rows of block_tables name the same blocks (those of the group's first request are read).
+ * group_starts: HOST [G+1], from 0 to B, non-decreasing.  shared_lens: HOST [G], multiples of block_size, 0 where nothing is shared,
+ * at most max_blocks_per_seq*block_size.  0 <= G <= 256 (requests that share nothing can stand together in one group of length 0).
+ * Both are read during the call alone; a captured call keeps them, and the tables and lengths may change under it.
+ * seq_lens count the shared tokens.  A request with 0 < seq_lens[b] < shared_lens of its group is invalid: its row is zeros and
+ * EKV_ERR_BLOCK_OOB is latched; seq_lens[b] = 0 gives a zero row.
+ * workspace: DEVICE, 256-byte aligned, of ekv_attn_decode_shared_workspace_bytes() bytes; calls that share it must be stream-ordered.
+ * The other arguments are those of ekv_attn_decode; scale > 0.  EKV_BF16 pools only.
+ */
+EKV_API size_t ekv_attn_decode_shared_workspace_bytes(const ekv_pool_t *pool, const int32_t *group_starts, const int32_t *shared_lens, int32_t G,
+                                              int32_t max_blocks_per_seq);
+EKV_API ekv_status_t ekv_attn_decode_shared(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
+                                    int32_t max_blocks_per_seq, const int32_t *seq_lens, int32_t B, const int32_t *group_starts,
+                                    const int32_t *shared_lens, int32_t G, float scale, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/*
  * ---- Block pool with a gated elastic id range, drain, and the one-step-ahead controller ----------
  * Paper, section "An Elastic KV Mechanism".  Paragraph "Two handles, one virtual range": the block
  * ids at the top of the range are gated inside the block pool, which hands them out only while the

@@ -16,4 +16,7 @@ from ._binding import (  # noqa: F401,E402
     ekv_controller_destroy, ekv_controller_stats, ekv_move_blocks)
 from ._binding import (  # noqa: F401,E402
     ekv_hoststep_create, ekv_hoststep_decode, ekv_hoststep_destroy, ekv_hoststep_flush, ekv_selftest_bounded_wait)
+from ._binding import (  # noqa: F401,E402
+    Scores, ekv_attn_decode_scored, ekv_attn_decode_shared, ekv_attn_decode_shared_workspace_bytes, ekv_attn_prefill_chunk_scored,
+    ekv_attn_prefill_scored_workspace_bytes)
 from .pool import HostStep, Pool  # noqa: F401,E402

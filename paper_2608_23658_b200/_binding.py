@@ -50,6 +50,10 @@ class Rope(ctypes.Structure):
                 ("pair_axis", ctypes.c_char_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
 
 
+class Scores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p), ("prefix_lens", ctypes.c_void_p)]
+
+
 class BlockPoolStats(ctypes.Structure):
     _fields_ = [("base_blocks", ctypes.c_int64), ("elastic_blocks", ctypes.c_int64), ("free_base", ctypes.c_int64),
                 ("free_elastic", ctypes.c_int64), ("elastic_in_use", ctypes.c_int64), ("num_gpu_blocks", ctypes.c_int64),
@@ -131,6 +135,11 @@ def load_library():
         "ekv_attn_decode_two_tensor": (i32, [vp, i32, vp, i64, vp, vp, vp, i32, vp, i32, f32, vp, sz, vp]),
         "ekv_attn_decode_static_scratch": (i32, [vp, i32, vp, vp, vp, i32, vp, i32, f32, vp]),
         "ekv_attn_prefill_chunk": (i32, [vp, i32, vp, vp, vp, i32, vp, vp, vp, i32, f32, vp]),
+        "ekv_attn_decode_scored": (i32, [vp, i32, vp, vp, vp, i32, vp, i32, f32, ctypes.POINTER(Scores), vp, sz, vp]),
+        "ekv_attn_prefill_scored_workspace_bytes": (sz, [vp]),
+        "ekv_attn_prefill_chunk_scored": (i32, [vp, i32, vp, vp, vp, i32, vp, vp, vp, i32, f32, ctypes.POINTER(Scores), vp, sz, vp]),
+        "ekv_attn_decode_shared_workspace_bytes": (sz, [vp, vp, vp, i32, i32]),
+        "ekv_attn_decode_shared": (i32, [vp, i32, vp, vp, vp, i32, vp, i32, vp, vp, i32, f32, vp, sz, vp]),
         "ekv_hoststep_create": (i32, [vp, i32, i32, i32, ctypes.POINTER(vp)]),
         "ekv_hoststep_destroy": (i32, [vp]),
         "ekv_hoststep_decode": (i32, [vp, i32, vp, vp, vp, vp, vp, i32, vp, i32, f32, vp, vp]),
@@ -419,6 +428,41 @@ def ekv_attn_prefill_chunk(pool: int, layer: int, q, out, block_tables, cu_q_len
     _check(load_library().ekv_attn_prefill_chunk(pool, layer, _dptr(q), _dptr(out), _dptr(block_tables), max_blocks,
                                                  _dptr(cu_q_lens), _dptr(cu_q_lens_host), _dptr(seq_lens), R,
                                                  float(scale), _stream(stream)))
+
+
+def _ws(workspace):
+    return (0, 0) if workspace is None else (_dptr(workspace), workspace.numel() * workspace.element_size())
+
+
+def ekv_attn_decode_scored(pool: int, layer: int, q, out, block_tables, seq_lens, scale: float, scores: Scores, workspace, stream=None):
+    """ekv_attn_decode with capped, biased or windowed scores (Pool.attn_decode_scored checks the tensors)."""
+    _check(load_library().ekv_attn_decode_scored(pool, layer, _dptr(q), _dptr(out), _dptr(block_tables), int(block_tables.shape[1]), _dptr(seq_lens),
+                                                 int(seq_lens.shape[0]), scale, ctypes.byref(scores), *_ws(workspace), _stream(stream)))
+
+
+def ekv_attn_prefill_scored_workspace_bytes(pool: int) -> int:
+    return int(load_library().ekv_attn_prefill_scored_workspace_bytes(pool))
+
+
+def ekv_attn_prefill_chunk_scored(pool: int, layer: int, q, out, block_tables, cu_q_lens, cu_q_lens_host, seq_lens, scale: float, scores: Scores,
+                                  workspace, stream=None):
+    """ekv_attn_prefill_chunk with capped, biased or windowed scores (Pool.attn_prefill_chunk_scored checks the tensors)."""
+    _check(load_library().ekv_attn_prefill_chunk_scored(pool, layer, _dptr(q), _dptr(out), _dptr(block_tables), int(block_tables.shape[1]),
+                                                        _dptr(cu_q_lens), _dptr(cu_q_lens_host), _dptr(seq_lens), int(seq_lens.shape[0]), scale,
+                                                        ctypes.byref(scores), *_ws(workspace), _stream(stream)))
+
+
+def ekv_attn_decode_shared_workspace_bytes(pool: int, group_starts, shared_lens, max_blocks_per_seq: int) -> int:
+    """group_starts [G+1], shared_lens [G]: int32 on the host."""
+    return int(load_library().ekv_attn_decode_shared_workspace_bytes(pool, _dptr(group_starts), _dptr(shared_lens), int(shared_lens.shape[0]),
+                                                                     max_blocks_per_seq))
+
+
+def ekv_attn_decode_shared(pool: int, layer: int, q, out, block_tables, seq_lens, group_starts, shared_lens, scale: float, workspace, stream=None):
+    """Decode of a batch whose requests share prefixes, group by group (Pool.attn_decode_shared checks the tensors)."""
+    _check(load_library().ekv_attn_decode_shared(pool, layer, _dptr(q), _dptr(out), _dptr(block_tables), int(block_tables.shape[1]), _dptr(seq_lens),
+                                                 int(seq_lens.shape[0]), _dptr(group_starts), _dptr(shared_lens), int(shared_lens.shape[0]), scale,
+                                                 *_ws(workspace), _stream(stream)))
 
 
 def ekv_poll_status(pool: int) -> Status:

@@ -1,0 +1,407 @@
+// Decode attention for the scores and masks of ekv_rows.cuh, and for the keys of a request behind those that its group shares.
+//
+// The split pass of ekv_decode.cu -- a CTA per (sequence, kv-head, range of keys), each warp a ring of TMA loads for every fourth block of 16
+// keys, the heads of the group as the rows of mma.m16n8k16, partial (m, l, O) per range -- over those blocks alone that the sequence sees:
+// of its prefix and of its window, or from the end of the shared keys on.  Bound by the bytes of these.  Where a sequence has a single
+// range the CTA writes the final rows itself; in a shared call it takes the shared keys' parts (left by the rows kernel, beside whose last
+// CTAs this launch comes up) along.  Otherwise combine_ext_kernel does, a warp a (sequence, head).
+#pragma once
+#include "ekv_rows.cuh"
+
+namespace ekv {
+namespace ext {
+
+using rows::kMaxGroups;
+
+static constexpr int kWarps = 4, kStages = 3;
+static constexpr int kBoxBytes = 16 * 128;  // 16 tokens x 64 channels
+
+struct Params {
+    const __nv_bfloat16 *q;
+    __nv_bfloat16 *out;
+    const int *block_tables, *seq_lens;
+    const long long *live;
+    unsigned *status;
+    const float *slopes;      // or null
+    const int *prefix_lens;   // or null
+    float *part_o;            // [B * Hq * nsplit][D], own ranges
+    float2 *part_ml;
+    const float *shared_o;    // [B * Hq * parts][D], of the shared keys
+    const float2 *shared_ml;
+    int max_blocks, num_q_heads, num_kv_heads, group;
+    int chunk_tokens, nsplit;
+    int window;
+    int parts, G;
+    float scale_log2;         // scale * log2 e; with a cap: cap * log2 e
+    float cap_scale;          // with a cap: 2 * log2 e * scale / cap
+    int start[kMaxGroups + 1];     // shared call: first request of a group,
+    int shared[kMaxGroups];        // its shared keys
+    uint8_t ns[kMaxGroups];        // and the parts that the rows kernel cut them into; 0: it did not, every request reads its own
+};
+
+// What of a sequence is to be read: blocks 0 .. n_pre - 1 and those from n_pre + skip on, `tokens` of them counted up to the last key.
+struct Span {
+    int L, lo, pre;       // keys lo .. L-1 and those below pre are seen
+    int n_pre, skip, tokens;
+    int parts;            // of the shared keys
+    bool invalid;
+};
+
+template <bool kShared>
+__device__ __forceinline__ Span span_of(const Params &p, int b) {
+    Span s;
+    s.L = max(0, min(p.seq_lens[b], p.max_blocks * 16));
+    s.parts = 0;
+    s.invalid = false;
+    s.lo = s.pre = s.n_pre = s.skip = 0;
+    if (kShared) {
+        int g = 0, hi = p.G;
+        while (hi - g > 1) {
+            const int mid = (g + hi) >> 1;
+            if (p.start[mid] <= b) g = mid;
+            else hi = mid;
+        }
+        s.invalid = s.L > 0 && s.L < p.shared[g];
+        if (s.invalid) s.L = 0;
+        s.parts = s.L > 0 ? p.ns[g] : 0;
+        if (s.parts > 0) s.lo = p.shared[g], s.skip = s.lo / 16;
+    } else {
+        s.lo = p.window > 0 ? max(0, s.L - p.window) : 0;
+        s.pre = p.prefix_lens ? max(0, min(p.prefix_lens[b], s.L)) : 0;
+        s.n_pre = (s.pre + 15) / 16;
+        s.skip = max(0, s.lo / 16 - s.n_pre);
+    }
+    s.tokens = s.L - s.skip * 16;
+    return s;
+}
+
+__device__ __forceinline__ float finish(float acc, float l) { return l == 0.f ? 0.f : acc / l; }
+
+template <int D, bool kShared, bool kCap, bool kBias>
+__global__ void __launch_bounds__(kWarps * 32, 2) decode_ext_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ Params p) {
+    constexpr int BOXES = D / 64;
+    constexpr int TILE_BYTES = BOXES * kBoxBytes;
+    constexpr int STAGE_BYTES = 2 * TILE_BYTES;
+    constexpr int KSTEPS = D / 16;
+    constexpr unsigned FULL = 0xffffffffu;
+
+    const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int r = lane >> 2, c = lane & 3;
+    const Span sp = span_of<kShared>(p, b);
+    const int t_begin = split * p.chunk_tokens;
+    if (split > 0 && t_begin >= sp.tokens) {  // whole CTA leaves before any barrier exists
+        if (kShared) asm volatile("griddepcontrol.wait;" ::: "memory");  // this launch is not over before the one it came up beside
+        return;
+    }
+    if (kShared && sp.invalid && split == 0 && g == 0 && threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+    const int t_end = min(sp.tokens, t_begin + p.chunk_tokens);  // counted over what is read
+    const int nblk = (max(t_end - t_begin, 0) + 15) >> 4;
+    const int nw = max(0, (nblk - warp + kWarps - 1) / kWarps);  // blocks this warp owns (<= 32)
+    auto block_of = [&](int i) {  // the warp's i-th block, in the sequence
+        const int l = (t_begin >> 4) + warp + kWarps * i;
+        return l < sp.n_pre ? l : l + sp.skip;
+    };
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_u32 = smem_u32(smem_raw);
+    const uint32_t base_u32 = (raw_u32 + 1023u) & ~1023u;
+    uint8_t *base_ptr = smem_raw + (base_u32 - raw_u32);
+    const uint32_t my_stages = base_u32 + warp * kStages * STAGE_BYTES;
+    const uint32_t my_bars = base_u32 + kWarps * kStages * STAGE_BYTES + warp * kStages * 8;
+    if (lane == 0) {
+        prefetch_tensormap(&kvmap);
+        for (int s = 0; s < kStages; ++s) mbar_init(my_bars + 8 * s, 1);
+        mbar_fence_init();
+    }
+    __syncwarp();
+
+    // Block ids of this warp's blocks: lane i holds the id of its i-th block.
+    const long long live = *p.live;
+    const int my_id = (lane < nw) ? p.block_tables[(size_t)b * p.max_blocks + block_of(lane)] : 0;
+    const bool my_ok = (lane < nw) && my_id >= 0 && (long long)my_id < live;
+    const unsigned valid_mask = __ballot_sync(FULL, my_ok);
+    if (lane < nw && !my_ok) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+
+    const uint64_t policy = policy_evict_first();
+    auto issue = [&](int i) {
+        const int id = __shfl_sync(FULL, my_id, i);
+        if (lane == 0 && ((valid_mask >> i) & 1u)) {
+            const int stage = i % kStages;
+            const uint32_t bar = my_bars + 8 * stage;
+            const uint32_t dst = my_stages + stage * STAGE_BYTES;
+            const int row_k = g * 16, row_v = row_k + p.num_kv_heads * 16;  // row inside the block: (K|V, kv-head, token)
+            mbar_expect_tx(bar, STAGE_BYTES);
+#pragma unroll
+            for (int x = 0; x < BOXES; ++x) {
+                tma_load_3d_hint(dst + x * kBoxBytes, &kvmap, 64 * x, row_k, id, bar, policy);
+                tma_load_3d_hint(dst + TILE_BYTES + x * kBoxBytes, &kvmap, 64 * x, row_v, id, bar, policy);
+            }
+        }
+    };
+    for (int s = 0; s < kStages && s < nw; ++s) issue(s);
+
+    // Q fragments (A operand): rows = heads of the group (r < group), zero above.
+    uint32_t qa[KSTEPS][2];
+    {
+        const __nv_bfloat16 *qrow = p.q + ((size_t)b * p.num_q_heads + (size_t)g * p.group + r) * D;
+#pragma unroll
+        for (int ks = 0; ks < KSTEPS; ++ks) {
+            qa[ks][0] = (r < p.group) ? *reinterpret_cast<const uint32_t *>(qrow + 16 * ks + 2 * c) : 0u;
+            qa[ks][1] = (r < p.group) ? *reinterpret_cast<const uint32_t *>(qrow + 16 * ks + 8 + 2 * c) : 0u;
+        }
+    }
+    const float slope = kBias && r < p.group ? p.slopes[g * p.group + r] * 1.4426950408889634f : 0.f;
+
+    // ldmatrix lane addressing inside one swizzled tile: matrix mi = lane/8, row rr = lane%8.
+    const int mi = lane >> 3, rr = lane & 7;
+    const uint32_t lane_row_off = (8 * (mi >> 1) + rr) * 128;
+    const int lane_par = mi & 1;
+
+    float o[KSTEPS][4];
+#pragma unroll
+    for (int mt = 0; mt < KSTEPS; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    bool failed = false;
+
+    uint32_t stage_parity = 0;  // of the copies that really went through a stage
+    int i = 0;
+    for (; i < nw; ++i) {
+        const int stage = i % kStages;
+        if ((valid_mask >> i) & 1u) {
+            const bool got = mbar_wait(my_bars + 8 * stage, (stage_parity >> stage) & 1u);
+            stage_parity ^= 1u << stage;
+            if (__any_sync(FULL, !got)) {
+                failed = true;
+                break;
+            }
+            const uint32_t kbase = my_stages + stage * STAGE_BYTES;
+            const uint32_t vbase = kbase + TILE_BYTES;
+            const int tok0 = block_of(i) * 16;
+            const bool partial = tok0 + 16 > sp.L || (tok0 < sp.lo && tok0 + 16 > sp.pre);
+
+            float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KSTEPS; ++ks) {
+                const int chunk = 2 * ks + lane_par;
+                const uint32_t addr = kbase + (chunk >> 3) * kBoxBytes + lane_row_off + (((chunk & 7) ^ rr) << 4);
+                uint32_t k0, k1, k2, k3;
+                ldmatrix_x4(addr, k0, k1, k2, k3);
+                mma_bf16_16816(s0, qa[ks][0], 0u, qa[ks][1], 0u, k0, k1);
+                mma_bf16_16816(s1, qa[ks][0], 0u, qa[ks][1], 0u, k2, k3);
+            }
+            const int t = tok0 + 2 * c;  // this lane's keys: t, t + 1, t + 8, t + 9
+            float x[4] = {s0[0], s0[1], s1[0], s1[1]};
+            uint32_t mask_lo = 0xffffffffu, mask_hi = 0xffffffffu;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (kCap) {  // 1 - 2 / (e^2y + 1): absolute error of some 2^-23
+                    const float ex = fast_exp2(x[e] * p.cap_scale);
+                    x[e] = p.scale_log2 - __fdividef(2.f * p.scale_log2, ex + 1.f);
+                } else {
+                    x[e] *= p.scale_log2;
+                }
+                if (kBias) x[e] -= slope * (float)(sp.L - 1 - (t + (e & 1) + 8 * (e >> 1)));
+            }
+            if (partial) {
+                auto seen = [&](int key) { return key < sp.L && (key >= sp.lo || key < sp.pre); };
+                const bool v0 = seen(t), v1 = seen(t + 1), v2 = seen(t + 8), v3 = seen(t + 9);
+                if (!v0) x[0] = -INFINITY;
+                if (!v1) x[1] = -INFINITY;
+                if (!v2) x[2] = -INFINITY;
+                if (!v3) x[3] = -INFINITY;
+                mask_lo = (v0 ? 0x0000ffffu : 0u) | (v1 ? 0xffff0000u : 0u);
+                mask_hi = (v2 ? 0x0000ffffu : 0u) | (v3 ? 0xffff0000u : 0u);
+            }
+            float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+            mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, 2));
+            const float m_new = fmaxf(m_run, mx);
+            const float m_use = m_new > -INFINITY ? m_new : 0.f;  // (scores of -infinity, as infinite keys give them, weigh nothing)
+            const float alpha = fast_exp2(m_run - m_use);
+            const float p0 = fast_exp2(x[0] - m_use), p1 = fast_exp2(x[1] - m_use);
+            const float p2 = fast_exp2(x[2] - m_use), p3 = fast_exp2(x[3] - m_use);
+            l_run = l_run * alpha + ((p0 + p1) + (p2 + p3));
+            m_run = m_new;
+            if (__any_sync(FULL, alpha != 1.f)) {
+                const float a_lo = __shfl_sync(FULL, alpha, 8 * c);
+                const float a_hi = __shfl_sync(FULL, alpha, 8 * c + 4);
+#pragma unroll
+                for (int mt = 0; mt < KSTEPS; ++mt) {
+                    o[mt][0] *= a_lo;
+                    o[mt][1] *= a_hi;
+                    o[mt][2] *= a_lo;
+                    o[mt][3] *= a_hi;
+                }
+            }
+            const uint32_t pb0 = pack_bf16x2(p0, p1), pb1 = pack_bf16x2(p2, p3);  // weights in bf16: half a step is 2^-9 of one
+#pragma unroll
+            for (int mt = 0; mt < KSTEPS; ++mt) {
+                const int chunk = 2 * mt + lane_par;
+                const uint32_t addr = vbase + (chunk >> 3) * kBoxBytes + lane_row_off + (((chunk & 7) ^ rr) << 4);
+                uint32_t v0, v1, v2, v3;
+                ldmatrix_x4_trans(addr, v0, v1, v2, v3);
+                if (partial) {  // values at keys that are not seen may be anything: 0 * NaN must not reach O
+                    v0 &= mask_lo;
+                    v1 &= mask_lo;
+                    v2 &= mask_hi;
+                    v3 &= mask_hi;
+                }
+                mma_bf16_16816(o[mt], v0, v1, v2, v3, pb0, pb1);
+            }
+        }
+        __syncwarp();  // every lane is done reading the stage before it is refilled
+        if (i + kStages < nw) issue(i + kStages);
+    }
+
+    if (failed) {
+        // A copy barrier never completed.  Latch the error, give copies still in flight a bounded chance to land (their destination
+        // must stay allocated), and contribute nothing.
+        if (lane == 0) atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);
+        stage_parity ^= 1u << (i % kStages);  // the wait that failed belongs to a copy still outstanding
+        for (int j = i; j < nw && j < i + kStages; ++j)
+            if ((valid_mask >> j) & 1u)
+                (void)mbar_wait(my_bars + 8 * (j % kStages), (stage_parity >> (j % kStages)) & 1u, 200000000ull);
+        m_run = -INFINITY;
+        l_run = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < KSTEPS; ++mt) o[mt][0] = o[mt][1] = o[mt][2] = o[mt][3] = 0.f;
+    }
+
+    l_run += __shfl_xor_sync(FULL, l_run, 1);
+    l_run += __shfl_xor_sync(FULL, l_run, 2);
+
+    // Merge the 4 warps through shared memory (each warp reuses its own, now idle, first stage).
+    float *wo = reinterpret_cast<float *>(base_ptr + warp * kStages * STAGE_BYTES);  // [8][D]
+    float *wm = wo + 8 * D;                                                          // [8] m, [8] l
+#pragma unroll
+    for (int mt = 0; mt < KSTEPS; ++mt) {
+        wo[(2 * c) * D + 16 * mt + r] = o[mt][0];
+        wo[(2 * c + 1) * D + 16 * mt + r] = o[mt][1];
+        wo[(2 * c) * D + 16 * mt + 8 + r] = o[mt][2];
+        wo[(2 * c + 1) * D + 16 * mt + 8 + r] = o[mt][3];
+    }
+    if (c == 0) {
+        wm[r] = m_run;
+        wm[8 + r] = l_run;
+    }
+    __syncthreads();
+    if (kShared) asm volatile("griddepcontrol.wait;" ::: "memory");  // the shared keys' parts are complete
+    for (int e = threadIdx.x; e < p.group * D; e += kWarps * 32) {
+        const int h = e / D, ch = e % D;
+        float mw[kWarps], mstar = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            mw[w] = reinterpret_cast<const float *>(base_ptr + w * kStages * STAGE_BYTES)[8 * D + h];
+            mstar = fmaxf(mstar, mw[w]);
+        }
+        const size_t row = (size_t)b * p.num_q_heads + (size_t)g * p.group + h;
+        const bool last = p.nsplit == 1;  // the only range of every sequence: finish here, no combine pass
+        if (kShared && last)
+            for (int s = 0; s < sp.parts; ++s) mstar = fmaxf(mstar, p.shared_ml[row * p.parts + s].x);
+        float acc = 0.f, lsum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {  // (a warp without a maximum holds zeros, or NaN if its scores were NaN: either counts)
+            const float *src = reinterpret_cast<const float *>(base_ptr + w * kStages * STAGE_BYTES);
+            const float wgt = (mw[w] > -INFINITY) ? fast_exp2(mw[w] - mstar) : 0.f;
+            acc += wgt * src[h * D + ch];
+            lsum += wgt * src[8 * D + 8 + h];
+        }
+        if (kShared && last)
+            for (int s = 0; s < sp.parts; ++s) {
+                const float2 ml = p.shared_ml[row * p.parts + s];
+                const float wgt = ml.x > -INFINITY ? fast_exp2(ml.x - mstar) : 0.f;
+                acc += wgt * p.shared_o[(row * p.parts + s) * D + ch];
+                lsum += wgt * ml.y;
+            }
+        if (last) {
+            p.out[row * D + ch] = __float2bfloat16_rn(finish(acc, lsum));
+        } else {
+            const size_t slot = row * p.nsplit + split;
+            p.part_o[slot * D + ch] = acc;
+            if (ch == 0) p.part_ml[slot] = make_float2(mstar, lsum);
+        }
+    }
+}
+
+// Adds the parts of a row, a list at a time: a warp a row, D / 32 channels a lane, eight parts' loads under way.
+template <int D>
+struct RowSum {
+    static constexpr int kC = D / 32;
+    float acc[kC], m = -INFINITY, l = 0.f;
+    __device__ __forceinline__ RowSum() {
+#pragma unroll
+        for (int c = 0; c < kC; ++c) acc[c] = 0.f;
+    }
+    __device__ __forceinline__ void add(const float *o, const float2 *ml, int n) {
+        const int lane = threadIdx.x & 31;
+        for (int s0 = 0; s0 < n; s0 += 32) {
+            const float2 v = s0 + lane < n ? ml[s0 + lane] : make_float2(-INFINITY, 0.f);
+            float top = v.x;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float m_new = fmaxf(m, top), alpha = m > -INFINITY ? fast_exp2(m - m_new) : 1.f;  // (nothing added yet, or NaN)
+            const float w = v.x > -INFINITY ? fast_exp2(v.x - m_new) : 0.f;
+            float sum = w * v.y;  // (a part whose scores were NaN has no maximum and a sum of NaN, which 0 leaves NaN)
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            l = l * alpha + sum;
+#pragma unroll
+            for (int c = 0; c < kC; ++c) acc[c] *= alpha;
+            m = m_new;
+            const int here = min(32, n - s0);
+#pragma unroll 8
+            for (int s = 0; s < here; ++s) {
+                const float ws = __shfl_sync(0xffffffffu, w, s);
+                const float ms = __shfl_sync(0xffffffffu, v.x, s);
+                if (!(ms > -INFINITY)) continue;  // nothing was written for it
+                const float *src = o + (size_t)(s0 + s) * D + lane * kC;
+                if (kC == 4) {
+                    const float4 x = *reinterpret_cast<const float4 *>(src);
+                    acc[0] += ws * x.x, acc[1] += ws * x.y, acc[kC - 2] += ws * x.z, acc[kC - 1] += ws * x.w;
+                } else {
+                    const float2 x = *reinterpret_cast<const float2 *>(src);
+                    acc[0] += ws * x.x, acc[kC - 1] += ws * x.y;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16 *out) const {
+        const int lane = threadIdx.x & 31;
+        uint32_t w[kC / 2];
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int c = 0; c < kC; c += 2) w[c / 2] = pack_bf16x2(acc[c] * inv, acc[c + 1] * inv);
+        if (kC == 4) *reinterpret_cast<uint2 *>(out + lane * kC) = make_uint2(w[0], w[kC / 2 - 1]);
+        else *reinterpret_cast<uint32_t *>(out + lane * kC) = w[0];
+    }
+};
+
+static constexpr int kCombineWarps = 4;
+
+template <int D, bool kShared>
+__global__ void __launch_bounds__(kCombineWarps * 32) combine_ext_kernel(const __grid_constant__ Params p, int rows) {
+    const int row = blockIdx.x * kCombineWarps + (threadIdx.x >> 5);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (row >= rows) return;
+    const Span sp = span_of<kShared>(p, row / p.num_q_heads);
+    RowSum<D> sum;
+    if (kShared) sum.add(p.shared_o + (size_t)row * p.parts * D, p.shared_ml + (size_t)row * p.parts, sp.parts);
+    sum.add(p.part_o + (size_t)row * p.nsplit * D, p.part_ml + (size_t)row * p.nsplit, max(1, (sp.tokens + p.chunk_tokens - 1) / p.chunk_tokens));
+    sum.store(p.out + (size_t)row * D);
+}
+
+// The parts of prefill rows: every row of a request has as many.
+template <int D>
+__global__ void __launch_bounds__(kCombineWarps * 32) combine_rows_kernel(const float *part_o, const float2 *part_ml, __nv_bfloat16 *out, const int *cu_q_lens, int R,
+                                                                          int num_q_heads, int parts, int rows) {
+    const int row = blockIdx.x * kCombineWarps + (threadIdx.x >> 5);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (row >= rows || row / num_q_heads >= cu_q_lens[R]) return;
+    RowSum<D> sum;
+    sum.add(part_o + (size_t)row * parts * D, part_ml + (size_t)row * parts, parts);
+    sum.store(out + (size_t)row * D);
+}
+
+}  // namespace ext
+}  // namespace ekv

@@ -1,0 +1,392 @@
+// Host side of ekv_attn_decode_scored, ekv_attn_prefill_chunk_scored and ekv_attn_decode_shared: checks, plans, launches.
+#include <cuda_bf16.h>
+#include <math.h>
+#include <string.h>
+
+#include "ekv_decode_ext.cuh"
+#include "ekv_internal.h"
+#include "ekv_rows.cuh"
+
+namespace ekv {
+
+static constexpr float kLog2e = 1.4426950408889634f;
+static constexpr float kSmallest = 1.17549435e-38f;  // stands for a scale of 0: -inf times it is still -inf
+
+// Shared-memory attributes of a kernel, once per device.
+template <typename Kernel>
+static cudaError_t ready(Kernel kernel, int bytes, int device, bool (&done)[64]) {
+    if (device < 64 && done[device]) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && device < 64) done[device] = true;
+    return e;
+}
+
+template <typename... P, typename... A>
+static cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, int bytes, bool early, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = early ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int D, int kMode, bool kCap, bool kBias>
+static cudaError_t launch_rows(ekv_pool *pool, int layer, const rows::Params &p, unsigned items, cudaStream_t stream) {
+    static bool done[64] = {false};
+    cudaError_t e = ready(rows::rows_kernel<D, kMode, kCap, kBias>, rows::Geo<D>::kSmemBytes, pool->desc.device, done);
+    if (e != cudaSuccess) return e;
+    return launch(rows::rows_kernel<D, kMode, kCap, kBias>, dim3(items), rows::kThreads, rows::Geo<D>::kSmemBytes, false, stream, pool->kv_map[layer], p,
+                  (const uint8_t *)pool->layer_base(layer), (long long)pool->block_stride);
+}
+
+template <int D, bool kShared, bool kCap, bool kBias>
+static cudaError_t launch_ext(ekv_pool *pool, int layer, const ext::Params &p, int B, bool early, cudaStream_t stream) {
+    constexpr int kBytes = ext::kWarps * ext::kStages * (2 * (D / 64) * ext::kBoxBytes + 8) + 1024;
+    static bool done[64] = {false};
+    cudaError_t e = ready(ext::decode_ext_kernel<D, kShared, kCap, kBias>, kBytes, pool->desc.device, done);
+    if (e != cudaSuccess) return e;
+    e = launch(ext::decode_ext_kernel<D, kShared, kCap, kBias>, dim3(p.nsplit, p.num_kv_heads, B), ext::kWarps * 32, kBytes, early, stream, pool->kv_map[layer], p);
+    if (e != cudaSuccess || p.nsplit == 1) return e;
+    const int n = B * p.num_q_heads;
+    return launch(ext::combine_ext_kernel<D, kShared>, dim3((n + ext::kCombineWarps - 1) / ext::kCombineWarps), ext::kCombineWarps * 32, 0, true, stream, p, n);
+}
+
+static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+// (m, l) pairs and rows of fp32 partial results
+static size_t parts_bytes(const ekv_pool *pool, size_t n) { return align256(n * sizeof(float2)) + align256(n * pool->desc.head_dim * sizeof(float)); }
+
+static ekv_status_t check_workspace(const char *who, const void *workspace, size_t bytes, size_t need) {
+    if (need > 0 && (!workspace || ((uintptr_t)workspace & 255) || bytes < need)) {
+        set_error("%s: workspace %p of %zu bytes; need %zu bytes, 256-byte aligned", who, workspace, bytes, need);
+        return EKV_ERR_WORKSPACE;
+    }
+    return EKV_OK;
+}
+
+static ekv_status_t check_scores(const char *who, const ekv_pool *pool, const ekv_scores_t *s, float scale) {
+    if (pool->e4m3()) {
+        set_error("%s: EKV_BF16 pools only", who);
+        return EKV_ERR_INVALID;
+    }
+    if (!s || !(s->cap >= 0.f) || isinf(s->cap) || s->window < 0 || isnan(scale) || isinf(scale)) {
+        set_error("%s: bad scores (cap=%g, window=%d, scale=%g)", who, s ? (double)s->cap : 0., s ? s->window : 0, (double)scale);
+        return EKV_ERR_INVALID;
+    }
+    return EKV_OK;
+}
+
+static ekv_status_t check_decode(const char *who, const void *q, const void *out, const int32_t *block_tables, int32_t max_blocks, const int32_t *seq_lens, int32_t B) {
+    if (B < 0 || max_blocks < 1 || max_blocks > (1 << 26) || B > 65535 || (B > 0 && (!q || !out || !block_tables || !seq_lens)) ||
+        (((uintptr_t)q | (uintptr_t)out) & 15)) {
+        set_error("%s: bad argument (B=%d, max_blocks_per_seq=%d)", who, B, max_blocks);
+        return EKV_ERR_INVALID;
+    }
+    return EKV_OK;
+}
+
+static void fill_ext(ext::Params &p, const ekv_pool *pool, const void *q, void *out, const int32_t *block_tables, int32_t max_blocks, const int32_t *seq_lens,
+                     const DecodePlan &plan) {
+    p.q = (const __nv_bfloat16 *)q, p.out = (__nv_bfloat16 *)out;
+    p.block_tables = block_tables, p.seq_lens = seq_lens;
+    p.live = pool->d_live, p.status = pool->d_status;
+    p.slopes = nullptr, p.prefix_lens = nullptr;
+    p.shared_o = nullptr, p.shared_ml = nullptr;
+    p.max_blocks = max_blocks, p.num_q_heads = pool->desc.num_q_heads, p.num_kv_heads = pool->desc.num_kv_heads;
+    p.group = p.num_q_heads / p.num_kv_heads;
+    p.chunk_tokens = plan.chunk_tokens, p.nsplit = plan.nsplit;
+    p.window = 0, p.parts = 0, p.G = 0;
+    p.cap_scale = 0.f;
+}
+
+static void fill_rows(rows::Params &p, const ekv_pool *pool, const void *q, void *out, const int32_t *block_tables, int32_t max_blocks) {
+    p.q = (const __nv_bfloat16 *)q, p.out = (__nv_bfloat16 *)out;
+    p.block_tables = block_tables, p.cu_q_lens = nullptr, p.seq_lens = nullptr;
+    p.live = pool->d_live, p.status = pool->d_status;
+    p.slopes = nullptr, p.prefix_lens = nullptr;
+    p.max_blocks = max_blocks, p.num_q_heads = pool->desc.num_q_heads, p.num_kv_heads = pool->desc.num_kv_heads;
+    p.group = p.num_q_heads / p.num_kv_heads;
+    p.group_magic = p.group > 1 ? (unsigned)(((1ull << 32) + p.group - 1) / p.group) : 0u;
+    p.window = 0, p.parts = 1, p.chunk_tiles = 0, p.q_flip = 0;
+    p.cap_scale = 0.f;
+}
+
+template <int D>
+static cudaError_t scored_decode(ekv_pool *pool, int layer, const ext::Params &p, bool cap, int B, cudaStream_t stream) {
+    if (cap) return p.slopes ? launch_ext<D, false, true, true>(pool, layer, p, B, false, stream) : launch_ext<D, false, true, false>(pool, layer, p, B, false, stream);
+    return p.slopes ? launch_ext<D, false, false, true>(pool, layer, p, B, false, stream) : launch_ext<D, false, false, false>(pool, layer, p, B, false, stream);
+}
+
+template <int D>
+static cudaError_t scored_prefill(ekv_pool *pool, int layer, const rows::Params &p, bool cap, unsigned items, cudaStream_t stream) {
+    using namespace rows;
+    if (cap) return p.slopes ? launch_rows<D, kScored, true, true>(pool, layer, p, items, stream) : launch_rows<D, kScored, true, false>(pool, layer, p, items, stream);
+    return p.slopes ? launch_rows<D, kScored, false, true>(pool, layer, p, items, stream) : launch_rows<D, kScored, false, false>(pool, layer, p, items, stream);
+}
+
+// Parts that an item's keys are cut into: as many as let all items run at the same time, while a part keeps two key tiles of the most that an item can see.
+static int plan_parts(const ekv_pool *pool, long long items, int max_blocks, int window, bool prefix, int max_rows) {
+    long long tiles = ((long long)max_blocks * 16 + rows::kBN - 1) / rows::kBN;
+    if (window > 0 && !prefix) {  // positions of an item, their windows, and a tile cut at each end
+        const long long span = ((long long)window + max_rows + rows::kBN - 1) / rows::kBN + 1;
+        if (span < tiles) tiles = span;
+    }
+    long long parts = pool->sm_count / (items > 0 ? items : 1);
+    if (parts > tiles / 2) parts = tiles / 2;
+    return parts < 1 ? 1 : (int)parts;
+}
+
+// How a shared call's groups are cut: items of the rows kernel are 256 (request, head) rows x chunk_tiles key tiles.
+struct SharedPlan {
+    int chunk_tiles, parts, tiles;  // tiles: items per kv-head
+    int own_blocks;                 // the longest table behind shared blocks
+    bool any;                       // some group's shared keys are read for all its requests at once
+};
+
+static bool takes_shared(int requests, int shared) { return requests > 1 && shared > 0; }
+
+static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const int32_t *shared, int G, int max_blocks) {
+    const int group = pool->desc.num_q_heads / pool->desc.num_kv_heads, Hk = pool->desc.num_kv_heads;
+    SharedPlan s;
+    s.any = false;
+    s.chunk_tiles = 1, s.parts = 0, s.tiles = 0, s.own_blocks = 1;
+    int longest = 0;
+    long long row_tiles = 0;
+    for (int g = 0; g < G; ++g) {
+        const int n = starts[g + 1] - starts[g];
+        if (n == 0) continue;
+        const bool takes = takes_shared(n, shared[g]);
+        const int own = max_blocks - (takes ? shared[g] / 16 : 0);
+        if (own > s.own_blocks) s.own_blocks = own;
+        if (!takes) continue;
+        s.any = true;
+        const int kt = (shared[g] + rows::kBN - 1) / rows::kBN;
+        if (kt > longest) longest = kt;
+        row_tiles += ((long long)n * group + rows::kItemRows - 1) / rows::kItemRows;
+    }
+    if (!s.any) return s;
+    // The cut with the shortest estimated time: rounds of the machine times an item's tiles and what it costs besides them.
+    const double fixed = 4.0;  // tiles' worth of an item's start and write-out
+    double best = 1e30;
+    long long most = 4LL * pool->sm_count / (row_tiles * Hk) + 1;
+    if (most > 64) most = 64;
+    if (most < 8) most = 8;
+    for (int ns = 1; ns <= most && ns <= longest; ++ns) {
+        const int chunk = (longest + ns - 1) / ns;
+        long long items = 0, work = 0;
+        for (int g = 0; g < G; ++g) {
+            const int n = starts[g + 1] - starts[g];
+            if (!takes_shared(n, shared[g])) continue;
+            const long long rt = ((long long)n * group + rows::kItemRows - 1) / rows::kItemRows * Hk, kt = (shared[g] + rows::kBN - 1) / rows::kBN;
+            items += rt * ((kt + chunk - 1) / chunk);
+            work += rt * kt;
+        }
+        const double rounds = (double)((items + pool->sm_count - 1) / pool->sm_count), mean = (double)work / items + fixed;
+        const double t = fmax(rounds * mean, chunk + fixed);
+        if (t < best) best = t, s.chunk_tiles = chunk;
+    }
+    s.parts = (longest + s.chunk_tiles - 1) / s.chunk_tiles;
+    return s;
+}
+
+static size_t shared_need(const ekv_pool *pool, const SharedPlan &s, const DecodePlan &own, int B) {
+    const size_t rows = (size_t)B * pool->desc.num_q_heads;
+    return (own.nsplit > 1 ? parts_bytes(pool, rows * own.nsplit) : 0) + (s.any ? parts_bytes(pool, rows * s.parts) : 0);
+}
+
+static ekv_status_t check_groups(const char *who, const ekv_pool *pool, const int32_t *starts, const int32_t *shared, int G, int max_blocks, int B) {
+    if (G < 0 || G > rows::kMaxGroups || (G > 0 && (!starts || !shared)) || (G == 0 && B > 0) || max_blocks < 1 || max_blocks > (1 << 26)) {
+        set_error("%s: bad groups (G=%d, B=%d, max_blocks_per_seq=%d; at most %d groups)", who, G, B, max_blocks, rows::kMaxGroups);
+        return EKV_ERR_INVALID;
+    }
+    for (int g = 0; g < G; ++g)
+        if (starts[g + 1] < starts[g] || (g == 0 && starts[0] != 0) || shared[g] < 0 || shared[g] % pool->desc.block_size != 0 ||
+            shared[g] / pool->desc.block_size > max_blocks) {
+            set_error("%s: bad group %d (requests %d .. %d, %d shared tokens)", who, g, starts[g], starts[g + 1], shared[g]);
+            return EKV_ERR_INVALID;
+        }
+    if (B >= 0 && G > 0 && starts[G] != B) {
+        set_error("%s: the groups hold %d requests, the call %d", who, starts[G], B);
+        return EKV_ERR_INVALID;
+    }
+    return EKV_OK;
+}
+
+template <int D>
+static cudaError_t shared_decode(ekv_pool *pool, int layer, const rows::Params &rp, const ext::Params &p, bool any, int B, cudaStream_t stream) {
+    if (any) {
+        const cudaError_t e = launch_rows<D, rows::kShared, false, false>(pool, layer, rp, (unsigned)(rp.tiles * rp.num_kv_heads), stream);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_ext<D, true, false, false>(pool, layer, p, B, any, stream);
+}
+
+}  // namespace ekv
+
+using namespace ekv;
+
+extern "C" ekv_status_t ekv_attn_decode_scored(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
+                                               int32_t max_blocks_per_seq, const int32_t *seq_lens, int32_t B, float scale,
+                                               const ekv_scores_t *scores, void *workspace, size_t workspace_bytes, void *stream) {
+    static const char who[] = "ekv_attn_decode_scored";
+    ekv_status_t st = check_compute(pool, layer, who);
+    if (st == EKV_OK) st = check_decode(who, q, out, block_tables, max_blocks_per_seq, seq_lens, B);
+    if (st == EKV_OK) st = check_scores(who, pool, scores, scale);
+    if (st != EKV_OK || B == 0) return st;
+    int seen = max_blocks_per_seq;  // blocks that a sequence reads at most
+    if (scores->window > 0 && !scores->prefix_lens && scores->window / 16 + 2 < seen) seen = scores->window / 16 + 2;
+    const DecodePlan plan = plan_decode(pool, B, seen);
+    const size_t n = (size_t)B * pool->desc.num_q_heads * plan.nsplit, need = plan.nsplit > 1 ? parts_bytes(pool, n) : 0;
+    st = check_workspace(who, workspace, workspace_bytes, need);
+    if (st != EKV_OK) return st;
+    ext::Params p;
+    fill_ext(p, pool, q, out, block_tables, max_blocks_per_seq, seq_lens, plan);
+    p.part_ml = (float2 *)workspace;
+    p.part_o = (float *)((uint8_t *)workspace + align256(n * sizeof(float2)));
+    p.slopes = scores->slopes, p.prefix_lens = scores->prefix_lens, p.window = scores->window;
+    const bool cap = scores->cap > 0.f;
+    p.scale_log2 = (cap ? scores->cap : scale) * kLog2e;
+    if (cap) p.cap_scale = 2.f * kLog2e * (scale / scores->cap);
+    const cudaError_t e = pool->desc.head_dim == 128 ? scored_decode<128>(pool, layer, p, cap, B, (cudaStream_t)stream)
+                                                     : scored_decode<64>(pool, layer, p, cap, B, (cudaStream_t)stream);
+    return e == cudaSuccess ? EKV_OK : cuda_fail(e, "ekv_attn_decode_scored launch");
+}
+
+extern "C" size_t ekv_attn_prefill_scored_workspace_bytes(const ekv_pool_t *pool) {
+    if (!pool || pool->host_only) return 0;
+    return parts_bytes(pool, (size_t)pool->sm_count * rows::kItemRows);  // a call is cut only as long as all its items run at the same time
+}
+
+extern "C" ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
+                                                      int32_t max_blocks_per_seq, const int32_t *cu_q_lens, const int32_t *cu_q_lens_host,
+                                                      const int32_t *seq_lens, int32_t R, float scale, const ekv_scores_t *scores,
+                                                      void *workspace, size_t workspace_bytes, void *stream) {
+    static const char who[] = "ekv_attn_prefill_chunk_scored";
+    ekv_status_t st = check_compute(pool, layer, who);
+    if (st != EKV_OK) return st;
+    if (R < 0 || max_blocks_per_seq < 1 || max_blocks_per_seq > (1 << 26) ||
+        (R > 0 && (!q || !out || !block_tables || !cu_q_lens || !cu_q_lens_host || !seq_lens)) || (((uintptr_t)q | (uintptr_t)out) & 15)) {
+        set_error("%s: bad argument (R=%d, max_blocks_per_seq=%d)", who, R, max_blocks_per_seq);
+        return EKV_ERR_INVALID;
+    }
+    st = check_scores(who, pool, scores, scale);
+    if (st != EKV_OK || R == 0) return st;
+    if (cu_q_lens_host[0] != 0) {
+        set_error("%s: cu_q_lens[0] must be 0", who);
+        return EKV_ERR_INVALID;
+    }
+    rows::Params p;
+    fill_rows(p, pool, q, out, block_tables, max_blocks_per_seq);
+    long long tiles = 0;
+    int longest = 0;
+    for (int r = 0; r < R; ++r) {
+        const int c = cu_q_lens_host[r + 1] - cu_q_lens_host[r];
+        if (cu_q_lens_host[r + 1] < cu_q_lens_host[r]) {
+            set_error("%s: cu_q_lens decreases at request %d", who, r);
+            return EKV_ERR_INVALID;
+        }
+        if (c > longest) longest = c;
+        if (R <= rows::kMaxGroups) p.tile_prefix[r] = (int)tiles;
+        tiles += ((long long)c * p.group + rows::kItemRows - 1) / rows::kItemRows;
+        if (tiles * p.num_kv_heads > (1LL << 30)) break;
+    }
+    const long long T = cu_q_lens_host[R];
+    if (T == 0) return EKV_OK;
+    if (R > rows::kMaxGroups) tiles = T * p.group / rows::kItemRows + R;
+    if (tiles * p.num_kv_heads > (1LL << 30) || T * p.num_q_heads >= (1LL << 31) || (long long)longest * p.group >= (1LL << 29)) {
+        set_error("%s: too many rows (%lld)", who, T);
+        return EKV_ERR_INVALID;
+    }
+    if (R <= rows::kMaxGroups) p.tile_prefix[R] = (int)tiles;
+    p.parts = plan_parts(pool, tiles * p.num_kv_heads, max_blocks_per_seq, scores->window, scores->prefix_lens != nullptr,
+                         longest < rows::kItemRows ? longest : rows::kItemRows);
+    const size_t n = (size_t)T * p.num_q_heads * p.parts;
+    st = check_workspace(who, workspace, workspace_bytes, p.parts > 1 ? parts_bytes(pool, n) : 0);
+    if (st != EKV_OK) return st;
+    p.part_ml = (float2 *)workspace;
+    p.part_o = (float *)((uint8_t *)workspace + align256(n * sizeof(float2)));
+    p.cu_q_lens = cu_q_lens, p.seq_lens = seq_lens, p.R = R, p.tiles = (int)tiles;
+    p.slopes = scores->slopes, p.prefix_lens = scores->prefix_lens, p.window = scores->window;
+    p.q_flip = scale < 0.f ? 0x80008000u : 0u;
+    const bool cap = scores->cap > 0.f;
+    p.scale_log2 = fmaxf((cap ? scores->cap : fabsf(scale)) * kLog2e, kSmallest);
+    if (cap) p.cap_scale = fabsf(scale) / scores->cap;
+    const unsigned items = (unsigned)(tiles * p.num_kv_heads * p.parts);
+    const bool d128 = pool->desc.head_dim == 128;
+    cudaError_t e = d128 ? scored_prefill<128>(pool, layer, p, cap, items, (cudaStream_t)stream) : scored_prefill<64>(pool, layer, p, cap, items, (cudaStream_t)stream);
+    if (e == cudaSuccess && p.parts > 1) {
+        const int all = (int)(T * p.num_q_heads);
+        const dim3 grid((all + ext::kCombineWarps - 1) / ext::kCombineWarps);
+        e = d128 ? launch(ext::combine_rows_kernel<128>, grid, ext::kCombineWarps * 32, 0, true, (cudaStream_t)stream, (const float *)p.part_o,
+                          (const float2 *)p.part_ml, p.out, cu_q_lens, R, p.num_q_heads, p.parts, all)
+                 : launch(ext::combine_rows_kernel<64>, grid, ext::kCombineWarps * 32, 0, true, (cudaStream_t)stream, (const float *)p.part_o,
+                          (const float2 *)p.part_ml, p.out, cu_q_lens, R, p.num_q_heads, p.parts, all);
+    }
+    return e == cudaSuccess ? EKV_OK : cuda_fail(e, "ekv_attn_prefill_chunk_scored launch");
+}
+
+extern "C" size_t ekv_attn_decode_shared_workspace_bytes(const ekv_pool_t *pool, const int32_t *group_starts, const int32_t *shared_lens,
+                                                         int32_t G, int32_t max_blocks_per_seq) {
+    if (!pool || pool->host_only || G < 1 || check_groups("ekv_attn_decode_shared_workspace_bytes", pool, group_starts, shared_lens, G, max_blocks_per_seq, -1) != EKV_OK ||
+        group_starts[G] < 1)
+        return 0;
+    const SharedPlan s = plan_shared(pool, group_starts, shared_lens, G, max_blocks_per_seq);
+    return shared_need(pool, s, plan_decode(pool, group_starts[G], s.own_blocks), group_starts[G]);
+}
+
+extern "C" ekv_status_t ekv_attn_decode_shared(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
+                                               int32_t max_blocks_per_seq, const int32_t *seq_lens, int32_t B, const int32_t *group_starts,
+                                               const int32_t *shared_lens, int32_t G, float scale, void *workspace, size_t workspace_bytes,
+                                               void *stream) {
+    static const char who[] = "ekv_attn_decode_shared";
+    ekv_status_t st = check_compute(pool, layer, who);
+    if (st == EKV_OK) st = check_decode(who, q, out, block_tables, max_blocks_per_seq, seq_lens, B);
+    if (st != EKV_OK) return st;
+    if (pool->e4m3() || !(scale > 0.f) || isinf(scale)) {
+        set_error("%s: EKV_BF16 pools and positive scales only (scale=%g)", who, (double)scale);
+        return EKV_ERR_INVALID;
+    }
+    st = check_groups(who, pool, group_starts, shared_lens, G, max_blocks_per_seq, B);
+    if (st != EKV_OK || B == 0) return st;
+    const SharedPlan s = plan_shared(pool, group_starts, shared_lens, G, max_blocks_per_seq);
+    const DecodePlan plan = plan_decode(pool, B, s.own_blocks);
+    st = check_workspace(who, workspace, workspace_bytes, shared_need(pool, s, plan, B));
+    if (st != EKV_OK) return st;
+    ext::Params p;
+    rows::Params rp;
+    fill_ext(p, pool, q, out, block_tables, max_blocks_per_seq, seq_lens, plan);
+    fill_rows(rp, pool, q, out, block_tables, max_blocks_per_seq);
+    const size_t head_rows = (size_t)B * p.num_q_heads;
+    uint8_t *at = (uint8_t *)workspace;
+    rp.part_ml = (float2 *)at;
+    rp.part_o = (float *)(at + align256(head_rows * s.parts * sizeof(float2)));
+    if (s.any) at += parts_bytes(pool, head_rows * s.parts);
+    p.part_ml = (float2 *)at;
+    p.part_o = (float *)(at + align256(head_rows * plan.nsplit * sizeof(float2)));
+    p.shared_ml = rp.part_ml, p.shared_o = rp.part_o;
+    p.parts = rp.parts = s.parts;
+    p.G = rp.R = G;
+    p.scale_log2 = rp.scale_log2 = scale * kLog2e;
+    rp.chunk_tiles = s.chunk_tiles;
+    int tiles = 0;
+    for (int g = 0; g < G; ++g) {
+        const int n = group_starts[g + 1] - group_starts[g];
+        const bool takes = takes_shared(n, shared_lens[g]);
+        const int kt = (shared_lens[g] + rows::kBN - 1) / rows::kBN, ns = takes ? (kt + s.chunk_tiles - 1) / s.chunk_tiles : 0;
+        p.start[g] = rp.start[g] = group_starts[g];
+        p.shared[g] = shared_lens[g], rp.shared[g] = takes ? shared_lens[g] : 0;
+        p.ns[g] = (uint8_t)ns;
+        rp.tile_prefix[g] = tiles;
+        tiles += (int)(((long long)n * p.group + rows::kItemRows - 1) / rows::kItemRows) * ns;
+    }
+    p.start[G] = rp.start[G] = B;
+    rp.tile_prefix[G] = rp.tiles = tiles;
+    const cudaError_t e = pool->desc.head_dim == 128 ? shared_decode<128>(pool, layer, rp, p, s.any, B, (cudaStream_t)stream)
+                                                     : shared_decode<64>(pool, layer, rp, p, s.any, B, (cudaStream_t)stream);
+    return e == cudaSuccess ? EKV_OK : cuda_fail(e, "ekv_attn_decode_shared launch");
+}

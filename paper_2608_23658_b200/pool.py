@@ -35,6 +35,7 @@ class Pool:
         self.num_layers = num_layers
         self.dtype = dtype
         self._ws = None
+        self._parts = None  # workspace of the scored prefill and of shared decode
 
     # -- lifetime
     def close(self):
@@ -42,7 +43,7 @@ class Pool:
             torch.cuda.synchronize(self.device)
             B.ekv_pool_destroy(self.handle)
             self.handle = None
-            self._ws = None
+            self._ws = self._parts = None
 
     def __enter__(self):
         return self
@@ -211,6 +212,73 @@ class Pool:
             out = torch.empty_like(q)
         B.ekv_attn_prefill_chunk(self.handle, layer, q, out, block_tables, cu_q_lens, cu_q_lens_host, seq_lens,
                                  scale, stream)
+        return out
+
+    # -- scores with a cap, a distance bias, a window, a prefix; batches that share prefixes
+    def _check_attn(self, call, q, out, block_tables, seq_lens, T):
+        if block_tables.dim() != 2:
+            B._refuse(call, "block_tables", block_tables, "int32 [requests, max_blocks_per_seq]")
+        n, shape = block_tables.shape[0], (T, self.num_q_heads, self.head_dim)
+        self._want(call, "block_tables", block_tables, torch.int32, tuple(block_tables.shape))
+        self._want(call, "seq_lens", seq_lens, torch.int32, (n,))
+        self._want(call, "q", q, torch.bfloat16, shape)
+        if out is None:
+            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        self._want(call, "out", out, torch.bfloat16, shape)
+        return out
+
+    def _scores(self, call, n, cap, window, slopes, prefix_lens):
+        if slopes is not None:
+            self._want(call, "slopes", slopes, torch.float32, (self.num_q_heads,))
+        if prefix_lens is not None:
+            self._want(call, "prefix_lens", prefix_lens, torch.int32, (n,))
+        return B.Scores(cap, window, None if slopes is None else slopes.data_ptr(), None if prefix_lens is None else prefix_lens.data_ptr())
+
+    def _parts_workspace(self, need):
+        if self._parts is None or self._parts.numel() < need:
+            self._parts = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self._parts
+
+    def attn_decode_scored(self, layer, q, block_tables, seq_lens, scale, cap=0.0, window=0, slopes=None, prefix_lens=None, out=None,
+                           workspace=None, stream=None):
+        """attn_decode with x = cap * tanh(x / cap), a bias of -slopes[head] * distance, a window of that many keys, and the keys below prefix_lens
+        always seen; any of them."""
+        n = block_tables.shape[0]
+        out = self._check_attn("attn_decode_scored", q, out, block_tables, seq_lens, n)
+        scores = self._scores("attn_decode_scored", n, cap, window, slopes, prefix_lens)
+        if workspace is None:
+            workspace = self.workspace(n, block_tables.shape[1] * self.block_size)
+        B.ekv_attn_decode_scored(self.handle, layer, q, out, block_tables, seq_lens, scale, scores, workspace, self._current(stream))
+        return out
+
+    def attn_prefill_chunk_scored(self, layer, q, block_tables, cu_q_lens, cu_q_lens_host, seq_lens, scale, cap=0.0, window=0, slopes=None,
+                                  prefix_lens=None, out=None, workspace=None, stream=None):
+        """attn_prefill_chunk with scores and masks as in attn_decode_scored, for every row at its own position."""
+        call, n = "attn_prefill_chunk_scored", block_tables.shape[0]
+        if cu_q_lens_host.dtype is not torch.int32 or cu_q_lens_host.is_cuda or cu_q_lens_host.numel() != n + 1 or not cu_q_lens_host.is_contiguous():
+            B._refuse(call, "cu_q_lens_host", cu_q_lens_host, f"contiguous int32 ({n + 1},) on the host")
+        self._want(call, "cu_q_lens", cu_q_lens, torch.int32, (n + 1,))
+        out = self._check_attn(call, q, out, block_tables, seq_lens, q.shape[0])
+        if q.shape[0] < int(cu_q_lens_host[-1]):
+            B._refuse(call, "q", q, f"of at least {int(cu_q_lens_host[-1])} rows")
+        scores = self._scores(call, n, cap, window, slopes, prefix_lens)
+        if workspace is None:
+            workspace = self._parts_workspace(B.ekv_attn_prefill_scored_workspace_bytes(self.handle))
+        B.ekv_attn_prefill_chunk_scored(self.handle, layer, q, out, block_tables, cu_q_lens, cu_q_lens_host, seq_lens, scale, scores, workspace,
+                                        self._current(stream))
+        return out
+
+    def attn_decode_shared(self, layer, q, block_tables, seq_lens, group_starts, shared_lens, scale, out=None, workspace=None, stream=None):
+        """attn_decode of a batch whose requests share prefixes: group_starts [G+1] and shared_lens [G] are int32 on the host.  The shared
+        tokens' blocks stand in every request's table; they are read once a group."""
+        call, n = "attn_decode_shared", block_tables.shape[0]
+        for name, t, size in (("group_starts", group_starts, shared_lens.numel() + 1), ("shared_lens", shared_lens, shared_lens.numel())):
+            if t.dtype is not torch.int32 or t.is_cuda or t.dim() != 1 or t.numel() != size or not t.is_contiguous():
+                B._refuse(call, name, t, f"contiguous int32 ({size},) on the host")
+        out = self._check_attn(call, q, out, block_tables, seq_lens, n)
+        if workspace is None:
+            workspace = self._parts_workspace(B.ekv_attn_decode_shared_workspace_bytes(self.handle, group_starts, shared_lens, block_tables.shape[1]))
+        B.ekv_attn_decode_shared(self.handle, layer, q, out, block_tables, seq_lens, group_starts, shared_lens, scale, workspace, self._current(stream))
         return out
 
 
