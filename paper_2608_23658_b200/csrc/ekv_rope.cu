@@ -4,21 +4,26 @@
 //   (a, b) -> factor * (a cos t - b sin t, b cos t + a sin t)          (pairs of channels), t = position[axis of the pair] * inv_freq[pair]
 //   queries -> q_out, keys and values -> their slots of the cache      (rounded to bf16 once, at the end)
 //
-// Bound by memory: every element is read once and written once, and 768 bytes of a row's arithmetic hide behind it.  A row of head_dim
-// channels belongs to D / 8 neighbouring lanes, 16 bytes each, so that the sum of squares and the exchange of a pair's halves are shuffles.
-// A CTA takes one or a few whole tokens: their sines and cosines are worked out once, into shared memory, for all heads, while the
-// first rows are on their way.  The angle is taken in turns in 64 bits (position * inv_freq needs up to 55 bits; in fp32 a position of 10^6
-// would be off by 0.06 rad) and only its fraction goes to sincospi.
+// Bound by memory: every element is read once and written once.  A row of head_dim channels belongs to D / 16 neighbouring lanes, two pieces
+// of 16 bytes each; where pairs are halves of a row the pieces are chosen so that both channels of a pair are in one thread, so a rotation is
+// register arithmetic and only the sum of squares is shuffled.  (With one piece a thread, and the partners' values by shuffles, the
+// arithmetic took longer than the bytes: 16384 tokens of 32q/8kv 119 us.)  A CTA takes one or a few whole tokens: their sines and cosines are worked out
+// once, into shared memory, for all heads, while the first rows are on their way, and the next rows are always on theirs.  The angle is taken
+// in turns in 64 bits (position * inv_freq needs up to 55 bits; in fp32 a position of 10^6 would be off by 0.06 rad) and only its
+// fraction is turned into a sine and a cosine.
 #include <cuda_bf16.h>
+
+#include <algorithm>
 
 #include "ekv_internal.h"
 #include "ptx.cuh"
 
 namespace ekv {
 
-static constexpr int kRopeThreads = 256;
-static constexpr int kRopeUnroll = 4;      // rows a thread has under way
-static constexpr int kRopeMaxTokens = 4;   // of a CTA
+static constexpr int kRopeThreads = 128;
+static constexpr int kRopeCtas = 4;        // an SM
+static constexpr int kRopeUnroll = 3;      // rows a thread works on, with as many of the next token under way
+static constexpr int kRopeTokens = 16;     // tokens whose angles a CTA works out at a time
 
 enum RopeStyle { kHalves = 0, kAdjacent = 1, kHalvesAnywhere = 2 };  // the last: halves that do not begin at a multiple of 8 channels
 
@@ -35,154 +40,224 @@ struct RopeParams {
     unsigned *status;
     long long q_stride, k_stride, v_stride, q_out_stride;  // elements between tokens
     long long block_stride;
-    int T, num_q_heads, num_kv_heads, pairs, tokens;  // tokens: of a CTA
+    int T, num_q_heads, num_kv_heads, pairs;
     float eps, offset, factor;
     uint8_t axis[64];
 };
 
-__device__ __forceinline__ float2 bf16x2_to_float2(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+
+// Two fp32 side by side in 64 bits.  (Through the intrinsics on float2 the halves were moved about between the operations.)
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair_of(float lo, float hi) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 halves(Pair a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+    return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t to_bf16x2(Pair a) {
+    const float2 v = halves(a);
+    return pack_bf16x2(v.x, v.y);
+}
 
 template <int D, int kStyle>
-__global__ void __launch_bounds__(kRopeThreads) rope_write_kernel(const __grid_constant__ RopeParams p) {
-    constexpr int kLanes = D / 8;  // of a row
-    constexpr int kRows = kRopeThreads / kLanes;
-    __shared__ float2 turn[kRopeMaxTokens][D / 2];
-    __shared__ float2 row_of[kStyle == kHalvesAnywhere ? kRopeThreads * 4 : 1];  // each thread's 8 channels
+__global__ void __launch_bounds__(kRopeThreads, kRopeCtas) rope_write_kernel(const __grid_constant__ RopeParams p) {
+    constexpr int kLanes = D / 16;  // of a row
+    constexpr int kRows = kRopeThreads / kLanes, kStep = kRows * kRopeUnroll;
+    __shared__ __align__(16) float2 turn[kRopeTokens][D / 2];
+    __shared__ __align__(16) float weights[2][D];
+    __shared__ __align__(16) float row_of[kStyle == kHalvesAnywhere ? kRopeThreads * 16 : 4];  // each thread's 16 channels
     const int lane = threadIdx.x % kLanes, first = threadIdx.x / kLanes;
-    const int per_token = p.num_q_heads + (p.k_out ? 1 : 2) * p.num_kv_heads;
-    const int t0 = blockIdx.x * p.tokens;
-    const int n_tokens = min(p.tokens, p.T - t0), n_rows = n_tokens * per_token;
+    const int q_heads = p.num_q_heads, qk_heads = q_heads + p.num_kv_heads, per_token = p.k_out ? qk_heads : qk_heads + p.num_kv_heads;
+    const int t0 = (int)((long long)p.T * blockIdx.x / gridDim.x), n_tokens = (int)((long long)p.T * (blockIdx.x + 1) / gridDim.x) - t0;
+    const int base = blockIdx.y * kStep;  // this CTA's rows of every token: base .. base + kStep - 1
     const long long live = *p.live;
+    // This thread's two pieces of a row.  Halves: the first channels of eight pairs and the second ones, or what lies behind the pairs.
+    const int half = kStyle == kHalves ? p.pairs / 8 : kLanes;
+    const bool turns = lane < half;
+    const int piece0 = turns ? lane : 2 * half + 2 * (lane - half), piece1 = turns ? lane + half : piece0 + 1;
 
-    uint4 x[kRopeUnroll];
-    int tok[kRopeUnroll], head[kRopeUnroll];
-    auto load = [&](int r0) {
+    // The thread's rows stand at the same heads of every token, so their addresses only step.  The next token's are on their way while one's
+    // are worked on.
+    const uint4 *src[kRopeUnroll];
+    uint4 x[kRopeUnroll][2], next[kRopeUnroll][2];
+    auto stride_of = [&](int h) { return h < q_heads ? p.q_stride : h < qk_heads ? p.k_stride : p.v_stride; };
+#pragma unroll
+    for (int u = 0; u < kRopeUnroll; ++u) {
+        const int h = min(base + first + u * kRows, per_token - 1);
+        const __nv_bfloat16 *row = h < q_heads ? p.q + h * D : h < qk_heads ? p.k + (h - q_heads) * D : p.v + (h - qk_heads) * D;
+        src[u] = reinterpret_cast<const uint4 *>(row + t0 * stride_of(h)) + piece0;
+    }
+    auto load = [&]() {
 #pragma unroll
         for (int u = 0; u < kRopeUnroll; ++u) {
-            const int r = r0 + u * kRows;
-            tok[u] = -1;
-            if (r >= n_rows) continue;
-            const int i = r / per_token, h = r - i * per_token;
-            tok[u] = i;
-            head[u] = h;
-            const long long t = t0 + i;
-            const __nv_bfloat16 *from = h < p.num_q_heads ? p.q + t * p.q_stride + h * D
-                                        : h < p.num_q_heads + p.num_kv_heads ? p.k + t * p.k_stride + (h - p.num_q_heads) * D
-                                                                              : p.v + t * p.v_stride + (h - p.num_q_heads - p.num_kv_heads) * D;
-            x[u] = reinterpret_cast<const uint4 *>(from)[lane];
+            next[u][0] = src[u][0];
+            next[u][1] = src[u][piece1 - piece0];
+            src[u] += stride_of(min(base + first + u * kRows, per_token - 1)) / 8;  // (a thread without a row takes the last one)
         }
     };
-    load(first);
-    for (int i = threadIdx.x; i < n_tokens * p.pairs; i += kRopeThreads) {
-        const int t = i / p.pairs, pair = i - t * p.pairs;
-        const double turns = (double)p.positions[(long long)p.axis[pair] * p.T + t0 + t] * (double)p.inv_freq[pair] * 0.15915494309189535;
-        float s, c;
-        sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-        turn[t][pair] = make_float2(c * p.factor, s * p.factor);
+    load();
+    const bool norms = p.q_weight || p.k_weight;
+    for (int i = threadIdx.x; norms && i < 2 * D; i += kRopeThreads) {
+        const __nv_bfloat16 *w = i < D ? p.q_weight : p.k_weight;
+        weights[i / D][i % D] = w ? p.offset + __bfloat162float(w[i % D]) : 1.f;
     }
-    __syncthreads();
-    // (the bound is the same for all threads: the shuffles below need whole warps)
-    for (int r0 = 0; r0 < n_rows; r0 += kRows * kRopeUnroll) {
-        if (r0 > 0) load(r0 + first);
+    // A thread works out the angles of one pair, of every kAngleRows-th token.  (|error| of the fast sine and cosine within half a turn: some 2^-21,
+    // an eighth of a percent of what the result is rounded to.)
+    constexpr int kAngleRows = kRopeThreads / (D / 2);
+    const int pair = threadIdx.x % (D / 2);
+    const bool has_pair = pair < p.pairs;
+    const double turns_per = has_pair ? (double)p.inv_freq[pair] * 0.15915494309189535 : 0.;
+    const int *position = p.positions + (has_pair ? (long long)p.axis[pair] * p.T + t0 : 0);
+    // (halves: eight pairs of a thread, laid out so that neighbouring lanes read neighbouring words)
+    const int angle_at = kStyle == kHalves ? pair % 8 / 2 * (2 * half) + pair / 8 * 2 + pair % 2 : pair;
+    auto angles = [&](int from) {  // of the tokens from there on
+        const int n = has_pair ? min(kRopeTokens, n_tokens - from) : 0;
+#pragma unroll 4
+        for (int t = threadIdx.x / (D / 2); t < n; t += kAngleRows) {
+            const double a = (double)position[from + t] * turns_per;
+            const float b = (float)(a - rint(a)) * 6.283185307179586f;
+            turn[t][angle_at] = make_float2(__cosf(b) * p.factor, __sinf(b) * p.factor);
+        }
+    };
+    Pair cos2[4], sin2[4], minus[4];  // halves: of this thread's eight pairs, two at a time
+    long long slot = p.k_out ? -1 : p.slots[t0];
+    __nv_bfloat16 *q_to = p.q_out + t0 * p.q_out_stride;
+    for (int i = 0; i < n_tokens; ++i, q_to += p.q_out_stride) {
+        const int in_batch = i % kRopeTokens;
+        if (in_batch == 0) {
+            if (i > 0) __syncthreads();
+            angles(i);
+            __syncthreads();
+        }
 #pragma unroll
-        for (int u = 0; u < kRopeUnroll; ++u) {
-            const int h = tok[u] < 0 ? 0 : head[u], i = max(tok[u], 0);
-            const bool is_q = h < p.num_q_heads, is_v = h >= p.num_q_heads + p.num_kv_heads;
-            const long long t = t0 + i;
-            if (tok[u] < 0) x[u] = make_uint4(0u, 0u, 0u, 0u);
-            const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-            float y[8];
+        for (int u = 0; u < kRopeUnroll; ++u) x[u][0] = next[u][0], x[u][1] = next[u][1];
+        if (i + 1 < n_tokens) load();
+        const long long s = slot;
+        if (i + 1 < n_tokens && !p.k_out) slot = p.slots[t0 + i + 1];
+        __nv_bfloat16 *kv_to = nullptr;  // the token's first K row; a row of another head lies kv_step further on
+        const int kv_step = p.k_out ? D : 16 * D;
+        if (p.k_out) kv_to = p.k_out + (long long)(t0 + i) * p.num_kv_heads * D;
+        else if (s >= 0 && (s >> 4) < live) kv_to = reinterpret_cast<__nv_bfloat16 *>(p.cache + (s >> 4) * p.block_stride) + (int)(s & 15) * D;
+        else if (s >= 0 && threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+        if (kStyle == kHalves && turns) {  // a token's angles stay in registers for all its rows
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const float2 a = bf16x2_to_float2(w[c]);
-                y[2 * c] = a.x, y[2 * c + 1] = a.y;
+                const float4 a = *reinterpret_cast<const float4 *>(&turn[in_batch][c * (2 * half) + lane * 2]);
+                cos2[c] = pair_of(a.x, a.z), sin2[c] = pair_of(a.y, a.w), minus[c] = pair_of(-a.y, -a.w);
             }
-            if (p.q_weight || p.k_weight) {
-                float sum = 0.f;
+        }
+        // All rows' sums side by side: one alone is a chain of shuffles and a root that nothing hides (16384 tokens of 32q/8kv one by one: 89 us).
+        float f[kRopeUnroll];
+        if (norms) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) sum += y[c] * y[c];
+            for (int u = 0; u < kRopeUnroll; ++u) {
+                const uint32_t w[8] = {x[u][0].x, x[u][0].y, x[u][0].z, x[u][0].w, x[u][1].x, x[u][1].y, x[u][1].z, x[u][1].w};
+                Pair sum = 0;
 #pragma unroll
-                for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                const __nv_bfloat16 *weight = is_q ? p.q_weight : p.k_weight;
-                if (weight && !is_v) {
-                    const float f = rsqrtf(sum * (1.f / D) + p.eps);
-                    const uint4 g = reinterpret_cast<const uint4 *>(weight)[lane];
-                    const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
+                for (int c = 0; c < 8; ++c) {
+                    const Pair y = pair_of(__uint_as_float(w[c] << 16), __uint_as_float(w[c] & 0xffff0000u));
+                    sum = fma2(y, y, sum);
+                }
+                f[u] = halves(sum).x + halves(sum).y;
+            }
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float2 a = bf16x2_to_float2(gw[c]);
-                        y[2 * c] *= f * (p.offset + a.x), y[2 * c + 1] *= f * (p.offset + a.y);
-                    }
+            for (int o = kLanes / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int u = 0; u < kRopeUnroll; ++u) f[u] += __shfl_xor_sync(0xffffffffu, f[u], o);
+#pragma unroll
+            for (int u = 0; u < kRopeUnroll; ++u) {
+                const float g = rsqrtf(f[u] * (1.f / D) + p.eps);
+                f[u] = (base + first + u * kRows < q_heads ? p.q_weight : p.k_weight) ? g : 1.f;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kRopeUnroll; ++u) {
+            const int h = base + first + u * kRows;
+            const uint32_t w[8] = {x[u][0].x, x[u][0].y, x[u][0].z, x[u][0].w, x[u][1].x, x[u][1].y, x[u][1].z, x[u][1].w};
+            Pair y[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) y[c] = pair_of(__uint_as_float(w[c] << 16), __uint_as_float(w[c] & 0xffff0000u));
+            if (norms) {
+                const Pair f2 = pair_of(f[u], f[u]);
+                const ulonglong2 *g = reinterpret_cast<const ulonglong2 *>(weights[h < q_heads ? 0 : 1]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const ulonglong2 a = g[(c < 2 ? piece0 : piece1) * 2 + c % 2];
+                    y[2 * c] = mul2(mul2(y[2 * c], f2), a.x), y[2 * c + 1] = mul2(mul2(y[2 * c + 1], f2), a.y);
                 }
             }
-            if (kStyle == kAdjacent) {
-                if (!is_v) {
+            if (kStyle == kHalves) {
+                if (turns) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const int pair = 4 * lane + c;
-                        if (pair < p.pairs) {
-                            const float2 cs = turn[i][pair];
-                            const float a = y[2 * c], b = y[2 * c + 1];
-                            y[2 * c] = a * cs.x - b * cs.y, y[2 * c + 1] = b * cs.x + a * cs.y;
-                        }
+                        const Pair a = y[c], b = y[4 + c];
+                        y[c] = fma2(b, minus[c], mul2(a, cos2[c]));
+                        y[4 + c] = fma2(a, sin2[c], mul2(b, cos2[c]));
                     }
                 }
-            } else if (kStyle == kHalves) {
-                const int half = p.pairs / 8;  // lanes that hold first channels of pairs; as many behind them hold the second ones
-                const bool low = lane < half, there = lane < 2 * half;
-                float other[8];
+            } else if (kStyle == kAdjacent) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) other[c] = __shfl_sync(0xffffffffu, y[c], low ? lane + half : lane - half, kLanes);
-                if (there && !is_v) {
-                    const float2 *cs = &turn[i][8 * (low ? lane : lane - half)];
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) y[c] = y[c] * cs[c].x + (low ? -other[c] : other[c]) * cs[c].y;
+                for (int c = 0; c < 8; ++c) {
+                    const int pair = 4 * (c < 4 ? piece0 : piece1) + c % 4;
+                    if (pair < p.pairs) {
+                        const float2 cs = turn[in_batch][pair], a = halves(y[c]);
+                        y[c] = pair_of(a.x * cs.x - a.y * cs.y, a.y * cs.x + a.x * cs.y);
+                    }
                 }
             } else {
-                float *mine = reinterpret_cast<float *>(row_of) + (threadIdx.x - lane) * 8;  // the row of this thread's lanes
+                float *mine = row_of + (threadIdx.x - lane) * 16;  // the row of this thread's lanes
                 __syncwarp();
 #pragma unroll
-                for (int c = 0; c < 8; ++c) mine[8 * lane + c] = y[c];
+                for (int c = 0; c < 8; ++c) *reinterpret_cast<float2 *>(mine + 8 * (c < 4 ? piece0 : piece1) + 2 * (c % 4)) = halves(y[c]);
                 __syncwarp();
-                if (!is_v) {
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const int ch = 8 * lane + c;
-                        if (ch < 2 * p.pairs) {
-                            const bool low = ch < p.pairs;
-                            const float2 cs = turn[i][low ? ch : ch - p.pairs];
-                            const float other = mine[low ? ch + p.pairs : ch - p.pairs];
-                            y[c] = y[c] * cs.x + (low ? -other : other) * cs.y;
-                        }
-                    }
+                for (int c = 0; c < 8; ++c) {
+                    const int ch0 = 8 * (c < 4 ? piece0 : piece1) + 2 * (c % 4);
+                    auto turned = [&](int ch, float own) {
+                        if (ch >= 2 * p.pairs) return own;
+                        const bool lower = ch < p.pairs;
+                        const float2 a = turn[in_batch][lower ? ch : ch - p.pairs];
+                        const float other = mine[lower ? ch + p.pairs : ch - p.pairs];
+                        return own * a.x + (lower ? -other : other) * a.y;
+                    };
+                    const float2 own = halves(y[c]);
+                    y[c] = pair_of(turned(ch0, own.x), turned(ch0 + 1, own.y));
                 }
             }
-            if (tok[u] < 0) continue;
-            const uint4 out = is_v ? x[u] : make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
-            if (is_q) {
-                reinterpret_cast<uint4 *>(p.q_out + t * p.q_out_stride + h * D)[lane] = out;
-                continue;
+            __nv_bfloat16 *row = h < q_heads ? q_to + h * D : kv_to ? kv_to + (h - q_heads) * kv_step : nullptr;  // K heads, then V heads: as they lie in a block
+            if (!row || h >= per_token) continue;
+            uint4 *to = reinterpret_cast<uint4 *>(row);
+            if (h >= qk_heads) {
+                to[piece0] = x[u][0];
+                to[piece1] = x[u][1];
+            } else {
+                to[piece0] = make_uint4(to_bf16x2(y[0]), to_bf16x2(y[1]), to_bf16x2(y[2]), to_bf16x2(y[3]));
+                to[piece1] = make_uint4(to_bf16x2(y[4]), to_bf16x2(y[5]), to_bf16x2(y[6]), to_bf16x2(y[7]));
             }
-            const int kv_row = h - p.num_q_heads;  // K heads, then V heads: as they lie in a block
-            if (p.k_out) {
-                if (!is_v) reinterpret_cast<uint4 *>(p.k_out + (t * p.num_kv_heads + kv_row) * D)[lane] = out;
-                continue;
-            }
-            const long long s = p.slots[t];
-            if (s < 0) continue;
-            const long long n = s >> 4;
-            if (n >= live) {
-                if (kv_row == 0 && lane == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
-                continue;
-            }
-            reinterpret_cast<uint4 *>(p.cache + n * p.block_stride + (kv_row * 16 + (int)(s & 15)) * (2 * D))[lane] = out;
         }
     }
 }
 
 template <int D>
-static cudaError_t launch_rope(const RopeParams &p, bool adjacent, cudaStream_t stream) {
-    const unsigned grid = (unsigned)(((long long)p.T + p.tokens - 1) / p.tokens);
+static cudaError_t launch_rope(const RopeParams &p, int sm_count, bool adjacent, cudaStream_t stream) {
+    constexpr int kStep = kRopeThreads / (D / 16) * kRopeUnroll;
+    const int per_token = p.num_q_heads + (p.k_out ? 1 : 2) * p.num_kv_heads;
+    const int steps = (per_token + kStep - 1) / kStep, fit = std::max(1, sm_count * kRopeCtas / steps);
+    const dim3 grid(std::min(p.T, fit), steps);  // CTAs that are all there at once share the tokens evenly
     if (adjacent) rope_write_kernel<D, kAdjacent><<<grid, kRopeThreads, 0, stream>>>(p);
     else if (p.pairs % 8 == 0) rope_write_kernel<D, kHalves><<<grid, kRopeThreads, 0, stream>>>(p);
     else rope_write_kernel<D, kHalvesAnywhere><<<grid, kRopeThreads, 0, stream>>>(p);
@@ -240,11 +315,8 @@ extern "C" ekv_status_t ekv_rope_write_kv(ekv_pool_t *pool, int32_t layer, const
     p.T = T, p.num_q_heads = Hq, p.num_kv_heads = Hk, p.pairs = rope->rotary_dim / 2;
     p.eps = rope->eps, p.offset = rope->weight_offset, p.factor = rope->factor;
     for (int i = 0; i < 64; ++i) p.axis[i] = rope->num_axes > 1 && i < p.pairs ? rope->pair_axis[i] : 0;
-    // A CTA's tokens share its start (positions, angles); with few tokens every one gets a CTA of its own.
-    p.tokens = 1;
-    while (p.tokens < kRopeMaxTokens && (long long)T >= (long long)pool->sm_count * 8 * 2 * p.tokens) p.tokens *= 2;
-    const cudaError_t e = D == 128 ? launch_rope<128>(p, rope->flags & EKV_ROPE_ADJACENT, (cudaStream_t)stream)
-                                   : launch_rope<64>(p, rope->flags & EKV_ROPE_ADJACENT, (cudaStream_t)stream);
+    const cudaError_t e = D == 128 ? launch_rope<128>(p, pool->sm_count, rope->flags & EKV_ROPE_ADJACENT, (cudaStream_t)stream)
+                                   : launch_rope<64>(p, pool->sm_count, rope->flags & EKV_ROPE_ADJACENT, (cudaStream_t)stream);
     if (e != cudaSuccess) return cuda_fail(e, "ekv_rope_write_kv launch");
     if (pool->e4m3()) return write_kv8(pool, layer, k_out, (int64_t)Hk * D, v, v_stride, slot_mapping, T, (cudaStream_t)stream);
     return EKV_OK;

@@ -7,6 +7,13 @@ import torch
 from . import _binding as B
 
 
+def _raw_stream(device: int) -> int:
+    """Address of torch's current stream on a device (by the raw call where torch has it: building the Stream object costs more than the
+    rest of a small call)."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw else torch.cuda.current_stream(device).cuda_stream
+
+
 class _RawCuda:
     """Minimal __cuda_array_interface__ carrier for a raw device range (int16 elements unless told otherwise).  A tensor
     made of it keeps it, and so the pool whose memory it views: a view that outlives the caller's last name for the pool
@@ -35,7 +42,7 @@ class Pool:
         self.num_layers = num_layers
         self.dtype = dtype
         self._ws = None
-        self._parts = None  # workspace of the scored prefill and of shared decode
+        self._parts = {}  # workspaces of scored and shared attention, by stream
 
     # -- lifetime
     def close(self):
@@ -43,7 +50,8 @@ class Pool:
             torch.cuda.synchronize(self.device)
             B.ekv_pool_destroy(self.handle)
             self.handle = None
-            self._ws = self._parts = None
+            self._ws = None
+            self._parts = {}
 
     def __enter__(self):
         return self
@@ -136,19 +144,22 @@ class Pool:
             raise ValueError(f"a tensor on {t.device} for a pool on {self.device}")
 
     def _current(self, stream):
-        """The given stream, or the current one of the pool's own device."""
-        return torch.cuda.current_stream(self.device) if stream is None and torch.cuda.current_device() != self.device.index else stream
+        """Address of the given stream, or of the current one on the pool's own device."""
+        if stream is None:
+            return _raw_stream(self.device.index)
+        return stream if isinstance(stream, int) else stream.cuda_stream
 
     def _want(self, call, name, t, dtype, shape):
-        if t.dtype is not dtype or tuple(t.shape) != shape or t.get_device() != self.device.index or not t.is_contiguous():
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device.index or not t.is_contiguous():
             B._refuse(call, name, t, f"contiguous {dtype} {shape} on {self.device}")
 
-    def _want_heads(self, call, name, t, T, heads):
-        """bf16 [T, heads, head_dim] whose tokens may stand apart (a part of a wider row)."""
-        if (t.dtype is not torch.bfloat16 or tuple(t.shape) != (T, heads, self.head_dim) or t.get_device() != self.device.index
-                or t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.head_dim)
-                or (T > 1 and (t.stride(0) % 8 or t.stride(0) < heads * self.head_dim)) or t.data_ptr() % 16):
-            B._refuse(call, name, t, f"bfloat16 {(T, heads, self.head_dim)} on {self.device}, a token's heads side by side, tokens a multiple of 8 elements apart, on 16 bytes")
+    def _heads(self, call, name, t, T, heads):
+        """bf16 [T, heads, head_dim] whose tokens may stand apart (a part of a wider row; the library looks at the distance)."""
+        stride = t.stride()
+        if (t.dtype is not torch.bfloat16 or t.shape != (T, heads, self.head_dim) or t.get_device() != self.device.index
+                or stride[2] != 1 or (stride[1] != self.head_dim and heads > 1)):
+            B._refuse(call, name, t, f"bfloat16 {(T, heads, self.head_dim)} on {self.device}, a token's heads side by side")
+        return stride[0]
 
     def rope_write_kv(self, layer, q, k, v, positions, inv_freq, slot_mapping, q_weight=None, k_weight=None, eps=1e-6, weight_offset=0.0,
                       factor=1.0, interleaved=False, axes=None, q_out=None, k_out=None, stream=None):
@@ -156,34 +167,37 @@ class Pool:
         into the slots, returns the queries.  q, k, v may be parts of one projection's rows.  positions: int32 [T], or [axes, T] with
         `axes` naming the axis of each pair of channels; inv_freq: float32 [rotary_dim / 2]; interleaved: pairs are neighbours.  q_out may be q.  8-bit pools: k_out
         receives the finished keys as bf16 before they are quantised (one is made if none is given)."""
-        call, (T,) = "rope_write_kv", slot_mapping.shape
-        self._want(call, "slot_mapping", slot_mapping, torch.int64, (T,))
-        self._want_heads(call, "q", q, T, self.num_q_heads)
-        self._want_heads(call, "k", k, T, self.num_kv_heads)
-        self._want_heads(call, "v", v, T, self.num_kv_heads)
-        pairs = inv_freq.numel()
-        self._want(call, "inv_freq", inv_freq, torch.float32, (pairs,))
-        num_axes = 1 if positions.dim() == 1 else positions.shape[0]
-        self._want(call, "positions", positions, torch.int32, (T,) if positions.dim() == 1 else (num_axes, T))
+        call, i32, f32, bf16, dev = "rope_write_kv", torch.int32, torch.float32, torch.bfloat16, self.device.index
+        T, pairs, where = slot_mapping.shape[0], inv_freq.shape[0], positions.shape
+        num_axes = 1 if len(where) == 1 else where[0]
+        heads, kv_heads = self.num_q_heads, self.num_kv_heads
+        q_stride, k_stride, v_stride = self._heads(call, "q", q, T, heads), self._heads(call, "k", k, T, kv_heads), self._heads(call, "v", v, T, kv_heads)
+        if not (slot_mapping.dtype is torch.int64 and inv_freq.dtype is f32 and positions.dtype is i32 and where[-1] == T and len(where) <= 2
+                and slot_mapping.dim() == 1 and inv_freq.dim() == 1 and slot_mapping.is_contiguous() and inv_freq.is_contiguous() and positions.is_contiguous()
+                and slot_mapping.get_device() == dev and inv_freq.get_device() == dev and positions.get_device() == dev):
+            self._want(call, "slot_mapping", slot_mapping, torch.int64, (T,))
+            self._want(call, "inv_freq", inv_freq, f32, (pairs,))
+            self._want(call, "positions", positions, i32, (num_axes, T) if num_axes > 1 else (T,))
         if num_axes > 1 and (axes is None or len(axes) != pairs):
             raise ValueError(f"rope_write_kv: axes has to name the axis of each of the {pairs} pairs")
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None:
-                self._want(call, name, w, torch.bfloat16, (self.head_dim,))
+        if q_weight is not None:
+            self._want(call, "q_weight", q_weight, bf16, (self.head_dim,))
+        if k_weight is not None:
+            self._want(call, "k_weight", k_weight, bf16, (self.head_dim,))
         if q_out is None:
-            q_out = torch.empty((T, self.num_q_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
+            q_out = torch.empty((T, heads, self.head_dim), dtype=bf16, device=self.device)
+            out_stride = heads * self.head_dim
         else:
-            self._want_heads(call, "q_out", q_out, T, self.num_q_heads)
+            out_stride = self._heads(call, "q_out", q_out, T, heads)
         if k_out is not None:
-            self._want(call, "k_out", k_out, torch.bfloat16, (T, self.num_kv_heads, self.head_dim))
+            self._want(call, "k_out", k_out, bf16, (T, kv_heads, self.head_dim))
         elif self.dtype == B.EKV_E4M3:
-            k_out = torch.empty((T, self.num_kv_heads, self.head_dim), dtype=torch.bfloat16, device=self.device)
-        rope = B.Rope(2 * pairs, num_axes, B.EKV_ROPE_ADJACENT if interleaved else 0, factor, eps, weight_offset, inv_freq.data_ptr() or None,
-                      positions.data_ptr() or None, bytes(axes) if num_axes > 1 else None, q_weight.data_ptr() if q_weight is not None else None,
+            k_out = torch.empty((T, kv_heads, self.head_dim), dtype=bf16, device=self.device)
+        rope = B.Rope(2 * pairs, num_axes, B.EKV_ROPE_ADJACENT if interleaved else 0, factor, eps, weight_offset, inv_freq.data_ptr(),
+                      positions.data_ptr(), bytes(axes) if num_axes > 1 else None, q_weight.data_ptr() if q_weight is not None else None,
                       k_weight.data_ptr() if k_weight is not None else None)
-        B.ekv_rope_write_kv(self.handle, layer, rope, q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
-                            q_out.data_ptr(), q_out.stride(0), k_out.data_ptr() if k_out is not None else None, slot_mapping.data_ptr(), T,
-                            self._current(stream))
+        B._check(B.load_library().ekv_rope_write_kv(self.handle, layer, rope, q.data_ptr(), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, q_out.data_ptr(), out_stride,
+                            None if k_out is None else k_out.data_ptr(), slot_mapping.data_ptr(), T, self._current(stream)))
         return q_out
 
     def extend_tables(self, new_tokens, seq_lens, block_tables, free_ids, free_cursor, slot_mapping, cu_q_lens,
@@ -216,16 +230,21 @@ class Pool:
 
     # -- scores with a cap, a distance bias, a window, a prefix; batches that share prefixes
     def _check_attn(self, call, q, out, block_tables, seq_lens, T):
-        if block_tables.dim() != 2:
-            B._refuse(call, "block_tables", block_tables, "int32 [requests, max_blocks_per_seq]")
-        n, shape = block_tables.shape[0], (T, self.num_q_heads, self.head_dim)
-        self._want(call, "block_tables", block_tables, torch.int32, tuple(block_tables.shape))
-        self._want(call, "seq_lens", seq_lens, torch.int32, (n,))
-        self._want(call, "q", q, torch.bfloat16, shape)
+        """Shape of the block tables; an output if none is given."""
+        at, shape, i32, bf16, dev = block_tables.shape, (T, self.num_q_heads, self.head_dim), torch.int32, torch.bfloat16, self.device.index
         if out is None:
-            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        self._want(call, "out", out, torch.bfloat16, shape)
-        return out
+            out = torch.empty(shape, dtype=bf16, device=self.device)
+        if not (len(at) == 2 and block_tables.dtype is i32 and seq_lens.dtype is i32 and q.dtype is bf16 and out.dtype is bf16
+                and seq_lens.shape == at[:1] and q.shape == shape and out.shape == shape and block_tables.is_contiguous() and seq_lens.is_contiguous()
+                and q.is_contiguous() and out.is_contiguous() and block_tables.get_device() == dev and seq_lens.get_device() == dev
+                and q.get_device() == dev and out.get_device() == dev):
+            if len(at) != 2:
+                B._refuse(call, "block_tables", block_tables, "int32 [requests, max_blocks_per_seq]")
+            self._want(call, "block_tables", block_tables, i32, at)
+            self._want(call, "seq_lens", seq_lens, i32, at[:1])
+            self._want(call, "q", q, bf16, shape)
+            self._want(call, "out", out, bf16, shape)
+        return at[1], out
 
     def _scores(self, call, n, cap, window, slopes, prefix_lens):
         if slopes is not None:
@@ -234,51 +253,67 @@ class Pool:
             self._want(call, "prefix_lens", prefix_lens, torch.int32, (n,))
         return B.Scores(cap, window, None if slopes is None else slopes.data_ptr(), None if prefix_lens is None else prefix_lens.data_ptr())
 
-    def _parts_workspace(self, need):
-        if self._parts is None or self._parts.numel() < need:
-            self._parts = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return self._parts
+    def _launch(self, call, need, workspace, stream):
+        """call(workspace, its bytes, stream), with the workspace that was handed in.  Without one: a captured call gets memory of its graph, so that
+        two graphs share none; others share one for each stream, which grows when the library says that it is too small."""
+        stream = self._current(stream)
+        if workspace is not None:
+            B._check(call(workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
+        elif torch.cuda.is_current_stream_capturing():
+            own = torch.empty(max(need(), 1), dtype=torch.uint8, device=self.device)
+            B._check(call(own.data_ptr(), own.numel(), stream))
+        else:
+            kept = self._parts.get(stream)
+            st = call(kept[-1].data_ptr(), kept[-1].numel(), stream) if kept else B.Status.ERR_WORKSPACE
+            if st == B.Status.ERR_WORKSPACE:  # (the ones that were too small stay: calls that are under way use them)
+                kept = self._parts.setdefault(stream, [])
+                kept.append(torch.empty(max(need(), 2 * kept[-1].numel() if kept else 1 << 20), dtype=torch.uint8, device=self.device))
+                st = call(kept[-1].data_ptr(), kept[-1].numel(), stream)
+            B._check(st)
 
     def attn_decode_scored(self, layer, q, block_tables, seq_lens, scale, cap=0.0, window=0, slopes=None, prefix_lens=None, out=None,
                            workspace=None, stream=None):
         """attn_decode with x = cap * tanh(x / cap), a bias of -slopes[head] * distance, a window of that many keys, and the keys below prefix_lens
         always seen; any of them."""
-        n = block_tables.shape[0]
-        out = self._check_attn("attn_decode_scored", q, out, block_tables, seq_lens, n)
+        n, lib = seq_lens.shape[0], B.load_library()
+        width, out = self._check_attn("attn_decode_scored", q, out, block_tables, seq_lens, n)
         scores = self._scores("attn_decode_scored", n, cap, window, slopes, prefix_lens)
-        if workspace is None:
-            workspace = self.workspace(n, block_tables.shape[1] * self.block_size)
-        B.ekv_attn_decode_scored(self.handle, layer, q, out, block_tables, seq_lens, scale, scores, workspace, self._current(stream))
+        self._launch(lambda ws, size, stream: lib.ekv_attn_decode_scored(self.handle, layer, q.data_ptr(), out.data_ptr(), block_tables.data_ptr(), width,
+                                                                         seq_lens.data_ptr(), n, scale, scores, ws, size, stream),
+                     lambda: lib.ekv_attn_workspace_bytes(self.handle, n, width * self.block_size), workspace, stream)
         return out
 
     def attn_prefill_chunk_scored(self, layer, q, block_tables, cu_q_lens, cu_q_lens_host, seq_lens, scale, cap=0.0, window=0, slopes=None,
                                   prefix_lens=None, out=None, workspace=None, stream=None):
         """attn_prefill_chunk with scores and masks as in attn_decode_scored, for every row at its own position."""
-        call, n = "attn_prefill_chunk_scored", block_tables.shape[0]
+        call, n, T, lib = "attn_prefill_chunk_scored", seq_lens.shape[0], q.shape[0], B.load_library()
         if cu_q_lens_host.dtype is not torch.int32 or cu_q_lens_host.is_cuda or cu_q_lens_host.numel() != n + 1 or not cu_q_lens_host.is_contiguous():
             B._refuse(call, "cu_q_lens_host", cu_q_lens_host, f"contiguous int32 ({n + 1},) on the host")
         self._want(call, "cu_q_lens", cu_q_lens, torch.int32, (n + 1,))
-        out = self._check_attn(call, q, out, block_tables, seq_lens, q.shape[0])
-        if q.shape[0] < int(cu_q_lens_host[-1]):
-            B._refuse(call, "q", q, f"of at least {int(cu_q_lens_host[-1])} rows")
+        width, out = self._check_attn(call, q, out, block_tables, seq_lens, T)
+        if T < cu_q_lens_host[n].item():
+            B._refuse(call, "q", q, f"of at least {cu_q_lens_host[n].item()} rows")
         scores = self._scores(call, n, cap, window, slopes, prefix_lens)
-        if workspace is None:
-            workspace = self._parts_workspace(B.ekv_attn_prefill_scored_workspace_bytes(self.handle))
-        B.ekv_attn_prefill_chunk_scored(self.handle, layer, q, out, block_tables, cu_q_lens, cu_q_lens_host, seq_lens, scale, scores, workspace,
-                                        self._current(stream))
+        self._launch(lambda ws, size, stream: lib.ekv_attn_prefill_chunk_scored(self.handle, layer, q.data_ptr(), out.data_ptr(), block_tables.data_ptr(), width,
+                                                                                cu_q_lens.data_ptr(), cu_q_lens_host.data_ptr(), seq_lens.data_ptr(), n, scale,
+                                                                                scores, ws, size, stream),
+                     lambda: lib.ekv_attn_prefill_scored_workspace_bytes(self.handle), workspace, stream)
         return out
 
     def attn_decode_shared(self, layer, q, block_tables, seq_lens, group_starts, shared_lens, scale, out=None, workspace=None, stream=None):
         """attn_decode of a batch whose requests share prefixes: group_starts [G+1] and shared_lens [G] are int32 on the host.  The shared
         tokens' blocks stand in every request's table; they are read once a group."""
-        call, n = "attn_decode_shared", block_tables.shape[0]
-        for name, t, size in (("group_starts", group_starts, shared_lens.numel() + 1), ("shared_lens", shared_lens, shared_lens.numel())):
-            if t.dtype is not torch.int32 or t.is_cuda or t.dim() != 1 or t.numel() != size or not t.is_contiguous():
-                B._refuse(call, name, t, f"contiguous int32 ({size},) on the host")
-        out = self._check_attn(call, q, out, block_tables, seq_lens, n)
-        if workspace is None:
-            workspace = self._parts_workspace(B.ekv_attn_decode_shared_workspace_bytes(self.handle, group_starts, shared_lens, block_tables.shape[1]))
-        B.ekv_attn_decode_shared(self.handle, layer, q, out, block_tables, seq_lens, group_starts, shared_lens, scale, workspace, self._current(stream))
+        call, n, G, lib = "attn_decode_shared", seq_lens.shape[0], shared_lens.numel(), B.load_library()
+        if not (group_starts.dtype is shared_lens.dtype is torch.int32 and group_starts.numel() == G + 1 and not group_starts.is_cuda
+                and not shared_lens.is_cuda and group_starts.is_contiguous() and shared_lens.is_contiguous()):
+            for name, t, size in (("group_starts", group_starts, G + 1), ("shared_lens", shared_lens, G)):
+                if t.dtype is not torch.int32 or t.is_cuda or t.numel() != size or not t.is_contiguous():
+                    B._refuse(call, name, t, f"contiguous int32 ({size},) on the host")
+        width, out = self._check_attn(call, q, out, block_tables, seq_lens, n)
+        starts, shared = group_starts.data_ptr(), shared_lens.data_ptr()
+        self._launch(lambda ws, size, stream: lib.ekv_attn_decode_shared(self.handle, layer, q.data_ptr(), out.data_ptr(), block_tables.data_ptr(), width,
+                                                                         seq_lens.data_ptr(), n, starts, shared, G, scale, ws, size, stream),
+                     lambda: lib.ekv_attn_decode_shared_workspace_bytes(self.handle, starts, shared, G, width), workspace, stream)
         return out
 
 
