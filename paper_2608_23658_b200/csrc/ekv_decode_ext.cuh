@@ -13,7 +13,8 @@ namespace ext {
 
 using rows::kMaxGroups;
 
-static constexpr int kWarps = 4, kStages = 3;
+static constexpr int kWarps = 4;
+static constexpr int kStages = 2;  // of a warp; 64 KB in all, so that three CTAs fit an SM: with three stages and two CTAs, 256 short own parts took 89 us for 79
 static constexpr int kBoxBytes = 16 * 128;  // 16 tokens x 64 channels
 
 struct Params {
@@ -56,6 +57,7 @@ __device__ __forceinline__ Span span_of(const Params &p, int b) {
     s.lo = s.pre = s.n_pre = s.skip = 0;
     if (kShared) {
         int g = 0, hi = p.G;
+#pragma unroll 1
         while (hi - g > 1) {
             const int mid = (g + hi) >> 1;
             if (p.start[mid] <= b) g = mid;
@@ -78,7 +80,7 @@ __device__ __forceinline__ Span span_of(const Params &p, int b) {
 __device__ __forceinline__ float finish(float acc, float l) { return l == 0.f ? 0.f : acc / l; }
 
 template <int D, bool kShared, bool kCap, bool kBias>
-__global__ void __launch_bounds__(kWarps * 32, 2) decode_ext_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ Params p) {
+__global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ Params p) {
     constexpr int BOXES = D / 64;
     constexpr int TILE_BYTES = BOXES * kBoxBytes;
     constexpr int STAGE_BYTES = 2 * TILE_BYTES;
@@ -88,6 +90,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) decode_ext_kernel(const __grid
     const int split = blockIdx.x, g = blockIdx.y, b = blockIdx.z;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int r = lane >> 2, c = lane & 3;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the combine pass comes up in the tail of this one
     const Span sp = span_of<kShared>(p, b);
     const int t_begin = split * p.chunk_tokens;
     if (split > 0 && t_begin >= sp.tokens) {  // whole CTA leaves before any barrier exists

@@ -14,14 +14,13 @@
 // Key tiles that no row of the item sees are not read: an item's tiles are those of the prefix and those of the window.
 // A call of few items cuts each one's tiles into `parts`; (m, l, O) of each part go to the workspace.
 //
-//   warp 0        MMA issuer: S = Q K^T (both from shared memory), O += P V (P from TMEM, V MN-major)
-//   warp 1        TMEM allocation
-//   warp 2        item scheduler: the kernel is persistent, a CTA an SM, items by cluster launch control (no word of device memory that two
-//                 launches or replays could share)
+//   warp 0        MMA issuer: S = Q K^T (both from shared memory), O += P V (P from TMEM, V MN-major), the slots by turns
+//   warp 1        TMEM; warp 2: item scheduler: the kernel is persistent, a CTA an SM, items by cluster launch control (no word of device memory that
+//                 two launches or replays could share)
 //   warps 4-7     softmax and write-out of slot 0: a thread a row
 //   warps 8-11    of slot 1
 //   warp 12       TMA producer of K and V tiles
-//   warps 13-15   Q rows into shared memory, and the care of V tiles that not every row sees whole: rows of V at keys nobody sees become 0;
+//   warps 13-15   Q rows into shared memory (by TMA where the group divides a tile), and the care of V tiles that not every row sees whole: rows of V at keys nobody sees become 0;
 //                 values that are not finite at keys that some rows see and others do not are taken out (a weight of 0 does not stop a NaN) and
 //                 given to the rows they belong to after the write-out.
 // All roles run on their own clocks through rings and barriers whose phases are counted over the CTA's whole life, so that an item's Q and
@@ -64,6 +63,7 @@ struct Params {
     int chunk_tiles;            // shared pass: key tiles of a part
     unsigned group_magic;       // ceil(2^32 / group)
     unsigned q_flip;            // 0x80008000 for a negative scale
+    int q_tma;                  // Q tiles come by TMA
     float scale_log2;           // |scale| * log2 e; with a cap: cap * log2 e
     float cap_scale;            // with a cap: |scale| / cap
     int tile_prefix[kMaxGroups + 1];  // items of requests (or groups) before r, if R <= kMaxGroups
@@ -80,14 +80,15 @@ struct Geo {
     static constexpr int kOffQ = 0;
     static constexpr int kOffK = 2 * kTileBytes;
     static constexpr int kOffV = kOffK + kStages * kTileBytes;
-    static constexpr int kOffBar = kOffV + kStages * kTileBytes;
+    static constexpr int kOffStage = kOffV + kStages * kTileBytes;  // of the write-out: [32 rows][128 B] a warp
+    static constexpr int kStageBytes = 32 * 128;
+    static constexpr int kOffBar = kOffStage + 8 * kStageBytes;
     enum Bar { Q_FULL = 0, Q_EMPTY = 1, K_FULL = 2, K_EMPTY = 4, V_RAW = 6, V_FULL = 8, V_EMPTY = 10, S_READY = 12, P_PART = 14, P_READY = 16,
                O_READY = 18, O_FREE = 20, MERGE = 22, ITEM_FULL = 23, ITEM_EMPTY = ITEM_FULL + kRing, WANT = ITEM_EMPTY + kRing, NEXT, DRAIN, NBAR };
     __device__ static __forceinline__ uint32_t arrivals(int bar) {
         if (bar == Q_FULL || (bar >= V_FULL && bar < V_EMPTY)) return 3;               // warps 13-15
-        if ((bar >= P_PART && bar < O_READY) || bar == MERGE) return 128;              // the threads of a slot
-        if (bar >= O_FREE && bar < MERGE) return 4;                                    // the warps that read the accumulator
-        if (bar >= ITEM_EMPTY && bar < WANT) return 13;                                // every warp that reads items
+        if ((bar >= P_PART && bar < O_READY) || (bar >= O_FREE && bar <= MERGE)) return 4;  // a slot's warps
+        if (bar >= ITEM_EMPTY && bar < WANT) return 13;                                      // every warp that reads items
         return 1;
     }
     static constexpr int kOffFlags = kOffBar + 8 * NBAR;                  // abort flag, TMEM address, 4 masks of invalid blocks
@@ -115,10 +116,16 @@ struct Smem {
     __device__ __forceinline__ float2 *merge() const { return (float2 *)(ptr + G::kOffMerge); }
 };
 
+// Bounded wait of a whole warp, as in ekv_prefill_tc.cuh: one poll and a vote, then a small polling loop.
 template <int D>
 __device__ __forceinline__ bool wait_warp(const Smem<D> &sh, int bar, uint32_t parity) {
     if (__all_sync(0xffffffffu, mbar_try_wait(sh.bar(bar), parity & 1u))) return true;
     return __all_sync(0xffffffffu, mbar_wait_polls(sh.bar(bar), parity & 1u, sh.base + Geo<D>::kOffFlags, tc::kPollLimit));
+}
+// keeps the compiler from making a copy of a loop for each value of a condition that the loop does not change
+__device__ __forceinline__ int opaque(int v) {
+    asm volatile("" : "+r"(v));
+    return v;
 }
 
 // An item as its roles see it: 14 numbers in a slot of the ring.
@@ -149,6 +156,7 @@ __device__ __forceinline__ long long spread_first(const Params &p, int r) { retu
 __device__ __forceinline__ int spread_request(const Params &p, int idx) {
     const int lane = threadIdx.x & 31;
     int lo = 0, hi = p.R;  // first(lo) <= idx < first(hi)
+#pragma unroll 1
     while (hi - lo > 1) {
         const int step = (hi - lo + 31) / 32, at = min(lo + (lane + 1) * step, hi);
         const unsigned below = __ballot_sync(0xffffffffu, at < hi && spread_first(p, at) <= idx);
@@ -159,17 +167,16 @@ __device__ __forceinline__ int spread_request(const Params &p, int idx) {
     return lo;
 }
 
-// tanh on [-1.2, 1.2] as y * P(y^2), a minimax polynomial fitted to the relative error (4e-7; in fp32 5e-7 in all); beyond, from the definition
-static constexpr float kTanhFast = 1.2f;
+// tanh on [-1, 1] as y * P(y^2), a minimax polynomial fitted to the relative error (6e-7, in fp32 too); beyond, from the definition
+static constexpr float kTanhFast = 1.f;
 __device__ __forceinline__ float2 tanh2_fast(float2 y) {
+    auto two = [](float c) { return make_float2(c, c); };
     const float2 u = __fmul2_rn(y, y);
-    float2 r = make_float2(0.00065901212f, 0.00065901212f);
-    r = __ffma2_rn(r, u, make_float2(-0.00493616471f, -0.00493616471f));
-    r = __ffma2_rn(r, u, make_float2(0.01870737038f, 0.01870737038f));
-    r = __ffma2_rn(r, u, make_float2(-0.05254373699f, -0.05254373699f));
-    r = __ffma2_rn(r, u, make_float2(0.13301366568f, 0.13301366568f));
-    r = __ffma2_rn(r, u, make_float2(-0.33330568671f, -0.33330568671f));
-    r = __ffma2_rn(r, u, make_float2(0.99999958277f, 0.99999958277f));
+    float2 r = __ffma2_rn(two(-0.00306705921f), u, two(0.01674311235f));
+    r = __ffma2_rn(r, u, two(-0.05160567164f));
+    r = __ffma2_rn(r, u, two(0.13281433284f));
+    r = __ffma2_rn(r, u, two(-0.33329042792f));
+    r = __ffma2_rn(r, u, two(0.99999940395f));
     return __fmul2_rn(r, y);
 }
 // 1 - 2 / (e^2y + 1): absolute error of some 2^-23; +-1 at +-infinity
@@ -177,6 +184,14 @@ __device__ __forceinline__ float tanh_any(float y) {
     const float e = fast_exp2(y * 2.8853900817779268f);
     return 1.f - __fdividef(2.f, e + 1.f);
 }
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// bits 0 .. k - 1 (k in any range)
+__device__ __forceinline__ unsigned below(int k) { return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u; }
 
 // Values that are not finite at keys that not all rows of the item see: those of the keys a row does see are added to its result (weights are
 // positive: an infinity stays one, NaN and opposite infinities give NaN).  A thread a row; hardly ever called.
@@ -200,7 +215,7 @@ __device__ __noinline__ void add_nonfinite(const Params &p, const uint8_t *cache
 
 template <int D, int kMode, bool kCap, bool kBias>
 __global__ void __launch_bounds__(kThreads, 1)
-rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ Params p, const uint8_t *cache, long long block_stride) {
+rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ Params p, const uint8_t *cache, long long block_stride) {
     using G = Geo<D>;
     extern __shared__ uint8_t smem_raw[];
     Smem<D> sh;
@@ -212,22 +227,28 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = p.group;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // a launch that reads the parts comes up in the tail of this one
-    if (threadIdx.x == 64) {
-        prefetch_tensormap(&kvmap);
-#pragma unroll 1
-        for (int i = 0; i < G::NBAR; ++i) mbar_init(sh.bar(i), G::arrivals(i));
+    // Set-up, side by side: barriers, TMEM, and (in the scheduler's loop) the first item.
+    if (warp == 3) {
+        if (lane == 0) {
+            prefetch_tensormap(&kvmap);
+            if (p.q_tma) prefetch_tensormap(&qmap);
+            *sh.abort_flag() = 0;
+        }
+        for (int i = lane; i < G::NBAR; i += 32) mbar_init(sh.bar(i), G::arrivals(i));
         mbar_fence_init();
-        *sh.abort_flag() = 0;
     }
     if (warp == 1) {
         cp::tcgen05_alloc(cp::cta_group_1, sh.tmem_slot(), 512);
         cp::tcgen05_relinquish_alloc_permit(cp::cta_group_1);
     }
+    auto set_up = [&]() {  // by every warp, once
+        fence_before();
+        __syncthreads();
+        fence_after();
+    };
     auto by_group = [&](int r) { return group == 1 ? r : (int)__umulhi((unsigned)r, p.group_magic); };
-    fence_before();
-    __syncthreads();
-    fence_after();
-    const uint32_t tmem = *sh.tmem_slot();
+    if (warp != 2) set_up();
+    const uint32_t tmem = warp != 2 ? *sh.tmem_slot() : 0u;
 
     auto wait = [&](int bar, uint32_t parity) { return wait_warp<D>(sh, bar, parity); };
     // the CTA's n-th item, 1 = to work on, 0 = the list has ended, -1 = given up
@@ -247,12 +268,13 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
     uint32_t issued = 0;  // producer: tiles under way or done
 
     if (warp < 4 || warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp != 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 2) {
         // =========================== item scheduler ===========================
         bool may_draw = true;
         uint32_t draws = 0;
-        auto draw = [&]() {  // number of a CTA that will not start now, or -1
+        int in = blockIdx.x;  // kv-head and part of the item; its rank is the other coordinate of the grid
+        auto draw = [&]() {  // rank (and kv-head, part) of a CTA that will not start now, or -1
             if (!may_draw) return -1;
             if (lane == 0) {
                 mbar_expect_tx(sh.bar(G::NEXT), 16);
@@ -269,15 +291,17 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
             fence_proxy_async_smem();  // read before the next answer is written there
             __syncwarp();
             may_draw = cp::clusterlaunchcontrol_query_cancel_is_canceled(response);  // nothing left: no further question is allowed
-            return may_draw ? cp::clusterlaunchcontrol_query_cancel_get_first_ctaid_x<int>(response) : -1;
+            in = may_draw ? cp::clusterlaunchcontrol_query_cancel_get_first_ctaid_x<int>(response) : 0;
+            return may_draw ? cp::clusterlaunchcontrol_query_cancel_get_first_ctaid_y<int>(response) : -1;
         };
         // Items are listed heaviest (latest) first, the kv-heads and parts of one next to each other.  false: nothing to post for this number
-        auto post = [&](int item, volatile int *slot) {
-            const int per = kMode == kShared ? p.num_kv_heads : p.num_kv_heads * p.parts;
-            const int rank = item / per, in = item - rank * per, g = in % p.num_kv_heads, idx = p.tiles - 1 - rank;
-            int part = in / p.num_kv_heads, req, q0, c_r, first;
+        auto post = [&](int rank, volatile int *slot) {
+            const int idx = p.tiles - 1 - rank;
+            int g = in, part = 0, req, q0, next_q0, first, L = 0, prefix = 0;
+            if (kMode == kScored && p.parts > 1) part = in / p.num_kv_heads, g = in - part * p.num_kv_heads;
             if (kMode == kShared || p.R <= kMaxGroups) {
                 int lo = 0, hi = p.R;
+#pragma unroll 1
                 while (hi - lo > 1) {
                     const int mid = (lo + hi) >> 1;
                     if (p.tile_prefix[mid] <= idx) lo = mid;
@@ -288,26 +312,29 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
                 req = spread_request(p, idx);
                 first = (int)spread_first(p, req);
             }
+            if (kMode == kShared) {
+                q0 = p.start[req], next_q0 = p.start[req + 1];
+            } else {  // all loads at once
+                q0 = p.cu_q_lens[req], next_q0 = p.cu_q_lens[req + 1], L = p.seq_lens[req];
+                if (p.prefix_lens) prefix = p.prefix_lens[req];
+            }
+            const int c_r = next_q0 - q0;
             int row0, past, pre, kv_end, n_pre, skip, tile0, n_tiles;
             if (kMode == kShared) {
                 const int all = (p.shared[req] + kBN - 1) / kBN, ns = (all + p.chunk_tiles - 1) / p.chunk_tiles, tile = (idx - first) / ns;
                 part = (idx - first) - tile * ns;
                 row0 = tile * kItemRows;
-                q0 = p.start[req];
-                c_r = p.start[req + 1] - q0;
                 past = 0, pre = kv_end = p.shared[req], n_pre = all, skip = 0;
                 tile0 = part * p.chunk_tiles;
                 n_tiles = min(p.chunk_tiles, all - tile0);
                 req = q0;  // the first request's table names the shared blocks
             } else {
-                q0 = p.cu_q_lens[req];
-                c_r = p.cu_q_lens[req + 1] - q0;
                 row0 = (idx - first) * kItemRows;
             }
             const int rows = min(kItemRows, c_r * group - row0);
             if (rows <= 0) return false;
             if (kMode == kScored) {
-                const int L = min(p.seq_lens[req], p.max_blocks * 16);
+                L = min(L, p.max_blocks * 16);
                 past = L - c_r;
                 if (past < 0) {  // malformed request: zero rows, latch
                     if (lane == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
@@ -323,7 +350,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
                     return false;
                 }
                 const int p0 = past + by_group(row0), p1 = past + by_group(row0 + rows - 1);
-                pre = p.prefix_lens ? max(0, min(p.prefix_lens[req], L)) : 0;
+                pre = max(0, min(prefix, L));
                 kv_end = max(p1 + 1, pre);
                 n_pre = (pre + kBN - 1) / kBN;
                 skip = max(0, low_of(p0) / kBN - n_pre);
@@ -337,16 +364,24 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
             }
             return true;
         };
-        int item = blockIdx.x;
+        int item = blockIdx.y;
 #pragma unroll 1
         for (uint32_t n = 0;; ++n) {
             volatile int *slot = sh.item(n);
-            if (n >= kRing && !wait(G::ITEM_EMPTY + (int)(n % kRing), n / kRing - 1)) break;
-            // not before the producer has come to the last tiles of the item before: an item drawn earlier would wait for this CTA while another
-            // stands idle
-            if (n > 0 && !wait(G::WANT, n - 1)) break;
-            if (n > 0) item = draw();
-            while (item >= 0 && !post(item, slot)) item = draw();
+            // not before the producer has come to the last four tiles of the item before: an item drawn earlier would wait for this CTA while another
+            // stands idle (drawing and decoding one takes some 4000 cycles)
+            if (n > 0) (void)wait(G::WANT, n - 1);
+            if (n >= kRing) (void)wait(G::ITEM_EMPTY + (int)(n % kRing), n / kRing - 1);
+            for (bool ask = n > 0;; ask = true) {
+                if (ask) item = draw();
+                // (a wait ran out: the CTAs that have not started, and would wait as long, are not to; the list ends when all are drawn)
+                const bool done = item < 0 || ((!ask || !*sh.abort_flag()) && post(item, slot));
+                if (n == 0 && !ask) {  // beside the rest of the set-up
+                    set_up();
+                    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+                }
+                if (done) break;
+            }
             if (lane == 0) {
                 slot[0] = item >= 0;
                 __threadfence_block();
@@ -355,8 +390,6 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
             __syncwarp();
             if (item < 0) break;
         }
-        if (*sh.abort_flag())  // a wait ran out: the CTAs that have not started, and would wait as long, are not to
-            while (draw() >= 0) {}
     } else if (warp == 0) {
         // =========================== MMA issuer ===========================
         constexpr uint64_t kHi = (uint64_t)tc::kDescHi << 32;
@@ -371,24 +404,26 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
             Item it;
             if (fetch(n, it) <= 0) break;
             const int n_tiles = it.n_tiles;
-            const int sh2 = it.rows > kBM ? 1 : 0;  // steps a tile takes: one for each slot, or one
+            const int sh2 = opaque(it.rows > kBM ? 1 : 0);  // steps a tile takes: one for each slot, or one
             release(n);
             ok = wait(G::Q_FULL, n);
             if (!ok) break;
-            // Steps alternate between the slots: step u is P V of slot x = u & 1 on its key tile number i = u >> 1, and Q K^T for the slot's next
-            // one; steps -2 and -1 only bring the first scores.
+            // Steps alternate between the slots, so that the softmax of one runs beside the MMAs of the other: step u is P V of slot x = u & 1 on
+            // its key tile number i = u >> 1, and Q K^T for the slot's next one; steps -2 and -1 only bring the first scores.
             const int step_max = n_tiles << sh2;
 #pragma unroll 1
             for (int u = -2; u < step_max && ok; ++u) {
                 const int x = u & 1, i = u >> 1;
                 const int j = u >> sh2, jn = (u + 2) >> sh2;  // the part's key tiles of the two
                 const uint32_t s = (t0 + (uint32_t)j) & 1u, s1 = (t0 + (uint32_t)jn) & 1u;
-                const bool pv = u >= 0, more = jn < n_tiles, closes = x >= sh2;  // closes: the last slot to read these stages
+                const int pv = opaque(u >= 0), more = opaque(jn < n_tiles), closes = opaque(x >= sh2), opens = opaque(x == 0 || sh2 == 0);  // the last and the first slot to read these stages
                 const uint32_t t_s = tmem + 128 * x, t_o = tmem + 256 + 128 * x;
                 const uint64_t vd = v_d + s * (G::kTileBytes >> 4);
                 if (!pv && !more) continue;
+                // (what comes early is waited for first, and once: a wait takes some 300 cycles beside busy special functions)
+                if (more && opens) ok = wait(G::K_FULL + (int)s1, (t0 + (uint32_t)jn) >> 1);
                 if (pv) {
-                    ok = wait(G::V_FULL + (int)s, (t0 + (uint32_t)j) >> 1);
+                    if (ok && opens) ok = wait(G::V_FULL + (int)s, (t0 + (uint32_t)j) >> 1);
                     // the slot's accumulator of the item before has been read
                     if (ok && i == 0 && co[x] > 0) ok = wait(G::O_FREE + x, co[x] - 1);
                     if (ok) ok = wait(G::P_PART + x, cs[x] + (uint32_t)i);
@@ -396,13 +431,11 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
                     fence_after();
                     if (tc::elect_one()) {  // keys 0..95 while the softmax warps finish the rest
 #pragma unroll
-                        for (int k = 0; k < tc::kPartSteps; ++k)
-                            tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, (i > 0 || k > 0) ? 1u : 0u);
+                        for (int k = 0; k < tc::kPartSteps; ++k) tc::mma_ts(t_o, t_s + 8 * k, vd + ((k * 2048) >> 4), G::kIdescPV, (i > 0 || k > 0) ? 1u : 0u);
                     }
                     __syncwarp();
                     ok = wait(G::P_READY + x, cs[x] + (uint32_t)i);
                 }
-                if (ok && more) ok = wait(G::K_FULL + (int)s1, (t0 + (uint32_t)jn) >> 1);
                 if (!ok) break;
                 fence_after();
                 if (tc::elect_one()) {
@@ -419,9 +452,9 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
                             const uint32_t off = ((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4;
                             tc::mma_ss(t_s, qd + off, kd + off, G::kIdescQK, k > 0 ? 1u : 0u);
                         }
+                        tc::mma_commit_one(sh.bar(G::S_READY + x));  // the slot's next scores, and its O up to this tile
                         if (closes) tc::mma_commit_one(sh.bar(G::K_EMPTY + (int)s1));
                         if (closes && jn + 1 == n_tiles) tc::mma_commit_one(sh.bar(G::Q_EMPTY));  // the item's last scores
-                        tc::mma_commit_one(sh.bar(G::S_READY + x));  // the slot's next scores, and its O up to this tile
                     }
                 }
                 __syncwarp();
@@ -469,7 +502,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
                 const int b = lane & (8 * G::kHalves - 1), blk = b / G::kHalves, half = b % G::kHalves;
                 const int my_id = __shfl_sync(0xffffffffu, id, blk);
                 const uint32_t s = issued & 1u;
-                if (j == max(0, it.n_tiles - 2) && lane == 0) mbar_arrive(sh.bar(G::WANT));
+                if (j == max(0, it.n_tiles - 4) && lane == 0) mbar_arrive(sh.bar(G::WANT));
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv) {
                     const int full = (kv ? G::V_RAW : G::K_FULL) + (int)s, empty = (kv ? G::V_EMPTY : G::K_EMPTY) + (int)s;
@@ -495,29 +528,42 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
     } else if (warp >= 13) {
         // =========================== Q rows, and the care of V tiles ===========================
         constexpr int kPieces = D / 8;  // 16-byte pieces of a row
-        const int ct = threadIdx.x - 13 * 32;
+        const int ct = threadIdx.x - 13 * 32;  // of 96
         uint32_t t = 0;
         bool ok = true;
         auto load_q = [&](const Item &it) {
-            const int pos0 = by_group(it.row0), head0 = it.row0 - pos0 * group;
+            const int pos0 = by_group(it.row0), tiles = it.rows > kBM ? 2 : 1;
+            if (p.q_tma) {  // (rows behind the item's last one are some other request's: nobody looks at their results)
+                if (lane == 0 && warp == 13) mbar_expect_tx(sh.bar(G::Q_FULL), tiles * G::kTileBytes);
+                else if (lane == 0) mbar_arrive(sh.bar(G::Q_FULL));
+                __syncwarp();
+                if (warp == 13 && lane < tiles * G::kHalves) {
+                    const int x = lane / G::kHalves, half = lane % G::kHalves;
+                    tma_load_3d(sh.base + G::kOffQ + x * G::kTileBytes + half * kHalfBytes, &qmap, 64 * half, it.g * group, it.q0 + pos0 + x * (kBM / group),
+                                sh.bar(G::Q_FULL));
+                }
+                return;
+            }
+            const int head0 = it.row0 - pos0 * group;
             const __nv_bfloat16 *src = p.q + ((size_t)(it.q0 + pos0) * p.num_q_heads + (size_t)it.g * group) * D;
-            const int n_rows = it.rows > kBM ? kItemRows : kBM;
-#pragma unroll 4
-            for (int i = ct; i < n_rows * kPieces; i += 96) {
+            auto place = [&](int i) {  // of piece i of the tiles
+                const int r = i / kPieces, c = i % kPieces;
+                return sh.base + G::kOffQ + (r >> 7) * G::kTileBytes + (c >> 3) * kHalfBytes + (r & 127) * 128 + (((c ^ r) & 7) << 4);
+            };
+#pragma unroll 2
+            for (int i = ct; i < tiles * kBM * kPieces; i += 96) {
                 const int r = i / kPieces, c = i % kPieces;
                 const bool there = r < it.rows;
                 const int h = head0 + (there ? r : 0);
-                const uint32_t to = sh.base + G::kOffQ + (r >> 7) * G::kTileBytes + (c >> 3) * kHalfBytes + (r & 127) * 128 + (((c ^ r) & 7) << 4);
-                cp_async_16(to, src + (size_t)(by_group(h) * (p.num_q_heads - group) + h) * D + c * 8, there ? 16u : 0u);
+                cp_async_16(place(i), src + (size_t)(by_group(h) * (p.num_q_heads - group) + h) * D + c * 8, there ? 16u : 0u);
             }
             cp_async_commit();
             cp_async_wait_all();
             if (p.q_flip) {  // a negative scale: its sign goes into Q
-                for (int i = ct; i < n_rows * kPieces; i += 96) {
-                    const int r = i / kPieces, c = i % kPieces;
-                    const uint32_t to = sh.base + G::kOffQ + (r >> 7) * G::kTileBytes + (c >> 3) * kHalfBytes + (r & 127) * 128 + (((c ^ r) & 7) << 4);
-                    const uint4 v = lds_16(to);
-                    sts_16(to, make_uint4(v.x ^ p.q_flip, v.y ^ p.q_flip, v.z ^ p.q_flip, v.w ^ p.q_flip));
+#pragma unroll 1
+                for (int i = ct; i < tiles * kBM * kPieces; i += 96) {
+                    const uint4 v = lds_16(place(i));
+                    sts_16(place(i), make_uint4(v.x ^ p.q_flip, v.y ^ p.q_flip, v.z ^ p.q_flip, v.w ^ p.q_flip));
                 }
             }
             fence_proxy_async_smem();
@@ -538,18 +584,19 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
                 ok = wait(G::V_RAW + (int)s, t >> 1);
                 if (!ok) break;
                 const int key0 = first_key(it, j), bad = *sh.bad_mask(t);
-                const bool whole = key0 + kBN <= it.pre || (kMode == kScored && key0 + kBN - 1 <= p0 && key0 >= lo1);
-                if (!whole || bad) {
-                    uint8_t *tile = sh.ptr + G::kOffV + s * G::kTileBytes;
+                uint8_t *tile = sh.ptr + G::kOffV + s * G::kTileBytes;
+                auto piece = [&](int i) { return reinterpret_cast<uint4 *>(tile + (i % kPieces >> 3) * kHalfBytes + (i / kPieces) * 128 + (i & 7) * 16); };
+                bool touched = false;
+                if (kMode == kScored && !(key0 + kBN <= it.pre || (key0 + kBN - 1 <= p0 && key0 >= lo1))) {
+                    // keys that some rows see and others do not: at the window's lower edge, and from the first row's position on
                     bool seen_nan = false;
+                    const int upper = max(p0 + 1, max(lo1, it.pre));
 #pragma unroll 1
-                    for (int i = ct; i < kBN * kPieces; i += 96) {
-                        const int r = i / kPieces, c = i % kPieces, key = key0 + r;
-                        uint4 *at = reinterpret_cast<uint4 *>(tile + (c >> 3) * kHalfBytes + r * 128 + (c & 7) * 16);
-                        if (key >= it.kv_end || ((bad >> (r >> 4)) & 1)) {
-                            *at = make_uint4(0u, 0u, 0u, 0u);  // nobody's: a slot that was never written may hold anything
-                        } else if (kMode == kScored && key >= it.pre && !(key <= p0 && key >= lo1)) {
-                            const uint4 v = *at;
+                    for (int edge = 0; edge < 2; ++edge) {
+                        const int from = max(0, (edge ? upper : it.pre) - key0), to = min(kBN, (edge ? it.kv_end : lo1) - key0);  // rows of the tile
+#pragma unroll 2
+                        for (int i = from * kPieces + ct; i < to * kPieces; i += 96) {
+                            const uint4 v = *piece(i);
                             uint32_t w[4] = {v.x, v.y, v.z, v.w}, any = 0;
 #pragma unroll
                             for (int k = 0; k < 4; ++k) any |= ((w[k] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
@@ -559,14 +606,24 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
                                     if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
                                     if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0x0000ffffu;
                                 }
-                                *at = make_uint4(w[0], w[1], w[2], w[3]);
+                                *piece(i) = make_uint4(w[0], w[1], w[2], w[3]);
                                 seen_nan = true;
                             }
                         }
                     }
                     if (seen_nan) sh.item(n)[kItemNan] = 1;
-                    fence_proxy_async_smem();
+                    touched = true;
                 }
+                if (key0 + kBN > it.kv_end || bad) {  // keys that nobody sees: a slot that was never written may hold anything
+                    const int end = max(0, it.kv_end - key0);
+#pragma unroll 2
+                    for (int i = (bad ? 0 : end * kPieces) + ct; i < kBN * kPieces; i += 96) {
+                        const int r = i / kPieces;
+                        if (r >= end || ((bad >> (r >> 4)) & 1)) *piece(i) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    touched = true;
+                }
+                if (touched) fence_proxy_async_smem();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(sh.bar(G::V_FULL + (int)s));
             }
@@ -583,10 +640,11 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
         const uint32_t t_o = tmem + ((uint32_t)wrow0 << 16) + 256 + 128 * x;
         uint32_t t0 = 0, cs = 0, co = 0, cm = 0;  // tiles of the items before, those of this slot, items in which it had any, merges
         bool ok = true;
-        auto publish = [&](int bar) {  // this thread's row of P is in TMEM
+        auto publish = [&](int bar) {  // this warp's rows of P are in TMEM
             cp::tcgen05_wait_st();
             fence_before();
-            mbar_arrive(sh.bar(bar));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.bar(bar));
         };
 #pragma unroll 1
         for (uint32_t n = 0; ok; ++n) {
@@ -595,6 +653,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
             const bool by_rows = it.rows > kBM;
             const int rx = by_rows ? x : 0;                                    // its row tile
             const int n_it = by_rows ? it.n_tiles : (it.n_tiles - x + 1) >> 1;  // its key tiles
+            const int dj = opaque(by_rows ? 0 : 1), j0 = opaque(by_rows ? 0 : x);  // the i-th of them is the part's tile (i << dj) + j0
             const int r_item = min(rx * kBM + row, it.rows - 1);
             const int pos_in = by_group(it.row0 + r_item);
             const int lim = it.past + pos_in, lo = kMode == kShared ? 0 : low_of(lim);  // the row's window: keys lo .. lim
@@ -608,7 +667,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
                 ok = wait(G::S_READY + x, cs + (uint32_t)i);
                 if (!ok) break;
                 fence_after();
-                const int j = by_rows ? i : 2 * i + x;  // the part's key tile
+                const int j = (i << dj) + j0;
                 const int key0 = first_key(it, j);
                 const int bad = *sh.bad_mask(t0 + (uint32_t)j);
                 float sv[128];
@@ -668,8 +727,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
 #pragma unroll
                     for (int cc = 0; cc < 4; ++cc) {
                         const int c0 = key0 + 32 * cc;
-                        auto below = [&](int k) { return k >= 32 ? 0xffffffffu : k <= 0 ? 0u : (1u << k) - 1u; };  // columns of keys < c0 + k
-                        const unsigned b2 = ((unsigned)bad >> (2 * cc)) & 3u;
+                                                const unsigned b2 = ((unsigned)bad >> (2 * cc)) & 3u;
                         const unsigned broken = ((b2 & 1u) ? 0x0000ffffu : 0u) | ((b2 & 2u) ? 0xffff0000u : 0u);
                         unsigned vis = below(it.pre - c0);
                         if (kMode == kScored) vis |= below(lim + 1 - c0) & ~below(lo - c0);
@@ -740,13 +798,14 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
             fence_after();  // every MMA that wrote the slot's O has completed
 
             // ---- slots that share rows: the second one leaves its (m, l) in shared memory, the first one takes both accumulators
-            const bool merge = !by_rows && it.n_tiles > 1;
+            const int merge = opaque(!by_rows && it.n_tiles > 1);
             float w0 = 1.f, w1 = 0.f;
             if (merge) {
                 if (x == 1) {
                     sh.merge()[row] = make_float2(m_run, l_run);
                     fence_before();
-                    mbar_arrive(sh.bar(G::MERGE));
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(sh.bar(G::MERGE));
                 } else {
                     if (!(ok = wait(G::MERGE, cm))) break;
                     fence_after();
@@ -762,53 +821,70 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ P
             if (by_rows || x == 0) {
                 const bool there = rx * kBM + row < it.rows;
                 const size_t at = (size_t)(it.q0 + pos_in) * p.num_q_heads + (size_t)(it.g * group + it.row0 + r_item - pos_in * group);
-                const bool to_parts = kMode == kShared || p.parts > 1;
+                const int to_parts = opaque(kMode == kShared || p.parts > 1);
                 const float inv = to_parts ? 1.f : (l_run == 0.f ? 0.f : 1.f / l_run);
                 w0 *= inv, w1 *= inv;
                 __nv_bfloat16 *out = p.out + at * D;
                 float *part_o = p.part_o + (at * p.parts + it.part) * D;
+                // 128 bytes of a row at a time -- 64 channels of bf16, or 32 of a part's fp32 -- go through shared memory, so that eight lanes write
+                // a row's 128 bytes together.  (A thread a row, straight from the registers, took four times as long.)
+                uint8_t *stage = sh.ptr + G::kOffStage + (warp - 4) * G::kStageBytes;
+                const int piece = lane & 7, sub = lane >> 3;
+                uint8_t *const to = to_parts ? reinterpret_cast<uint8_t *>(p.part_o) : reinterpret_cast<uint8_t *>(p.out);
+                const int row_bytes = to_parts ? 4 * D : 2 * D, out_parts = to_parts ? p.parts : 1, out_part = to_parts ? it.part : 0;
+                auto put = [&](int i, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+                    *reinterpret_cast<uint4 *>(stage + lane * 128 + ((i ^ (lane & 7)) << 4)) = make_uint4(a, b, c, d);
+                };
+                const int chunks = n_it > 0 ? D / 32 : 0;
 #pragma unroll 1
-                for (int cc = 0; cc < D / 32 && n_it > 0; ++cc) {
+                for (int ch = 0; ch < chunks; ++ch) {  // 32 channels of the result
                     float ov[32];
-                    tc::tmem_ld32(ov, t_o + 32 * cc);
+                    tc::tmem_ld32(ov, t_o + 32 * ch);
                     if (merge) {
                         float o1[32];
-                        tc::tmem_ld32(o1, t_o + 128 + 32 * cc);
+                        tc::tmem_ld32(o1, t_o + 128 + 32 * ch);
 #pragma unroll
                         for (int c = 0; c < 32; ++c) ov[c] = ov[c] * w0 + o1[c] * w1;
                     } else {
 #pragma unroll
                         for (int c = 0; c < 32; ++c) ov[c] *= w0;
                     }
-                    if (there && to_parts) {
-#pragma unroll
-                        for (int c = 0; c < 32; c += 8) {
-                            uint32_t(&w)[32] = reinterpret_cast<uint32_t(&)[32]>(ov);
-                            st_global_32(part_o + 32 * cc + c, make_uint4(w[c], w[c + 1], w[c + 2], w[c + 3]), make_uint4(w[c + 4], w[c + 5], w[c + 6], w[c + 7]));
-                        }
-                    } else if (there) {
-#pragma unroll
-                        for (int c = 0; c < 32; c += 16) {
-                            uint4 a, b;
-                            a.x = pack_bf16x2(ov[c], ov[c + 1]), a.y = pack_bf16x2(ov[c + 2], ov[c + 3]);
-                            a.z = pack_bf16x2(ov[c + 4], ov[c + 5]), a.w = pack_bf16x2(ov[c + 6], ov[c + 7]);
-                            b.x = pack_bf16x2(ov[c + 8], ov[c + 9]), b.y = pack_bf16x2(ov[c + 10], ov[c + 11]);
-                            b.z = pack_bf16x2(ov[c + 12], ov[c + 13]), b.w = pack_bf16x2(ov[c + 14], ov[c + 15]);
-                            uint4 *to = reinterpret_cast<uint4 *>(out + 32 * cc + c);
-                            to[0] = a;
-                            to[1] = b;
+                    if (ch == chunks - 1) {  // the accumulator has been read
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive(sh.bar(G::O_FREE + x));
+                            if (merge) mbar_arrive(sh.bar(G::O_FREE + 1));
                         }
                     }
+                    if (to_parts) {
+                        uint32_t(&w)[32] = reinterpret_cast<uint32_t(&)[32]>(ov);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) put(i, w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            put((ch & 1) * 4 + i, pack_bf16x2(ov[8 * i], ov[8 * i + 1]), pack_bf16x2(ov[8 * i + 2], ov[8 * i + 3]),
+                                pack_bf16x2(ov[8 * i + 4], ov[8 * i + 5]), pack_bf16x2(ov[8 * i + 6], ov[8 * i + 7]));
+                        if ((ch & 1) == 0) continue;
+                    }
+                    __syncwarp();
+                    uint4 v[8];  // all reads at once: one takes some 300 cycles beside busy special functions
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const uint4 *>(stage + (4 * k + sub) * 128 + ((piece ^ ((4 * k + sub) & 7)) << 4));
+                    uint8_t *const at_piece = to + (to_parts ? ch : ch >> 1) * 128 + piece * 16;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int rr = rx * kBM + wrow0 + 4 * k + sub;
+                        const int pos = by_group(it.row0 + rr);
+                        const int i = (it.q0 + pos) * p.num_q_heads + it.g * group + it.row0 + rr - pos * group;  // (T * heads < 2^31)
+                        if (rr < it.rows) *reinterpret_cast<uint4 *>(at_piece + ((size_t)i * out_parts + out_part) * row_bytes) = v[k];
+                    }
+                    __syncwarp();
                 }
                 if (n_it == 0 && there && !to_parts)
                     for (int c = 0; c < D / 8; ++c) reinterpret_cast<uint4 *>(out)[c] = make_uint4(0u, 0u, 0u, 0u);
                 if (there && to_parts) p.part_ml[at * p.parts + it.part] = make_float2(n_it > 0 ? m_run : -INFINITY, n_it > 0 ? l_run : 0.f);
-                fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (n_it > 0) mbar_arrive(sh.bar(G::O_FREE + x));
-                    if (merge) mbar_arrive(sh.bar(G::O_FREE + 1));
-                }
                 if (kMode == kScored && sh.item(n)[kItemNan] && there) {
                     const int p0 = it.past + by_group(it.row0), lo1 = low_of(it.past + by_group(it.row0 + it.rows - 1));
                     auto add = [&](int c, float v) {

@@ -37,11 +37,14 @@ static cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, int byte
 }
 
 template <int D, int kMode, bool kCap, bool kBias>
-static cudaError_t launch_rows(ekv_pool *pool, int layer, const rows::Params &p, unsigned items, cudaStream_t stream) {
+static cudaError_t launch_rows(ekv_pool *pool, int layer, const rows::Params &p, long long q_rows, cudaStream_t stream) {
     static bool done[64] = {false};
     cudaError_t e = ready(rows::rows_kernel<D, kMode, kCap, kBias>, rows::Geo<D>::kSmemBytes, pool->desc.device, done);
     if (e != cudaSuccess) return e;
-    return launch(rows::rows_kernel<D, kMode, kCap, kBias>, dim3(items), rows::kThreads, rows::Geo<D>::kSmemBytes, false, stream, pool->kv_map[layer], p,
+    // Q by TMA: a box of all heads of a group x as many tokens as make a tile
+    CUtensorMap qmap = pool->kv_map[layer];
+    if (p.q_tma && encode_q_map(p.q, (uint64_t)q_rows, p.num_q_heads, D, rows::kBM / p.group, &qmap, p.group) != EKV_OK) return cudaErrorInvalidValue;
+    return launch(rows::rows_kernel<D, kMode, kCap, kBias>, dim3(p.num_kv_heads * (kMode == rows::kShared ? 1 : p.parts), p.tiles), rows::kThreads, rows::Geo<D>::kSmemBytes, false, stream, pool->kv_map[layer], qmap, p,
                   (const uint8_t *)pool->layer_base(layer), (long long)pool->block_stride);
 }
 
@@ -113,6 +116,7 @@ static void fill_rows(rows::Params &p, const ekv_pool *pool, const void *q, void
     p.group = p.num_q_heads / p.num_kv_heads;
     p.group_magic = p.group > 1 ? (unsigned)(((1ull << 32) + p.group - 1) / p.group) : 0u;
     p.window = 0, p.parts = 1, p.chunk_tiles = 0, p.q_flip = 0;
+    p.q_tma = rows::kBM % p.group == 0;
     p.cap_scale = 0.f;
 }
 
@@ -123,10 +127,10 @@ static cudaError_t scored_decode(ekv_pool *pool, int layer, const ext::Params &p
 }
 
 template <int D>
-static cudaError_t scored_prefill(ekv_pool *pool, int layer, const rows::Params &p, bool cap, unsigned items, cudaStream_t stream) {
+static cudaError_t scored_prefill(ekv_pool *pool, int layer, const rows::Params &p, bool cap, long long q_rows, cudaStream_t stream) {
     using namespace rows;
-    if (cap) return p.slopes ? launch_rows<D, kScored, true, true>(pool, layer, p, items, stream) : launch_rows<D, kScored, true, false>(pool, layer, p, items, stream);
-    return p.slopes ? launch_rows<D, kScored, false, true>(pool, layer, p, items, stream) : launch_rows<D, kScored, false, false>(pool, layer, p, items, stream);
+    if (cap) return p.slopes ? launch_rows<D, kScored, true, true>(pool, layer, p, q_rows, stream) : launch_rows<D, kScored, true, false>(pool, layer, p, q_rows, stream);
+    return p.slopes ? launch_rows<D, kScored, false, true>(pool, layer, p, q_rows, stream) : launch_rows<D, kScored, false, false>(pool, layer, p, q_rows, stream);
 }
 
 // Parts that an item's keys are cut into: as many as let all items run at the same time, while a part keeps two key tiles of the most that an item can see.
@@ -220,7 +224,7 @@ static ekv_status_t check_groups(const char *who, const ekv_pool *pool, const in
 template <int D>
 static cudaError_t shared_decode(ekv_pool *pool, int layer, const rows::Params &rp, const ext::Params &p, bool any, int B, cudaStream_t stream) {
     if (any) {
-        const cudaError_t e = launch_rows<D, rows::kShared, false, false>(pool, layer, rp, (unsigned)(rp.tiles * rp.num_kv_heads), stream);
+        const cudaError_t e = launch_rows<D, rows::kShared, false, false>(pool, layer, rp, B, stream);
         if (e != cudaSuccess) return e;
     }
     return launch_ext<D, true, false, false>(pool, layer, p, B, any, stream);
@@ -293,12 +297,11 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t 
         if (c > longest) longest = c;
         if (R <= rows::kMaxGroups) p.tile_prefix[r] = (int)tiles;
         tiles += ((long long)c * p.group + rows::kItemRows - 1) / rows::kItemRows;
-        if (tiles * p.num_kv_heads > (1LL << 30)) break;
     }
     const long long T = cu_q_lens_host[R];
     if (T == 0) return EKV_OK;
     if (R > rows::kMaxGroups) tiles = T * p.group / rows::kItemRows + R;
-    if (tiles * p.num_kv_heads > (1LL << 30) || T * p.num_q_heads >= (1LL << 31) || (long long)longest * p.group >= (1LL << 29)) {
+    if (tiles > 65535 || T * p.num_q_heads >= (1LL << 31) || (long long)longest * p.group >= (1LL << 29)) {
         set_error("%s: too many rows (%lld)", who, T);
         return EKV_ERR_INVALID;
     }
@@ -313,12 +316,12 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t 
     p.cu_q_lens = cu_q_lens, p.seq_lens = seq_lens, p.R = R, p.tiles = (int)tiles;
     p.slopes = scores->slopes, p.prefix_lens = scores->prefix_lens, p.window = scores->window;
     p.q_flip = scale < 0.f ? 0x80008000u : 0u;
+    if (p.q_flip) p.q_tma = 0;
     const bool cap = scores->cap > 0.f;
     p.scale_log2 = fmaxf((cap ? scores->cap : fabsf(scale)) * kLog2e, kSmallest);
     if (cap) p.cap_scale = fabsf(scale) / scores->cap;
-    const unsigned items = (unsigned)(tiles * p.num_kv_heads * p.parts);
     const bool d128 = pool->desc.head_dim == 128;
-    cudaError_t e = d128 ? scored_prefill<128>(pool, layer, p, cap, items, (cudaStream_t)stream) : scored_prefill<64>(pool, layer, p, cap, items, (cudaStream_t)stream);
+    cudaError_t e = d128 ? scored_prefill<128>(pool, layer, p, cap, T, (cudaStream_t)stream) : scored_prefill<64>(pool, layer, p, cap, T, (cudaStream_t)stream);
     if (e == cudaSuccess && p.parts > 1) {
         const int all = (int)(T * p.num_q_heads);
         const dim3 grid((all + ext::kCombineWarps - 1) / ext::kCombineWarps);
