@@ -66,6 +66,8 @@ struct Params {
     int q_tma;                  // Q tiles come by TMA
     float scale_log2;           // |scale| * log2 e; with a cap: cap * log2 e
     float cap_scale;            // with a cap: |scale| / cap
+    float near_limit;           // scores q.k up to there take the short polynomial s * (near[0] + near[1] s^2 + near[2] s^4 + near[3] s^6), in units of log2
+    float near[4];
     int tile_prefix[kMaxGroups + 1];  // items of requests (or groups) before r, if R <= kMaxGroups
     int start[kMaxGroups + 1];        // shared pass: first request of a group ...
     int shared[kMaxGroups];           // ... and its shared keys (a multiple of 16; 0: none are taken here)
@@ -680,31 +682,46 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                     cp::tcgen05_wait_ld();
                 };
                 load_s();
-                if (kCap) {  // tanh of scale * s / cap, in place
+                const bool whole = (key0 + kBN <= it.pre || (kMode == kScored && key0 + kBN - 1 <= lim_all && key0 >= lo_all)) && bad == 0;
+                // ---- the cap.  Small scores that every row sees wait for the exponential, whose code has the polynomial in it; with a bias, up to the
+                // cap, they are worked on in place; the rest goes through TMEM in a small loop.
+                constexpr bool kNear = kCap && !kBias;
+                auto near_score = [&](float v) { return v * (p.near[0] + v * v * (p.near[1] + v * v * (p.near[2] + v * v * p.near[3]))); };
+                bool near = false;
+                float mul = p.scale_log2;
+                if (kCap) {
                     float b0 = 0.f, b1 = 0.f;
 #pragma unroll
-                    for (int c = 0; c < 128; c += 2) b0 = fmaxf(b0, fabsf(sv[c])), b1 = fmaxf(b1, fabsf(sv[c + 1]));
-                    if (__all_sync(0xffffffffu, fmaxf(b0, b1) * p.cap_scale <= kTanhFast)) {
+                    for (int c = 0; c < 128; c += 4) b0 = max3(b0, fabsf(sv[c]), fabsf(sv[c + 1])), b1 = max3(b1, fabsf(sv[c + 2]), fabsf(sv[c + 3]));
+                    const float far = fmaxf(b0, b1);
+                    const bool small = __all_sync(0xffffffffu, kNear ? far <= p.near_limit : far * p.cap_scale <= kTanhFast);
+                    near = kNear && small && whole;
+                    if (kBias && small) {
                         const float2 a = make_float2(p.cap_scale, p.cap_scale);
 #pragma unroll
                         for (int c = 0; c < 128; c += 2) {
                             const float2 v = tanh2_fast(__fmul2_rn(make_float2(sv[c], sv[c + 1]), a));
                             sv[c] = v.x, sv[c + 1] = v.y;
                         }
-                    } else {  // some score is far up: through TMEM, a small loop
+                    } else if (!near) {
+                        if (kNear) mul = 1.f;
 #pragma unroll 1
                         for (int cc = 0; cc < 4; ++cc) {
                             float v[32];
                             tc::tmem_ld32(v, t_s + 32 * cc);
+                            if (kNear && small) {
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) v[c] = tanh_any(v[c] * p.cap_scale);
+                                for (int c = 0; c < 32; ++c) v[c] = near_score(v[c]);
+                            } else {
+#pragma unroll
+                                for (int c = 0; c < 32; ++c) v[c] = tanh_any(v[c] * p.cap_scale) * (kNear ? p.scale_log2 : 1.f);
+                            }
                             tc::tmem_st32(t_s + 32 * cc, v);
                         }
                         cp::tcgen05_wait_st();
                         load_s();
                     }
                 }
-                float mul = p.scale_log2;
                 if (kBias) {  // sv becomes the whole score in units of log2
                     const float2 sc = make_float2(mul, mul);
                     if (key0 + kBN - 1 <= lim_all) {  // keys behind every row: |p - j| = p - j
@@ -723,7 +740,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                     }
                     mul = 1.f;
                 }
-                if (!(key0 + kBN <= it.pre || (kMode == kScored && key0 + kBN - 1 <= lim_all && key0 >= lo_all)) || bad) {
+                if (!whole) {
 #pragma unroll
                     for (int cc = 0; cc < 4; ++cc) {
                         const int c0 = key0 + 32 * cc;
@@ -747,7 +764,8 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                     mx2 = fmaxf(mx2, sv[c + 2]);
                     mx3 = fmaxf(mx3, sv[c + 3]);
                 }
-                const float m_tile = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * mul;
+                float m_tile = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+                m_tile = near ? near_score(m_tile) : m_tile * mul;  // (tanh grows with its argument)
                 // ---- lazy rescale: raise the reference max only when it is far behind
                 const bool raise = m_tile > m_run + tc::kRescaleThreshold;  // also true for the first finite tile
                 if (__any_sync(0xffffffffu, raise)) {
@@ -770,22 +788,33 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                 // ---- P = exp2(x - m) (a masked -inf gives 0), row sum, bf16 pairs into the S columns
                 float2 acc_a = make_float2(0.f, 0.f), acc_b = make_float2(0.f, 0.f);
                 const float2 sc2 = make_float2(mul, mul), nm2 = make_float2(-m_use, -m_use);
+                auto weights = [&](auto score) {  // score(v): x - m of two keys
+    #pragma unroll
+                    for (int cc = 0; cc < 4; ++cc) {
+                        uint32_t pk[16];
 #pragma unroll
-                for (int cc = 0; cc < 4; ++cc) {
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        const float2 xa = __ffma2_rn(make_float2(sv[32 * cc + c], sv[32 * cc + c + 1]), sc2, nm2);
-                        const float2 xb = __ffma2_rn(make_float2(sv[32 * cc + c + 2], sv[32 * cc + c + 3]), sc2, nm2);
-                        const float2 pa = make_float2(fast_exp2(xa.x), fast_exp2(xa.y));
-                        const float2 pb = make_float2(fast_exp2(xb.x), fast_exp2(xb.y));
-                        acc_a = __fadd2_rn(acc_a, pa);
-                        acc_b = __fadd2_rn(acc_b, pb);
-                        pk[c >> 1] = pack_bf16x2(pa.x, pa.y);
-                        pk[(c >> 1) + 1] = pack_bf16x2(pb.x, pb.y);
+                        for (int c = 0; c < 32; c += 4) {
+                            const float2 xa = score(make_float2(sv[32 * cc + c], sv[32 * cc + c + 1]));
+                            const float2 xb = score(make_float2(sv[32 * cc + c + 2], sv[32 * cc + c + 3]));
+                            const float2 pa = make_float2(fast_exp2(xa.x), fast_exp2(xa.y));
+                            const float2 pb = make_float2(fast_exp2(xb.x), fast_exp2(xb.y));
+                            acc_a = __fadd2_rn(acc_a, pa);
+                            acc_b = __fadd2_rn(acc_b, pb);
+                            pk[c >> 1] = pack_bf16x2(pa.x, pa.y);
+                            pk[(c >> 1) + 1] = pack_bf16x2(pb.x, pb.y);
+                        }
+                        cp::tcgen05_st_32x32b(t_s + 16 * cc, pk);
+                        if (cc == tc::kPartSteps / 2 - 1) publish(G::P_PART + x);  // 96 keys stored
                     }
-                    cp::tcgen05_st_32x32b(t_s + 16 * cc, pk);
-                    if (cc == tc::kPartSteps / 2 - 1) publish(G::P_PART + x);  // 96 keys stored
+                };
+                if (kNear && near) {
+                    const float2 c0 = make_float2(p.near[0], p.near[0]), c1 = make_float2(p.near[1], p.near[1]), c2 = make_float2(p.near[2], p.near[2]), c3 = make_float2(p.near[3], p.near[3]);
+                    weights([&](float2 v) {
+                        const float2 u = __fmul2_rn(v, v);
+                        return __ffma2_rn(v, __ffma2_rn(u, __ffma2_rn(u, __ffma2_rn(u, c3, c2), c1), c0), nm2);
+                    });
+                } else {
+                    weights([&](float2 v) { return __ffma2_rn(v, sc2, nm2); });
                 }
                 l_run += (acc_a.x + acc_a.y) + (acc_b.x + acc_b.y);
                 publish(G::P_READY + x);

@@ -117,7 +117,8 @@ static void fill_rows(rows::Params &p, const ekv_pool *pool, const void *q, void
     p.group_magic = p.group > 1 ? (unsigned)(((1ull << 32) + p.group - 1) / p.group) : 0u;
     p.window = 0, p.parts = 1, p.chunk_tiles = 0, p.q_flip = 0;
     p.q_tma = rows::kBM % p.group == 0;
-    p.cap_scale = 0.f;
+    p.cap_scale = p.near_limit = 0.f;
+    for (float &c : p.near) c = 0.f;
 }
 
 template <int D>
@@ -319,7 +320,13 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t 
     if (p.q_flip) p.q_tma = 0;
     const bool cap = scores->cap > 0.f;
     p.scale_log2 = fmaxf((cap ? scores->cap : fabsf(scale)) * kLog2e, kSmallest);
-    if (cap) p.cap_scale = fabsf(scale) / scores->cap;
+    if (cap) {
+        // cap * log2 e * tanh(a s) for |a s| <= 1/2: a minimax polynomial in a s (3e-7), its powers of a in the coefficients
+        const double a = p.cap_scale = fabsf(scale) / scores->cap, c = (double)scores->cap * kLog2e * a;
+        p.near[0] = (float)(0.99999946 * c), p.near[1] = (float)(-0.33326319 * c * a * a);
+        p.near[2] = (float)(0.13190296 * c * a * a * a * a), p.near[3] = (float)(-0.04440222 * c * a * a * a * a * a * a);
+        p.near_limit = p.near[3] < -1e-36f ? 0.5f / p.cap_scale : -1.f;  // (not where a coefficient leaves fp32's range)
+    }
     const bool d128 = pool->desc.head_dim == 128;
     cudaError_t e = d128 ? scored_prefill<128>(pool, layer, p, cap, T, (cudaStream_t)stream) : scored_prefill<64>(pool, layer, p, cap, T, (cudaStream_t)stream);
     if (e == cudaSuccess && p.parts > 1) {
