@@ -3,7 +3,7 @@
 // The split pass of ekv_decode.cu -- a CTA per (sequence, kv-head, range of keys), each warp a ring of TMA loads for every fourth block of 16
 // keys, the heads of the group as the rows of mma.m16n8k16, partial (m, l, O) per range -- over those blocks alone that the sequence sees:
 // of its prefix and of its window, or from the end of the shared keys on.  Bound by the bytes of these.  Where a sequence has a single
-// range the CTA writes the final rows itself; in a shared call it takes the shared keys' parts (left by the rows kernel, beside whose last
+// range (many do, where the tables are wider than the sequences long) the CTA writes the final rows itself; in a shared call it takes the shared keys' parts (left by the rows kernel, beside whose last
 // CTAs this launch comes up) along.  Otherwise combine_ext_kernel does, a warp a (sequence, head).
 #pragma once
 #include "ekv_rows.cuh"
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
             mstar = fmaxf(mstar, mw[w]);
         }
         const size_t row = (size_t)b * p.num_q_heads + (size_t)g * p.group + h;
-        const bool last = p.nsplit == 1;  // the only range of every sequence: finish here, no combine pass
+        const bool last = sp.tokens <= p.chunk_tokens;  // the sequence's only range: finish here
         if (kShared && last)
             for (int s = 0; s < sp.parts; ++s) mstar = fmaxf(mstar, p.shared_ml[row * p.parts + s].x);
         float acc = 0.f, lsum = 0.f;
@@ -385,12 +385,16 @@ static constexpr int kCombineWarps = 4;
 template <int D, bool kShared>
 __global__ void __launch_bounds__(kCombineWarps * 32) combine_ext_kernel(const __grid_constant__ Params p, int rows) {
     const int row = blockIdx.x * kCombineWarps + (threadIdx.x >> 5);
+    if (row >= rows) {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
+    const Span sp = span_of<kShared>(p, row / p.num_q_heads);  // (lengths and offsets were there before the split pass)
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (row >= rows) return;
-    const Span sp = span_of<kShared>(p, row / p.num_q_heads);
+    if (sp.tokens <= p.chunk_tokens) return;  // finished by the split pass
     RowSum<D> sum;
     if (kShared) sum.add(p.shared_o + (size_t)row * p.parts * D, p.shared_ml + (size_t)row * p.parts, sp.parts);
-    sum.add(p.part_o + (size_t)row * p.nsplit * D, p.part_ml + (size_t)row * p.nsplit, max(1, (sp.tokens + p.chunk_tokens - 1) / p.chunk_tokens));
+    sum.add(p.part_o + (size_t)row * p.nsplit * D, p.part_ml + (size_t)row * p.nsplit, (sp.tokens + p.chunk_tokens - 1) / p.chunk_tokens);
     sum.store(p.out + (size_t)row * D);
 }
 

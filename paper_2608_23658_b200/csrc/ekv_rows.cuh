@@ -15,11 +15,11 @@
 // A call of few items cuts each one's tiles into `parts`; (m, l, O) of each part go to the workspace.
 //
 //   warp 0        MMA issuer: S = Q K^T (both from shared memory), O += P V (P from TMEM, V MN-major), the slots by turns
-//   warp 1        TMEM; warp 2: item scheduler: the kernel is persistent, a CTA an SM, items by cluster launch control (no word of device memory that
+//   warp 1        TMEM; TMA producer of V tiles; warp 2: item scheduler: the kernel is persistent, a CTA an SM, items by cluster launch control (no word of device memory that
 //                 two launches or replays could share)
 //   warps 4-7     softmax and write-out of slot 0: a thread a row
 //   warps 8-11    of slot 1
-//   warp 12       TMA producer of K and V tiles
+//   warp 12       TMA producer of K tiles
 //   warps 13-15   Q rows into shared memory (by TMA where the group divides a tile), and the care of V tiles that not every row sees whole: rows of V at keys nobody sees become 0;
 //                 values that are not finite at keys that some rows see and others do not are taken out (a weight of 0 does not stop a NaN) and
 //                 given to the rows they belong to after the write-out.
@@ -38,7 +38,7 @@ using tc::fence_before;
 static constexpr int kBM = 128, kBN = 128;
 static constexpr int kItemRows = 2 * kBM;
 static constexpr int kThreads = 512;
-static constexpr int kStages = 2, kRing = 4;
+static constexpr int kRing = 4;
 static constexpr int kHalfBytes = 128 * 128;  // [128 rows][64 channels], 128-byte swizzle
 static constexpr int kMaxGroups = 256;
 // setmaxnreg: warps 0-3 and 12-15 kRegsUtil, 4-11 kRegsSoftmax; the shares add up to what the CTA is launched with
@@ -60,7 +60,7 @@ struct Params {
     int tiles;                  // items of the call per kv-head and part (an upper bound if R > kMaxGroups)
     int window;                 // 0: none
     int parts;                  // parts an item's keys are cut into (shared pass: the most that any group has)
-    int chunk_tiles;            // shared pass: key tiles of a part
+    int chunk_tiles;            // shared pass: key tiles of a part (part_tiles)
     unsigned group_magic;       // ceil(2^32 / group)
     unsigned q_flip;            // 0x80008000 for a negative scale
     int q_tma;                  // Q tiles come by TMA
@@ -75,9 +75,13 @@ struct Params {
 
 enum Mode { kScored = 0, kShared = 1 };
 
+// Shared pass: key tiles of a part, for a group of so many rows.  Up to 128 of them take half the time for a tile (the slots share the tiles out).
+__host__ __device__ __forceinline__ int part_tiles(int chunk, long long rows) { return rows > kBM ? chunk : 2 * chunk; }
+
 template <int D>
 struct Geo {
     static constexpr int kHalves = D / 64;
+    static constexpr int kStages = D == 64 ? 4 : 2;  // of K, and of V
     static constexpr int kTileBytes = kHalves * kHalfBytes;
     static constexpr int kOffQ = 0;
     static constexpr int kOffK = 2 * kTileBytes;
@@ -85,16 +89,17 @@ struct Geo {
     static constexpr int kOffStage = kOffV + kStages * kTileBytes;  // of the write-out: [32 rows][128 B] a warp
     static constexpr int kStageBytes = 32 * 128;
     static constexpr int kOffBar = kOffStage + 8 * kStageBytes;
-    enum Bar { Q_FULL = 0, Q_EMPTY = 1, K_FULL = 2, K_EMPTY = 4, V_RAW = 6, V_FULL = 8, V_EMPTY = 10, S_READY = 12, P_PART = 14, P_READY = 16,
-               O_READY = 18, O_FREE = 20, MERGE = 22, ITEM_FULL = 23, ITEM_EMPTY = ITEM_FULL + kRing, WANT = ITEM_EMPTY + kRing, NEXT, DRAIN, NBAR };
+    enum Bar { Q_FULL = 0, Q_EMPTY = 1, K_FULL = 2, K_EMPTY = K_FULL + kStages, V_RAW = K_EMPTY + kStages, V_FULL = V_RAW + kStages, V_EMPTY = V_FULL + kStages,
+               S_READY = V_EMPTY + kStages, P_PART = S_READY + 2, P_READY = P_PART + 2, O_READY = P_READY + 2, O_FREE = O_READY + 2, MERGE = O_FREE + 2,
+               ITEM_FULL = MERGE + 1, ITEM_EMPTY = ITEM_FULL + kRing, WANT = ITEM_EMPTY + kRing, NEXT, DRAIN, NBAR };
     __device__ static __forceinline__ uint32_t arrivals(int bar) {
         if (bar == Q_FULL || (bar >= V_FULL && bar < V_EMPTY)) return 3;               // warps 13-15
         if ((bar >= P_PART && bar < O_READY) || (bar >= O_FREE && bar <= MERGE)) return 4;  // a slot's warps
-        if (bar >= ITEM_EMPTY && bar < WANT) return 13;                                      // every warp that reads items
+        if (bar >= ITEM_EMPTY && bar < WANT) return 14;                                      // every warp that reads items
         return 1;
     }
-    static constexpr int kOffFlags = kOffBar + 8 * NBAR;                  // abort flag, TMEM address, 4 masks of invalid blocks
-    static constexpr int kOffNext = (kOffFlags + 24 + 15) / 16 * 16;      // answer of the launch control
+    static constexpr int kOffFlags = kOffBar + 8 * NBAR;                  // abort flag, TMEM address, two rings of 8 masks of invalid blocks
+    static constexpr int kOffNext = (kOffFlags + 72 + 15) / 16 * 16;      // answer of the launch control
     static constexpr int kOffItems = kOffNext + 16;                        // kRing slots of 16 numbers
     static constexpr int kOffMerge = kOffItems + kRing * 64;               // (m, l) of slot 1's rows
     static constexpr int kSmemBytes = kOffMerge + 128 * 8 + 1024;          // + alignment slack
@@ -111,8 +116,9 @@ struct Smem {
     __device__ __forceinline__ uint32_t bar(int i) const { return base + G::kOffBar + 8 * i; }
     __device__ __forceinline__ volatile int *abort_flag() const { return (volatile int *)(ptr + G::kOffFlags); }
     __device__ __forceinline__ uint32_t *tmem_slot() const { return (uint32_t *)(ptr + G::kOffFlags + 4); }
-    // ring of 4 by key tile: the producer writes tile t + 4's after the scores of tile t + 2 are done, for which the slots' softmax of tile t is
-    __device__ __forceinline__ volatile int *bad_mask(uint32_t t) const { return (volatile int *)(ptr + G::kOffFlags + 8 + 4 * (t & 3)); }
+    // Invalid blocks of a key tile, from the producer of K (for the softmax) and from that of V (for its care).  Rings of 8: a producer writes tile
+    // t + 8's entry after the MMAs of tile t + 8 - kStages have read its stage, for which everything of tile t + 6 - kStages is done.
+    __device__ __forceinline__ volatile int *bad_mask(int kv, uint32_t t) const { return (volatile int *)(ptr + G::kOffFlags + 8 + 32 * kv + 4 * (t & 7)); }
     __device__ __forceinline__ uint4 *response() const { return (uint4 *)(ptr + G::kOffNext); }
     __device__ __forceinline__ volatile int *item(uint32_t n) const { return (volatile int *)(ptr + G::kOffItems) + 16 * (n % kRing); }
     __device__ __forceinline__ float2 *merge() const { return (float2 *)(ptr + G::kOffMerge); }
@@ -267,7 +273,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
         return (l < it.n_pre ? l : l + it.skip) * kBN;
     };
     auto low_of = [&](int pos) { return p.window > 0 ? max(0, pos - p.window + 1) : 0; };  // first key of a row's window
-    uint32_t issued = 0;  // producer: tiles under way or done
+    uint32_t issued = 0;  // producers: tiles under way or done
 
     if (warp < 4 || warp >= 12) {
     if (warp != 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -323,12 +329,13 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
             const int c_r = next_q0 - q0;
             int row0, past, pre, kv_end, n_pre, skip, tile0, n_tiles;
             if (kMode == kShared) {
-                const int all = (p.shared[req] + kBN - 1) / kBN, ns = (all + p.chunk_tiles - 1) / p.chunk_tiles, tile = (idx - first) / ns;
+                const int chunk = part_tiles(p.chunk_tiles, c_r * group);
+                const int all = (p.shared[req] + kBN - 1) / kBN, ns = (all + chunk - 1) / chunk, tile = (idx - first) / ns;
                 part = (idx - first) - tile * ns;
                 row0 = tile * kItemRows;
                 past = 0, pre = kv_end = p.shared[req], n_pre = all, skip = 0;
-                tile0 = part * p.chunk_tiles;
-                n_tiles = min(p.chunk_tiles, all - tile0);
+                tile0 = part * chunk;
+                n_tiles = min(chunk, all - tile0);
                 req = q0;  // the first request's table names the shared blocks
             } else {
                 row0 = (idx - first) * kItemRows;
@@ -417,15 +424,15 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
             for (int u = -2; u < step_max && ok; ++u) {
                 const int x = u & 1, i = u >> 1;
                 const int j = u >> sh2, jn = (u + 2) >> sh2;  // the part's key tiles of the two
-                const uint32_t s = (t0 + (uint32_t)j) & 1u, s1 = (t0 + (uint32_t)jn) & 1u;
+                const uint32_t s = (t0 + (uint32_t)j) % G::kStages, s1 = (t0 + (uint32_t)jn) % G::kStages;
                 const int pv = opaque(u >= 0), more = opaque(jn < n_tiles), closes = opaque(x >= sh2), opens = opaque(x == 0 || sh2 == 0);  // the last and the first slot to read these stages
                 const uint32_t t_s = tmem + 128 * x, t_o = tmem + 256 + 128 * x;
                 const uint64_t vd = v_d + s * (G::kTileBytes >> 4);
                 if (!pv && !more) continue;
                 // (what comes early is waited for first, and once: a wait takes some 300 cycles beside busy special functions)
-                if (more && opens) ok = wait(G::K_FULL + (int)s1, (t0 + (uint32_t)jn) >> 1);
+                if (more && opens) ok = wait(G::K_FULL + (int)s1, (t0 + (uint32_t)jn) / G::kStages);
                 if (pv) {
-                    if (ok && opens) ok = wait(G::V_FULL + (int)s, (t0 + (uint32_t)j) >> 1);
+                    if (ok && opens) ok = wait(G::V_FULL + (int)s, (t0 + (uint32_t)j) / G::kStages);
                     // the slot's accumulator of the item before has been read
                     if (ok && i == 0 && co[x] > 0) ok = wait(G::O_FREE + x, co[x] - 1);
                     if (ok) ok = wait(G::P_PART + x, cs[x] + (uint32_t)i);
@@ -473,8 +480,12 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
         // every MMA this thread issued must be finished before TMEM is released
         tc::mma_commit(sh.bar(G::DRAIN));
         (void)wait(G::DRAIN, 0);
-    } else if (warp == 12) {
-        // =========================== TMA producer of K and V tiles ===========================
+    } else if (warp == 12 || warp == 1) {
+        // =========================== TMA producers: K tiles, V tiles ===========================
+        // (One for each: a V tile waits for P V two tiles before, and the K tile after it must not wait with it.)
+        const int kv = warp == 1;
+        const int full = kv ? G::V_RAW : G::K_FULL, empty = kv ? G::V_EMPTY : G::K_EMPTY;
+        const uint32_t to = sh.base + (kv ? G::kOffV : G::kOffK);
         const long long live = *p.live;
         bool ok = true;
 #pragma unroll 1
@@ -493,9 +504,9 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                 return id;
             };
             int id_next = load_id(0);
-            if (it.n_tiles == 0 && lane == 0) mbar_arrive(sh.bar(G::WANT));
+            if (it.n_tiles == 0 && lane == 0 && !kv) mbar_arrive(sh.bar(G::WANT));
 #pragma unroll 1
-            for (int j = 0; j < it.n_tiles && ok; ++j) {
+            for (int j = 0; j < it.n_tiles; ++j) {
                 const int id_raw = id_next;
                 id_next = load_id(j + 1);
                 const unsigned oob = __ballot_sync(0xffffffffu, id_raw == -2) & 0xffu;
@@ -503,27 +514,18 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                 const int id = id_raw < 0 ? 0 : id_raw;  // masked later; block 0 is always mapped
                 const int b = lane & (8 * G::kHalves - 1), blk = b / G::kHalves, half = b % G::kHalves;
                 const int my_id = __shfl_sync(0xffffffffu, id, blk);
-                const uint32_t s = issued & 1u;
-                if (j == max(0, it.n_tiles - 4) && lane == 0) mbar_arrive(sh.bar(G::WANT));
-#pragma unroll
-                for (int kv = 0; kv < 2; ++kv) {
-                    const int full = (kv ? G::V_RAW : G::K_FULL) + (int)s, empty = (kv ? G::V_EMPTY : G::K_EMPTY) + (int)s;
-                    if (issued >= kStages && !wait(empty, (issued >> 1) - 1)) {
-                        ok = false;
-                        break;
-                    }
-                    if (lane == 0) {
-                        if (!kv) {
-                            if (oob) atomicOr(p.status, EKV_DEV_FLAG_OOB);
-                            *sh.bad_mask(issued) = (int)bad;
-                        }
-                        mbar_expect_tx(sh.bar(full), G::kTileBytes);
-                    }
-                    __syncwarp();
-                    if (lane < 8 * G::kHalves)
-                        tma_load_3d(sh.base + (kv ? G::kOffV : G::kOffK) + s * G::kTileBytes + half * kHalfBytes + blk * 2048, &kvmap, 64 * half,
-                                    (it.g + (kv ? p.num_kv_heads : 0)) * 16, my_id, sh.bar(full));
+                const uint32_t s = issued % G::kStages;
+                if (j == max(0, it.n_tiles - 4) && lane == 0 && !kv) mbar_arrive(sh.bar(G::WANT));
+                if (issued >= G::kStages && !(ok = wait(empty + (int)s, issued / G::kStages - 1))) break;
+                if (lane == 0) {
+                    if (oob && !kv) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+                    *sh.bad_mask(kv, issued) = (int)bad;
+                    mbar_expect_tx(sh.bar(full + (int)s), G::kTileBytes);
                 }
+                __syncwarp();
+                if (lane < 8 * G::kHalves)
+                    tma_load_3d(to + s * G::kTileBytes + half * kHalfBytes + blk * 2048, &kvmap, 64 * half, (it.g + (kv ? p.num_kv_heads : 0)) * 16, my_id,
+                                sh.bar(full + (int)s));
                 ++issued;
             }
         }
@@ -582,10 +584,10 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
             const int lo1 = kMode == kShared ? 0 : low_of(p1);
 #pragma unroll 1
             for (int j = 0; j < it.n_tiles && ok; ++j, ++t) {
-                const uint32_t s = t & 1u;
-                ok = wait(G::V_RAW + (int)s, t >> 1);
+                const uint32_t s = t % G::kStages;
+                ok = wait(G::V_RAW + (int)s, t / G::kStages);
                 if (!ok) break;
-                const int key0 = first_key(it, j), bad = *sh.bad_mask(t);
+                const int key0 = first_key(it, j), bad = *sh.bad_mask(1, t);
                 uint8_t *tile = sh.ptr + G::kOffV + s * G::kTileBytes;
                 auto piece = [&](int i) { return reinterpret_cast<uint4 *>(tile + (i % kPieces >> 3) * kHalfBytes + (i / kPieces) * 128 + (i & 7) * 16); };
                 bool touched = false;
@@ -671,7 +673,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                 fence_after();
                 const int j = (i << dj) + j0;
                 const int key0 = first_key(it, j);
-                const int bad = *sh.bad_mask(t0 + (uint32_t)j);
+                const int bad = *sh.bad_mask(0, t0 + (uint32_t)j);
                 float sv[128];
                 uint32_t(&raw)[128] = reinterpret_cast<uint32_t(&)[128]>(sv);
                 auto load_s = [&]() {
@@ -939,11 +941,9 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
     __syncthreads();
     fence_after();
     if (*sh.abort_flag()) {
-        if (warp == 12 && issued > 0)
-            for (uint32_t t = issued > kStages ? issued - kStages - 1 : 0; t < issued; ++t) {  // (the last one's may not have been started)
-                (void)mbar_wait(sh.bar(G::K_FULL + (int)(t & 1u)), (t >> 1) & 1u, 100000000ull);
-                (void)mbar_wait(sh.bar(G::V_RAW + (int)(t & 1u)), (t >> 1) & 1u, 100000000ull);
-            }
+        if (warp == 12 || warp == 1)
+            for (uint32_t t = issued > G::kStages ? issued - G::kStages : 0; t < issued; ++t)
+                (void)mbar_wait(sh.bar((warp == 1 ? G::V_RAW : G::K_FULL) + (int)(t % G::kStages)), (t / G::kStages) & 1u, 100000000ull);
         if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);  // a wait ran out
     }
     __syncthreads();

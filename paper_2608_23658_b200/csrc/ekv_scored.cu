@@ -183,19 +183,24 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
     if (most < 8) most = 8;
     for (int ns = 1; ns <= most && ns <= longest; ++ns) {
         const int chunk = (longest + ns - 1) / ns;
-        long long items = 0, work = 0;
+        long long items = 0;
+        double work = 0., worst = 0.;
+        int parts = 0;
         for (int g = 0; g < G; ++g) {
             const int n = starts[g + 1] - starts[g];
             if (!takes_shared(n, shared[g])) continue;
             const long long rt = ((long long)n * group + rows::kItemRows - 1) / rows::kItemRows * Hk, kt = (shared[g] + rows::kBN - 1) / rows::kBN;
-            items += rt * ((kt + chunk - 1) / chunk);
-            work += rt * kt;
+            const int mine = rows::part_tiles(chunk, (long long)n * group), cut = (int)((kt + mine - 1) / mine);
+            const double tile = (double)chunk / mine;  // time of a tile
+            items += rt * cut;
+            work += rt * kt * tile;
+            worst = fmax(worst, fmin((double)kt, (double)mine) * tile);
+            if (cut > parts) parts = cut;
         }
-        const double rounds = (double)((items + pool->sm_count - 1) / pool->sm_count), mean = (double)work / items + fixed;
-        const double t = fmax(rounds * mean, chunk + fixed);
-        if (t < best) best = t, s.chunk_tiles = chunk;
+        const double rounds = (double)((items + pool->sm_count - 1) / pool->sm_count), mean = work / items + fixed;
+        const double t = fmax(rounds * mean, worst + fixed);
+        if (t < best) best = t, s.chunk_tiles = chunk, s.parts = parts;
     }
-    s.parts = (longest + s.chunk_tiles - 1) / s.chunk_tiles;
     return s;
 }
 
@@ -387,7 +392,8 @@ extern "C" ekv_status_t ekv_attn_decode_shared(ekv_pool_t *pool, int32_t layer, 
     for (int g = 0; g < G; ++g) {
         const int n = group_starts[g + 1] - group_starts[g];
         const bool takes = takes_shared(n, shared_lens[g]);
-        const int kt = (shared_lens[g] + rows::kBN - 1) / rows::kBN, ns = takes ? (kt + s.chunk_tiles - 1) / s.chunk_tiles : 0;
+        const int kt = (shared_lens[g] + rows::kBN - 1) / rows::kBN, mine = rows::part_tiles(s.chunk_tiles, (long long)n * p.group);
+        const int ns = takes ? (kt + mine - 1) / mine : 0;
         p.start[g] = rp.start[g] = group_starts[g];
         p.shared[g] = shared_lens[g], rp.shared[g] = takes ? shared_lens[g] : 0;
         p.ns[g] = (uint8_t)ns;
