@@ -16,6 +16,7 @@ using rows::kMaxGroups;
 static constexpr int kWarps = 4;
 static constexpr int kStages = 2;  // of a warp; 64 KB in all, so that three CTAs fit an SM: with three stages and two CTAs, 256 short own parts took 89 us for 79
 static constexpr int kBoxBytes = 16 * 128;  // 16 tokens x 64 channels
+static constexpr int kMaxParts = 64;        // that the rows kernel cuts shared keys into
 
 struct Params {
     const __nv_bfloat16 *q;
@@ -45,6 +46,7 @@ struct Span {
     int L, lo, pre;       // keys lo .. L-1 and those below pre are seen
     int n_pre, skip, tokens;
     int parts;            // of the shared keys
+    int first, common;    // blocks below `common` are named by the table of request `first`
     bool invalid;
 };
 
@@ -54,7 +56,8 @@ __device__ __forceinline__ Span span_of(const Params &p, int b) {
     s.L = max(0, min(p.seq_lens[b], p.max_blocks * 16));
     s.parts = 0;
     s.invalid = false;
-    s.lo = s.pre = s.n_pre = s.skip = 0;
+    s.lo = s.pre = s.n_pre = s.skip = s.common = 0;
+    s.first = b;
     if (kShared) {
         int g = 0, hi = p.G;
 #pragma unroll 1
@@ -64,6 +67,7 @@ __device__ __forceinline__ Span span_of(const Params &p, int b) {
             else hi = mid;
         }
         s.invalid = s.L > 0 && s.L < p.shared[g];
+        s.first = p.start[g], s.common = p.shared[g] / 16;
         if (s.invalid) s.L = 0;
         s.parts = s.L > 0 ? p.ns[g] : 0;
         if (s.parts > 0) s.lo = p.shared[g], s.skip = s.lo / 16;
@@ -121,7 +125,8 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
 
     // Block ids of this warp's blocks: lane i holds the id of its i-th block.
     const long long live = *p.live;
-    const int my_id = (lane < nw) ? p.block_tables[(size_t)b * p.max_blocks + block_of(lane)] : 0;
+    const int my_block = block_of(lane);
+    const int my_id = (lane < nw) ? p.block_tables[(size_t)(my_block < sp.common ? sp.first : b) * p.max_blocks + my_block] : 0;
     const bool my_ok = (lane < nw) && my_id >= 0 && (long long)my_id < live;
     const unsigned valid_mask = __ballot_sync(FULL, my_ok);
     if (lane < nw && !my_ok) atomicOr(p.status, EKV_DEV_FLAG_OOB);
@@ -290,39 +295,62 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
     }
     __syncthreads();
     if (kShared) asm volatile("griddepcontrol.wait;" ::: "memory");  // the shared keys' parts are complete
+    // The weights of what a head's row is made of -- the four warps' results and, where the sequence ends here, the shared keys' parts -- once a
+    // head, by a warp; then a thread a channel.  (In warp 0's second stage: idle, too.)
+    constexpr int kTerms = kWarps + kMaxParts;
+    const bool last = sp.tokens <= p.chunk_tokens;  // the sequence's only range: finish here
+    const int n_parts = kShared && last ? sp.parts : 0;
+    float *weights = reinterpret_cast<float *>(base_ptr + STAGE_BYTES);  // [8][kTerms]
+    float *rowsum = weights + 8 * kTerms;                                // [8] l, [8] m
+    static_assert((8 * kTerms + 16) * 4 <= STAGE_BYTES && (8 * D + 16) * 4 <= STAGE_BYTES, "merge area");
+    for (int h = warp; h < p.group; h += kWarps) {
+        const size_t row = (size_t)b * p.num_q_heads + (size_t)g * p.group + h;
+        float2 ml[kTerms / 32 + 1];
+        float mstar = -INFINITY;
+#pragma unroll
+        for (int k = 0; k <= kTerms / 32; ++k) {
+            const int i = 32 * k + lane;
+            const float *own = reinterpret_cast<const float *>(base_ptr + (i & (kWarps - 1)) * kStages * STAGE_BYTES) + 8 * D;
+            ml[k] = i < kWarps ? make_float2(own[h], own[8 + h]) : i - kWarps < n_parts ? p.shared_ml[row * p.parts + i - kWarps] : make_float2(-INFINITY, 0.f);
+            mstar = fmaxf(mstar, ml[k].x);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) mstar = fmaxf(mstar, __shfl_xor_sync(FULL, mstar, d));
+        float lsum = 0.f;
+#pragma unroll
+        for (int k = 0; k <= kTerms / 32; ++k) {  // (a term without a maximum holds zeros, or NaN if its scores were NaN: either counts)
+            const float w = ml[k].x > -INFINITY ? fast_exp2(ml[k].x - mstar) : 0.f;
+            lsum += w * ml[k].y;
+            if (32 * k + lane < kTerms) weights[h * kTerms + 32 * k + lane] = w;
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) lsum += __shfl_xor_sync(FULL, lsum, d);
+        if (lane == 0) rowsum[h] = lsum, rowsum[8 + h] = mstar;
+    }
+    __syncthreads();
     for (int e = threadIdx.x; e < p.group * D; e += kWarps * 32) {
         const int h = e / D, ch = e % D;
-        float mw[kWarps], mstar = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            mw[w] = reinterpret_cast<const float *>(base_ptr + w * kStages * STAGE_BYTES)[8 * D + h];
-            mstar = fmaxf(mstar, mw[w]);
-        }
         const size_t row = (size_t)b * p.num_q_heads + (size_t)g * p.group + h;
-        const bool last = sp.tokens <= p.chunk_tokens;  // the sequence's only range: finish here
-        if (kShared && last)
-            for (int s = 0; s < sp.parts; ++s) mstar = fmaxf(mstar, p.shared_ml[row * p.parts + s].x);
-        float acc = 0.f, lsum = 0.f;
+        float acc = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {  // (a warp without a maximum holds zeros, or NaN if its scores were NaN: either counts)
-            const float *src = reinterpret_cast<const float *>(base_ptr + w * kStages * STAGE_BYTES);
-            const float wgt = (mw[w] > -INFINITY) ? fast_exp2(mw[w] - mstar) : 0.f;
-            acc += wgt * src[h * D + ch];
-            lsum += wgt * src[8 * D + 8 + h];
-        }
-        if (kShared && last)
-            for (int s = 0; s < sp.parts; ++s) {
-                const float2 ml = p.shared_ml[row * p.parts + s];
-                const float wgt = ml.x > -INFINITY ? fast_exp2(ml.x - mstar) : 0.f;
-                acc += wgt * p.shared_o[(row * p.parts + s) * D + ch];
-                lsum += wgt * ml.y;
+        for (int w = 0; w < kWarps; ++w) acc += weights[h * kTerms + w] * reinterpret_cast<const float *>(base_ptr + w * kStages * STAGE_BYTES)[h * D + ch];
+        const float *part = p.shared_o + (row * p.parts) * D + ch;
+        for (int s = 0; s < n_parts; s += 4) {  // four loads under way, whatever their number
+            float w[4], o[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                w[u] = s + u < n_parts ? weights[h * kTerms + kWarps + s + u] : 0.f;
+                o[u] = w[u] != 0.f ? part[(size_t)(s + u) * D] : 0.f;  // (0: nothing may have been written for it)
             }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) acc += w[u] * o[u];
+        }
         if (last) {
-            p.out[row * D + ch] = __float2bfloat16_rn(finish(acc, lsum));
+            p.out[row * D + ch] = __float2bfloat16_rn(finish(acc, rowsum[h]));
         } else {
             const size_t slot = row * p.nsplit + split;
             p.part_o[slot * D + ch] = acc;
-            if (ch == 0) p.part_ml[slot] = make_float2(mstar, lsum);
+            if (ch == 0) p.part_ml[slot] = make_float2(rowsum[8 + h], rowsum[h]);
         }
     }
 }

@@ -150,7 +150,7 @@ static int plan_parts(const ekv_pool *pool, long long items, int max_blocks, int
 struct SharedPlan {
     int chunk_tiles, parts, tiles;  // tiles: items per kv-head
     int own_blocks;                 // the longest table behind shared blocks
-    bool any;                       // some group's shared keys are read for all its requests at once
+    bool worth, any;                // shared keys are read for all requests of a group at once; some group has any
 };
 
 static bool takes_shared(int requests, int shared) { return requests > 1 && shared > 0; }
@@ -158,14 +158,24 @@ static bool takes_shared(int requests, int shared) { return requests > 1 && shar
 static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const int32_t *shared, int G, int max_blocks) {
     const int group = pool->desc.num_q_heads / pool->desc.num_kv_heads, Hk = pool->desc.num_kv_heads;
     SharedPlan s;
-    s.any = false;
+    s.any = s.worth = false;
     s.chunk_tiles = 1, s.parts = 0, s.tiles = 0, s.own_blocks = 1;
-    int longest = 0;
-    long long row_tiles = 0;
+    int longest = 0, longest_shared = 0;
+    long long row_tiles = 0, saved = 0;
+    for (int g = 0; g < G; ++g)
+        if (takes_shared(starts[g + 1] - starts[g], shared[g])) {
+            saved += (long long)(starts[g + 1] - starts[g] - 1) * shared[g];
+            if (shared[g] > longest_shared) longest_shared = shared[g];
+        }
+    // Worth it?  The pass over the shared keys costs some 5 us (8 where Q does not come by TMA), and saves their bytes, read from L2 for the most part,
+    // and the walk through ranges that are as long as the prefix.  Measured with own parts of up to 200 keys, us with / without: 32q/8kv, 2
+    // requests over 4096 keys 14.3 / 12.1, over 8192 17.8 / 21.6; 16 over 512 12.8 / 10.8, over 1024 13.1 / 17.4; 4q/2kv d64, 4 over 2048
+    // 9.6 / 8.6, over 8192 11.0 / 17.6.
+    s.worth = saved * Hk * pool->desc.head_dim * 4 / 9e6 + longest_shared * (0.7 / 1024) > (rows::kBM % group == 0 ? 5. : 8.);
     for (int g = 0; g < G; ++g) {
         const int n = starts[g + 1] - starts[g];
         if (n == 0) continue;
-        const bool takes = takes_shared(n, shared[g]);
+        const bool takes = s.worth && takes_shared(n, shared[g]);
         const int own = max_blocks - (takes ? shared[g] / 16 : 0);
         if (own > s.own_blocks) s.own_blocks = own;
         if (!takes) continue;
@@ -179,7 +189,7 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
     const double fixed = 4.0;  // tiles' worth of an item's start and write-out
     double best = 1e30;
     long long most = 4LL * pool->sm_count / (row_tiles * Hk) + 1;
-    if (most > 64) most = 64;
+    if (most > ext::kMaxParts) most = ext::kMaxParts;
     if (most < 8) most = 8;
     for (int ns = 1; ns <= most && ns <= longest; ++ns) {
         const int chunk = (longest + ns - 1) / ns;
@@ -391,7 +401,7 @@ extern "C" ekv_status_t ekv_attn_decode_shared(ekv_pool_t *pool, int32_t layer, 
     int tiles = 0;
     for (int g = 0; g < G; ++g) {
         const int n = group_starts[g + 1] - group_starts[g];
-        const bool takes = takes_shared(n, shared_lens[g]);
+        const bool takes = s.worth && takes_shared(n, shared_lens[g]);
         const int kt = (shared_lens[g] + rows::kBN - 1) / rows::kBN, mine = rows::part_tiles(s.chunk_tiles, (long long)n * p.group);
         const int ns = takes ? (kt + mine - 1) / mine : 0;
         p.start[g] = rp.start[g] = group_starts[g];
