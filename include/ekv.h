@@ -472,7 +472,7 @@ EKV_API ekv_status_t ekv_attn_decode_scored(ekv_pool_t *pool, int32_t layer, con
 /* ekv_attn_prefill_chunk with such scores (tcgen05; any group, head_dim 64 or 128, any scale; calls share nothing but what they are
  * given).  workspace: DEVICE, 256-byte aligned, ekv_attn_prefill_scored_workspace_bytes(pool) bytes cover every call of the
  * pool; calls that share it must be stream-ordered.  Only a call of few rows over many keys uses it (its keys are cut into parts); one that does and has not enough is refused with EKV_ERR_WORKSPACE.
- * A NaN or an infinity in a key or value reaches the rows that see it and no others. */
+ * A NaN or an infinity in a key or value reaches the rows that see it and no others.  At most 65535 * 256 (row, head of the group) pairs a call. */
 EKV_API size_t ekv_attn_prefill_scored_workspace_bytes(const ekv_pool_t *pool);
 EKV_API ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
                                            int32_t max_blocks_per_seq, const int32_t *cu_q_lens, const int32_t *cu_q_lens_host,

@@ -11,6 +11,7 @@ namespace ekv {
 
 static constexpr float kLog2e = 1.4426950408889634f;
 static constexpr float kSmallest = 1.17549435e-38f;  // stands for a scale of 0: -inf times it is still -inf
+static constexpr float kLargest = 1e30f;             // bounds scale / cap: a score of 0 times it is still 0
 
 // Shared-memory attributes of a kernel, once per device.
 template <typename Kernel>
@@ -271,7 +272,7 @@ extern "C" ekv_status_t ekv_attn_decode_scored(ekv_pool_t *pool, int32_t layer, 
     p.slopes = scores->slopes, p.prefix_lens = scores->prefix_lens, p.window = scores->window;
     const bool cap = scores->cap > 0.f;
     p.scale_log2 = (cap ? scores->cap : scale) * kLog2e;
-    if (cap) p.cap_scale = 2.f * kLog2e * (scale / scores->cap);
+    if (cap) p.cap_scale = fmaxf(-kLargest, fminf(2.f * kLog2e * (scale / scores->cap), kLargest));
     const cudaError_t e = pool->desc.head_dim == 128 ? scored_decode<128>(pool, layer, p, cap, B, (cudaStream_t)stream)
                                                      : scored_decode<64>(pool, layer, p, cap, B, (cudaStream_t)stream);
     return e == cudaSuccess ? EKV_OK : cuda_fail(e, "ekv_attn_decode_scored launch");
@@ -337,10 +338,10 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t 
     p.scale_log2 = fmaxf((cap ? scores->cap : fabsf(scale)) * kLog2e, kSmallest);
     if (cap) {
         // cap * log2 e * tanh(a s) for |a s| <= 1/2: a minimax polynomial in a s (3e-7), its powers of a in the coefficients
-        const double a = p.cap_scale = fabsf(scale) / scores->cap, c = (double)scores->cap * kLog2e * a;
+        const double a = p.cap_scale = fminf(fabsf(scale) / scores->cap, kLargest), c = (double)scores->cap * kLog2e * a;
         p.near[0] = (float)(0.99999946 * c), p.near[1] = (float)(-0.33326319 * c * a * a);
         p.near[2] = (float)(0.13190296 * c * a * a * a * a), p.near[3] = (float)(-0.04440222 * c * a * a * a * a * a * a);
-        p.near_limit = p.near[3] < -1e-36f ? 0.5f / p.cap_scale : -1.f;  // (not where a coefficient leaves fp32's range)
+        p.near_limit = p.near[3] < -1e-36f && p.near[3] > -1e30f ? 0.5f / p.cap_scale : -1.f;  // (not where a coefficient leaves fp32's range)
     }
     const bool d128 = pool->desc.head_dim == 128;
     cudaError_t e = d128 ? scored_prefill<128>(pool, layer, p, cap, T, (cudaStream_t)stream) : scored_prefill<64>(pool, layer, p, cap, T, (cudaStream_t)stream);

@@ -56,6 +56,15 @@ def test_scores_far_beyond_the_cap():
         check(*run(b, cap=cap))
 
 
+def test_caps_of_any_size_and_queries_of_zeros():
+    b = Batch(4, 2, 64, [200, 60], [1, 1], seed=16, magnitude=20.0)
+    for cap in (1e-42, 1e-30, 1e-3, 3e3, 1e6, 1e30):
+        check(*run(b, cap=cap), str(cap))
+    b.q.zero_()
+    for cap in (1e-42, 1e-30, 50.0, 1e6):
+        check(*run(b, cap=cap), str(cap))
+
+
 def test_what_a_row_does_not_see_does_not_reach_it():
     b = Batch(4, 2, 128, [199, 150], [1, 1], seed=4)
     _, want = run(b, window=40, prefix=20)

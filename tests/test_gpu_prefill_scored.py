@@ -69,6 +69,15 @@ def test_scores_far_beyond_the_cap():
         check(*run(b, cap=cap))
 
 
+def test_caps_of_any_size_and_queries_of_zeros():
+    b = Batch(4, 2, 64, [200, 0], [40, 160], seed=16, magnitude=20.0)
+    for cap in (1e-42, 1e-30, 1e-3, 3e3, 1e6, 1e30):
+        check(*run(b, cap=cap), str(cap))
+    b.q.zero_()
+    for cap in (1e-42, 1e-30, 50.0, 1e6):
+        check(*run(b, cap=cap), str(cap))
+
+
 def test_malformed_requests_come_out_as_zeros():
     b = Batch(8, 2, 128, [10, 10, 3000], [200, 30, 5], seed=12)
     for lens in ([210, 29, 3005], [210, 40, 4]):
