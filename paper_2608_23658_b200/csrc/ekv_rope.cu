@@ -293,7 +293,8 @@ extern "C" ekv_status_t ekv_rope_write_kv(ekv_pool_t *pool, int32_t layer, const
                   q, k, v, q_out, (const void *)slot_mapping, (const void *)rope->inv_freq, (const void *)rope->positions);
         return EKV_ERR_INVALID;
     }
-    if (T > 1 && (q_stride < (int64_t)Hq * D || q_out_stride < (int64_t)Hq * D || k_stride < (int64_t)Hk * D || v_stride < (int64_t)Hk * D)) {
+    if (T > 1 && (q_stride < (int64_t)Hq * D || q_out_stride < (int64_t)Hq * D || k_stride < (int64_t)Hk * D || v_stride < (int64_t)Hk * D ||
+                  (q == q_out && q_stride != q_out_stride))) {
         set_error("ekv_rope_write_kv: rows of different tokens overlap (strides %lld, %lld, %lld, %lld)", (long long)q_stride, (long long)k_stride,
                   (long long)v_stride, (long long)q_out_stride);
         return EKV_ERR_INVALID;

@@ -2,6 +2,8 @@
 mapped part of a layer's range and keeps a decode workspace.  No arithmetic happens here."""
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import _binding as B
@@ -149,6 +151,13 @@ class Pool:
             return _raw_stream(self.device.index)
         return stream if isinstance(stream, int) else stream.cuda_stream
 
+    def _on(self, stream):
+        """Where memory that a call keeps to itself is made: on the call's own stream, so that what else becomes of it later is in that
+        stream's order, and belongs to that stream's graph while it is captured."""
+        if stream == _raw_stream(self.device.index) and torch.cuda.current_device() == self.device.index:
+            return contextlib.nullcontext()
+        return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device))
+
     def _want(self, call, name, t, dtype, shape):
         if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device.index or not t.is_contiguous():
             B._refuse(call, name, t, f"contiguous {dtype} {shape} on {self.device}")
@@ -192,7 +201,8 @@ class Pool:
         if k_out is not None:
             self._want(call, "k_out", k_out, bf16, (T, kv_heads, self.head_dim))
         elif self.dtype == B.EKV_E4M3:
-            k_out = torch.empty((T, kv_heads, self.head_dim), dtype=bf16, device=self.device)
+            with self._on(self._current(stream)):
+                k_out = torch.empty((T, kv_heads, self.head_dim), dtype=bf16, device=self.device)
         rope = B.Rope(2 * pairs, num_axes, B.EKV_ROPE_ADJACENT if interleaved else 0, factor, eps, weight_offset, inv_freq.data_ptr(),
                       positions.data_ptr(), bytes(axes) if num_axes > 1 else None, q_weight.data_ptr() if q_weight is not None else None,
                       k_weight.data_ptr() if k_weight is not None else None)
@@ -258,11 +268,11 @@ class Pool:
         two graphs share none; others share one for each stream, which grows when the library says that it is too small."""
         stream = self._current(stream)
         if workspace is not None:
-            B._check(call(workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
-        elif torch.cuda.is_current_stream_capturing():
-            own = torch.empty(max(need(), 1), dtype=torch.uint8, device=self.device)
-            B._check(call(own.data_ptr(), own.numel(), stream))
-        else:
+            return B._check(call(workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
+        with self._on(stream):
+            if torch.cuda.is_current_stream_capturing():
+                own = torch.empty(max(need(), 1), dtype=torch.uint8, device=self.device)
+                return B._check(call(own.data_ptr(), own.numel(), stream))
             kept = self._parts.get(stream)
             st = call(kept[-1].data_ptr(), kept[-1].numel(), stream) if kept else B.Status.ERR_WORKSPACE
             if st == B.Status.ERR_WORKSPACE:  # (the ones that were too small stay: calls that are under way use them)

@@ -139,3 +139,25 @@ def test_refusals():
         b.pool.attn_decode_scored(0, b.q, long, b.seq_lens, b.scale, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
     assert e.value.status == ekv.Status.ERR_WORKSPACE
     assert b.pool.attn_decode_scored(0, b.q[:0], b.tables[:0], b.seq_lens[:0], b.scale, cap=1.0).shape == (0, 4, 64)
+
+
+def test_workspaces_belong_to_the_streams_that_use_them():
+    b, side = Batch(8, 2, 128, [5011, 800], [1, 1], seed=12), torch.cuda.Stream()
+    want = b.pool.attn_decode_scored(0, b.q, b.tables, b.seq_lens, b.scale, cap=9.0)
+    out = torch.empty_like(want)
+    torch.cuda.synchronize()
+    b.pool.attn_decode_scored(0, b.q, b.tables, b.seq_lens, b.scale, cap=9.0, out=out, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want)
+    mine = b.pool._parts[side.cuda_stream][-1].data_ptr()
+    assert [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= mine < s["address"] + s["total_size"]] == [side.cuda_stream]
+    graph = torch.cuda.CUDAGraph()      # captured on a stream, the call given another one that was forked from it
+    out.zero_()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        b.pool.attn_decode_scored(0, b.q, b.tables, b.seq_lens, b.scale, cap=9.0, out=out, stream=side)
+        main.wait_stream(side)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)

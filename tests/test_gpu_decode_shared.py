@@ -121,7 +121,7 @@ def test_bad_shared_block_ids_are_skipped_and_latched(p):
 def test_replayed_while_the_requests_grow_two_graphs_side_by_side():
     b = make(8, 2, 128, [(20, 8000), (3, 64)], [70, 200], seed=6, stale=False)
     need = ekv.ekv_attn_decode_shared_workspace_bytes(b.pool.handle, b.starts, b.shared, b.tables.shape[1])
-    lens, outs, graphs = b.seq_lens.clone(), [], []
+    lens, outs, graphs, kept = b.seq_lens.clone(), [], [], []
     run(b)
     torch.cuda.synchronize()
     for _ in range(2):
@@ -129,7 +129,7 @@ def test_replayed_while_the_requests_grow_two_graphs_side_by_side():
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
             b.pool.attn_decode_shared(0, b.q, b.tables, lens, b.starts, b.shared, b.scale, out=out, workspace=ws)
-        outs.append(out), graphs.append(g)
+        outs.append(out), graphs.append(g), kept.append(ws)             # (a graph does not keep what it was handed)
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
     for drop in (0, 13, 60):
         lens.copy_(b.seq_lens - drop)

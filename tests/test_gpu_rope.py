@@ -172,3 +172,40 @@ def test_on_a_stream_of_its_own_and_replayed():
         pool.rope_write_kv(0, q, k, v, positions, inv_freq, slots2, q_weight=qw, k_weight=kw, q_out=out)
     side.synchronize()
     assert torch.equal(out, want)
+
+
+def test_refusals():
+    pool, q, k, v, slots, positions, axes, inv_freq, qw, kw = make(6, 4, 2, 64, 64, 2, True)
+    call = lambda pool=pool, layer=0, q=q, k=k, v=v, axes=axes, inv_freq=inv_freq, **more: pool.rope_write_kv(
+        layer, q, k, v, positions, inv_freq, slots, axes=axes, **{"q_weight": qw, "k_weight": kw, **more})
+    before = pool.layer_tensor(0).clone()
+    wide = torch.zeros(6 * 8 * 64 + 8, dtype=BF16, device=DEV)
+    apart = lambda heads, stride, first=0: torch.as_strided(wide, (6, heads, 64), (stride, 64, 1), first)
+    long = torch.ones(33, device=DEV)
+    for bad in ({"layer": 1}, {"layer": -1}, {"axes": [0] * 31 + [2]}, {"eps": -1.0}, {"eps": float("nan")}, {"inv_freq": long, "axes": [0] * 33},
+                {"q": apart(4, 64)}, {"k": apart(2, 64)}, {"v": apart(2, 64)}, {"q_out": apart(4, 192)},      # tokens over one another
+                {"q": apart(4, 256), "q_out": apart(4, 320)},
+                {"q": apart(4, 260)}, {"k": apart(2, 132)}, {"v": apart(2, 256, 4)}, {"q_out": apart(4, 256, 1)},   # off 16 bytes
+                {"k_weight": torch.zeros(72, dtype=BF16, device=DEV)[1:65]}, {"k_out": torch.empty((6, 2, 64), dtype=BF16, device=DEV)}):
+        with pytest.raises(ekv.EkvError) as e:
+            call(**bad)
+        assert e.value.status == ekv.Status.ERR_INVALID, bad
+    torch.cuda.synchronize()
+    assert torch.equal(pool.layer_tensor(0).view(torch.int16), before.view(torch.int16)) and not wide.any()
+    call()
+
+
+def test_the_keys_of_an_8bit_pool_pass_through_memory_of_the_calls_stream():
+    T, side = 400, torch.cuda.Stream()
+    pool, q, k, v, slots, positions, axes, inv_freq, qw, kw = make(T, 4, 2, 128, 128, 1, True, dtype=ekv.EKV_E4M3)
+    slots, out = torch.arange(T, device=DEV), torch.empty((T, 4, 128), dtype=BF16, device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    before = torch.cuda.memory_stats()["allocation.all.allocated"]
+    pool.rope_write_kv(0, q, k, v, positions, inv_freq, slots, q_weight=qw, k_weight=kw, q_out=out, stream=side)
+    assert torch.cuda.memory_stats()["allocation.all.allocated"] == before + 1
+    assert any(s["stream"] == side.cuda_stream for s in torch.cuda.memory_snapshot())
+    side.synchronize()
+    got = pool.read_kv(0, slots)
+    pool.rope_write_kv(0, q, k, v, positions, inv_freq, slots, q_weight=qw, k_weight=kw, q_out=out)
+    assert all(torch.equal(a, b) for a, b in zip(got, pool.read_kv(0, slots)))
