@@ -158,14 +158,14 @@ def test_replayed_side_by_side():
     slopes = slopes_of(8)
     want = b.model(cap=9.0, window=200, slopes=slopes)
     run(b, cap=9.0, window=200, bias=True)
-    graphs, outs, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    graphs, outs, kept, streams = [], [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
     need = ekv.ekv_attn_prefill_scored_workspace_bytes(b.pool.handle)
     torch.cuda.synchronize()
     for _ in range(2):
         g, out, ws = torch.cuda.CUDAGraph(), torch.zeros_like(b.q), torch.empty(need, dtype=torch.uint8, device=DEV)
         with torch.cuda.graph(g):
             b.pool.attn_prefill_chunk_scored(0, b.q, b.tables, b.cu, b.cu_host, b.seq_lens, b.scale, cap=9.0, window=200, slopes=slopes, out=out, workspace=ws)
-        graphs.append(g), outs.append(out)
+        graphs.append(g), outs.append(out), kept.append(ws)             # (a graph does not keep what it was handed)
     for _ in range(5):
         for s, g in zip(streams, graphs):
             with torch.cuda.stream(s):
@@ -194,3 +194,43 @@ def test_refusals():
     e4m3 = ekv.Pool(num_q_heads=4, num_kv_heads=2, head_dim=64, base_blocks=16, dtype=ekv.EKV_E4M3)
     with pytest.raises(ekv.EkvError):
         e4m3.attn_prefill_chunk_scored(0, b.q, b.tables, b.cu, b.cu_host, b.seq_lens, b.scale, cap=3.0)
+
+
+# A few more items than SMs, over long tables.
+SECOND_ROUND = [
+    (32, 8, 128, [9000], [1300], 0, {"cap": 30.0}),                    # 168 items
+    (28, 4, 128, [8500], [1400], 0, {"bias": True}),                   # 156, whose rows end inside a position's heads
+    (5, 1, 64, [700], [8000], 0, {"prefix": 8400}),
+    (8, 8, 64, [4000], [4900], 0, {"window": 8300}),                   # 160, a head each
+    (32, 8, 128, [9000, 3, 0, 100], [1100, 40, 0, 200], 0, {}),
+    (32, 8, 128, [100, 3, 0, 9000], [200, 40, 0, 1100], 0, {}),
+    (32, 8, 128, [0], [1300], 700, {"cap": 30.0}),                     # long tables, few keys
+    (32, 8, 128, [0, 1200], [700, 700], 700, {}),
+]
+
+
+@pytest.mark.parametrize("Hq,Hk,D,past,new,extra,mods", SECOND_ROUND, ids=str)
+def test_a_second_round_of_items(Hq, Hk, D, past, new, extra, mods):
+    b = Batch(Hq, Hk, D, past, new, seed=Hq + D, table_extra=extra, magnitude=4.0 if "cap" in mods else 1.0)
+    got, want = run(b, **mods)
+    check(got, want, str(mods))
+    for _ in range(3):
+        assert torch.equal(run(b, skip=range(len(new)), **mods)[0], got)
+
+
+def test_a_second_round_with_values_that_are_not_finite_and_a_malformed_request():
+    b = Batch(32, 8, 128, [9000, 5000], [700, 600], seed=21)
+    got, (want, bound) = run(b)
+    check(got, (want, bound))
+    key = 5000 + 300                                                # of the second request, seen by its rows from 300 on
+    b.cache[int(b.tables[1, key // 16]), 1, :, key % 16, 7] = float("inf")
+    key = 9000 + 20                                                 # of the first
+    b.cache[int(b.tables[0, key // 16]), 1, 2, key % 16, 9] = float("nan")
+    hurt = run(b, skip=[0, 1])[0]
+    assert (hurt[1000:, :, 7] == float("inf")).all() and torch.isnan(hurt[20:700, 8:12, 9]).all()
+    hurt[1000:, :, 7], hurt[20:700, 8:12, 9] = got[1000:, :, 7], got[20:700, 8:12, 9]
+    assert torch.equal(hurt, got)
+    b.seq_lens[0] = 699
+    hurt = run(b, skip=[0, 1])[0]
+    torch.cuda.synchronize()
+    assert (hurt[:700] == 0).all() and b.pool.poll_status() == ekv.Status.ERR_BLOCK_OOB
