@@ -2,9 +2,13 @@
 //
 // The split pass of ekv_decode.cu -- a CTA per (sequence, kv-head, range of keys), each warp a ring of TMA loads for every fourth block of 16
 // keys, the heads of the group as the rows of mma.m16n8k16, partial (m, l, O) per range -- over those blocks alone that the sequence sees:
-// of its prefix and of its window, or from the end of the shared keys on.  Bound by the bytes of these.  Where a sequence has a single
-// range (many do, where the tables are wider than the sequences long) the CTA writes the final rows itself; in a shared call it takes the shared keys' parts (left by the rows kernel, beside whose last
-// CTAs this launch comes up) along.  Otherwise combine_ext_kernel does, a warp a (sequence, head).
+// of its prefix and of its window, or from the end of the shared keys on.  Bound by the bytes of these: 64 sequences of up to 16000 keys, 32q/8kv, 1.04 GB
+// in 158 to 164 us = 6.4 to 6.6 TB/s.  Where a sequence has a single range (many do, where the tables are wider than the sequences long) the CTA
+// writes the final rows itself; otherwise combine_ext_kernel does, a warp a (sequence, head).
+// In a shared call this launch comes up beside the rows kernel's, which takes an SM for an item and is cut so that SMs are left, and fills the rest as its
+// items end; combine_ext_kernel adds the parts of both.  256 requests of 17..700 own keys behind 16384 shared ones: 114 us, one after the other
+// 130; nine groups of 28q/4kv 37 for 48.  Only the last CTA waits for the rows kernel, so that the launch behind this one finds both done.
+// With next to no own keys each CTA waits and takes the shared keys' parts along instead, which saves a launch.
 #pragma once
 #include "ekv_rows.cuh"
 
@@ -14,7 +18,7 @@ namespace ext {
 using rows::kMaxGroups;
 
 static constexpr int kWarps = 4;
-static constexpr int kStages = 2;  // of a warp; 64 KB in all, so that three CTAs fit an SM: with three stages and two CTAs, 256 short own parts took 89 us for 79
+static constexpr int kStages = 2;  // of a warp; 64 KB in all, so that three CTAs fit an SM: with three stages and two CTAs, own parts of 256 requests took 88 us for 75
 static constexpr int kBoxBytes = 16 * 128;  // 16 tokens x 64 channels
 static constexpr int kMaxParts = 64;        // that the rows kernel cuts shared keys into
 
@@ -34,6 +38,7 @@ struct Params {
     int chunk_tokens, nsplit;
     int window;
     int parts, G;
+    int beside;               // shared call: the two passes run side by side, and combine_ext_kernel adds the shared keys' parts
     float scale_log2;         // scale * log2 e; with a cap: cap * log2 e
     float cap_scale;          // with a cap: 2 * log2 e * scale / cap
     int start[kMaxGroups + 1];     // shared call: first request of a group,
@@ -97,8 +102,9 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the combine pass comes up in the tail of this one
     const Span sp = span_of<kShared>(p, b);
     const int t_begin = split * p.chunk_tokens;
+    const bool is_last = split == (int)gridDim.x - 1 && g == (int)gridDim.y - 1 && b == (int)gridDim.z - 1;
     if (split > 0 && t_begin >= sp.tokens) {  // whole CTA leaves before any barrier exists
-        if (kShared) asm volatile("griddepcontrol.wait;" ::: "memory");  // this launch is not over before the one it came up beside
+        if (kShared && (!p.beside || is_last)) asm volatile("griddepcontrol.wait;" ::: "memory");  // this launch is not over before the one it came up beside
         return;
     }
     if (kShared && sp.invalid && split == 0 && g == 0 && threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
@@ -294,11 +300,11 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
         wm[8 + r] = l_run;
     }
     __syncthreads();
-    if (kShared) asm volatile("griddepcontrol.wait;" ::: "memory");  // the shared keys' parts are complete
+    if (kShared && (!p.beside || is_last)) asm volatile("griddepcontrol.wait;" ::: "memory");  // the shared keys' parts are complete
     // The weights of what a head's row is made of -- the four warps' results and, where the sequence ends here, the shared keys' parts -- once a
     // head, by a warp; then a thread a channel.  (In warp 0's second stage: idle, too.)
     constexpr int kTerms = kWarps + kMaxParts;
-    const bool last = sp.tokens <= p.chunk_tokens;  // the sequence's only range: finish here
+    const bool last = sp.tokens <= p.chunk_tokens && !(kShared && p.beside && sp.parts > 0);  // the sequence's only range: finish here
     const int n_parts = kShared && last ? sp.parts : 0;
     float *weights = reinterpret_cast<float *>(base_ptr + STAGE_BYTES);  // [8][kTerms]
     float *rowsum = weights + 8 * kTerms;                                // [8] l, [8] m
@@ -419,7 +425,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) combine_ext_kernel(const _
     }
     const Span sp = span_of<kShared>(p, row / p.num_q_heads);  // (lengths and offsets were there before the split pass)
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (sp.tokens <= p.chunk_tokens) return;  // finished by the split pass
+    if (sp.tokens <= p.chunk_tokens && !(kShared && p.beside && sp.parts > 0)) return;  // finished by the split pass
     RowSum<D> sum;
     if (kShared) sum.add(p.shared_o + (size_t)row * p.parts * D, p.shared_ml + (size_t)row * p.parts, sp.parts);
     sum.add(p.part_o + (size_t)row * p.nsplit * D, p.part_ml + (size_t)row * p.nsplit, (sp.tokens + p.chunk_tokens - 1) / p.chunk_tokens);

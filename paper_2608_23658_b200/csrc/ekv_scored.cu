@@ -56,7 +56,7 @@ static cudaError_t launch_ext(ekv_pool *pool, int layer, const ext::Params &p, i
     cudaError_t e = ready(ext::decode_ext_kernel<D, kShared, kCap, kBias>, kBytes, pool->desc.device, done);
     if (e != cudaSuccess) return e;
     e = launch(ext::decode_ext_kernel<D, kShared, kCap, kBias>, dim3(p.nsplit, p.num_kv_heads, B), ext::kWarps * 32, kBytes, early, stream, pool->kv_map[layer], p);
-    if (e != cudaSuccess || p.nsplit == 1) return e;
+    if (e != cudaSuccess || (p.nsplit == 1 && !p.beside)) return e;
     const int n = B * p.num_q_heads;
     return launch(ext::combine_ext_kernel<D, kShared>, dim3((n + ext::kCombineWarps - 1) / ext::kCombineWarps), ext::kCombineWarps * 32, 0, true, stream, p, n);
 }
@@ -104,7 +104,7 @@ static void fill_ext(ext::Params &p, const ekv_pool *pool, const void *q, void *
     p.max_blocks = max_blocks, p.num_q_heads = pool->desc.num_q_heads, p.num_kv_heads = pool->desc.num_kv_heads;
     p.group = p.num_q_heads / p.num_kv_heads;
     p.chunk_tokens = plan.chunk_tokens, p.nsplit = plan.nsplit;
-    p.window = 0, p.parts = 0, p.G = 0;
+    p.window = 0, p.parts = 0, p.G = 0, p.beside = 0;
     p.cap_scale = 0.f;
 }
 
@@ -151,6 +151,7 @@ static int plan_parts(const ekv_pool *pool, long long items, int max_blocks, int
 struct SharedPlan {
     int chunk_tiles, parts, tiles;  // tiles: items per kv-head
     int own_blocks;                 // the longest table behind shared blocks
+    double own_work;                // estimate of the pass over the requests' own keys, in key tiles
     bool worth, any;                // shared keys are read for all requests of a group at once; some group has any
 };
 
@@ -160,9 +161,10 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
     const int group = pool->desc.num_q_heads / pool->desc.num_kv_heads, Hk = pool->desc.num_kv_heads;
     SharedPlan s;
     s.any = s.worth = false;
-    s.chunk_tiles = 1, s.parts = 0, s.tiles = 0, s.own_blocks = 1;
+    s.chunk_tiles = 1, s.parts = 0, s.tiles = 0, s.own_blocks = 1, s.own_work = 0.;
     int longest = 0, longest_shared = 0;
     long long row_tiles = 0, saved = 0;
+    long long requests = 0, alone = 0, room = max_blocks;
     for (int g = 0; g < G; ++g)
         if (takes_shared(starts[g + 1] - starts[g], shared[g])) {
             saved += (long long)(starts[g + 1] - starts[g] - 1) * shared[g];
@@ -178,6 +180,9 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
         if (n == 0) continue;
         const bool takes = s.worth && takes_shared(n, shared[g]);
         const int own = max_blocks - (takes ? shared[g] / 16 : 0);
+        requests += n;
+        if (!takes) alone += (long long)n * (shared[g] / 16);
+        if (max_blocks - shared[g] / 16 < room) room = max_blocks - shared[g] / 16;
         if (own > s.own_blocks) s.own_blocks = own;
         if (!takes) continue;
         s.any = true;
@@ -186,7 +191,13 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
         row_tiles += ((long long)n * group + rows::kItemRows - 1) / rows::kItemRows;
     }
     if (!s.any) return s;
-    // The cut with the shortest estimated time: rounds of the machine times an item's tiles and what it costs besides them.
+    // Keys of their own that requests have are known as an upper bound, the room in the tables; taken as half of what the longest prefix leaves.  In units
+    // of a tile's time on an SM (2.1 us), of which an SM reads 84 KB.
+    s.own_work = (alone + 0.5 * requests * room) * (64 * Hk * pool->desc.head_dim) / 84e3;
+    // The cut with the shortest estimated time: rounds of the machine times an item's tiles and what it costs besides them; or, as the own keys
+    // are read on SMs that this pass leaves free, all of both (an item's SM comes free late: 8 tiles; own work counts up to as much as the shared, since
+    // tables may be far wider than the sequences are long); and the adding up of parts.  Measured, us, by items: nine groups of 28q/4kv 32 items 97, 64 41,
+    // 68 37, 96 42, 136 50; 256 requests over 16384 keys 64 items 137, 96 114, 128 124, 256 134; 16 over 8192 64 items 21.3, 128 20.5, 256 25.3.
     const double fixed = 4.0;  // tiles' worth of an item's start and write-out
     double best = 1e30;
     long long most = 4LL * pool->sm_count / (row_tiles * Hk) + 1;
@@ -209,7 +220,8 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
             if (cut > parts) parts = cut;
         }
         const double rounds = (double)((items + pool->sm_count - 1) / pool->sm_count), mean = work / items + fixed;
-        const double t = fmax(rounds * mean, worst + fixed);
+        const double beside = fmin(s.own_work / work, 1.);
+        const double t = fmax(fmax(rounds * mean, worst + fixed), (items * (mean + 8. * beside) + work * beside) / pool->sm_count) + 0.08 * parts;
         if (t < best) best = t, s.chunk_tiles = chunk, s.parts = parts;
     }
     return s;
@@ -217,7 +229,7 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
 
 static size_t shared_need(const ekv_pool *pool, const SharedPlan &s, const DecodePlan &own, int B) {
     const size_t rows = (size_t)B * pool->desc.num_q_heads;
-    return (own.nsplit > 1 ? parts_bytes(pool, rows * own.nsplit) : 0) + (s.any ? parts_bytes(pool, rows * s.parts) : 0);
+    return (own.nsplit > 1 || s.any ? parts_bytes(pool, rows * own.nsplit) : 0) + (s.any ? parts_bytes(pool, rows * s.parts) : 0);
 }
 
 static ekv_status_t check_groups(const char *who, const ekv_pool *pool, const int32_t *starts, const int32_t *shared, int G, int max_blocks, int B) {
@@ -397,6 +409,9 @@ extern "C" ekv_status_t ekv_attn_decode_shared(ekv_pool_t *pool, int32_t layer, 
     p.shared_ml = rp.part_ml, p.shared_o = rp.part_o;
     p.parts = rp.parts = s.parts;
     p.G = rp.R = G;
+    // Side by side, and added up by a launch of their own, unless there is next to nothing to read beside the shared keys (4 requests over 16384 shared
+    // keys, up to 64 own ones: 22.4 us for 20.5).
+    p.beside = s.any && (plan.nsplit > 1 || s.own_work > 32.);
     p.scale_log2 = rp.scale_log2 = scale * kLog2e;
     rp.chunk_tiles = s.chunk_tiles;
     int tiles = 0;
