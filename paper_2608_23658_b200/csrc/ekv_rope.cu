@@ -4,13 +4,15 @@
 //   (a, b) -> factor * (a cos t - b sin t, b cos t + a sin t)          (pairs of channels), t = position[axis of the pair] * inv_freq[pair]
 //   queries -> q_out, keys and values -> their slots of the cache      (rounded to bf16 once, at the end)
 //
-// Bound by memory: every element is read once and written once.  A row of head_dim channels belongs to D / 16 neighbouring lanes, two pieces
-// of 16 bytes each; where pairs are halves of a row the pieces are chosen so that both channels of a pair are in one thread, so a rotation is
-// register arithmetic and only the sum of squares is shuffled.  (With one piece a thread, and the partners' values by shuffles, the
-// arithmetic took longer than the bytes: 16384 tokens of 32q/8kv 119 us.)  A CTA takes one or a few whole tokens: their sines and cosines are worked out
-// once, into shared memory, for all heads, while the first rows are on their way, and the next rows are always on theirs.  The angle is taken
-// in turns in 64 bits (position * inv_freq needs up to 55 bits; in fp32 a position of 10^6 would be off by 0.06 rad) and only its
-// fraction is turned into a sine and a cosine.
+// Every element is read once and written once: 403 MB for 16384 tokens of 32q/8kv, 76 to 80 us = 5.0 to 5.3 TB/s of the 6.5 that a copy gets; the
+// arithmetic between takes two thirds of the issue slots and is what keeps it from the rest.  2049 tokens of 28q/4kv 8 us, 256 of 32q/8kv 4, 31 of
+// 4q/2kv 3, on the device.
+// A row of head_dim channels belongs to D / 16 neighbouring lanes, two pieces of 16 bytes each; where pairs are halves of a row the pieces are
+// chosen so that both channels of a pair are in one thread, so a rotation is register arithmetic and only the sum of squares is shuffled.
+// (With one piece a thread, and the partners' values by shuffles: 16384 tokens of 32q/8kv 119 us.)  A CTA takes some whole tokens: their sines
+// and cosines are worked out once, into shared memory, for all heads, while the first rows are on their way, and the next rows are always on
+// theirs.  The angle is taken in turns in 64 bits (position * inv_freq needs up to 55 bits; in fp32 a position of 10^6 would be off by 0.06 rad) and
+// only its fraction is turned into a sine and a cosine.
 #include <cuda_bf16.h>
 
 #include <algorithm>

@@ -7,24 +7,35 @@
 // partial results go to the workspace.
 //
 // A work item is 256 rows of ONE kv-head -- (position, head of the group) pairs in that order, in a shared pass (request, head) -- so all
-// heads that share a K/V tile meet it in one place, whatever their number, and rows of many short requests fill a tile.  The CTA has two
-// slots (S and O in TMEM, 128 columns each, and a softmax warpgroup with a thread a row) that take turns: the softmax of one runs beside the MMAs of
-// the other.  More than 128 rows: a slot for each half, both on every key tile.  Fewer: both slots hold the SAME rows and take every
-// other key tile; their results meet in TMEM, where the first slot's warps can read the other's accumulator, row by row.
+// heads that share a K/V tile meet it in one place, whatever their number, and rows of many short requests fill a tile.  The CTA has two slots (S and O in
+// TMEM, 128 columns each, and a softmax warpgroup with a thread a row) that take turns: the softmax of one runs beside the MMAs of the other.
+// More than 128 rows: a slot for each half, both on every key tile.  Fewer: both slots hold the SAME rows and take every other key tile; their
+// results meet in TMEM, where the first slot's warps can read the other's accumulator, row by row.
 // Key tiles that no row of the item sees are not read: an item's tiles are those of the prefix and those of the window.
 // A call of few items cuts each one's tiles into `parts`; (m, l, O) of each part go to the workspace.
 //
 //   warp 0        MMA issuer: S = Q K^T (both from shared memory), O += P V (P from TMEM, V MN-major), the slots by turns
-//   warp 1        TMEM; TMA producer of V tiles; warp 2: item scheduler: the kernel is persistent, a CTA an SM, items by cluster launch control (no word of device memory that
-//                 two launches or replays could share)
+//   warp 1        TMEM; TMA producer of V tiles
+//   warp 2        item scheduler: the kernel is persistent, a CTA an SM, items by cluster launch control (no word of device memory that two
+//                 launches or replays could share)
+//   warp 3        barriers, before anything else
 //   warps 4-7     softmax and write-out of slot 0: a thread a row
 //   warps 8-11    of slot 1
 //   warp 12       TMA producer of K tiles
-//   warps 13-15   Q rows into shared memory (by TMA where the group divides a tile), and the care of V tiles that not every row sees whole: rows of V at keys nobody sees become 0;
-//                 values that are not finite at keys that some rows see and others do not are taken out (a weight of 0 does not stop a NaN) and
-//                 given to the rows they belong to after the write-out.
+//   warps 13-15   Q rows into shared memory (by TMA where the group divides a tile), and the care of V tiles that not every row sees whole: rows of V
+//                 at keys nobody sees become 0; values that are not finite at keys that some rows see and others do not are taken out (a weight of 0
+//                 does not stop a NaN) and given to the rows they belong to after the write-out
 // All roles run on their own clocks through rings and barriers whose phases are counted over the CTA's whole life, so that an item's Q and
 // first tiles are under way while the one before is finished.
+//
+// What bounds it is the chain of a slot: S ready, maximum, 128 weights a thread, P stored, P V issued; the tensor pipe is busy 43 to 54 % of a long
+// item.  Measured, one B200, head_dim 128, back to back, us, without modifications / capped / with the distance bias:
+//   2048 positions over 14001 keys, 32q/8kv   443 to 460 (1100 to 1140 TFLOP/s) / 600 to 670, by the scores' size and the power cap / 560 to 580
+//   a prompt of 8192, 32q/8kv                 465 to 510 / 655 / 593 to 620
+//   24 prompts of up to 1500, 28q/4kv         202 / 283 / 229 to 253
+//   64 positions over 8000 keys, 32q/8kv      28 / 32 / 30
+// With a window of 257 keys the first takes 35.  256 requests' rows over 16384 shared keys, 32q/8kv: 76 = 920 TFLOP/s.
+// A thread a row: two threads a row halve the chain's exponentials but pay shuffles and twice the fixed work (754 -> 791 us for 2048 capped rows).
 #pragma once
 #include "ekv_prefill_tc.cuh"
 

@@ -152,11 +152,9 @@ class Pool:
         return stream if isinstance(stream, int) else stream.cuda_stream
 
     def _on(self, stream):
-        """Where memory that a call keeps to itself is made: on the call's own stream, so that what else becomes of it later is in that
-        stream's order, and belongs to that stream's graph while it is captured."""
-        if stream == _raw_stream(self.device.index) and torch.cuda.current_device() == self.device.index:
-            return contextlib.nullcontext()
-        return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=self.device))
+        """Where memory that a call keeps to itself is made, if a stream was given: on that stream, so that what becomes of the memory later is
+        in the stream's order, and so that it belongs to the stream's graph while one is captured."""
+        return torch.cuda.stream(torch.cuda.ExternalStream(self._current(stream), device=self.device))
 
     def _want(self, call, name, t, dtype, shape):
         if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device.index or not t.is_contiguous():
@@ -201,7 +199,7 @@ class Pool:
         if k_out is not None:
             self._want(call, "k_out", k_out, bf16, (T, kv_heads, self.head_dim))
         elif self.dtype == B.EKV_E4M3:
-            with self._on(self._current(stream)):
+            with contextlib.nullcontext() if stream is None else self._on(stream):
                 k_out = torch.empty((T, kv_heads, self.head_dim), dtype=bf16, device=self.device)
         rope = B.Rope(2 * pairs, num_axes, B.EKV_ROPE_ADJACENT if interleaved else 0, factor, eps, weight_offset, inv_freq.data_ptr(),
                       positions.data_ptr(), bytes(axes) if num_axes > 1 else None, q_weight.data_ptr() if q_weight is not None else None,
@@ -266,20 +264,25 @@ class Pool:
     def _launch(self, call, need, workspace, stream):
         """call(workspace, its bytes, stream), with the workspace that was handed in.  Without one: a captured call gets memory of its graph, so that
         two graphs share none; others share one for each stream, which grows when the library says that it is too small."""
-        stream = self._current(stream)
         if workspace is not None:
-            return B._check(call(workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
-        with self._on(stream):
-            if torch.cuda.is_current_stream_capturing():
-                own = torch.empty(max(need(), 1), dtype=torch.uint8, device=self.device)
-                return B._check(call(own.data_ptr(), own.numel(), stream))
-            kept = self._parts.get(stream)
-            st = call(kept[-1].data_ptr(), kept[-1].numel(), stream) if kept else B.Status.ERR_WORKSPACE
-            if st == B.Status.ERR_WORKSPACE:  # (the ones that were too small stay: calls that are under way use them)
-                kept = self._parts.setdefault(stream, [])
-                kept.append(torch.empty(max(need(), 2 * kept[-1].numel() if kept else 1 << 20), dtype=torch.uint8, device=self.device))
-                st = call(kept[-1].data_ptr(), kept[-1].numel(), stream)
-            B._check(st)
+            B._check(call(workspace.data_ptr(), workspace.numel() * workspace.element_size(), self._current(stream)))
+        elif stream is None and torch.cuda.current_device() == self.device.index:
+            self._launch_here(call, need, self._current(None))
+        else:
+            with self._on(stream):
+                self._launch_here(call, need, self._current(stream))
+
+    def _launch_here(self, call, need, stream):
+        if torch.cuda.is_current_stream_capturing():
+            own = torch.empty(max(need(), 1), dtype=torch.uint8, device=self.device)
+            return B._check(call(own.data_ptr(), own.numel(), stream))
+        kept = self._parts.get(stream)
+        st = call(kept[-1].data_ptr(), kept[-1].numel(), stream) if kept else B.Status.ERR_WORKSPACE
+        if st == B.Status.ERR_WORKSPACE:  # (the ones that were too small stay: calls that are under way use them)
+            kept = self._parts.setdefault(stream, [])
+            kept.append(torch.empty(max(need(), 2 * kept[-1].numel() if kept else 1 << 20), dtype=torch.uint8, device=self.device))
+            st = call(kept[-1].data_ptr(), kept[-1].numel(), stream)
+        B._check(st)
 
     def attn_decode_scored(self, layer, q, block_tables, seq_lens, scale, cap=0.0, window=0, slopes=None, prefix_lens=None, out=None,
                            workspace=None, stream=None):
