@@ -20,6 +20,7 @@ using rows::kMaxGroups;
 static constexpr int kWarps = 4;
 static constexpr int kStages = 2;  // of a warp; 64 KB in all, so that three CTAs fit an SM: with three stages and two CTAs, own parts of 256 requests took 88 us for 75
 static constexpr int kBoxBytes = 16 * 128;  // 16 tokens x 64 channels
+static constexpr int kCluster = 8;          // ranges of a sequence that are a cluster, at most
 static constexpr int kMaxParts = 64;        // that the rows kernel cuts shared keys into
 
 struct Params {
@@ -38,6 +39,7 @@ struct Params {
     int chunk_tokens, nsplit;
     int window;
     int parts, G;
+    int cluster;              // a sequence's ranges are a cluster, which adds them up itself
     int beside;               // shared call: the two passes run side by side, and combine_ext_kernel adds the shared keys' parts
     float scale_log2;         // scale * log2 e; with a cap: cap * log2 e
     float cap_scale;          // with a cap: 2 * log2 e * scale / cap
@@ -103,7 +105,9 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
     const Span sp = span_of<kShared>(p, b);
     const int t_begin = split * p.chunk_tokens;
     const bool is_last = split == (int)gridDim.x - 1 && g == (int)gridDim.y - 1 && b == (int)gridDim.z - 1;
-    if (split > 0 && t_begin >= sp.tokens) {  // whole CTA leaves before any barrier exists
+    // Ranges of a cluster meet at its end if there are several: those without keys then stay.
+    const bool meet = p.cluster && sp.tokens > p.chunk_tokens;
+    if (split > 0 && t_begin >= sp.tokens && !meet) {  // whole CTA leaves before any barrier exists
         if (kShared && (!p.beside || is_last)) asm volatile("griddepcontrol.wait;" ::: "memory");  // this launch is not over before the one it came up beside
         return;
     }
@@ -308,6 +312,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
     const int n_parts = kShared && last ? sp.parts : 0;
     float *weights = reinterpret_cast<float *>(base_ptr + STAGE_BYTES);  // [8][kTerms]
     float *rowsum = weights + 8 * kTerms;                                // [8] l, [8] m
+    float *result = reinterpret_cast<float *>(base_ptr + (kStages + 1) * STAGE_BYTES);  // [8][D], in warp 1's second stage
     static_assert((8 * kTerms + 16) * 4 <= STAGE_BYTES && (8 * D + 16) * 4 <= STAGE_BYTES, "merge area");
     for (int h = warp; h < p.group; h += kWarps) {
         const size_t row = (size_t)b * p.num_q_heads + (size_t)g * p.group + h;
@@ -353,12 +358,38 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
         }
         if (last) {
             p.out[row * D + ch] = __float2bfloat16_rn(finish(acc, rowsum[h]));
+        } else if (meet) {
+            result[e] = acc;
         } else {
             const size_t slot = row * p.nsplit + split;
             p.part_o[slot * D + ch] = acc;
             if (ch == 0) p.part_ml[slot] = make_float2(rowsum[8 + h], rowsum[h]);
         }
     }
+    if (!meet) return;
+    // ---- ranges: each CTA adds up a share of the elements out of the shared memories of all of the cluster
+    cluster_barrier();
+    const uint32_t result_at = base_u32 + (uint32_t)((uint8_t *)result - base_ptr), rowsum_at = base_u32 + (uint32_t)((uint8_t *)rowsum - base_ptr);
+    for (int e = split * kWarps * 32 + threadIdx.x; e < p.group * D; e += p.nsplit * kWarps * 32) {
+        const int h = e / D;
+        float l[kCluster], m[kCluster], mstar = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) {
+            const uint32_t at = map_to_cta(rowsum_at + 4 * h, min(i, p.nsplit - 1));
+            l[i] = i < p.nsplit ? ld_cluster_f1(at) : 0.f;
+            m[i] = i < p.nsplit ? ld_cluster_f1(at + 32) : -INFINITY;
+            mstar = fmaxf(mstar, m[i]);
+        }
+        float acc = 0.f, lsum = 0.f;
+#pragma unroll
+        for (int i = 0; i < kCluster; ++i) {  // (a range without a maximum has a sum of 0, or NaN if its scores were NaN)
+            const float w = m[i] > -INFINITY ? fast_exp2(m[i] - mstar) : 0.f;
+            lsum += w * l[i];
+            if (w != 0.f) acc += w * ld_cluster_f1(map_to_cta(result_at + 4 * e, i));
+        }
+        p.out[((size_t)b * p.num_q_heads + (size_t)g * p.group) * D + e] = __float2bfloat16_rn(finish(acc, lsum));
+    }
+    cluster_barrier();  // nobody leaves while its shared memory is read
 }
 
 // Adds the parts of a row, a list at a time: a warp a row, D / 32 channels a lane, eight parts' loads under way.

@@ -23,17 +23,25 @@ static cudaError_t ready(Kernel kernel, int bytes, int device, bool (&done)[64])
 }
 
 template <typename... P, typename... A>
-static cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, int bytes, bool early, cudaStream_t stream, A... args) {
+static cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, int bytes, bool early, int cluster, cudaStream_t stream, A... args) {
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
-    cfg.attrs = &attr;
-    cfg.numAttrs = early ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 0;
+    if (early) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim.x = (unsigned)cluster;
+        attr[cfg.numAttrs].val.clusterDim.y = 1;
+        attr[cfg.numAttrs++].val.clusterDim.z = 1;
+    }
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -45,20 +53,22 @@ static cudaError_t launch_rows(ekv_pool *pool, int layer, const rows::Params &p,
     // Q by TMA: a box of all heads of a group x as many tokens as make a tile
     CUtensorMap qmap = pool->kv_map[layer];
     if (p.q_tma && encode_q_map(p.q, (uint64_t)q_rows, p.num_q_heads, D, rows::kBM / p.group, &qmap, p.group) != EKV_OK) return cudaErrorInvalidValue;
-    return launch(rows::rows_kernel<D, kMode, kCap, kBias>, dim3(p.num_kv_heads * (kMode == rows::kShared ? 1 : p.parts), p.tiles), rows::kThreads, rows::Geo<D>::kSmemBytes, false, stream, pool->kv_map[layer], qmap, p,
+    return launch(rows::rows_kernel<D, kMode, kCap, kBias>, dim3(p.num_kv_heads * (kMode == rows::kShared ? 1 : p.parts), p.tiles), rows::kThreads, rows::Geo<D>::kSmemBytes, false, 1, stream, pool->kv_map[layer], qmap, p,
                   (const uint8_t *)pool->layer_base(layer), (long long)pool->block_stride);
 }
 
 template <int D, bool kShared, bool kCap, bool kBias>
-static cudaError_t launch_ext(ekv_pool *pool, int layer, const ext::Params &p, int B, bool early, cudaStream_t stream) {
+static cudaError_t launch_ext(ekv_pool *pool, int layer, ext::Params p, int B, bool early, cudaStream_t stream) {
     constexpr int kBytes = ext::kWarps * ext::kStages * (2 * (D / 64) * ext::kBoxBytes + 8) + 1024;
     static bool done[64] = {false};
     cudaError_t e = ready(ext::decode_ext_kernel<D, kShared, kCap, kBias>, kBytes, pool->desc.device, done);
     if (e != cudaSuccess) return e;
-    e = launch(ext::decode_ext_kernel<D, kShared, kCap, kBias>, dim3(p.nsplit, p.num_kv_heads, B), ext::kWarps * 32, kBytes, early, stream, pool->kv_map[layer], p);
-    if (e != cudaSuccess || (p.nsplit == 1 && !p.beside)) return e;
+    // Ranges that are few, and all there at once, add themselves up as a cluster.  (In larger calls CTAs that wait for their cluster would keep others out.)
+    p.cluster = !p.beside && p.nsplit > 1 && p.nsplit <= ext::kCluster && (long long)B * p.num_kv_heads * p.nsplit <= 3LL * pool->sm_count;
+    e = launch(ext::decode_ext_kernel<D, kShared, kCap, kBias>, dim3(p.nsplit, p.num_kv_heads, B), ext::kWarps * 32, kBytes, early, p.cluster ? p.nsplit : 1, stream, pool->kv_map[layer], p);
+    if (e != cudaSuccess || ((p.nsplit == 1 || p.cluster) && !p.beside)) return e;
     const int n = B * p.num_q_heads;
-    return launch(ext::combine_ext_kernel<D, kShared>, dim3((n + ext::kCombineWarps - 1) / ext::kCombineWarps), ext::kCombineWarps * 32, 0, true, stream, p, n);
+    return launch(ext::combine_ext_kernel<D, kShared>, dim3((n + ext::kCombineWarps - 1) / ext::kCombineWarps), ext::kCombineWarps * 32, 0, true, 1, stream, p, n);
 }
 
 static size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -360,9 +370,9 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t 
     if (e == cudaSuccess && p.parts > 1) {
         const int all = (int)(T * p.num_q_heads);
         const dim3 grid((all + ext::kCombineWarps - 1) / ext::kCombineWarps);
-        e = d128 ? launch(ext::combine_rows_kernel<128>, grid, ext::kCombineWarps * 32, 0, true, (cudaStream_t)stream, (const float *)p.part_o,
+        e = d128 ? launch(ext::combine_rows_kernel<128>, grid, ext::kCombineWarps * 32, 0, true, 1, (cudaStream_t)stream, (const float *)p.part_o,
                           (const float2 *)p.part_ml, p.out, cu_q_lens, R, p.num_q_heads, p.parts, all)
-                 : launch(ext::combine_rows_kernel<64>, grid, ext::kCombineWarps * 32, 0, true, (cudaStream_t)stream, (const float *)p.part_o,
+                 : launch(ext::combine_rows_kernel<64>, grid, ext::kCombineWarps * 32, 0, true, 1, (cudaStream_t)stream, (const float *)p.part_o,
                           (const float2 *)p.part_ml, p.out, cu_q_lens, R, p.num_q_heads, p.parts, all);
     }
     return e == cudaSuccess ? EKV_OK : cuda_fail(e, "ekv_attn_prefill_chunk_scored launch");
