@@ -4,7 +4,9 @@
 // keys, the heads of the group as the rows of mma.m16n8k16, partial (m, l, O) per range -- over those blocks alone that the sequence sees:
 // of its prefix and of its window, or from the end of the shared keys on.  Bound by the bytes of these: 64 sequences of up to 16000 keys, 32q/8kv, 1.04 GB
 // in 158 to 164 us = 6.4 to 6.6 TB/s.  Where a sequence has a single range (many do, where the tables are wider than the sequences long) the CTA
-// writes the final rows itself; otherwise combine_ext_kernel does, a warp a (sequence, head).
+// writes the final rows itself.  Up to eight ranges that are all there at once are a cluster and add themselves up out of each other's shared memory
+// (5 sequences of up to 1000 keys, 4q/2kv d64: 5.5 us on the device for 6.6 with a second launch; 32q/8kv 7.5 to 7.9 for 9.0 to 9.5); for more,
+// combine_ext_kernel does, a warp a (sequence, head).
 // In a shared call this launch comes up beside the rows kernel's, which takes an SM for an item and is cut so that SMs are left, and fills the rest as its
 // items end; combine_ext_kernel adds the parts of both.  256 requests of 17..700 own keys behind 16384 shared ones: 114 us, one after the other
 // 130; nine groups of 28q/4kv 37 for 48.  Only the last CTA waits for the rows kernel, so that the launch behind this one finds both done.
