@@ -174,12 +174,18 @@ class Pool:
         into the slots, returns the queries.  q, k, v may be parts of one projection's rows.  positions: int32 [T], or [axes, T] with
         `axes` naming the axis of each pair of channels; inv_freq: float32 [rotary_dim / 2]; interleaved: pairs are neighbours.  q_out may be q.  8-bit pools: k_out
         receives the finished keys as bf16 before they are quantised (one is made if none is given)."""
-        call, i32, f32, bf16, dev = "rope_write_kv", torch.int32, torch.float32, torch.bfloat16, self.device.index
+        call, i32, f32, bf16, dev, D = "rope_write_kv", torch.int32, torch.float32, torch.bfloat16, self.device.index, self.head_dim
         T, pairs, where = slot_mapping.shape[0], inv_freq.shape[0], positions.shape
-        num_axes = 1 if len(where) == 1 else where[0]
+        num_axes = where[0] if len(where) == 2 else 1
         heads, kv_heads = self.num_q_heads, self.num_kv_heads
-        q_stride, k_stride, v_stride = self._heads(call, "q", q, T, heads), self._heads(call, "k", k, T, kv_heads), self._heads(call, "v", v, T, kv_heads)
-        if not (slot_mapping.dtype is torch.int64 and inv_freq.dtype is f32 and positions.dtype is i32 and where[-1] == T and len(where) <= 2
+        rows, row, qs, ks, vs = (T, kv_heads, D), (D,), q.stride(), k.stride(), v.stride()
+        # (one look at everything; what is wrong is found out after that)
+        if not (q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and q.shape == (T, heads, D) and k.shape == rows and v.shape == rows
+                and qs[2] == 1 and ks[2] == 1 and vs[2] == 1 and qs[1] == D and ks[1] == D and vs[1] == D
+                and q.get_device() == dev and k.get_device() == dev and v.get_device() == dev):
+            for name, t, n in (("q", q, heads), ("k", k, kv_heads), ("v", v, kv_heads)):
+                self._heads(call, name, t, T, n)
+        if not (slot_mapping.dtype is torch.int64 and inv_freq.dtype is f32 and positions.dtype is i32 and 1 <= len(where) <= 2 and where[-1] == T
                 and slot_mapping.dim() == 1 and inv_freq.dim() == 1 and slot_mapping.is_contiguous() and inv_freq.is_contiguous() and positions.is_contiguous()
                 and slot_mapping.get_device() == dev and inv_freq.get_device() == dev and positions.get_device() == dev):
             self._want(call, "slot_mapping", slot_mapping, torch.int64, (T,))
@@ -187,24 +193,23 @@ class Pool:
             self._want(call, "positions", positions, i32, (num_axes, T) if num_axes > 1 else (T,))
         if num_axes > 1 and (axes is None or len(axes) != pairs):
             raise ValueError(f"rope_write_kv: axes has to name the axis of each of the {pairs} pairs")
-        if q_weight is not None:
-            self._want(call, "q_weight", q_weight, bf16, (self.head_dim,))
-        if k_weight is not None:
-            self._want(call, "k_weight", k_weight, bf16, (self.head_dim,))
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None and not (w.dtype is bf16 and w.shape == row and w.get_device() == dev and w.is_contiguous()):
+                self._want(call, name, w, bf16, row)
         if q_out is None:
-            q_out = torch.empty((T, heads, self.head_dim), dtype=bf16, device=self.device)
-            out_stride = heads * self.head_dim
+            q_out = torch.empty((T, heads, D), dtype=bf16, device=self.device)
+            out_stride = heads * D
         else:
             out_stride = self._heads(call, "q_out", q_out, T, heads)
         if k_out is not None:
-            self._want(call, "k_out", k_out, bf16, (T, kv_heads, self.head_dim))
+            self._want(call, "k_out", k_out, bf16, rows)
         elif self.dtype == B.EKV_E4M3:
             with contextlib.nullcontext() if stream is None else self._on(stream):
-                k_out = torch.empty((T, kv_heads, self.head_dim), dtype=bf16, device=self.device)
+                k_out = torch.empty(rows, dtype=bf16, device=self.device)
         rope = B.Rope(2 * pairs, num_axes, B.EKV_ROPE_ADJACENT if interleaved else 0, factor, eps, weight_offset, inv_freq.data_ptr(),
                       positions.data_ptr(), bytes(axes) if num_axes > 1 else None, q_weight.data_ptr() if q_weight is not None else None,
                       k_weight.data_ptr() if k_weight is not None else None)
-        B._check(B.load_library().ekv_rope_write_kv(self.handle, layer, rope, q.data_ptr(), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, q_out.data_ptr(), out_stride,
+        B._check(B.load_library().ekv_rope_write_kv(self.handle, layer, rope, q.data_ptr(), qs[0], k.data_ptr(), ks[0], v.data_ptr(), vs[0], q_out.data_ptr(), out_stride,
                             None if k_out is None else k_out.data_ptr(), slot_mapping.data_ptr(), T, self._current(stream)))
         return q_out
 

@@ -161,3 +161,22 @@ def test_workspaces_belong_to_the_streams_that_use_them():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("Hq,Hk,D", [(8, 2, 128), (5, 1, 64), (8, 8, 64), (16, 2, 128)])
+def test_ranges_of_a_sequence_in_one_launch(Hq, Hk, D):
+    lens = [2048, 1793, 257, 256, 1, 2000, 513]                     # up to eight ranges, some sequences fewer than the table has room for
+    b = Batch(Hq, Hk, D, [x - 1 for x in lens], [1] * len(lens), seed=Hq)
+    b.seq_lens[3] = b.lens[3] = 0
+    got, want = run(b, window=1900, cap=20.0)
+    check(got, want)
+    assert (got[3] == 0).all()
+    b.cache[int(b.tables[0, 600 // 16]), 0, 0, 600 % 16, 5] = float("nan")      # key 600 of the first, kv-head 0: the third of its ranges
+    hurt = run(b, window=1900, cap=20.0)[0]
+    assert torch.isnan(hurt[0, :Hq // Hk]).all()
+    hurt[0, :Hq // Hk] = got[0, :Hq // Hk]
+    assert torch.equal(hurt, got)
+    short = b.seq_lens.clone()
+    b.seq_lens[0] = b.lens[0] = 500                                 # the key lies behind the end
+    check(*run(b, cap=20.0))
+    b.seq_lens.copy_(short)
