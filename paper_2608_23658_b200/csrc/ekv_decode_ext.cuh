@@ -4,8 +4,8 @@
 // keys, the heads of the group as the rows of mma.m16n8k16, partial (m, l, O) per range -- over those blocks alone that the sequence sees:
 // of its prefix and of its window, or from the end of the shared keys on.  Bound by the bytes of these: 64 sequences of up to 16000 keys, 32q/8kv, 1.04 GB
 // in 158 to 164 us = 6.4 to 6.6 TB/s.  Where a sequence has a single range (many do, where the tables are wider than the sequences long) the CTA
-// writes the final rows itself.  Up to eight ranges that are all there at once are a cluster and add themselves up out of each other's shared memory
-// (5 sequences of up to 1000 keys, 4q/2kv d64: 5.5 us on the device for 6.6 with a second launch; 32q/8kv 7.5 to 7.9 for 9.0 to 9.5); for more,
+// writes the final rows itself.  Up to sixteen ranges whose CTAs are all there at once are a cluster and add themselves up out of each other's shared
+// memory (5 sequences of up to 1000 keys, 4q/2kv d64: 5.5 us on the device for 6.6 with a second launch; one of 4000 6.5 for 11.2); for more,
 // combine_ext_kernel does, a warp a (sequence, head).
 // In a shared call this launch comes up beside the rows kernel's, which takes an SM for an item and is cut so that SMs are left, and fills the rest as its
 // items end; combine_ext_kernel adds the parts of both.  256 requests of 17..700 own keys behind 16384 shared ones: 114 us, one after the other
@@ -22,7 +22,7 @@ using rows::kMaxGroups;
 static constexpr int kWarps = 4;
 static constexpr int kStages = 2;  // of a warp; 64 KB in all, so that three CTAs fit an SM: with three stages and two CTAs, own parts of 256 requests took 88 us for 75
 static constexpr int kBoxBytes = 16 * 128;  // 16 tokens x 64 channels
-static constexpr int kCluster = 8;          // ranges of a sequence that are a cluster, at most
+static constexpr int kCluster = 16;         // ranges of a sequence that are a cluster, at most
 static constexpr int kMaxParts = 64;        // that the rows kernel cuts shared keys into
 
 struct Params {
@@ -377,6 +377,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
         float l[kCluster], m[kCluster], mstar = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kCluster; ++i) {
+            if (i == 8 && p.nsplit <= 8) break;
             const uint32_t at = map_to_cta(rowsum_at + 4 * h, min(i, p.nsplit - 1));
             l[i] = i < p.nsplit ? ld_cluster_f1(at) : 0.f;
             m[i] = i < p.nsplit ? ld_cluster_f1(at + 32) : -INFINITY;
@@ -385,6 +386,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
         float acc = 0.f, lsum = 0.f;
 #pragma unroll
         for (int i = 0; i < kCluster; ++i) {  // (a range without a maximum has a sum of 0, or NaN if its scores were NaN)
+            if (i == 8 && p.nsplit <= 8) break;
             const float w = m[i] > -INFINITY ? fast_exp2(m[i] - mstar) : 0.f;
             lsum += w * l[i];
             if (w != 0.f) acc += w * ld_cluster_f1(map_to_cta(result_at + 4 * e, i));

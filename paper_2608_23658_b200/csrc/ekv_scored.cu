@@ -57,14 +57,28 @@ static cudaError_t launch_rows(ekv_pool *pool, int layer, const rows::Params &p,
                   (const uint8_t *)pool->layer_base(layer), (long long)pool->block_stride);
 }
 
+template <int D>
+static constexpr int ext_bytes() { return ext::kWarps * ext::kStages * (2 * (D / 64) * ext::kBoxBytes + 8) + 1024; }
+
+template <int D, bool kShared, bool kCap, bool kBias>
+static cudaError_t ready_ext(int device) {
+    static bool done[64] = {false}, wide[64] = {false};
+    cudaError_t e = ready(ext::decode_ext_kernel<D, kShared, kCap, kBias>, ext_bytes<D>(), device, done);
+    if (e != cudaSuccess || (device < 64 && wide[device])) return e;
+    e = cudaFuncSetAttribute(ext::decode_ext_kernel<D, kShared, kCap, kBias>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);  // more than eight CTAs
+    if (e == cudaSuccess && device < 64) wide[device] = true;
+    return e;
+}
+
+static int clusters_of(const ekv_pool *pool, long long clusters);
+
 template <int D, bool kShared, bool kCap, bool kBias>
 static cudaError_t launch_ext(ekv_pool *pool, int layer, ext::Params p, int B, bool early, cudaStream_t stream) {
-    constexpr int kBytes = ext::kWarps * ext::kStages * (2 * (D / 64) * ext::kBoxBytes + 8) + 1024;
-    static bool done[64] = {false};
-    cudaError_t e = ready(ext::decode_ext_kernel<D, kShared, kCap, kBias>, kBytes, pool->desc.device, done);
+    constexpr int kBytes = ext_bytes<D>();
+    cudaError_t e = ready_ext<D, kShared, kCap, kBias>(pool->desc.device);
     if (e != cudaSuccess) return e;
     // Ranges that are few, and all there at once, add themselves up as a cluster.  (In larger calls CTAs that wait for their cluster would keep others out.)
-    p.cluster = !p.beside && p.nsplit > 1 && p.nsplit <= ext::kCluster && (long long)B * p.num_kv_heads * p.nsplit <= 3LL * pool->sm_count;
+    p.cluster = !p.beside && p.nsplit > 1 && p.nsplit <= clusters_of(pool, (long long)B * p.num_kv_heads);
     e = launch(ext::decode_ext_kernel<D, kShared, kCap, kBias>, dim3(p.nsplit, p.num_kv_heads, B), ext::kWarps * 32, kBytes, early, p.cluster ? p.nsplit : 1, stream, pool->kv_map[layer], p);
     if (e != cudaSuccess || ((p.nsplit == 1 || p.cluster) && !p.beside)) return e;
     const int n = B * p.num_q_heads;
@@ -157,6 +171,48 @@ static int plan_parts(const ekv_pool *pool, long long items, int max_blocks, int
     return parts < 1 ? 1 : (int)parts;
 }
 
+// CTAs of the largest cluster of which so many are there at once; 1: of none.
+static int clusters_of(const ekv_pool *pool, long long clusters) {
+    static int fit[64][ext::kCluster + 1] = {};  // by device and size, + 1; the same for all of the kernels, whose registers let three CTAs into an SM
+    const int device = pool->desc.device;
+    int size = ext::kCluster;
+    for (; size > 1; --size) {
+        int known = device < 64 ? fit[device][size] : 0;
+        if (known == 0) {
+            cudaLaunchConfig_t cfg = {};
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = (unsigned)size, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cfg.gridDim = dim3((unsigned)size), cfg.blockDim = dim3(ext::kWarps * 32), cfg.dynamicSmemBytes = ext_bytes<128>();
+            cfg.attrs = &attr, cfg.numAttrs = 1;
+            int n = 0;
+            if (ready_ext<128, false, false, false>(device) != cudaSuccess ||
+                cudaOccupancyMaxActiveClusters(&n, ext::decode_ext_kernel<128, false, false, false>, &cfg) != cudaSuccess)
+                n = 0, (void)cudaGetLastError();
+            known = n + 1;
+            if (device < 64) fit[device][size] = known;
+        }
+        if (clusters <= known - 1) break;
+    }
+    return size;
+}
+
+// Ranges of decode's sequences: those of ekv_attn_decode, or, where they can be a cluster, or one, with up to 1024 keys each, as few as that takes.
+// Device, us: a sequence of 16000, 32q/8kv 28.8 -> 17.6, 4 of 4000 19.7 -> 13.5, 8 of up to 4000 17.7 -> 13.7; 20 of 2000, 28q/4kv 20.1 -> 14.3;
+// 64 of up to 700, 32q/8kv, as one range each 19.5 -> 15.5.  With 2048 keys, 4 of 16000 53.9 -> 55.9.
+static constexpr int kRangeKeys = 1024;
+static DecodePlan plan_ranges(const ekv_pool *pool, int B, int blocks) {
+    DecodePlan plan = plan_decode(pool, B, blocks);
+    const long long units = (long long)B * pool->desc.num_kv_heads, len = (long long)blocks * 16;
+    const int n = plan.nsplit > 1 ? clusters_of(pool, units) : 1;
+    if (plan.nsplit <= n) return plan;
+    const long long chunk = ((len + n - 1) / n + 63) / 64 * 64;
+    if (chunk > kRangeKeys) return plan;
+    plan.chunk_tokens = (int)chunk;
+    plan.nsplit = (int)((len + chunk - 1) / chunk);
+    return plan;
+}
+
 // How a shared call's groups are cut: items of the rows kernel are 256 (request, head) rows x chunk_tiles key tiles.
 struct SharedPlan {
     int chunk_tiles, parts, tiles;  // tiles: items per kv-head
@@ -180,11 +236,11 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
             saved += (long long)(starts[g + 1] - starts[g] - 1) * shared[g];
             if (shared[g] > longest_shared) longest_shared = shared[g];
         }
-    // Worth it?  The pass over the shared keys costs some 5 us (8 where Q does not come by TMA), and saves their bytes, read from L2 for the most part,
-    // and the walk through ranges that are as long as the prefix.  Measured with own parts of up to 200 keys, us with / without: 32q/8kv, 2
-    // requests over 4096 keys 14.3 / 12.1, over 8192 17.8 / 21.6; 16 over 512 12.8 / 10.8, over 1024 13.1 / 17.4; 4q/2kv d64, 4 over 2048
-    // 9.6 / 8.6, over 8192 11.0 / 17.6.
-    s.worth = saved * Hk * pool->desc.head_dim * 4 / 9e6 + longest_shared * (0.7 / 1024) > (rows::kBM % group == 0 ? 5. : 8.);
+    // Worth it?  The pass over the shared keys costs a launch more and its items' starts and ends; it saves their bytes, read from L2 for the most part.
+    // Measured with own parts of up to 200 keys, us with / without: 32q/8kv, 2 requests over 8192 keys 16.5 / 14.5, 4 over 4096 14.7 / 12.9, over 8192 16.5 /
+    // 18.5; 16 over 1024 14.7 / 12.7, over 2048 17.2 / 16.7, over 4096 17.3 / 33.6; 64 over 512 16.6 / 23.0; 28q/4kv, 16 over 2048 16.1 / 13.3, over 4096
+    // 17.2 / 18.2, 64 over 1024 20.3 / 28.7; 4q/2kv d64, 16 over 4096 10.3 / 9.8.
+    s.worth = saved * Hk * pool->desc.head_dim * 4 / 9e6 + longest_shared * (0.4 / 1024) > 13.;
     for (int g = 0; g < G; ++g) {
         const int n = starts[g + 1] - starts[g];
         if (n == 0) continue;
@@ -283,7 +339,7 @@ extern "C" ekv_status_t ekv_attn_decode_scored(ekv_pool_t *pool, int32_t layer, 
     if (st != EKV_OK || B == 0) return st;
     int seen = max_blocks_per_seq;  // blocks that a sequence reads at most
     if (scores->window > 0 && !scores->prefix_lens && scores->window / 16 + 2 < seen) seen = scores->window / 16 + 2;
-    const DecodePlan plan = plan_decode(pool, B, seen);
+    const DecodePlan plan = plan_ranges(pool, B, seen);
     const size_t n = (size_t)B * pool->desc.num_q_heads * plan.nsplit, need = plan.nsplit > 1 ? parts_bytes(pool, n) : 0;
     st = check_workspace(who, workspace, workspace_bytes, need);
     if (st != EKV_OK) return st;
@@ -384,7 +440,7 @@ extern "C" size_t ekv_attn_decode_shared_workspace_bytes(const ekv_pool_t *pool,
         group_starts[G] < 1)
         return 0;
     const SharedPlan s = plan_shared(pool, group_starts, shared_lens, G, max_blocks_per_seq);
-    return shared_need(pool, s, plan_decode(pool, group_starts[G], s.own_blocks), group_starts[G]);
+    return shared_need(pool, s, s.any ? plan_decode(pool, group_starts[G], s.own_blocks) : plan_ranges(pool, group_starts[G], s.own_blocks), group_starts[G]);
 }
 
 extern "C" ekv_status_t ekv_attn_decode_shared(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
@@ -402,7 +458,7 @@ extern "C" ekv_status_t ekv_attn_decode_shared(ekv_pool_t *pool, int32_t layer, 
     st = check_groups(who, pool, group_starts, shared_lens, G, max_blocks_per_seq, B);
     if (st != EKV_OK || B == 0) return st;
     const SharedPlan s = plan_shared(pool, group_starts, shared_lens, G, max_blocks_per_seq);
-    const DecodePlan plan = plan_decode(pool, B, s.own_blocks);
+    const DecodePlan plan = s.any ? plan_decode(pool, B, s.own_blocks) : plan_ranges(pool, B, s.own_blocks);
     st = check_workspace(who, workspace, workspace_bytes, shared_need(pool, s, plan, B));
     if (st != EKV_OK) return st;
     ext::Params p;

@@ -41,7 +41,7 @@ def test_against_the_model(Hq, Hk, D, groups, own):
 @pytest.mark.parametrize("Hq,Hk,D", [(4, 2, 64), (28, 4, 128), (8, 8, 64), (6, 2, 128), (5, 1, 64), (64, 8, 128)])
 @pytest.mark.parametrize("groups,own", [
     ([(2, 12000)], [1, 40]), ([(2, 16), (4, 64), (2, 12000), (3, 128), (1, 48), (0, 0), (5, 0)], [3, 100, 15, 1]), ([(40, 11904), (3, 2000)], [1, 9, 33]),
-    ([(37, 1040), (70, 12016), (33, 48)], [20, 64])], ids=str)
+    ([(37, 1040), (70, 12016), (33, 48)], [20, 64]), ([(2, 36000)], [1, 40]), ([(2, 16), (4, 64), (2, 36000), (3, 128), (1, 48), (0, 0), (5, 0)], [3, 100, 15, 1])], ids=str)
 def test_beside_a_prefix_that_is_long_enough_to_be_read_once(Hq, Hk, D, groups, own):
     b = make(Hq, Hk, D, groups, own, seed=len(own))
     assert ekv.ekv_attn_decode_shared_workspace_bytes(b.pool.handle, b.starts, b.shared, b.tables.shape[1]) > 0
@@ -56,7 +56,7 @@ def test_large_groups_and_long_prefixes(Hq, Hk, D, n, p, own):
     check(run(b), b.model())
 
 
-@pytest.mark.parametrize("p", [160, 12000])
+@pytest.mark.parametrize("p", [160, 12000, 36000])
 def test_requests_that_have_no_keys_of_their_own(p):
     b = make(8, 2, 128, [(5, p), (2, 32)], [16], seed=1)
     b.seq_lens[1], b.seq_lens[4], b.seq_lens[6] = p, p, 32
@@ -64,7 +64,7 @@ def test_requests_that_have_no_keys_of_their_own(p):
     check(run(b), b.model())
 
 
-@pytest.mark.parametrize("p", [320, 12000])
+@pytest.mark.parametrize("p", [320, 12000, 36000])
 def test_rows_of_padding_and_requests_shorter_than_their_prefix(p):
     b = make(4, 2, 64, [(6, p), (3, 0)], [30], seed=2)
     want = run(b)
@@ -91,7 +91,7 @@ def test_as_plain_decode_within_rounding_and_the_same_bits_every_time():
         assert torch.equal(run(b), got)
 
 
-@pytest.mark.parametrize("p", [256, 12000])
+@pytest.mark.parametrize("p", [256, 12000, 36000])
 def test_a_nan_reaches_its_own_request_alone(p):
     b = make(8, 2, 64, [(6, p)], [20], seed=4)
     want = run(b)
@@ -106,7 +106,7 @@ def test_a_nan_reaches_its_own_request_alone(p):
     assert torch.isnan(run(b)[:, :4]).all() and torch.isfinite(run(b)[[0, 1, 2, 4]][:, 4:]).all()
 
 
-@pytest.mark.parametrize("p", [400, 12000])
+@pytest.mark.parametrize("p", [400, 12000, 36000])
 def test_bad_shared_block_ids_are_skipped_and_latched(p):
     b = make(8, 2, 128, [(4, p)], [20], seed=5)
     want = run(b)

@@ -50,7 +50,7 @@ class Requests:
         return b.model(**mods)
 
 
-@pytest.mark.parametrize("n,prefix", [(5, 64), (6, 12000)])
+@pytest.mark.parametrize("n,prefix", [(5, 64), (6, 12000), (6, 36000)])
 def test_samples_of_one_prompt(n, prefix):
     r = Requests(n, prefix, room=40)
     q, k, v = r.rows(prefix)
