@@ -185,10 +185,11 @@ static int clusters_of(const ekv_pool *pool, long long clusters) {
             attr.val.clusterDim.x = (unsigned)size, attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
             cfg.gridDim = dim3((unsigned)size), cfg.blockDim = dim3(ext::kWarps * 32), cfg.dynamicSmemBytes = ext_bytes<128>();
             cfg.attrs = &attr, cfg.numAttrs = 1;
-            int n = 0;
-            if (ready_ext<128, false, false, false>(device) != cudaSuccess ||
+            int n = 0, current = device;
+            if (cudaGetDevice(&current) != cudaSuccess || cudaSetDevice(device) != cudaSuccess || ready_ext<128, false, false, false>(device) != cudaSuccess ||
                 cudaOccupancyMaxActiveClusters(&n, ext::decode_ext_kernel<128, false, false, false>, &cfg) != cudaSuccess)
                 n = 0, (void)cudaGetLastError();
+            if (current != device) (void)cudaSetDevice(current);
             known = n + 1;
             if (device < 64) fit[device][size] = known;
         }
