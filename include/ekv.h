@@ -481,7 +481,8 @@ EKV_API ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t lay
 
 /*
  * ekv_attn_decode_shared -- ekv_attn_decode for a batch whose requests share prefixes (a system prompt, samples of one prompt, questions
- * about one document): the result is ekv_attn_decode's within rounding, but the shared keys are read once for a group instead of once for each request.
+ * about one document): the result is ekv_attn_decode's within rounding, but the shared keys are read once for a group instead of
+ * once for each request, where by the sizes that pays.
  * Group g is the requests group_starts[g] .. group_starts[g+1]-1; their first shared_lens[g] tokens are the same, i.e. the first
  * shared_lens[g]/block_size entries of their rows of block_tables name the same blocks (those of the group's first request are read).
  * group_starts: HOST [G+1], from 0 to B, non-decreasing.  shared_lens: HOST [G], multiples of block_size, 0 where nothing is shared,
