@@ -246,7 +246,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int group = p.group;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // a launch that reads the parts comes up in the tail of this one
-    // Set-up, side by side: barriers, TMEM, and (in the scheduler's loop) the first item.
+    // Set-up, side by side: barriers, TMEM, and the first item.
     if (warp == 3) {
         if (lane == 0) {
             prefetch_tensormap(&kvmap);
@@ -260,14 +260,87 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
         cp::tcgen05_alloc(cp::cta_group_1, sh.tmem_slot(), 512);
         cp::tcgen05_relinquish_alloc_permit(cp::cta_group_1);
     }
-    auto set_up = [&]() {  // by every warp, once
-        fence_before();
-        __syncthreads();
-        fence_after();
-    };
     auto by_group = [&](int r) { return group == 1 ? r : (int)__umulhi((unsigned)r, p.group_magic); };
-    if (warp != 2) set_up();
-    const uint32_t tmem = warp != 2 ? *sh.tmem_slot() : 0u;
+    auto low_of = [&](int pos) { return p.window > 0 ? max(0, pos - p.window + 1) : 0; };  // first key of a row's window
+    int in = blockIdx.x;  // scheduler: kv-head and part of the item; its rank is the other coordinate of the grid
+    // Items are listed heaviest (latest) first, the kv-heads and parts of one next to each other.  false: nothing to post for this number
+    auto post = [&](int rank, volatile int *slot) {
+        const int idx = p.tiles - 1 - rank;
+        int g = in, part = 0, req, q0, next_q0, first, L = 0, prefix = 0;
+        if (kMode == kScored && p.parts > 1) part = in / p.num_kv_heads, g = in - part * p.num_kv_heads;
+        if (kMode == kShared || p.R <= kMaxGroups) {
+            int lo = 0, hi = p.R;
+#pragma unroll 1
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (p.tile_prefix[mid] <= idx) lo = mid;
+                else hi = mid;
+            }
+            req = lo, first = p.tile_prefix[lo];
+        } else {
+            req = spread_request(p, idx);
+            first = (int)spread_first(p, req);
+        }
+        if (kMode == kShared) {
+            q0 = p.start[req], next_q0 = p.start[req + 1];
+        } else {  // all loads at once
+            q0 = p.cu_q_lens[req], next_q0 = p.cu_q_lens[req + 1], L = p.seq_lens[req];
+            if (p.prefix_lens) prefix = p.prefix_lens[req];
+        }
+        const int c_r = next_q0 - q0;
+        int row0, past, pre, kv_end, n_pre, skip, tile0, n_tiles;
+        if (kMode == kShared) {
+            const int chunk = part_tiles(p.chunk_tiles, c_r * group);
+            const int all = (p.shared[req] + kBN - 1) / kBN, ns = (all + chunk - 1) / chunk, tile = (idx - first) / ns;
+            part = (idx - first) - tile * ns;
+            row0 = tile * kItemRows;
+            past = 0, pre = kv_end = p.shared[req], n_pre = all, skip = 0;
+            tile0 = part * chunk;
+            n_tiles = min(chunk, all - tile0);
+            req = q0;  // the first request's table names the shared blocks
+        } else {
+            row0 = (idx - first) * kItemRows;
+        }
+        const int rows = min(kItemRows, c_r * group - row0);
+        if (rows <= 0) return false;
+        if (kMode == kScored) {
+            L = min(L, p.max_blocks * 16);
+            past = L - c_r;
+            if (past < 0) {  // malformed request: zero rows, latch
+                if (lane == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
+                for (int r = 0; r < rows; ++r) {
+                    const int pos = by_group(row0 + r);
+                    const size_t at = (size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + row0 + r - pos * group);
+                    if (p.parts > 1) {
+                        if (lane == 0) p.part_ml[at * p.parts + part] = make_float2(-INFINITY, 0.f);
+                    } else if (lane < D / 8) {
+                        reinterpret_cast<uint4 *>(p.out + at * D)[lane] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+                return false;
+            }
+            const int p0 = past + by_group(row0), p1 = past + by_group(row0 + rows - 1);
+            pre = max(0, min(prefix, L));
+            kv_end = max(p1 + 1, pre);
+            n_pre = (pre + kBN - 1) / kBN;
+            skip = max(0, low_of(p0) / kBN - n_pre);
+            const int n = (kv_end + kBN - 1) / kBN - skip;
+            tile0 = (int)((long long)n * part / p.parts);
+            n_tiles = (int)((long long)n * (part + 1) / p.parts) - tile0;
+        }
+        if (lane == 0) {
+            slot[1] = req, slot[2] = g, slot[3] = row0, slot[4] = rows, slot[5] = q0, slot[6] = past, slot[7] = pre, slot[8] = kv_end;
+            slot[9] = tile0, slot[10] = n_tiles, slot[11] = n_pre, slot[12] = skip, slot[13] = part, slot[kItemNan] = 0;
+        }
+        return true;
+    };
+    bool first_posted = false;
+    if (warp == 2) first_posted = post(blockIdx.y, sh.item(0));
+    // One place for all warps, and the register split right behind it: every warp of a warpgroup has to execute the same setmaxnreg.
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *sh.tmem_slot();
 
     auto wait = [&](int bar, uint32_t parity) { return wait_warp<D>(sh, bar, parity); };
     // the CTA's n-th item, 1 = to work on, 0 = the list has ended, -1 = given up
@@ -283,16 +356,14 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
         const int l = it.tile0 + t;
         return (l < it.n_pre ? l : l + it.skip) * kBN;
     };
-    auto low_of = [&](int pos) { return p.window > 0 ? max(0, pos - p.window + 1) : 0; };  // first key of a row's window
     uint32_t issued = 0;  // producers: tiles under way or done
 
     if (warp < 4 || warp >= 12) {
-    if (warp != 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 2) {
         // =========================== item scheduler ===========================
         bool may_draw = true;
         uint32_t draws = 0;
-        int in = blockIdx.x;  // kv-head and part of the item; its rank is the other coordinate of the grid
         auto draw = [&]() {  // rank (and kv-head, part) of a CTA that will not start now, or -1
             if (!may_draw) return -1;
             if (lane == 0) {
@@ -313,78 +384,8 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
             in = may_draw ? cp::clusterlaunchcontrol_query_cancel_get_first_ctaid_x<int>(response) : 0;
             return may_draw ? cp::clusterlaunchcontrol_query_cancel_get_first_ctaid_y<int>(response) : -1;
         };
-        // Items are listed heaviest (latest) first, the kv-heads and parts of one next to each other.  false: nothing to post for this number
-        auto post = [&](int rank, volatile int *slot) {
-            const int idx = p.tiles - 1 - rank;
-            int g = in, part = 0, req, q0, next_q0, first, L = 0, prefix = 0;
-            if (kMode == kScored && p.parts > 1) part = in / p.num_kv_heads, g = in - part * p.num_kv_heads;
-            if (kMode == kShared || p.R <= kMaxGroups) {
-                int lo = 0, hi = p.R;
-#pragma unroll 1
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (p.tile_prefix[mid] <= idx) lo = mid;
-                    else hi = mid;
-                }
-                req = lo, first = p.tile_prefix[lo];
-            } else {
-                req = spread_request(p, idx);
-                first = (int)spread_first(p, req);
-            }
-            if (kMode == kShared) {
-                q0 = p.start[req], next_q0 = p.start[req + 1];
-            } else {  // all loads at once
-                q0 = p.cu_q_lens[req], next_q0 = p.cu_q_lens[req + 1], L = p.seq_lens[req];
-                if (p.prefix_lens) prefix = p.prefix_lens[req];
-            }
-            const int c_r = next_q0 - q0;
-            int row0, past, pre, kv_end, n_pre, skip, tile0, n_tiles;
-            if (kMode == kShared) {
-                const int chunk = part_tiles(p.chunk_tiles, c_r * group);
-                const int all = (p.shared[req] + kBN - 1) / kBN, ns = (all + chunk - 1) / chunk, tile = (idx - first) / ns;
-                part = (idx - first) - tile * ns;
-                row0 = tile * kItemRows;
-                past = 0, pre = kv_end = p.shared[req], n_pre = all, skip = 0;
-                tile0 = part * chunk;
-                n_tiles = min(chunk, all - tile0);
-                req = q0;  // the first request's table names the shared blocks
-            } else {
-                row0 = (idx - first) * kItemRows;
-            }
-            const int rows = min(kItemRows, c_r * group - row0);
-            if (rows <= 0) return false;
-            if (kMode == kScored) {
-                L = min(L, p.max_blocks * 16);
-                past = L - c_r;
-                if (past < 0) {  // malformed request: zero rows, latch
-                    if (lane == 0) atomicOr(p.status, EKV_DEV_FLAG_OOB);
-                    for (int r = 0; r < rows; ++r) {
-                        const int pos = by_group(row0 + r);
-                        const size_t at = (size_t)(q0 + pos) * p.num_q_heads + (size_t)(g * group + row0 + r - pos * group);
-                        if (p.parts > 1) {
-                            if (lane == 0) p.part_ml[at * p.parts + part] = make_float2(-INFINITY, 0.f);
-                        } else if (lane < D / 8) {
-                            reinterpret_cast<uint4 *>(p.out + at * D)[lane] = make_uint4(0u, 0u, 0u, 0u);
-                        }
-                    }
-                    return false;
-                }
-                const int p0 = past + by_group(row0), p1 = past + by_group(row0 + rows - 1);
-                pre = max(0, min(prefix, L));
-                kv_end = max(p1 + 1, pre);
-                n_pre = (pre + kBN - 1) / kBN;
-                skip = max(0, low_of(p0) / kBN - n_pre);
-                const int n = (kv_end + kBN - 1) / kBN - skip;
-                tile0 = (int)((long long)n * part / p.parts);
-                n_tiles = (int)((long long)n * (part + 1) / p.parts) - tile0;
-            }
-            if (lane == 0) {
-                slot[1] = req, slot[2] = g, slot[3] = row0, slot[4] = rows, slot[5] = q0, slot[6] = past, slot[7] = pre, slot[8] = kv_end;
-                slot[9] = tile0, slot[10] = n_tiles, slot[11] = n_pre, slot[12] = skip, slot[13] = part, slot[kItemNan] = 0;
-            }
-            return true;
-        };
         int item = blockIdx.y;
+        bool posted = first_posted;
 #pragma unroll 1
         for (uint32_t n = 0;; ++n) {
             volatile int *slot = sh.item(n);
@@ -392,16 +393,12 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
             // stands idle (drawing and decoding one takes some 4000 cycles)
             if (n > 0) (void)wait(G::WANT, n - 1);
             if (n >= kRing) (void)wait(G::ITEM_EMPTY + (int)(n % kRing), n / kRing - 1);
-            for (bool ask = n > 0;; ask = true) {
-                if (ask) item = draw();
+            while (!posted) {
+                item = draw();
                 // (a wait ran out: the CTAs that have not started, and would wait as long, are not to; the list ends when all are drawn)
-                const bool done = item < 0 || ((!ask || !*sh.abort_flag()) && post(item, slot));
-                if (n == 0 && !ask) {  // beside the rest of the set-up
-                    set_up();
-                    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-                }
-                if (done) break;
+                posted = item < 0 || (!*sh.abort_flag() && post(item, slot));
             }
+            posted = false;
             if (lane == 0) {
                 slot[0] = item >= 0;
                 __threadfence_block();
