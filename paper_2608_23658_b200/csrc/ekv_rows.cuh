@@ -356,7 +356,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
         const int l = it.tile0 + t;
         return (l < it.n_pre ? l : l + it.skip) * kBN;
     };
-    uint32_t issued = 0;  // producers: tiles under way or done
+    uint32_t issued = 0;  // producers: tiles under way or done (Q: items)
 
     if (warp < 4 || warp >= 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -588,6 +588,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
             if (fetch(n, it) <= 0) break;
             if (n > 0 && !wait(G::Q_EMPTY, n - 1)) break;
             load_q(it);
+            if (p.q_tma) ++issued;
             const int p0 = it.past + by_group(it.row0), p1 = it.past + by_group(it.row0 + it.rows - 1);
             const int lo1 = kMode == kShared ? 0 : low_of(p1);
 #pragma unroll 1
@@ -952,6 +953,8 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
         if (warp == 12 || warp == 1)
             for (uint32_t t = issued > G::kStages ? issued - G::kStages : 0; t < issued; ++t)
                 (void)mbar_wait(sh.bar((warp == 1 ? G::V_RAW : G::K_FULL) + (int)(t % G::kStages)), (t / G::kStages) & 1u, 100000000ull);
+        if (warp == 13 && issued > 0)  // (the other two warps may have given up in front of it, without arriving: then the limit is the chance)
+            (void)mbar_wait(sh.bar(G::Q_FULL), (issued - 1) & 1u, 100000000ull);
         if (threadIdx.x == 0) atomicOr(p.status, EKV_DEV_FLAG_TIMEOUT);  // a wait ran out
     }
     __syncthreads();

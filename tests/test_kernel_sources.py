@@ -24,3 +24,12 @@ def test_a_register_split_is_one_instruction_for_all_warps_of_a_warpgroup(name):
         assert not line, f"{name}: a condition stands in front of setmaxnreg: {line}"
         before = text[:m.start()].rstrip().rsplit("\n", 1)[-1].strip()
         assert not re.search(r"warp\s*[!=]=\s*\d", before) and not before.endswith("set_up();"), f"{name}: setmaxnreg for one warp: {before}"
+
+
+def test_the_rows_kernel_gives_every_copy_a_chance_to_land_when_it_gives_up():
+    """A bulk copy that is still under way when its CTA has left lands in the shared memory of the next one."""
+    text = source("ekv_rows.cuh")
+    kernel = text[text.index("rows_kernel("):]
+    teardown = kernel[kernel.rindex("if (*sh.abort_flag()) {"):kernel.rindex("tcgen05_dealloc")]
+    for bar in ("K_FULL", "V_RAW", "Q_FULL"):                       # what its tma_load_3d complete on
+        assert re.search(r"mbar_wait\([^;]*\b" + bar + r"\b", teardown), bar
