@@ -43,8 +43,8 @@ struct Params {
     int parts, G;
     int cluster;              // a sequence's ranges are a cluster, which adds them up itself
     int beside;               // shared call: the two passes run side by side, and combine_ext_kernel adds the shared keys' parts
-    float scale_log2;         // scale * log2 e; with a cap: cap * log2 e
-    float cap_scale;          // with a cap: 2 * log2 e * scale / cap
+    float scale_log2;           // scale * log2 e
+    float cap_scale, cap_log2;  // with a cap: scale / cap, cap * log2 e (both within fp32's normal range)
     int start[kMaxGroups + 1];     // shared call: first request of a group,
     int shared[kMaxGroups];        // its shared keys
     uint8_t ns[kMaxGroups];        // and the parts that the rows kernel cut them into; 0: it did not, every request reads its own
@@ -215,12 +215,8 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
             uint32_t mask_lo = 0xffffffffu, mask_hi = 0xffffffffu;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if (kCap) {  // 1 - 2 / (e^2y + 1): absolute error of some 2^-23
-                    const float ex = fast_exp2(x[e] * p.cap_scale);
-                    x[e] = p.scale_log2 - __fdividef(2.f * p.scale_log2, ex + 1.f);
-                } else {
-                    x[e] *= p.scale_log2;
-                }
+                if (kCap) x[e] = rows::capped(x[e], p.cap_scale, p.scale_log2, p.cap_log2);
+                else x[e] *= p.scale_log2;
                 if (kBias) x[e] -= slope * (float)(sp.L - 1 - (t + (e & 1) + 8 * (e >> 1)));
             }
             if (partial) {

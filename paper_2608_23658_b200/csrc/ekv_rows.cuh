@@ -75,8 +75,8 @@ struct Params {
     unsigned group_magic;       // ceil(2^32 / group)
     unsigned q_flip;            // 0x80008000 for a negative scale
     int q_tma;                  // Q tiles come by TMA
-    float scale_log2;           // |scale| * log2 e; with a cap: cap * log2 e
-    float cap_scale;            // with a cap: |scale| / cap
+    float scale_log2;           // |scale| * log2 e
+    float cap_scale, cap_log2;  // with a cap: |scale| / cap, cap * log2 e (both within fp32's normal range)
     float near_limit;           // scores q.k up to there take the short polynomial s * (near[0] + near[1] s^2 + near[2] s^4 + near[3] s^6), in units of log2
     float near[4];
     int tile_prefix[kMaxGroups + 1];  // items of requests (or groups) before r, if R <= kMaxGroups
@@ -186,22 +186,34 @@ __device__ __forceinline__ int spread_request(const Params &p, int idx) {
     return lo;
 }
 
-// tanh on [-1, 1] as y * P(y^2), a minimax polynomial fitted to the relative error (6e-7, in fp32 too); beyond, from the definition
+// cap * tanh(v a) of two scores v for |v a| <= 1, in units of the score: v * (1 + u Q(u)) with u = (v a)^2, fitted (by reweighted least squares) to
+// the relative error, 8e-7 in fp32.  What is left of 1 and what is left of the cap go with u, so a cap far above the scores leaves them as they are.
 static constexpr float kTanhFast = 1.f;
-__device__ __forceinline__ float2 tanh2_fast(float2 y) {
+__device__ __forceinline__ float2 capped2_fast(float2 v, float2 a) {
     auto two = [](float c) { return make_float2(c, c); };
-    const float2 u = __fmul2_rn(y, y);
-    float2 r = __ffma2_rn(two(-0.00306705921f), u, two(0.01674311235f));
-    r = __ffma2_rn(r, u, two(-0.05160567164f));
-    r = __ffma2_rn(r, u, two(0.13281433284f));
-    r = __ffma2_rn(r, u, two(-0.33329042792f));
-    r = __ffma2_rn(r, u, two(0.99999940395f));
-    return __fmul2_rn(r, y);
+    const float2 y = __fmul2_rn(v, a), u = __fmul2_rn(y, y);
+    float2 r = __ffma2_rn(two(-0.00312658f), u, two(0.01690641f));
+    r = __ffma2_rn(r, u, two(-0.05176829f));
+    r = __ffma2_rn(r, u, two(0.1328849f));
+    r = __ffma2_rn(r, u, two(-0.3333028f));
+    r = __ffma2_rn(r, u, two(1.f));
+    return __fmul2_rn(r, v);
 }
 // 1 - 2 / (e^2y + 1): absolute error of some 2^-23; +-1 at +-infinity
 __device__ __forceinline__ float tanh_any(float y) {
     const float e = fast_exp2(y * 2.8853900817779268f);
     return 1.f - __fdividef(2.f, e + 1.f);
+}
+// A capped score in units of log2, for v = q.k of any size: c v (1 + u Q(u)), the same kind of fit (relative error 2e-7), as far as 1 - 2 / (e^2y + 1) would lose
+// the score's own accuracy; from there on that, whose 2^-22 is then 2^-21 of the result.  (That form alone is off by 2^-23 of the CAP at every score: by 0.13 at a cap of 10^6.)
+static constexpr float kTanhOwn = 0.625f;
+__device__ __forceinline__ float capped(float v, float a, float c, float top) {  // a: scale / cap, c: scale * log2 e, top: cap * log2 e
+    const float y = v * a, u = y * y;
+    float r = fmaf(0.01519537f, u, -0.0519479f);
+    r = fmaf(r, u, 0.13308175f);
+    r = fmaf(r, u, -0.33332341f);
+    const float own = v * c * fmaf(r, u, 1.f), far = top * tanh_any(y);
+    return fabsf(y) <= kTanhOwn ? own : far;
 }
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -695,7 +707,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                 load_s();
                 const bool whole = (key0 + kBN <= it.pre || (kMode == kScored && key0 + kBN - 1 <= lim_all && key0 >= lo_all)) && bad == 0;
                 // ---- the cap.  Small scores that every row sees wait for the exponential, whose code has the polynomial in it; with a bias, up to the
-                // cap, they are worked on in place; the rest goes through TMEM in a small loop.
+                // cap, they are worked on in place; the rest goes through TMEM in a small loop, score by score as large as it is.
                 constexpr bool kNear = kCap && !kBias;
                 auto near_score = [&](float v) { return v * (p.near[0] + v * v * (p.near[1] + v * v * (p.near[2] + v * v * p.near[3]))); };
                 bool near = false;
@@ -711,11 +723,11 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                         const float2 a = make_float2(p.cap_scale, p.cap_scale);
 #pragma unroll
                         for (int c = 0; c < 128; c += 2) {
-                            const float2 v = tanh2_fast(__fmul2_rn(make_float2(sv[c], sv[c + 1]), a));
+                            const float2 v = capped2_fast(make_float2(sv[c], sv[c + 1]), a);
                             sv[c] = v.x, sv[c + 1] = v.y;
                         }
                     } else if (!near) {
-                        if (kNear) mul = 1.f;
+                        mul = 1.f;
 #pragma unroll 1
                         for (int cc = 0; cc < 4; ++cc) {
                             float v[32];
@@ -725,7 +737,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                                 for (int c = 0; c < 32; ++c) v[c] = near_score(v[c]);
                             } else {
 #pragma unroll
-                                for (int c = 0; c < 32; ++c) v[c] = tanh_any(v[c] * p.cap_scale) * (kNear ? p.scale_log2 : 1.f);
+                                for (int c = 0; c < 32; ++c) v[c] = capped(v[c], p.cap_scale, p.scale_log2, p.cap_log2);
                             }
                             tc::tmem_st32(t_s + 32 * cc, v);
                         }

@@ -13,6 +13,10 @@ static constexpr float kLog2e = 1.4426950408889634f;
 static constexpr float kSmallest = 1.17549435e-38f;  // stands for a scale of 0: -inf times it is still -inf
 static constexpr float kLargest = 1e30f;             // bounds scale / cap: a score of 0 times it is still 0
 
+// scale / cap and cap * log2 e as the kernels take them: fp32 numbers that are neither flushed to 0 (an infinite score still reaches the cap) nor infinite.
+static float cap_scale_of(float scale, float cap) { return copysignf(fmaxf(kSmallest, fminf(fabsf(scale) / cap, kLargest)), scale); }
+static float cap_log2_of(float cap) { return fminf(cap * kLog2e, 3.402823466e38f); }
+
 // Shared-memory attributes of a kernel, once per device.
 template <typename Kernel>
 static cudaError_t ready(Kernel kernel, int bytes, int device, bool (&done)[64]) {
@@ -129,7 +133,7 @@ static void fill_ext(ext::Params &p, const ekv_pool *pool, const void *q, void *
     p.group = p.num_q_heads / p.num_kv_heads;
     p.chunk_tokens = plan.chunk_tokens, p.nsplit = plan.nsplit;
     p.window = 0, p.parts = 0, p.G = 0, p.beside = 0;
-    p.cap_scale = 0.f;
+    p.cap_scale = p.cap_log2 = 0.f;
 }
 
 static void fill_rows(rows::Params &p, const ekv_pool *pool, const void *q, void *out, const int32_t *block_tables, int32_t max_blocks) {
@@ -142,7 +146,7 @@ static void fill_rows(rows::Params &p, const ekv_pool *pool, const void *q, void
     p.group_magic = p.group > 1 ? (unsigned)(((1ull << 32) + p.group - 1) / p.group) : 0u;
     p.window = 0, p.parts = 1, p.chunk_tiles = 0, p.q_flip = 0;
     p.q_tma = rows::kBM % p.group == 0;
-    p.cap_scale = p.near_limit = 0.f;
+    p.cap_scale = p.cap_log2 = p.near_limit = 0.f;
     for (float &c : p.near) c = 0.f;
 }
 
@@ -350,8 +354,8 @@ extern "C" ekv_status_t ekv_attn_decode_scored(ekv_pool_t *pool, int32_t layer, 
     p.part_o = (float *)((uint8_t *)workspace + align256(n * sizeof(float2)));
     p.slopes = scores->slopes, p.prefix_lens = scores->prefix_lens, p.window = scores->window;
     const bool cap = scores->cap > 0.f;
-    p.scale_log2 = (cap ? scores->cap : scale) * kLog2e;
-    if (cap) p.cap_scale = fmaxf(-kLargest, fminf(2.f * kLog2e * (scale / scores->cap), kLargest));
+    p.scale_log2 = scale * kLog2e;
+    if (cap) p.cap_scale = cap_scale_of(scale, scores->cap), p.cap_log2 = cap_log2_of(scores->cap);
     const cudaError_t e = pool->desc.head_dim == 128 ? scored_decode<128>(pool, layer, p, cap, B, (cudaStream_t)stream)
                                                      : scored_decode<64>(pool, layer, p, cap, B, (cudaStream_t)stream);
     return e == cudaSuccess ? EKV_OK : cuda_fail(e, "ekv_attn_decode_scored launch");
@@ -414,13 +418,14 @@ extern "C" ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t 
     p.q_flip = scale < 0.f ? 0x80008000u : 0u;
     if (p.q_flip) p.q_tma = 0;
     const bool cap = scores->cap > 0.f;
-    p.scale_log2 = fmaxf((cap ? scores->cap : fabsf(scale)) * kLog2e, kSmallest);
+    p.scale_log2 = fmaxf(fabsf(scale) * kLog2e, kSmallest);
     if (cap) {
-        // cap * log2 e * tanh(a s) for |a s| <= 1/2: a minimax polynomial in a s (3e-7), its powers of a in the coefficients
-        const double a = p.cap_scale = fminf(fabsf(scale) / scores->cap, kLargest), c = (double)scores->cap * kLog2e * a;
+        p.cap_scale = cap_scale_of(fabsf(scale), scores->cap), p.cap_log2 = cap_log2_of(scores->cap);
+        // cap * log2 e * tanh(a s) for |a s| <= 1/2: a fitted polynomial in a s (6e-7), its powers of a in the coefficients
+        const double a = p.cap_scale, c = p.scale_log2;
         p.near[0] = (float)(0.99999946 * c), p.near[1] = (float)(-0.33326319 * c * a * a);
         p.near[2] = (float)(0.13190296 * c * a * a * a * a), p.near[3] = (float)(-0.04440222 * c * a * a * a * a * a * a);
-        p.near_limit = p.near[3] < -1e-36f && p.near[3] > -1e30f ? 0.5f / p.cap_scale : -1.f;  // (not where a coefficient leaves fp32's range)
+        p.near_limit = p.near[3] < -1e-36f && p.near[3] > -1e30f ? 0.5f / p.cap_scale : -1.f;  // (where a coefficient leaves fp32's range: `capped` alone)
     }
     const bool d128 = pool->desc.head_dim == 128;
     cudaError_t e = d128 ? scored_prefill<128>(pool, layer, p, cap, T, (cudaStream_t)stream) : scored_prefill<64>(pool, layer, p, cap, T, (cudaStream_t)stream);
