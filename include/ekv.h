@@ -454,7 +454,8 @@ EKV_API ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, con
  * prefix_lens[r] makes the first keys of request r visible to all its rows, also to rows before them (a prompt's image part, a
  * prefix language model) and to rows whose window has moved on (tokens that stay in sight); values are clamped to 0 .. seq_len.
  * Keys of a chunk's later rows below prefix_lens must be in the cache already, and a prompt that is cut into chunks must not be cut inside its prefix.
- * Only keys that some row sees are read.  EKV_BF16 pools only.
+ * Only keys that some row sees are read, in decode by whole blocks, in prefill by tiles of 128 keys.  Table entries of blocks without such a key -- those that
+ * a window has passed and that were given back -- may hold anything.  EKV_BF16 pools only.
  */
 typedef struct ekv_scores {
     float cap;                  /* 0: none */

@@ -514,12 +514,15 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
             if (fetch(n, it) <= 0) break;
             release(n);
             const int *bt = p.block_tables + (size_t)it.req * p.max_blocks;
-            auto load_id = [&](int t) {  // lane l: id of block l % 8 of the part's tile t (-1 past the last key, -2 invalid)
+            // Keys between the prefix and the first row's window are seen by no row of the item: what the table names for blocks of nothing else does not
+            // matter (they may have been given back since the window passed them).
+            const int past_by = kMode == kShared ? 0 : low_of(it.past + by_group(it.row0));
+            auto load_id = [&](int t) {  // lane l: id of block l % 8 of the part's tile t (-1 nothing to load, -2 invalid)
                 int id = -1;
                 const int bi = (first_key(it, t) >> 4) + (lane & 7);
                 if (t < it.n_tiles && bi * 16 < it.kv_end) {
                     id = bt[bi];
-                    if (id < 0 || (long long)id >= live) id = -2;
+                    if (id < 0 || (long long)id >= live) id = bi * 16 < it.pre || bi * 16 + 16 > past_by ? -2 : -1;
                 }
                 return id;
             };
