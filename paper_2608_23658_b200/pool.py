@@ -127,11 +127,11 @@ class Pool:
             B._refuse("read_kv", "slot_mapping", slot_mapping, f"contiguous int64 on {self.device}")
         shape = (T, self.num_kv_heads, self.head_dim)
         if k_out is None:
-            k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            k_out = self._made(shape, stream)
         else:
             self._check_rows("k_out", k_out, shape)
         if v_out is None:
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+            v_out = self._made(shape, stream)
         else:
             self._check_rows("v_out", v_out, shape)
         B._check(B.load_library().ekv_read_kv(self.handle, layer, k_out.data_ptr(), v_out.data_ptr(), slot_mapping.data_ptr(), T, B._stream(stream)))
@@ -152,9 +152,16 @@ class Pool:
         return stream if isinstance(stream, int) else stream.cuda_stream
 
     def _on(self, stream):
-        """Where memory that a call keeps to itself is made, if a stream was given: on that stream, so that what becomes of the memory later is
-        in the stream's order, and so that it belongs to the stream's graph while one is captured."""
+        """Where memory that a call makes is made, if a stream was given: on that stream, so that no kernel under way elsewhere may still use it, what
+        becomes of it later is in the stream's order, and it belongs to the stream's graph while one is captured."""
         return torch.cuda.stream(torch.cuda.ExternalStream(self._current(stream), device=self.device))
+
+    def _made(self, shape, stream):
+        """A bf16 tensor that the call on that stream writes."""
+        if stream is None:
+            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        with self._on(stream):
+            return torch.empty(shape, dtype=torch.bfloat16, device=self.device)
 
     def _want(self, call, name, t, dtype, shape):
         if t.dtype is not dtype or t.shape != shape or t.get_device() != self.device.index or not t.is_contiguous():
@@ -197,15 +204,14 @@ class Pool:
             if w is not None and not (w.dtype is bf16 and w.shape == row and w.get_device() == dev and w.is_contiguous()):
                 self._want(call, name, w, bf16, row)
         if q_out is None:
-            q_out = torch.empty((T, heads, D), dtype=bf16, device=self.device)
+            q_out = self._made((T, heads, D), stream)
             out_stride = heads * D
         else:
             out_stride = self._heads(call, "q_out", q_out, T, heads)
         if k_out is not None:
             self._want(call, "k_out", k_out, bf16, rows)
         elif self.dtype == B.EKV_E4M3:
-            with contextlib.nullcontext() if stream is None else self._on(stream):
-                k_out = torch.empty(rows, dtype=bf16, device=self.device)
+            k_out = self._made(rows, stream)
         rope = B.Rope(2 * pairs, num_axes, B.EKV_ROPE_ADJACENT if interleaved else 0, factor, eps, weight_offset, inv_freq.data_ptr(),
                       positions.data_ptr(), bytes(axes) if num_axes > 1 else None, q_weight.data_ptr() if q_weight is not None else None,
                       k_weight.data_ptr() if k_weight is not None else None)
@@ -227,7 +233,8 @@ class Pool:
 
     def attn_decode(self, layer, q, block_tables, seq_lens, scale, out=None, workspace=None, stream=None):
         if out is None:
-            out = torch.empty_like(q)
+            with contextlib.nullcontext() if stream is None else self._on(stream):
+                out = torch.empty_like(q)
         if workspace is None:
             workspace = self.workspace(int(seq_lens.shape[0]), int(block_tables.shape[1]) * self.block_size)
         B.ekv_attn_decode(self.handle, layer, q, out, block_tables, seq_lens, scale, workspace, stream)
@@ -236,17 +243,18 @@ class Pool:
     def attn_prefill_chunk(self, layer, q, block_tables, cu_q_lens, cu_q_lens_host, seq_lens, scale, out=None,
                            stream=None):
         if out is None:
-            out = torch.empty_like(q)
+            with contextlib.nullcontext() if stream is None else self._on(stream):
+                out = torch.empty_like(q)
         B.ekv_attn_prefill_chunk(self.handle, layer, q, out, block_tables, cu_q_lens, cu_q_lens_host, seq_lens,
                                  scale, stream)
         return out
 
     # -- scores with a cap, a distance bias, a window, a prefix; batches that share prefixes
-    def _check_attn(self, call, q, out, block_tables, seq_lens, T):
+    def _check_attn(self, call, q, out, block_tables, seq_lens, T, stream):
         """Shape of the block tables; an output if none is given."""
         at, shape, i32, bf16, dev = block_tables.shape, (T, self.num_q_heads, self.head_dim), torch.int32, torch.bfloat16, self.device.index
         if out is None:
-            out = torch.empty(shape, dtype=bf16, device=self.device)
+            out = self._made(shape, stream)
         if not (len(at) == 2 and block_tables.dtype is i32 and seq_lens.dtype is i32 and q.dtype is bf16 and out.dtype is bf16
                 and seq_lens.shape == at[:1] and q.shape == shape and out.shape == shape and block_tables.is_contiguous() and seq_lens.is_contiguous()
                 and q.is_contiguous() and out.is_contiguous() and block_tables.get_device() == dev and seq_lens.get_device() == dev
@@ -294,7 +302,7 @@ class Pool:
         """attn_decode with x = cap * tanh(x / cap), a bias of -slopes[head] * distance, a window of that many keys, and the keys below prefix_lens
         always seen; any of them."""
         n, lib = seq_lens.shape[0], B.load_library()
-        width, out = self._check_attn("attn_decode_scored", q, out, block_tables, seq_lens, n)
+        width, out = self._check_attn("attn_decode_scored", q, out, block_tables, seq_lens, n, stream)
         scores = self._scores("attn_decode_scored", n, cap, window, slopes, prefix_lens)
         self._launch(lambda ws, size, stream: lib.ekv_attn_decode_scored(self.handle, layer, q.data_ptr(), out.data_ptr(), block_tables.data_ptr(), width,
                                                                          seq_lens.data_ptr(), n, scale, scores, ws, size, stream),
@@ -308,7 +316,7 @@ class Pool:
         if cu_q_lens_host.dtype is not torch.int32 or cu_q_lens_host.is_cuda or cu_q_lens_host.numel() != n + 1 or not cu_q_lens_host.is_contiguous():
             B._refuse(call, "cu_q_lens_host", cu_q_lens_host, f"contiguous int32 ({n + 1},) on the host")
         self._want(call, "cu_q_lens", cu_q_lens, torch.int32, (n + 1,))
-        width, out = self._check_attn(call, q, out, block_tables, seq_lens, T)
+        width, out = self._check_attn(call, q, out, block_tables, seq_lens, T, stream)
         if T < cu_q_lens_host[n].item():
             B._refuse(call, "q", q, f"of at least {cu_q_lens_host[n].item()} rows")
         scores = self._scores(call, n, cap, window, slopes, prefix_lens)
@@ -327,7 +335,7 @@ class Pool:
             for name, t, size in (("group_starts", group_starts, G + 1), ("shared_lens", shared_lens, G)):
                 if t.dtype is not torch.int32 or t.is_cuda or t.numel() != size or not t.is_contiguous():
                     B._refuse(call, name, t, f"contiguous int32 ({size},) on the host")
-        width, out = self._check_attn(call, q, out, block_tables, seq_lens, n)
+        width, out = self._check_attn(call, q, out, block_tables, seq_lens, n, stream)
         starts, shared = group_starts.data_ptr(), shared_lens.data_ptr()
         self._launch(lambda ws, size, stream: lib.ekv_attn_decode_shared(self.handle, layer, q.data_ptr(), out.data_ptr(), block_tables.data_ptr(), width,
                                                                          seq_lens.data_ptr(), n, starts, shared, G, scale, ws, size, stream),
