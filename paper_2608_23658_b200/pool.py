@@ -3,6 +3,7 @@ mapped part of a layer's range and keeps a decode workspace.  No arithmetic happ
 from __future__ import annotations
 
 import contextlib
+import threading
 
 import torch
 
@@ -45,6 +46,7 @@ class Pool:
         self.dtype = dtype
         self._ws = None
         self._parts = {}  # workspaces of scored and shared attention, by stream
+        self._lock = threading.Lock()  # held while a call that uses one makes its launches: another thread's must not fall between them
 
     # -- lifetime
     def close(self):
@@ -289,12 +291,13 @@ class Pool:
         if torch.cuda.is_current_stream_capturing():
             own = torch.empty(max(need(), 1), dtype=torch.uint8, device=self.device)
             return B._check(call(own.data_ptr(), own.numel(), stream))
-        kept = self._parts.get(stream)
-        st = call(kept[-1].data_ptr(), kept[-1].numel(), stream) if kept else B.Status.ERR_WORKSPACE
-        if st == B.Status.ERR_WORKSPACE:  # (the ones that were too small stay: calls that are under way use them)
-            kept = self._parts.setdefault(stream, [])
-            kept.append(torch.empty(max(need(), 2 * kept[-1].numel() if kept else 1 << 20), dtype=torch.uint8, device=self.device))
-            st = call(kept[-1].data_ptr(), kept[-1].numel(), stream)
+        with self._lock:
+            kept = self._parts.get(stream)
+            st = call(kept[-1].data_ptr(), kept[-1].numel(), stream) if kept else B.Status.ERR_WORKSPACE
+            if st == B.Status.ERR_WORKSPACE:  # (the ones that were too small stay: calls that are under way use them)
+                kept = self._parts.setdefault(stream, [])
+                kept.append(torch.empty(max(need(), 2 * kept[-1].numel() if kept else 1 << 20), dtype=torch.uint8, device=self.device))
+                st = call(kept[-1].data_ptr(), kept[-1].numel(), stream)
         B._check(st)
 
     def attn_decode_scored(self, layer, q, block_tables, seq_lens, scale, cap=0.0, window=0, slopes=None, prefix_lens=None, out=None,
