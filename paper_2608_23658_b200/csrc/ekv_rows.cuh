@@ -708,6 +708,14 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                     cp::tcgen05_wait_ld();
                 };
                 load_s();
+                auto seen = [&](int cc) {  // which of keys 32 cc .. + 31 of the tile the row sees
+                    const int c0 = key0 + 32 * cc;
+                    const unsigned b2 = ((unsigned)bad >> (2 * cc)) & 3u;
+                    const unsigned broken = ((b2 & 1u) ? 0x0000ffffu : 0u) | ((b2 & 2u) ? 0xffff0000u : 0u);
+                    unsigned vis = below(it.pre - c0);
+                    if (kMode == kScored) vis |= below(lim + 1 - c0) & ~below(lo - c0);
+                    return vis & ~broken;
+                };
                 const bool whole = (key0 + kBN <= it.pre || (kMode == kScored && key0 + kBN - 1 <= lim_all && key0 >= lo_all)) && bad == 0;
                 // ---- the cap.  Small scores that every row sees wait for the exponential, whose code has the polynomial in it; with a bias, up to the
                 // cap, they are worked on in place; the rest goes through TMEM in a small loop, score by score as large as it is.
@@ -720,8 +728,9 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
 #pragma unroll
                     for (int c = 0; c < 128; c += 4) b0 = max3(b0, fabsf(sv[c]), fabsf(sv[c + 1])), b1 = max3(b1, fabsf(sv[c + 2]), fabsf(sv[c + 3]));
                     const float far = fmaxf(b0, b1);
-                    const bool small = __all_sync(0xffffffffu, kNear ? far <= p.near_limit : far * p.cap_scale <= kTanhFast);
-                    near = kNear && small && whole;
+                    // (where rows do not see all of the tile, what they do not see may be anything, and no bit of the result is to depend on it)
+                    const bool small = __all_sync(0xffffffffu, whole && (kNear ? far <= p.near_limit : far * p.cap_scale <= kTanhFast));
+                    near = kNear && small;
                     if (kBias && small) {
                         const float2 a = make_float2(p.cap_scale, p.cap_scale);
 #pragma unroll
@@ -735,13 +744,8 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                         for (int cc = 0; cc < 4; ++cc) {
                             float v[32];
                             tc::tmem_ld32(v, t_s + 32 * cc);
-                            if (kNear && small) {
 #pragma unroll
-                                for (int c = 0; c < 32; ++c) v[c] = near_score(v[c]);
-                            } else {
-#pragma unroll
-                                for (int c = 0; c < 32; ++c) v[c] = capped(v[c], p.cap_scale, p.scale_log2, p.cap_log2);
-                            }
+                            for (int c = 0; c < 32; ++c) v[c] = capped(v[c], p.cap_scale, p.scale_log2, p.cap_log2);
                             tc::tmem_st32(t_s + 32 * cc, v);
                         }
                         cp::tcgen05_wait_st();
@@ -769,12 +773,7 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                 if (!whole) {
 #pragma unroll
                     for (int cc = 0; cc < 4; ++cc) {
-                        const int c0 = key0 + 32 * cc;
-                                                const unsigned b2 = ((unsigned)bad >> (2 * cc)) & 3u;
-                        const unsigned broken = ((b2 & 1u) ? 0x0000ffffu : 0u) | ((b2 & 2u) ? 0xffff0000u : 0u);
-                        unsigned vis = below(it.pre - c0);
-                        if (kMode == kScored) vis |= below(lim + 1 - c0) & ~below(lo - c0);
-                        vis &= ~broken;
+                        const unsigned vis = seen(cc);
                         if (vis != 0xffffffffu) {
 #pragma unroll
                             for (int c = 0; c < 32; ++c)
