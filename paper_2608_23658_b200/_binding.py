@@ -430,6 +430,13 @@ def ekv_attn_prefill_chunk(pool: int, layer: int, q, out, block_tables, cu_q_len
                                                  float(scale), _stream(stream)))
 
 
+def _host_ints(call, name, t, n):
+    """What the library reads on the host: contiguous int32 [n] there."""
+    if t.dtype is not _torch().int32 or t.get_device() >= 0 or t.numel() != n or not t.is_contiguous():
+        _refuse(call, name, t, f"contiguous int32 ({n},) on the host")
+    return t.data_ptr()
+
+
 def _ws(workspace):
     return (0, 0) if workspace is None else (_dptr(workspace), workspace.numel() * workspace.element_size())
 
@@ -446,23 +453,30 @@ def ekv_attn_prefill_scored_workspace_bytes(pool: int) -> int:
 
 def ekv_attn_prefill_chunk_scored(pool: int, layer: int, q, out, block_tables, cu_q_lens, cu_q_lens_host, seq_lens, scale: float, scores: Scores,
                                   workspace, stream=None):
-    """ekv_attn_prefill_chunk with capped, biased or windowed scores (Pool.attn_prefill_chunk_scored checks the tensors)."""
+    """ekv_attn_prefill_chunk with capped, biased or windowed scores (Pool.attn_prefill_chunk_scored checks the device's tensors)."""
+    R = int(seq_lens.shape[0])
+    on_host = _host_ints("ekv_attn_prefill_chunk_scored", "cu_q_lens_host", cu_q_lens_host, R + 1)
     _check(load_library().ekv_attn_prefill_chunk_scored(pool, layer, _dptr(q), _dptr(out), _dptr(block_tables), int(block_tables.shape[1]),
-                                                        _dptr(cu_q_lens), _dptr(cu_q_lens_host), _dptr(seq_lens), int(seq_lens.shape[0]), scale,
+                                                        _dptr(cu_q_lens), on_host, _dptr(seq_lens), R, scale,
                                                         ctypes.byref(scores), *_ws(workspace), _stream(stream)))
+
+
+def _groups(call, group_starts, shared_lens):
+    G = shared_lens.numel()
+    return _host_ints(call, "group_starts", group_starts, G + 1), _host_ints(call, "shared_lens", shared_lens, G), G
 
 
 def ekv_attn_decode_shared_workspace_bytes(pool: int, group_starts, shared_lens, max_blocks_per_seq: int) -> int:
     """group_starts [G+1], shared_lens [G]: int32 on the host."""
-    return int(load_library().ekv_attn_decode_shared_workspace_bytes(pool, _dptr(group_starts), _dptr(shared_lens), int(shared_lens.shape[0]),
-                                                                     max_blocks_per_seq))
+    starts, shared, G = _groups("ekv_attn_decode_shared_workspace_bytes", group_starts, shared_lens)
+    return int(load_library().ekv_attn_decode_shared_workspace_bytes(pool, starts, shared, G, max_blocks_per_seq))
 
 
 def ekv_attn_decode_shared(pool: int, layer: int, q, out, block_tables, seq_lens, group_starts, shared_lens, scale: float, workspace, stream=None):
-    """Decode of a batch whose requests share prefixes, group by group (Pool.attn_decode_shared checks the tensors)."""
+    """Decode of a batch whose requests share prefixes, group by group (Pool.attn_decode_shared checks the device's tensors)."""
+    starts, shared, G = _groups("ekv_attn_decode_shared", group_starts, shared_lens)
     _check(load_library().ekv_attn_decode_shared(pool, layer, _dptr(q), _dptr(out), _dptr(block_tables), int(block_tables.shape[1]), _dptr(seq_lens),
-                                                 int(seq_lens.shape[0]), _dptr(group_starts), _dptr(shared_lens), int(shared_lens.shape[0]), scale,
-                                                 *_ws(workspace), _stream(stream)))
+                                                 int(seq_lens.shape[0]), starts, shared, G, scale, *_ws(workspace), _stream(stream)))
 
 
 def ekv_poll_status(pool: int) -> Status:
