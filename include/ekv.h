@@ -238,7 +238,7 @@ EKV_API ekv_status_t ekv_write_kv(ekv_pool_t *pool, int32_t layer, const void *k
  * k_out and v follows (two or three launches).
  * rope: HOST; its pointers are marked there.  q: DEVICE bf16, token t's heads at q + t*q_stride elements, [num_q_heads, D] contiguous;
  * k, v: the same with [num_kv_heads, D] -- so the three may be parts of one fused projection's rows.  q_out: likewise, and may be q
- * itself with the same stride.  Addresses on 16-byte boundaries, strides multiples of 8.
+ * itself with the same stride.  Addresses on 16-byte boundaries, strides multiples of 8 (of any value where T is 1: nothing is read from them).
  * k_out: EKV_E4M3 pools: DEVICE bf16 [T, num_kv_heads, D] contiguous; NULL on others.
  * slot_mapping: DEVICE int64 [T], as ekv_write_kv takes it: a negative slot writes nothing to the cache, a slot outside the live
  * range neither and latches EKV_ERR_BLOCK_OOB; the queries of such tokens are written all the same.

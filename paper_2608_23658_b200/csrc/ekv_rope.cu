@@ -290,7 +290,7 @@ extern "C" ekv_status_t ekv_rope_write_kv(ekv_pool_t *pool, int32_t layer, const
     if (T == 0) return EKV_OK;
     const uintptr_t at = (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)q_out | (uintptr_t)k_out | (uintptr_t)rope->q_weight | (uintptr_t)rope->k_weight;
     if (!q || !k || !v || !q_out || !slot_mapping || (rope->rotary_dim > 0 && (!rope->inv_freq || !rope->positions)) || (at & 15) ||
-        ((q_stride | k_stride | v_stride | q_out_stride) & 7)) {
+        (T > 1 && ((q_stride | k_stride | v_stride | q_out_stride) & 7))) {
         set_error("ekv_rope_write_kv: bad argument (q=%p, k=%p, v=%p, q_out=%p, slot_mapping=%p, inv_freq=%p, positions=%p; rows and weights on 16-byte boundaries)",
                   q, k, v, q_out, (const void *)slot_mapping, (const void *)rope->inv_freq, (const void *)rope->positions);
         return EKV_ERR_INVALID;
