@@ -233,7 +233,8 @@ EKV_API ekv_status_t ekv_write_kv(ekv_pool_t *pool, int32_t layer, const void *k
  *   for every pair i < rotary_dim/2 of channels (a, b) -- channels (i, i + rotary_dim/2), or (2i, 2i + 1) with EKV_ROPE_ADJACENT --
  *     t = positions[pair_axis[i]][token] * inv_freq[i],  (a, b) <- factor * (a cos t - b sin t, b cos t + a sin t);
  *   channels from rotary_dim on are not turned.  fp32, the angle in 64 bits; rounded to bf16 (nearest even) once.  The sum of
- *   squares is taken in fp32: a row of elements of some 10^18 and more overflows it.
+ *   squares is taken in fp32, whose range bounds a normed row: elements of some 10^18 and more overflow it, elements below 10^-19 count as 0 in
+ *   it (which matters where eps is as small as their squares).
  * Values go to the cache as they are.  EKV_E4M3 pools: the finished keys go to k_out first, as bf16, and what ekv_write_kv does with
  * k_out and v follows (two or three launches).
  * rope: HOST; its pointers are marked there.  q: DEVICE bf16, token t's heads at q + t*q_stride elements, [num_q_heads, D] contiguous;
@@ -451,6 +452,8 @@ EKV_API ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, con
  *   x = scale * q.k;   x = cap * tanh(x / cap) if cap > 0;   x = x - slopes[h] * |p - j| if slopes is given;
  *   the row sees the key if  p - window < j <= p  (j <= p if window is 0),  or if  j < prefix_lens[r];
  *   out = sum_j softmax(x)_j v_j  over the keys it sees.
+ * Scores, their cap (within 2^-20 of the capped score, whatever the cap's size), sums and results are fp32; the weights are rounded to bf16 before they
+ * meet the values (half a step, up to 2^-8 of each), as in the library's other attention calls, and the result once.  A row that sees no key is zeros.
  * prefix_lens[r] makes the first keys of request r visible to all its rows, also to rows before them (a prompt's image part, a
  * prefix language model) and to rows whose window has moved on (tokens that stay in sight); values are clamped to 0 .. seq_len.
  * Keys of a chunk's later rows below prefix_lens must be in the cache already, and a prompt that is cut into chunks must not be cut inside its prefix.
@@ -458,7 +461,7 @@ EKV_API ekv_status_t ekv_attn_prefill_chunk(ekv_pool_t *pool, int32_t layer, con
  * a window has passed and that were given back -- may hold anything.  EKV_BF16 pools only.
  */
 typedef struct ekv_scores {
-    float cap;                  /* 0: none */
+    float cap;                  /* 0: none; else any finite number above 0 */
     int32_t window;             /* 0: none; else >= 1 */
     const float *slopes;        /* DEVICE [num_q_heads], or NULL: no bias */
     const int32_t *prefix_lens; /* DEVICE [B] or [R], or NULL: none */
@@ -473,7 +476,9 @@ EKV_API ekv_status_t ekv_attn_decode_scored(ekv_pool_t *pool, int32_t layer, con
 /* ekv_attn_prefill_chunk with such scores (tcgen05; any group, head_dim 64 or 128, any scale; calls share nothing but what they are
  * given).  workspace: DEVICE, 256-byte aligned, ekv_attn_prefill_scored_workspace_bytes(pool) bytes cover every call of the
  * pool; calls that share it must be stream-ordered.  Only a call of few rows over many keys uses it (its keys are cut into parts); one that does and has not enough is refused with EKV_ERR_WORKSPACE.
- * A NaN or an infinity in a key or value reaches the rows that see it and no others.  At most 65535 * 256 (row, head of the group) pairs a call. */
+ * A NaN or an infinity in a key or value reaches the rows that see it and no others, and no bit of a result depends on keys that no row sees.  At most 65535 * 256
+ * (row, head of the group) pairs a call, each request's counted up to a multiple of 256 (with more than 256 requests: all of them, and 256 for each).  Rows behind
+ * the last request's are left as they are. */
 EKV_API size_t ekv_attn_prefill_scored_workspace_bytes(const ekv_pool_t *pool);
 EKV_API ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t layer, const void *q, void *out, const int32_t *block_tables,
                                            int32_t max_blocks_per_seq, const int32_t *cu_q_lens, const int32_t *cu_q_lens_host,
@@ -482,7 +487,7 @@ EKV_API ekv_status_t ekv_attn_prefill_chunk_scored(ekv_pool_t *pool, int32_t lay
 
 /*
  * ekv_attn_decode_shared -- ekv_attn_decode for a batch whose requests share prefixes (a system prompt, samples of one prompt, questions
- * about one document): the result is ekv_attn_decode's within rounding, but the shared keys are read once for a group instead of
+ * about one document): the result is ekv_attn_decode's within rounding (of weights to bf16, as there), but the shared keys are read once for a group instead of
  * once for each request, where by the sizes that pays.
  * Group g is the requests group_starts[g] .. group_starts[g+1]-1; their first shared_lens[g] tokens are the same, i.e. the first
  * shared_lens[g]/block_size entries of their rows of block_tables name the same blocks (those of the group's first request are read).

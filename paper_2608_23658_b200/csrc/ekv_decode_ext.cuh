@@ -3,7 +3,7 @@
 // The split pass of ekv_decode.cu -- a CTA per (sequence, kv-head, range of keys), each warp a ring of TMA loads for every fourth block of 16
 // keys, the heads of the group as the rows of mma.m16n8k16, partial (m, l, O) per range -- over those blocks alone that the sequence sees:
 // of its prefix and of its window, or from the end of the shared keys on.  Bound by the bytes of these: 64 sequences of up to 16000 keys, 32q/8kv, 1.04 GB
-// in 158 to 164 us = 6.4 to 6.6 TB/s.  Where a sequence has a single range (many do, where the tables are wider than the sequences long) the CTA
+// in 158 to 166 us = 6.3 to 6.6 TB/s.  Where a sequence has a single range (many do, where the tables are wider than the sequences long) the CTA
 // writes the final rows itself.  Up to sixteen ranges whose CTAs are all there at once are a cluster and add themselves up out of each other's shared
 // memory (5 sequences of up to 1000 keys, 4q/2kv d64: 5.5 us on the device for 6.6 with a second launch; one of 4000 6.5 for 11.2); for more,
 // combine_ext_kernel does, a warp a (sequence, head).
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
                     o[mt][3] *= a_hi;
                 }
             }
-            const uint32_t pb0 = pack_bf16x2(p0, p1), pb1 = pack_bf16x2(p2, p3);  // weights in bf16: half a step is 2^-9 of one
+            const uint32_t pb0 = pack_bf16x2(p0, p1), pb1 = pack_bf16x2(p2, p3);  // weights in bf16: half a step is up to 2^-8 of one
 #pragma unroll
             for (int mt = 0; mt < KSTEPS; ++mt) {
                 const int chunk = 2 * mt + lane_par;

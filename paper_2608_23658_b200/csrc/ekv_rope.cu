@@ -5,7 +5,7 @@
 //   queries -> q_out, keys and values -> their slots of the cache      (rounded to bf16 once, at the end)
 //
 // Every element is read once and written once: 403 MB for 16384 tokens of 32q/8kv, 76 to 80 us = 5.0 to 5.3 TB/s of the 6.5 that a copy gets; the
-// arithmetic between takes two thirds of the issue slots and is what keeps it from the rest.  2049 tokens of 28q/4kv 8 us, 256 of 32q/8kv 4, 31 of
+// arithmetic between takes two thirds of the issue slots and is what keeps it from the rest.  2049 tokens of 28q/4kv 11 us, 256 of 32q/8kv 4, 31 of
 // 4q/2kv 3, on the device.
 // A row of head_dim channels belongs to D / 16 neighbouring lanes, two pieces of 16 bytes each; where pairs are halves of a row the pieces are
 // chosen so that both channels of a pair are in one thread, so a rotation is register arithmetic and only the sum of squares is shuffled.
@@ -117,8 +117,8 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeCtas) rope_write_kernel(con
         const __nv_bfloat16 *w = i < D ? p.q_weight : p.k_weight;
         weights[i / D][i % D] = w ? p.offset + __bfloat162float(w[i % D]) : 1.f;
     }
-    // A thread works out the angles of one pair, of every kAngleRows-th token.  (|error| of the fast sine and cosine within half a turn: some 2^-21,
-    // an eighth of a percent of what the result is rounded to.)
+    // A thread works out the angles of one pair, of every kAngleRows-th token.  (|error| of the fast sine and cosine within half a turn: some 2^-21, so
+    // some 2^-20 of the larger channel of the pair in the result, however small that comes out; the rounding to bf16 is up to 2^-8 of the result.)
     constexpr int kAngleRows = kRopeThreads / (D / 2);
     const int pair = threadIdx.x % (D / 2);
     const bool has_pair = pair < p.pairs;

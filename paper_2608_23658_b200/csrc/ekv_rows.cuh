@@ -30,11 +30,12 @@
 //
 // What bounds it is the chain of a slot: S ready, maximum, 128 weights a thread, P stored, P V issued; the tensor pipe is busy 43 to 54 % of a long
 // item.  Measured, one B200, head_dim 128, back to back, us, without modifications / capped / with the distance bias:
-//   2048 positions over 14001 keys, 32q/8kv   443 to 460 (1100 to 1140 TFLOP/s) / 600 to 670, by the scores' size and the power cap / 560 to 580
-//   a prompt of 8192, 32q/8kv                 465 to 510 / 655 / 593 to 620
-//   24 prompts of up to 1500, 28q/4kv         202 / 283 / 229 to 253
-//   64 positions over 8000 keys, 32q/8kv      28 / 32 / 30
-// With a window of 257 keys the first takes 35.  256 requests' rows over 16384 shared keys, 32q/8kv: 76 = 920 TFLOP/s.
+//   2048 positions over 14001 keys, 32q/8kv   443 to 514 (980 to 1140 TFLOP/s), by the machine / 600 to 670, by the scores' size and the power cap / 560 to 603
+//   a prompt of 8192, 32q/8kv                 465 to 524 / 655 to 682 / 593 to 627
+//   24 prompts of up to 1500, 28q/4kv         202 to 215 / 283 to 313 / 229 to 253
+//   64 positions over 8000 keys, 32q/8kv      27 to 31 / 32 to 35 / 30 to 32
+// Scores mostly beyond half the cap, the first: 1200.  With a window of 257 keys the first takes 32 to 36.  256 requests' rows over 16384 shared keys, 32q/8kv:
+// 76 = 904 TFLOP/s in 128 items, with next to no own keys; beside own keys the pass is cut into 96 items and takes 99, under the profiler.
 // A thread a row: two threads a row halve the chain's exponentials but pay shuffles and twice the fixed work (754 -> 791 us for 2048 capped rows).
 #pragma once
 #include "ekv_prefill_tc.cuh"

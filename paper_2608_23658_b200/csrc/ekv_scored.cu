@@ -244,7 +244,8 @@ static SharedPlan plan_shared(const ekv_pool *pool, const int32_t *starts, const
     // Worth it?  The pass over the shared keys costs a launch more and its items' starts and ends; it saves their bytes, read from L2 for the most part.
     // Measured with own parts of up to 200 keys, us with / without: 32q/8kv, 2 requests over 8192 keys 16.5 / 14.5, 4 over 4096 14.7 / 12.9, over 8192 16.5 /
     // 18.5; 16 over 1024 14.7 / 12.7, over 2048 17.2 / 16.7, over 4096 17.3 / 33.6; 64 over 512 16.6 / 23.0; 28q/4kv, 16 over 2048 16.1 / 13.3, over 4096
-    // 17.2 / 18.2, 64 over 1024 20.3 / 28.7; 4q/2kv d64, 16 over 4096 10.3 / 9.8.
+    // 17.2 / 18.2, 64 over 1024 20.3 / 28.7; 4q/2kv d64, 16 over 4096 10.3 / 9.8.  (16 over 2048 of 32q/8kv are shared all the same: half a microsecond lost, for
+    // a rule of two terms.)
     s.worth = saved * Hk * pool->desc.head_dim * 4 / 9e6 + longest_shared * (0.4 / 1024) > 13.;
     for (int g = 0; g < G; ++g) {
         const int n = starts[g + 1] - starts[g];
