@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) decode_ext_kernel(const __grid
                     o[mt][3] *= a_hi;
                 }
             }
-            const uint32_t pb0 = pack_bf16x2(p0, p1), pb1 = pack_bf16x2(p2, p3);  // weights in bf16: half a step is up to 2^-8 of one
+            const uint32_t pb0 = pack_bf16x2(p0, p1), pb1 = pack_bf16x2(p2, p3);  // weights in bf16, V's type, as the MMA wants: off by up to 2^-8 of themselves
 #pragma unroll
             for (int mt = 0; mt < KSTEPS; ++mt) {
                 const int chunk = 2 * mt + lane_par;

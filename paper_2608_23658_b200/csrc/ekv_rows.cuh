@@ -811,7 +811,9 @@ rows_kernel(const __grid_constant__ CUtensorMap kvmap, const __grid_constant__ C
                     }
                 }
                 const float m_use = m_run > -INFINITY ? m_run : 0.f;
-                // ---- P = exp2(x - m) (a masked -inf gives 0), row sum, bf16 pairs into the S columns
+                // ---- P = exp2(x - m) (a masked -inf gives 0), row sum in fp32, bf16 pairs into the S columns.  bf16 because both operands of an MMA have one type and
+                // V is bf16: a weight is off by up to 2^-8 of itself, the sum that divides is not.  (Two bf16 a weight would double the P V MMAs.)  Against
+                // 64 bits relative errors are 0.0019 to 0.0023 (2048 over 14001 keys 0.0021), of which 0.0017 is the result's own rounding.
                 float2 acc_a = make_float2(0.f, 0.f), acc_b = make_float2(0.f, 0.f);
                 const float2 sc2 = make_float2(mul, mul), nm2 = make_float2(-m_use, -m_use);
                 auto weights = [&](auto score) {  // score(v): x - m of two keys
