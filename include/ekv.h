@@ -22,6 +22,8 @@
  *     marked HOST are ordinary host memory.  The pool owns the KV ranges and physical handles.
  *   - ekv_write_kv / ekv_attn_* are asynchronous: they enqueue work on `stream` (a cudaStream_t /
  *     CUstream passed as void*, NULL = legacy default stream) and return without synchronising.
+ *   - A call may make several launches.  Calls that have to be stream-ordered (they share a workspace, or write the same
+ *     blocks) are made one after the other, not by two threads at once.
  *   - ekv_grow / ekv_shrink are host-synchronous and must not run concurrently with any other
  *     call on the same pool (the caller serialises them at a step boundary).
  *   - There is no CPU fallback: without a CUDA device every compute call fails with EKV_ERR_CUDA.
